@@ -15,6 +15,13 @@
  *   specvlm_tree_attn / specvlm_accept_tree   the same two steps for a draft tree (App. B)
  *   specvlm_baseline_keep  retention sets of the attention-agnostic pruners (Sec. 2.2, 5.2)
  *
+ * and, for programs that keep their caches in pages, the same step over them:
+ *
+ *   specvlm_paged_attn   attention of the block over a paged cache, also with a window
+ *   specvlm_rope_append  the block's queries and keys turned to their positions and written to the pages
+ *   specvlm_pages_assign which pages every request holds next: grown, cut short, forked, freed
+ *   specvlm_pages_copy   rows between pages: accepted tree nodes, a pruned cache, a fork's last page
+ *
  * Conventions shared by every call
  * --------------------------------
  *  - Return value: SPECVLM_OK (0) or a negative SPECVLM_E* code.  Arguments are
@@ -57,12 +64,13 @@ extern "C" {
 #define SPECVLM_EUNSUPPORTED (-2)  /* shape outside the supported set */
 #define SPECVLM_EWORKSPACE   (-3)  /* workspace missing, misaligned or too small */
 #define SPECVLM_ELAUNCH      (-4)  /* the HIP runtime refused a launch */
+#define SPECVLM_ENOPAGES     (-5)  /* (device-side status) a request got no pages: too few are free */
 
 /* Static text for a return code (host pointer, never NULL). */
 const char* specvlm_status_string(int status);
 
 /* Library version as major*10000 + minor*100 + patch: that of the header it was built with. */
-#define SPECVLM_VERSION 100
+#define SPECVLM_VERSION 200
 int specvlm_version(void);
 
 /* --------------------------------------------------------------------------
@@ -341,6 +349,188 @@ int specvlm_tree_attn(
     int n_q_heads, int n_kv_heads, int head_dim, float softmax_scale,
     const uint64_t* ancestor_mask, void* out, float* lse, int num_splits,
     void* workspace, size_t workspace_bytes, void* stream);
+
+/* --------------------------------------------------------------------------
+ * Paged caches.  A pool holds n_pages pages of page_size tokens (a multiple of
+ * 16), for keys and for values:
+ *
+ *   k_pages, v_pages  bf16 [n_pages, page_size, H_kv, d], one set of page / token /
+ *                     head strides (elements, multiples of 8) for both, d contiguous
+ *   page_table        int32 [batch, max_pages], rows table_stride apart: token i of
+ *                     request b is row i % page_size of page page_table[b][i / page_size]
+ *   kv_lens           int32 [batch]: tokens in each request's cache, the block of new
+ *                     tokens, which are the last ones, included
+ *   cu_q              int32 [batch + 1] prefix offsets of the requests' new tokens, or
+ *                     NULL: every request has as many
+ *
+ * An entry of a table outside [0, n_pages) is no page.  Nothing is read or written
+ * through it: its keys are hidden, its rows are dropped.  Entries that no token of a
+ * request lies in are not looked at.
+ * All of these live on the device, so a captured call serves caches as they grow.
+ * -------------------------------------------------------------------------- */
+
+/* --------------------------------------------------------------------------
+ * specvlm_paged_attn -- specvlm_decode_attn over a paged cache, with a window.
+ * Request b has q_len_b queries, the last ones of its kv_lens[b] tokens: query t
+ * is at position p = kv_lens[b] - q_len_b + t and sees key j iff
+ *
+ *   j <= p, or with ancestor_mask: j lies before the block, or bit
+ *     j - (kv_lens[b] - q_len_b) of the query's mask is set    (as in specvlm_tree_attn)
+ *   and window == 0, or j > p - window, or j < n_sinks
+ *     (the query's own position counts as one of the window's; a tree node's position
+ *     is its place in the block)
+ *   and the key's page is one of the pool's.
+ *
+ *   q    bf16 [sum q_len_b, H_q, d]      out  bf16, same shape and strides as q
+ *   lse  optional fp32 [sum q_len_b, H_q]: natural log of each row's softmax sum
+ * A row that sees no key gets 0, and -infinity in lse.  What a hidden key or value
+ * holds (a page's rows behind the last token, NaN, infinities) changes nothing.
+ *   q_len   the maximum over the requests with cu_q, else every request's number
+ *   kv_len  the maximum that kv_lens may hold, at most max_pages * page_size
+ * A request with q_len_b or kv_lens[b] beyond these, with none of either, or with
+ * fewer tokens than queries, is skipped: its rows of out and lse are left as they
+ * are, as are rows behind the last request.
+ * With a window, pages that lie wholly between the first n_sinks tokens and every
+ * query's window are never looked at and may be freed.
+ * Results do not depend on the run; they may differ by roundings when the other
+ * requests of the batch change, since the lengths of all decide how each is cut.
+ * Limits: q_len <= 64, kv_len <= 2^30.
+ * -------------------------------------------------------------------------- */
+size_t specvlm_paged_attn_workspace_bytes(int batch, int q_len, int n_q_heads, int n_kv_heads, int head_dim);
+
+int specvlm_paged_attn(
+    const void* q, int64_t q_tok_stride, int64_t q_head_stride,
+    const void* k_pages, const void* v_pages, int64_t page_stride, int64_t tok_stride, int64_t head_stride,
+    int n_pages, int page_size, const int32_t* page_table, int64_t table_stride, int max_pages,
+    const int32_t* kv_lens, const int32_t* cu_q, int batch, int q_len, int kv_len,
+    int n_q_heads, int n_kv_heads, int head_dim, float softmax_scale, int window, int n_sinks,
+    const uint64_t* ancestor_mask, void* out, float* lse,
+    void* workspace, size_t workspace_bytes, void* stream);
+
+/* --------------------------------------------------------------------------
+ * specvlm_rope_turns -- the frequencies of rotary positions, as specvlm_rope_append
+ * takes them: turns[i], i < rot_dim / 2, is the part of a full turn by which pair i
+ * turns a position, in units of 2^-64.  HOST memory; nothing is launched.
+ *   SPECVLM_ROPE_PLAIN     base^(-2i / rot_dim) rad
+ *   SPECVLM_ROPE_LINEAR    the same divided by factor (position interpolation)
+ *   SPECVLM_ROPE_BASE      base * factor^(rot_dim / (rot_dim - 2)) as the base: the first
+ *                          pair turns as before, the last by 1 / factor
+ *   SPECVLM_ROPE_BY_PARTS  (arXiv 2309.00071) a pair that turns r times over original_len
+ *                          positions keeps its frequency for r >= beta_fast, has it divided by
+ *                          factor for r <= beta_slow, and a mixture linear in r between
+ * Fields that a kind does not name are not looked at; factor >= 1.
+ * -------------------------------------------------------------------------- */
+#define SPECVLM_ROPE_PLAIN    0
+#define SPECVLM_ROPE_LINEAR   1
+#define SPECVLM_ROPE_BASE     2
+#define SPECVLM_ROPE_BY_PARTS 3
+typedef struct {
+    int kind;                    /* one of the four */
+    double base, factor;
+    double original_len, beta_fast, beta_slow;
+} specvlm_rope_spec;
+int specvlm_rope_turns(int rot_dim, const specvlm_rope_spec* spec, uint64_t* turns);
+
+/* --------------------------------------------------------------------------
+ * specvlm_rope_append -- the new tokens of every request: queries and keys turned to
+ * their positions, keys and values written to the pages, in one launch.
+ *
+ *   q      bf16 [n_tokens, H_q, d] or NULL;  q_out  the same with strides of its own
+ *          (q itself is allowed)
+ *   k, v   bf16 [n_tokens, H_kv, d], one token / head stride pair, or both NULL: only the
+ *          queries are turned (the pool and the table are then not looked at)
+ *   Token t of request b is its token kv_lens[b] - q_len_b + t of the cache, which is also
+ *   its position unless positions, int32 [n_tokens], names another.
+ *   turns      device uint64 [rot_dim / 2], see specvlm_rope_turns
+ *   rot_dim    columns that are turned, the first of the head, a multiple of 16 (0: none);
+ *              the others are copied
+ *   interleaved  pair i is columns 2i and 2i + 1, else i and i + rot_dim / 2
+ *   magnitude  the turned columns of q and k are multiplied by it
+ * The angle is exact modulo a turn at every position; results are rounded to bf16 once.
+ * Without cu_q n_tokens is a multiple of batch.  kv_lens may be NULL with k NULL and
+ * positions given.  Tokens behind the last request, and those of a request with fewer
+ * cached tokens than new ones, are left alone.  k, v must not overlap the pool.
+ * -------------------------------------------------------------------------- */
+int specvlm_rope_append(
+    const void* q, int64_t q_tok_stride, int64_t q_head_stride, void* q_out, int64_t out_tok_stride, int64_t out_head_stride,
+    const void* k, const void* v, int64_t kv_tok_stride, int64_t kv_head_stride,
+    void* k_pages, void* v_pages, int64_t page_stride, int64_t tok_stride, int64_t head_stride,
+    int n_pages, int page_size, const int32_t* page_table, int64_t table_stride, int max_pages,
+    const int32_t* kv_lens, const int32_t* cu_q, int batch, int n_tokens, const int32_t* positions,
+    const uint64_t* turns, int rot_dim, int interleaved, float magnitude,
+    int n_q_heads, int n_kv_heads, int head_dim, void* stream);
+
+/* --------------------------------------------------------------------------
+ * specvlm_pages_assign -- which pages every request holds next.  The new table has a
+ * row for every request, which goes on from row parent[b] of the old table (-1: from
+ * nothing), keeps its first keep_len[b] tokens and gets room for new_len[b] in all.
+ * Growing, going back, forking, reordering and ending (new_len 0) are all this.
+ *
+ *   - Pages that lie wholly in the kept tokens are shared with whoever else keeps them.
+ *   - The page in which the kept tokens end will be written.  It stays with the lowest
+ *     row that goes on in it, unless a row keeps it as a whole page; the other rows get a
+ *     page of their own, and copy_rows[b] tokens from copy_start[b] on are to be copied
+ *     into it from row parent[b] of the old table (specvlm_pages_copy takes both arrays
+ *     as they are); 0 and 0 where there is nothing to copy.
+ *   - A page that no row keeps is free.  Free pages are handed out lowest first, to the
+ *     lowest rows first.
+ *   - With window > 0, kept pages that no later token will see (wholly behind the first
+ *     n_sinks tokens and wholly before the window of the next one) are given up: -1.
+ *
+ *   old_table   int32 [old_rows, old_max_pages], rows old_stride apart; an entry that is no
+ *               page of the pool stays -1
+ *   page_table  int32 [batch, max_pages], rows table_stride apart (>= max_pages); every entry is
+ *               written, -1 behind the last page.  Must not overlap old_table.
+ *   ref_counts  int32 [n_pages]: rows of the new table that hold each page
+ *   status      int32 [batch]: SPECVLM_OK; SPECVLM_EINVAL for a row that does not fit together
+ *               (parent outside [-1, old_rows), keep_len > new_len, negative, kept tokens of
+ *               nothing, more pages than a table has), which gets none; SPECVLM_ENOPAGES for a
+ *               row for which too few pages were left: it has what it shares and -1 for the rest
+ * A row that needs pages gets them if the needs of all rows up to it fit the free ones.
+ * The table has to hold all rows that own pages of the pool: what is in no row is free.
+ * Integer arithmetic throughout: the result depends on the arguments alone.
+ * -------------------------------------------------------------------------- */
+size_t specvlm_pages_assign_workspace_bytes(int batch, int n_pages);
+
+int specvlm_pages_assign(
+    const int32_t* old_table, int64_t old_stride, int old_rows, int old_max_pages,
+    const int32_t* parent, const int32_t* keep_len, const int32_t* new_len, int batch,
+    int32_t* page_table, int64_t table_stride, int max_pages, int n_pages, int page_size, int window, int n_sinks,
+    int32_t* copy_start, int32_t* copy_rows, int32_t* ref_counts, int32_t* status,
+    void* workspace, size_t workspace_bytes, void* stream);
+
+/* --------------------------------------------------------------------------
+ * specvlm_pages_copy -- rows of paged caches, copied bit for bit in every layer.  For
+ * request b and i < n_b, token
+ *
+ *   src_start[b] + (row_idx ? its i-th index : i)   of row  src_row[b] (NULL: b) of src_table
+ *
+ * goes to token  dst_start[b] + i  of row b of dst_table.  NULL starts are 0.
+ *   n_b      n_rows[b], at most max_rows (host); n_rows NULL: as many as the list has with
+ *            cu_idx, else max_rows
+ *   row_idx  int32, request b's list at row_idx + b * idx_stride, or with cu_idx (int32
+ *            [batch + 1]) from cu_idx[b] to cu_idx[b + 1]
+ * Accepted tree nodes move to the front of their block with row_idx = accepted_nodes,
+ * n_rows = n_accepted (specvlm_accept_tree), src_start = the block's first token and
+ * dst_start = the one behind it; a draft's pruned cache takes the indices that
+ * specvlm_select keeps; a fork's last page what specvlm_pages_assign says.
+ *   pools    bf16 [n_layers, pages, page_size, H_kv, d] with strides of their own (elements,
+ *            multiples of 8) for source and destination, one set for K and V each; page sizes
+ *            may differ.  v_src and v_dst may both be NULL.
+ * A source token without a page gives zeros, a destination token without one is dropped.
+ * Source and destination may be the same pool (the same addresses and strides): rows of a
+ * request may then overlap if its indices ascend and no row moves to a later token of the
+ * same table row.  No request's destination may be another's source or destination.  Pools that are not
+ * the same must not overlap.
+ * -------------------------------------------------------------------------- */
+int specvlm_pages_copy(
+    const void* k_src, const void* v_src, int64_t src_layer_stride, int64_t src_page_stride, int64_t src_tok_stride, int64_t src_head_stride,
+    int src_pages, int src_page_size, const int32_t* src_table, int64_t src_table_stride, int src_rows, int src_max_pages,
+    void* k_dst, void* v_dst, int64_t dst_layer_stride, int64_t dst_page_stride, int64_t dst_tok_stride, int64_t dst_head_stride,
+    int dst_pages, int dst_page_size, const int32_t* dst_table, int64_t dst_table_stride, int dst_max_pages,
+    int n_layers, int batch, const int32_t* n_rows, int max_rows, const int32_t* src_row, const int32_t* src_start,
+    const int32_t* dst_start, const int32_t* row_idx, int64_t idx_stride, const int32_t* cu_idx,
+    int n_kv_heads, int head_dim, void* stream);
 
 /* --------------------------------------------------------------------------
  * specvlm_accept -- which drafted tokens survive verification  (Sec. 2.1).

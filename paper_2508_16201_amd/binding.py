@@ -38,7 +38,15 @@ EXPORTS = (
     "specvlm_tree_attn", "specvlm_accept_tree_workspace_bytes", "specvlm_accept_tree",
     "specvlm_baseline_count", "specvlm_baseline_workspace_bytes", "specvlm_baseline_keep",
     "specvlm_probe_read",
+    "specvlm_paged_attn_workspace_bytes", "specvlm_paged_attn",
+    "specvlm_rope_turns", "specvlm_rope_append",
+    "specvlm_pages_assign_workspace_bytes", "specvlm_pages_assign", "specvlm_pages_copy",
 )
+
+
+class _RopeSpec(C.Structure):
+    _fields_ = [("kind", C.c_int), ("base", C.c_double), ("factor", C.c_double), ("original_len", C.c_double),
+                ("beta_fast", C.c_double), ("beta_slow", C.c_double)]
 
 
 class SpecVLMError(RuntimeError):
@@ -98,8 +106,19 @@ def lib() -> C.CDLL:
         l.specvlm_accept.argtypes = [vp, vp, vp, vp, i32, i32, i32, f32, vp, vp, vp, sz, vp]
         for name in ("specvlm_score", "specvlm_select", "specvlm_top_p_count", "specvlm_gather_kv",
                      "specvlm_decode_attn", "specvlm_decode_attn_static", "specvlm_accept", "specvlm_tree_attn",
-                     "specvlm_accept_tree"):
+                     "specvlm_accept_tree", "specvlm_paged_attn", "specvlm_rope_turns", "specvlm_rope_append", "specvlm_pages_assign",
+                     "specvlm_pages_copy"):
             getattr(l, name).restype = C.c_int
+        l.specvlm_paged_attn_workspace_bytes.argtypes = [i32] * 5
+        l.specvlm_paged_attn.argtypes = [vp, i64, i64, vp, vp, i64, i64, i64, i32, i32, vp, i64, i32, vp, vp, i32, i32, i32,
+                                         i32, i32, i32, f32, i32, i32, vp, vp, vp, vp, sz, vp]
+        l.specvlm_rope_turns.argtypes = [i32, C.POINTER(_RopeSpec), vp]
+        l.specvlm_rope_append.argtypes = [vp, i64, i64, vp, i64, i64, vp, vp, i64, i64, vp, vp, i64, i64, i64, i32, i32, vp, i64, i32,
+                                          vp, vp, i32, i32, vp, vp, i32, i32, f32, i32, i32, i32, vp]
+        l.specvlm_pages_assign_workspace_bytes.argtypes = [i32] * 2
+        l.specvlm_pages_assign.argtypes = [vp, i64, i32, i32, vp, vp, vp, i32, vp, i64, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+        l.specvlm_pages_copy.argtypes = [vp, vp, i64, i64, i64, i64, i32, i32, vp, i64, i32, i32, vp, vp, i64, i64, i64, i64, i32, i32,
+                                         vp, i64, i32, i32, i32, vp, i32, vp, vp, vp, vp, i64, vp, i32, i32, vp]
         _lib = l
     return _lib
 
@@ -487,6 +506,230 @@ def decode_attn_static(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, softma
 def tree_attn(q, k, v, softmax_scale, ancestor_mask: torch.Tensor, **kw):
     """decode_attn for a block of draft-tree nodes; ancestor_mask int64/uint64 [sum q_len]."""
     return decode_attn(q, k, v, softmax_scale, ancestor_mask=ancestor_mask, **kw)
+
+
+# ------------------------------------------------------------------- paged caches
+def _on_device(**tensors: Optional[torch.Tensor]):
+    """Tensors of one call lie on the current device, whose stream the call goes to."""
+    for name, t in tensors.items():
+        if t is not None and (not t.is_cuda or t.device.index != _current_device()):
+            raise ValueError(f"{name} must live on the current GPU")
+
+
+def _typed(dtype: torch.dtype, **tensors: Optional[torch.Tensor]):
+    for name, t in tensors.items():
+        if t is not None and t.dtype != dtype:
+            raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+
+
+def _int32s(n: Optional[int], **tensors: Optional[torch.Tensor]):
+    """Contiguous int32 vectors, of n entries."""
+    _typed(torch.int32, **tensors)
+    for name, t in tensors.items():
+        if t is not None and (t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n)):
+            raise ValueError(f"{name} must be a contiguous vector" + ("" if n is None else f" of {n} entries"))
+
+
+def _table(name: str, t: torch.Tensor):
+    """(row stride, entries a row) of a page table."""
+    _typed(torch.int32, **{name: t})
+    if t.dim() != 2 or (t.numel() > 0 and t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be [requests, pages] with contiguous rows")
+    return t.stride(0), t.shape[1]
+
+
+def _pool(k: torch.Tensor, v: Optional[torch.Tensor], dims: int, what: str = "pools"):
+    """Strides of a pool [(layers,) pages, page_size, heads, d] that K and V share."""
+    _typed(torch.bfloat16, k_pages=k, v_pages=v)
+    if k.dim() != dims or k.stride(dims - 1) != 1:
+        raise ValueError(f"{what} must be {'[layers, ' if dims == 5 else '['}pages, page_size, heads, d] with contiguous d")
+    if v is not None and (v.shape != k.shape or v.stride() != k.stride()):
+        raise ValueError("K and V must share shape and strides")
+    return k.stride()
+
+
+def paged_attn_workspace_bytes(batch, q_len, n_q_heads, n_kv_heads, head_dim) -> int:
+    return lib().specvlm_paged_attn_workspace_bytes(batch, q_len, n_q_heads, n_kv_heads, head_dim)
+
+
+def paged_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, kv_lens: torch.Tensor,
+               softmax_scale: float, *, cu_q: Optional[torch.Tensor] = None, max_q_len: Optional[int] = None,
+               max_kv_len: Optional[int] = None, window: int = 0, n_sinks: int = 0, ancestor_mask: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None, want_lse: bool = False, workspace: Optional[torch.Tensor] = None):
+    """Attention of every request's block of new tokens, q [sum q_len, H_q, d] bf16, over its cache in pages
+    [pages, page_size, H_kv, d] bf16 -> out like q (and lse fp32).
+
+    page_table int32 [batch, max_pages], kv_lens int32 [batch] (the block included); without cu_q every request has
+    q.shape[0] / batch queries, with it max_q_len says the most.  max_kv_len: the most that kv_lens may hold (the whole
+    table's worth by default).  window > 0: a query sees that many tokens up to its own, and the first n_sinks.
+    ancestor_mask int64/uint64 [sum q_len]: a draft tree's, as in tree_attn."""
+    _on_device(q=q, k_pages=k_pages, v_pages=v_pages, page_table=page_table, kv_lens=kv_lens, cu_q=cu_q,
+               ancestor_mask=ancestor_mask, out=out, workspace=workspace)
+    _typed(torch.bfloat16, q=q, out=out)
+    (page, tok, head, _), (row, max_pages) = _pool(k_pages, v_pages, 4), _table("page_table", page_table)
+    batch, (tq, hq, d), (n_pages, page_size, hkv, kd) = page_table.shape[0], q.shape, k_pages.shape
+    if kd != d:
+        raise ValueError("q and the pages must have one head dimension")
+    _int32s(batch, kv_lens=kv_lens)
+    if cu_q is None:
+        if batch and tq % batch:
+            raise ValueError("without cu_q every request has as many queries")
+        q_len = tq // batch if batch else 0
+    else:
+        _int32s(batch + 1, cu_q=cu_q)
+        if max_q_len is None:
+            raise ValueError("max_q_len is required with cu_q")
+        q_len = max_q_len
+    kv_len = max_pages * page_size if max_kv_len is None else max_kv_len
+    if ancestor_mask is not None and (ancestor_mask.dtype not in (torch.int64, torch.uint64) or not ancestor_mask.is_contiguous()
+                                      or ancestor_mask.numel() < tq):
+        raise ValueError("ancestor_mask must be a contiguous int64 or uint64 value for every query")
+    if out is None:
+        out = torch.empty_like(q)
+    if out.shape != q.shape or out.stride() != q.stride():
+        raise ValueError("out must share q's shape and strides")
+    lse = torch.empty((tq, hq), dtype=torch.float32, device=q.device) if want_lse else None
+    if workspace is None:
+        workspace = new_workspace(paged_attn_workspace_bytes(batch, q_len, hq, hkv, d), q.device)
+    q_tok, q_head = _thd(q)
+    rc = lib().specvlm_paged_attn(_ptr(q), q_tok, q_head, _ptr(k_pages), _ptr(v_pages), page, tok, head, n_pages, page_size,
+                                  _ptr(page_table), row, max_pages, _ptr(kv_lens), _ptr(cu_q), batch, q_len, kv_len, hq, hkv, d,
+                                  float(softmax_scale), window, n_sinks, _ptr(ancestor_mask), _ptr(out), _ptr(lse),
+                                  _ptr(workspace), workspace.numel(), _stream())
+    _check("specvlm_paged_attn", rc)
+    return (out, lse) if want_lse else out
+
+
+ROPE_SCALINGS = {None: 0, "linear": 1, "base": 2, "by-parts": 3}
+
+
+def rope_turns(rot_dim: int, base: float, *, scaling: Optional[str] = None, factor: float = 1.0, original_len: float = 0.0,
+               beta_fast: float = 32.0, beta_slow: float = 1.0, device=None) -> torch.Tensor:
+    """The frequencies of rotary positions for rope_append: int64 [rot_dim / 2], turns a position in units of 2^-64."""
+    turns = np.zeros(max(rot_dim, 0) // 2, dtype=np.uint64)
+    spec = _RopeSpec(ROPE_SCALINGS[scaling], base, factor, original_len, beta_fast, beta_slow)
+    _check("specvlm_rope_turns", lib().specvlm_rope_turns(rot_dim, C.byref(spec), turns.ctypes.data))
+    return torch.from_numpy(turns.view(np.int64)).to(device or "cuda")
+
+
+def rope_append(k: Optional[torch.Tensor], v: Optional[torch.Tensor], k_pages: Optional[torch.Tensor], v_pages: Optional[torch.Tensor],
+                page_table: Optional[torch.Tensor], kv_lens: Optional[torch.Tensor], *, q: Optional[torch.Tensor] = None,
+                q_out: Optional[torch.Tensor] = None, turns: Optional[torch.Tensor] = None, interleaved: bool = False,
+                magnitude: float = 1.0, positions: Optional[torch.Tensor] = None, cu_q: Optional[torch.Tensor] = None):
+    """The new tokens of every request: q [tokens, H_q, d] and k [tokens, H_kv, d] turned to their positions (turns: from
+    rope_turns, int64 [rot_dim / 2]; None turns nothing), k and v written to the last rows of the requests' caches -> q_out.
+
+    kv_lens counts the new tokens.  positions int32 [tokens] where they are not the places in the cache.  q_out may be q.
+    With k, v and the pages None only q is turned."""
+    one = q if k is None else k
+    if one is None:
+        raise ValueError("neither q nor k")
+    if (k is None) != (v is None):
+        raise ValueError("k and v go together")
+    _on_device(q=q, q_out=q_out, k=k, v=v, turns=turns, positions=positions, cu_q=cu_q, kv_lens=kv_lens, page_table=page_table)
+    _typed(torch.bfloat16, q=q, q_out=q_out, k=k, v=v)
+    n, _, d = one.shape
+    batch = kv_lens.numel() if kv_lens is not None else cu_q.numel() - 1 if cu_q is not None else 1
+    _int32s(batch, kv_lens=kv_lens)
+    _int32s(batch + 1, cu_q=cu_q)
+    _int32s(n, positions=positions)
+    if turns is not None and (turns.dtype not in (torch.int64, torch.uint64) or turns.dim() != 1 or not turns.is_contiguous()):
+        raise ValueError("turns must be a contiguous int64 or uint64 vector")
+    qs = os_ = ks = (0, 0)
+    hq = hkv = 0
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty_like(q)
+        if q.shape[0] != n or q.shape[2] != d or q_out.shape != q.shape:
+            raise ValueError("q, q_out and k must agree in tokens and head dimension")
+        qs, os_, hq = _thd(q), _thd(q_out), q.shape[1]
+    page = tok = head = row = n_pages = page_size = max_pages = 0
+    if k is not None:
+        if k_pages is None or v_pages is None or page_table is None or kv_lens is None:
+            raise ValueError("k and v need pages, a page table and kv_lens")
+        if v.shape != k.shape or v.stride() != k.stride():
+            raise ValueError("K and V must share shape and strides")
+        _on_device(k_pages=k_pages, v_pages=v_pages)
+        (page, tok, head, _), (row, max_pages) = _pool(k_pages, v_pages, 4), _table("page_table", page_table)
+        n_pages, page_size, hkv, pd = k_pages.shape
+        if pd != d or hkv != k.shape[1] or page_table.shape[0] != batch:
+            raise ValueError("k, the pages and the page table must agree in heads, head dimension and requests")
+        ks = _thd(k)
+    rc = lib().specvlm_rope_append(_ptr(q), *qs, _ptr(q_out), *os_, _ptr(k), _ptr(v), *ks, _ptr(k_pages), _ptr(v_pages), page, tok, head,
+                                   n_pages, page_size, _ptr(page_table), row, max_pages, _ptr(kv_lens), _ptr(cu_q), batch, n,
+                                   _ptr(positions), _ptr(turns), 0 if turns is None else 2 * turns.numel(), int(interleaved),
+                                   float(magnitude), hq, hkv, d, _stream())
+    _check("specvlm_rope_append", rc)
+    return q_out
+
+
+def pages_assign(page_table: torch.Tensor, parent: torch.Tensor, keep_len: torch.Tensor, new_len: torch.Tensor, n_pages: int,
+                 page_size: int, *, max_pages: Optional[int] = None, window: int = 0, n_sinks: int = 0,
+                 out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """The next page table: row b goes on from row parent[b] of page_table (-1: from nothing), keeps keep_len[b] tokens and has
+    room for new_len[b]; int32 vectors on the device.
+    -> (table [batch, max_pages], copy_start [batch], copy_rows [batch], ref_counts [n_pages], status [batch]), all int32:
+    copy_rows[b] tokens from copy_start[b] on are to be copied from row parent[b] of the old table to row b of the new one
+    (pages_copy), ref_counts says how many rows hold each page, status is 0, -1 (the row does not fit together) or -5 (too
+    few pages are free)."""
+    _on_device(page_table=page_table, parent=parent, keep_len=keep_len, new_len=new_len, out=out, workspace=workspace)
+    old_row, old_pages = _table("page_table", page_table)
+    batch = parent.numel()
+    _int32s(batch, parent=parent, keep_len=keep_len, new_len=new_len)
+    if max_pages is None:
+        max_pages = old_pages if out is None else out.shape[1]
+    if out is None:
+        out = page_table.new_empty((batch, max_pages))
+    row, width = _table("out", out)
+    if out.shape[0] != batch or width != max_pages:
+        raise ValueError("out must be [batch, max_pages]")
+    if n_pages < 0:
+        raise ValueError("n_pages must not be negative")
+    copies = page_table.new_empty((3, batch))
+    refs = page_table.new_empty(n_pages)
+    if workspace is None:
+        workspace = new_workspace(lib().specvlm_pages_assign_workspace_bytes(batch, n_pages), page_table.device)
+    at = copies.data_ptr()
+    rc = lib().specvlm_pages_assign(_ptr(page_table), old_row, page_table.shape[0], old_pages, _ptr(parent), _ptr(keep_len), _ptr(new_len),
+                                    batch, _ptr(out), row, max_pages, n_pages, page_size, window, n_sinks, at, at + 4 * batch,
+                                    _ptr(refs), at + 8 * batch, _ptr(workspace), workspace.numel(), _stream())
+    _check("specvlm_pages_assign", rc)
+    return out, copies[0], copies[1], refs, copies[2]
+
+
+def pages_copy(k_src: torch.Tensor, v_src: Optional[torch.Tensor], src_table: torch.Tensor, k_dst: torch.Tensor, v_dst: Optional[torch.Tensor],
+               dst_table: torch.Tensor, n_rows: Optional[torch.Tensor], max_rows: int, *, src_row: Optional[torch.Tensor] = None,
+               src_start: Optional[torch.Tensor] = None, dst_start: Optional[torch.Tensor] = None,
+               row_idx: Optional[torch.Tensor] = None, cu_idx: Optional[torch.Tensor] = None) -> None:
+    """Rows between pools [layers, pages, page_size, H_kv, d] bf16, in every layer: for request b (a row of dst_table) and
+    i < n_rows[b] (at most max_rows) token src_start[b] + (row_idx's i-th of the request, or i) of row src_row[b] (b) of
+    src_table goes to token dst_start[b] + i of row b of dst_table.  Vectors are int32 [batch]; row_idx is [batch, entries],
+    or one list cut by cu_idx [batch + 1] (n_rows may then be None).  Source and destination may be one pool if no row moves up."""
+    _on_device(k_src=k_src, v_src=v_src, src_table=src_table, k_dst=k_dst, v_dst=v_dst, dst_table=dst_table, n_rows=n_rows, src_row=src_row,
+               src_start=src_start, dst_start=dst_start, row_idx=row_idx, cu_idx=cu_idx)
+    if (v_src is None) != (v_dst is None):
+        raise ValueError("v_src and v_dst go together")
+    src, dst = _pool(k_src, v_src, 5, "source pools"), _pool(k_dst, v_dst, 5, "destination pools")
+    (src_stride, src_pages), (dst_stride, dst_pages) = _table("src_table", src_table), _table("dst_table", dst_table)
+    layers, _, _, hkv, d = k_src.shape
+    if k_dst.shape[0] != layers or k_dst.shape[3:] != k_src.shape[3:]:
+        raise ValueError("the pools must agree in layers, heads and head dimension")
+    batch = dst_table.shape[0]
+    _int32s(batch, n_rows=n_rows, src_row=src_row, src_start=src_start, dst_start=dst_start)
+    _typed(torch.int32, row_idx=row_idx)
+    idx_stride = 0
+    if cu_idx is not None:
+        _int32s(batch + 1, cu_idx=cu_idx)
+        _int32s(None, row_idx=row_idx)
+    elif row_idx is not None:
+        if row_idx.dim() != 2 or row_idx.shape[0] != batch or row_idx.shape[1] < max_rows or (row_idx.shape[1] > 1 and row_idx.stride(1) != 1):
+            raise ValueError("row_idx must be [batch, at least max_rows] with contiguous rows")
+        idx_stride = row_idx.stride(0)
+    rc = lib().specvlm_pages_copy(_ptr(k_src), _ptr(v_src), *src[:4], k_src.shape[1], k_src.shape[2], _ptr(src_table), src_stride,
+                                  src_table.shape[0], src_pages, _ptr(k_dst), _ptr(v_dst), *dst[:4], k_dst.shape[1], k_dst.shape[2],
+                                  _ptr(dst_table), dst_stride, dst_pages, layers, batch, _ptr(n_rows), max_rows, _ptr(src_row),
+                                  _ptr(src_start), _ptr(dst_start), _ptr(row_idx), idx_stride, _ptr(cu_idx), hkv, d, _stream())
+    _check("specvlm_pages_copy", rc)
 
 
 # -------------------------------------------------------------------------- accept

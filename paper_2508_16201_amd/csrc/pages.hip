@@ -1,0 +1,384 @@
+// specvlm_pages_assign and specvlm_pages_copy: which pages every request holds, and rows moved between pages.
+//
+// Assignment.  Every row of the new table goes on from a prefix of a row of the old one.  Whole pages of the prefix
+// are shared.  The page that it ends in is written next: it stays with one row, the lowest that goes on in it, if no row
+// holds it as a whole page; the others get a page of their own, with rows to copy into it.  With  whole/first(page) =
+// minimum over the rows that keep it of (-1 if it is a whole page there, else the row),  row b keeps its page iff first == b.
+// Free pages (kept by no row) go out lowest first to the lowest rows first: page of rank r to the row whose prefix sum of needs
+// holds r.  Everything is a sum, a minimum or a prefix sum of integers: the order of the atomics does not matter.
+// Bound: launches and round trips (four launches: clear, mark, plan, write); the table is read once, a count a page.
+//
+// Copy.  Bound by HBM: 16 bytes a lane and row, several rows in flight.  Where source and destination are one pool the rows of a
+// request may lie in each other's way: a workgroup then has its columns of all the request's rows, and reads a run of them before
+// it writes it, which is right as long as no row moves up.
+#include "common.h"
+
+#include <climits>
+
+namespace specvlm {
+
+struct AssignParams {
+    const int32_t* old_table;
+    int64_t old_row;
+    const int32_t *parent, *keep_len, *new_len;
+    int32_t* table;
+    int64_t row;
+    int32_t *copy_start, *copy_rows, *ref_counts, *status;
+    int32_t *first, *start, *block_free;        // workspace: [n_pages], [batch + 1], [blocks of pages + 1]
+    int batch, n_old, old_pages, max_pages, n_pages, page_size, window, n_sinks;
+    uint32_t inv_page;
+    int n_blocks;
+    int row_chunks;
+};
+
+constexpr int kAssignThreads = 256;
+constexpr int kPlanThreads = 1024;
+constexpr int kPageBlock = 1024;                 // pages of a block, whose free ones are counted together
+
+// A row of the new table: pages [0, whole) whole, one more if `part`; pages [0, wanted) in the end.
+struct AssignRow { int parent, keep, whole, kept, wanted; bool valid; };
+__device__ __forceinline__ AssignRow assign_row(const AssignParams& p, int b)
+{
+    AssignRow r;
+    r.parent = p.parent[b]; r.keep = p.keep_len[b];
+    const int n = p.new_len[b];
+    // (lengths are compared in pages: a product with the page size might not fit)
+    r.valid = r.parent >= -1 && r.parent < p.n_old && r.keep >= 0 && r.keep <= n && (r.keep == 0 || r.parent >= 0);
+    const QuotRem k = divide(r.valid ? r.keep : 0, p.page_size, p.inv_page), w = divide(r.valid ? n : 0, p.page_size, p.inv_page);
+    r.whole = k.q; r.kept = k.q + (k.r > 0); r.wanted = w.q + (w.r > 0);
+    r.valid = r.valid && r.kept <= p.old_pages && r.wanted <= p.max_pages;
+    if (!r.valid) r.whole = r.kept = r.wanted = 0;
+    return r;
+}
+// Page i of the prefix, or -1: none of the pool's, or hidden for good by the window.
+__device__ __forceinline__ int assign_page(const AssignParams& p, const AssignRow& r, int i)
+{
+    const int id = p.old_table[(int64_t)r.parent * p.old_row + i];
+    if (p.window > 0) {
+        const int64_t begin = (int64_t)i * p.page_size, end = begin + p.page_size;
+        if (end <= (int64_t)r.keep - p.window + 1 && begin >= p.n_sinks) return -1;
+    }
+    return (uint32_t)id < (uint32_t)p.n_pages ? id : -1;
+}
+// Whether row b goes on in another page than the one that its prefix ends in (`page`), and whether it needs one.
+__device__ __forceinline__ bool assign_leaves(const AssignParams& p, int page, int b) { return page >= 0 && p.first[page] != b; }
+
+__global__ __launch_bounds__(kAssignThreads)
+void assign_clear_kernel(const AssignParams p)
+{
+    const int i = blockIdx.x * kAssignThreads + threadIdx.x;
+    if (i < p.n_pages) { p.ref_counts[i] = 0; p.first[i] = INT_MAX; }
+}
+
+__global__ __launch_bounds__(kAssignThreads)
+void assign_mark_kernel(const AssignParams p)
+{
+    const int b = blockIdx.x / p.row_chunks, i = (blockIdx.x % p.row_chunks) * kAssignThreads + threadIdx.x;
+    const AssignRow r = assign_row(p, b);
+    if (i >= r.kept) return;
+    const int page = assign_page(p, r, i);
+    if (page < 0) return;
+    atomicAdd(p.ref_counts + page, 1);
+    atomicMin(p.first + page, i < r.whole ? -1 : b);
+}
+
+// Prefix sum over the workgroup's threads: what is before the thread's x, and the total.
+__device__ __forceinline__ int block_before(int x, int* total, int* s_wave)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int upto = x;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const int y = __shfl_up(upto, d);
+        if (lane >= d) upto += y;
+    }
+    __syncthreads();
+    if (lane == kWave - 1) s_wave[wave] = upto;
+    __syncthreads();
+    int before = upto - x, all = 0;
+    for (int i = 0; i < (int)blockDim.x / kWave; ++i) {
+        if (i < wave) before += s_wave[i];
+        all += s_wave[i];
+    }
+    *total = all;
+    return before;
+}
+
+__global__ __launch_bounds__(kPlanThreads)
+void assign_plan_kernel(const AssignParams p)
+{
+    __shared__ int s_wave[kPlanThreads / kWave];
+    int free = 0;
+    for (int base = 0; base < p.n_blocks; base += kPlanThreads / kWave) {
+        // a wave counts a block of pages
+        const int block = base + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+        int n = 0;
+        if (block < p.n_blocks) {
+#pragma unroll
+            for (int i = 0; i < kPageBlock / kWave; ++i) {
+                const int page = block * kPageBlock + i * kWave + lane;
+                n += page < p.n_pages && p.ref_counts[page] == 0;
+            }
+        }
+        int all;
+        const int before = block_before(n, &all, s_wave);
+        if (block < p.n_blocks && lane == 0) p.block_free[block] = free + before;
+        free += all;
+    }
+    int needed = 0;
+    for (int base = 0; base < p.batch; base += kPlanThreads) {
+        const int b = base + threadIdx.x;
+        AssignRow r = {};
+        int need = 0, all;
+        bool leaves = false;
+        if (b < p.batch) {
+            r = assign_row(p, b);
+            const int page = r.kept > r.whole ? assign_page(p, r, r.whole) : -1;
+            leaves = assign_leaves(p, page, b);
+            need = r.wanted - (page >= 0 && !leaves ? r.kept : r.whole);
+        }
+        const int before = needed + block_before(need, &all, s_wave);
+        needed += all;
+        if (b < p.batch) {
+            const bool fits = need == 0 || before + need <= free, copies = leaves && fits;
+            p.start[b] = before;
+            p.status[b] = !r.valid ? SPECVLM_EINVAL : fits ? SPECVLM_OK : SPECVLM_ENOPAGES;
+            p.copy_start[b] = copies ? r.whole * p.page_size : 0;
+            p.copy_rows[b] = copies ? r.keep - r.whole * p.page_size : 0;
+        }
+    }
+    if (threadIdx.x == 0) { p.start[p.batch] = needed; p.block_free[p.n_blocks] = free; }
+}
+
+// The first workgroups hand out the free pages of a block each, the others write what the rows keep.
+__global__ __launch_bounds__(kAssignThreads)
+void assign_write_kernel(const AssignParams p)
+{
+    __shared__ int s_wave[kAssignThreads / kWave];
+    const int free = p.block_free[p.n_blocks];
+    if ((int)blockIdx.x < p.n_blocks) {
+        constexpr int EACH = kPageBlock / kAssignThreads;
+        const int block = blockIdx.x, before = p.block_free[block], needed = p.start[p.batch];
+        if (before >= needed) return;
+        const int page0 = block * kPageBlock + threadIdx.x * EACH;
+        bool is_free[EACH];
+        int n = 0, all;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            is_free[i] = page0 + i < p.n_pages && p.ref_counts[page0 + i] == 0;
+            n += is_free[i];
+        }
+        int rank = before + block_before(n, &all, s_wave);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            if (!is_free[i]) continue;
+            if (rank >= needed) break;
+            int lo = 0, hi = p.batch;                // the last row that starts at or before the rank
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (p.start[mid] <= rank) lo = mid; else hi = mid;
+            }
+            const int need = p.start[lo + 1] - p.start[lo];
+            if (p.start[lo] + need <= free) {
+                p.table[(int64_t)lo * p.row + assign_row(p, lo).wanted - need + rank - p.start[lo]] = page0 + i;
+                p.ref_counts[page0 + i] = 1;
+            }
+            ++rank;
+        }
+        return;
+    }
+    const int w = blockIdx.x - p.n_blocks, b = w / p.row_chunks, i = (w % p.row_chunks) * kAssignThreads + threadIdx.x;
+    if (i >= p.max_pages) return;
+    const AssignRow r = assign_row(p, b);
+    const int need = p.start[b + 1] - p.start[b];
+    if (i >= r.wanted - need && i < r.wanted && p.start[b] + need <= free) {
+        // (handed out by the others; a page that the row leaves has one row less)
+        if (i == r.whole && r.kept > r.whole) {
+            const int page = assign_page(p, r, i);
+            if (page >= 0) atomicSub(p.ref_counts + page, 1);
+        }
+        return;
+    }
+    int page = -1;
+    if (i < r.kept) {
+        page = assign_page(p, r, i);
+        if (i == r.whole && assign_leaves(p, page, b)) {             // (no page was left for it)
+            atomicSub(p.ref_counts + page, 1);
+            page = -1;
+        }
+    }
+    p.table[(int64_t)b * p.row + i] = page;
+}
+
+// ------------------------------------------------------------------------------------------------------- copy ----
+struct CopySide { int64_t layer, page, tok, head; const int32_t* table; int64_t row; int n_pages, page_size, max_pages; uint32_t inv_page; };
+struct CopyParams {
+    const __bf16 *k_src, *v_src;
+    __bf16 *k_dst, *v_dst;
+    CopySide src, dst;
+    const int32_t *src_row, *n_rows, *src_start, *dst_start, *row_idx, *cu_idx;
+    int64_t idx_stride;
+    int max_rows, n_table_rows, n_layers, batch, n_mats;
+    int pieces, head_pieces, slices, row_blocks;     // 16-byte pieces of a row and of a head; workgroups that share them; workgroups over the rows
+    uint32_t inv_head;
+};
+
+constexpr int kCopyThreads = 256, kCopyEach = 4;     // rows of a thread that are in flight together
+
+// Where row `token` begins, or -1: it has no page.
+__device__ __forceinline__ int64_t copy_row_at(const CopySide& s, int request, int64_t token)
+{
+    if (token < 0 || token > INT_MAX) return -1;
+    const QuotRem at = divide((int)token, s.page_size, s.inv_page);
+    const int id = at.q < s.max_pages ? s.table[(int64_t)request * s.row + at.q] : -1;
+    return (uint32_t)id < (uint32_t)s.n_pages ? id * s.page + at.r * s.tok : -1;
+}
+
+// IN_PLACE: a workgroup goes over all rows of its request, in order.
+template <bool IN_PLACE>
+__global__ __launch_bounds__(kCopyThreads)
+void pages_copy_kernel(const CopyParams p)
+{
+    const int b = blockIdx.y, layer = blockIdx.z / p.n_mats, mat = blockIdx.z % p.n_mats;
+    const int slice = blockIdx.x % p.slices, block = blockIdx.x / p.slices;
+    const int first = p.cu_idx ? p.cu_idx[b] : 0;
+    int n = p.max_rows;
+    if (p.cu_idx) n = min(n, p.cu_idx[b + 1] - first);
+    if (p.n_rows) n = min(n, p.n_rows[b]);
+    const int from = p.src_row ? p.src_row[b] : b;
+    const bool there = from >= 0 && from < p.n_table_rows;
+    const int32_t* const idx = p.row_idx ? p.row_idx + (p.cu_idx ? (int64_t)first : b * p.idx_stride) : nullptr;
+    const int64_t src0 = p.src_start ? p.src_start[b] : 0, dst0 = p.dst_start ? p.dst_start[b] : 0;
+    // the lanes lie over the pieces of a row, several rows at once where a row is short
+    const int per_row = min(p.pieces, kCopyThreads), rows = kCopyThreads / per_row;
+    const int lane_row = threadIdx.x / per_row, piece = slice * kCopyThreads + threadIdx.x % per_row;
+    const bool on = lane_row < rows && piece < p.pieces;
+    const QuotRem at = divide(piece, p.head_pieces, p.inv_head);
+    const __bf16* const src = (mat ? p.v_src : p.k_src) + layer * p.src.layer + at.q * p.src.head + at.r * 8;
+    __bf16* const dst = (mat ? p.v_dst : p.k_dst) + layer * p.dst.layer + at.q * p.dst.head + at.r * 8;
+    const int step = rows * kCopyEach;
+    for (int i0 = block * step; i0 < n; i0 += IN_PLACE ? step : step * p.row_blocks) {
+        u32x4 x[kCopyEach];
+        int64_t to[kCopyEach];
+#pragma unroll
+        for (int e = 0; e < kCopyEach; ++e) {
+            const int i = i0 + e * rows + lane_row;
+            to[e] = -1;
+            x[e] = u32x4{0u, 0u, 0u, 0u};
+            if (on && i < n) {
+                to[e] = copy_row_at(p.dst, b, dst0 + i);
+                const int64_t s = there ? copy_row_at(p.src, from, src0 + (idx ? idx[i] : i)) : -1;
+                if (to[e] >= 0 && s >= 0) x[e] = *reinterpret_cast<const u32x4*>(src + s);
+            }
+        }
+        if constexpr (IN_PLACE) __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kCopyEach; ++e)
+            if (to[e] >= 0) *reinterpret_cast<u32x4*>(dst + to[e]) = x[e];
+        if constexpr (IN_PLACE) __syncthreads();
+    }
+}
+
+}  // namespace specvlm
+
+using namespace specvlm;
+
+static int assign_blocks(int n_pages) { return (n_pages + kPageBlock - 1) / kPageBlock; }
+
+extern "C" size_t specvlm_pages_assign_workspace_bytes(int batch, int n_pages)
+{
+    if (batch <= 0 || n_pages < 0) return 0;
+    return align256(sizeof(int32_t) * (size_t)n_pages) + align256(sizeof(int32_t) * ((size_t)batch + 1)) +
+           align256(sizeof(int32_t) * ((size_t)assign_blocks(n_pages) + 1));
+}
+
+extern "C" int specvlm_pages_assign(
+    const int32_t* old_table, int64_t old_stride, int old_rows, int old_max_pages,
+    const int32_t* parent, const int32_t* keep_len, const int32_t* new_len, int batch,
+    int32_t* page_table, int64_t table_stride, int max_pages, int n_pages, int page_size, int window, int n_sinks,
+    int32_t* copy_start, int32_t* copy_rows, int32_t* ref_counts, int32_t* status,
+    void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (old_rows < 0 || old_max_pages < 0 || batch < 0 || max_pages < 0 || n_pages < 0 || page_size <= 0 || window < 0 || n_sinks < 0 ||
+        old_stride < 0)
+        return SPECVLM_EINVAL;
+    if (page_size % 16) return SPECVLM_EUNSUPPORTED;
+    if (batch == 0) return SPECVLM_OK;
+    if (!parent || !keep_len || !new_len || !copy_start || !copy_rows || !status || (!ref_counts && n_pages > 0)) return SPECVLM_EINVAL;
+    if ((!old_table && old_rows > 0 && old_max_pages > 0) || (!page_table && max_pages > 0)) return SPECVLM_EINVAL;
+    if (batch > 1 && table_stride < max_pages) return SPECVLM_EINVAL;                  // (rows that overlap)
+    const int most = old_max_pages > max_pages ? old_max_pages : max_pages;
+    const int chunks = most ? (most + kAssignThreads - 1) / kAssignThreads : 1;
+    if ((int64_t)batch * max_pages > INT_MAX / 2 || (int64_t)batch * chunks + assign_blocks(n_pages) > INT_MAX / 2) return SPECVLM_EUNSUPPORTED;
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < specvlm_pages_assign_workspace_bytes(batch, n_pages)) return SPECVLM_EWORKSPACE;
+
+    AssignParams p;
+    p.old_table = old_table; p.old_row = old_stride; p.parent = parent; p.keep_len = keep_len; p.new_len = new_len;
+    p.table = page_table; p.row = table_stride;
+    p.copy_start = copy_start; p.copy_rows = copy_rows; p.ref_counts = ref_counts; p.status = status;
+    p.first = (int32_t*)workspace;
+    p.start = (int32_t*)((char*)p.first + align256(sizeof(int32_t) * (size_t)n_pages));
+    p.block_free = (int32_t*)((char*)p.start + align256(sizeof(int32_t) * ((size_t)batch + 1)));
+    p.batch = batch; p.n_old = old_rows; p.old_pages = old_max_pages; p.max_pages = max_pages;
+    p.n_pages = n_pages; p.page_size = page_size; p.window = window; p.n_sinks = n_sinks;
+    p.inv_page = reciprocal(page_size);
+    p.n_blocks = assign_blocks(n_pages);
+    p.row_chunks = chunks;
+    hipStream_t s = (hipStream_t)stream;
+    int rc;
+    if (n_pages) {
+        hipLaunchKernelGGL(assign_clear_kernel, dim3((n_pages + kAssignThreads - 1) / kAssignThreads), dim3(kAssignThreads), 0, s, p);
+        if ((rc = launch_status()) != SPECVLM_OK) return rc;
+        hipLaunchKernelGGL(assign_mark_kernel, dim3(batch * chunks), dim3(kAssignThreads), 0, s, p);
+        if ((rc = launch_status()) != SPECVLM_OK) return rc;
+    }
+    hipLaunchKernelGGL(assign_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p);
+    if ((rc = launch_status()) != SPECVLM_OK) return rc;
+    hipLaunchKernelGGL(assign_write_kernel, dim3(p.n_blocks + batch * chunks), dim3(kAssignThreads), 0, s, p);
+    return launch_status();
+}
+
+extern "C" int specvlm_pages_copy(
+    const void* k_src, const void* v_src, int64_t src_layer_stride, int64_t src_page_stride, int64_t src_tok_stride, int64_t src_head_stride,
+    int src_pages, int src_page_size, const int32_t* src_table, int64_t src_table_stride, int src_rows, int src_max_pages,
+    void* k_dst, void* v_dst, int64_t dst_layer_stride, int64_t dst_page_stride, int64_t dst_tok_stride, int64_t dst_head_stride,
+    int dst_pages, int dst_page_size, const int32_t* dst_table, int64_t dst_table_stride, int dst_max_pages,
+    int n_layers, int batch, const int32_t* n_rows, int max_rows, const int32_t* src_row, const int32_t* src_start,
+    const int32_t* dst_start, const int32_t* row_idx, int64_t idx_stride, const int32_t* cu_idx,
+    int n_kv_heads, int head_dim, void* stream)
+{
+    if (src_pages < 0 || src_rows < 0 || src_max_pages < 0 || dst_pages < 0 || dst_max_pages < 0 || src_page_size <= 0 || dst_page_size <= 0 ||
+        n_layers < 0 || batch < 0 || max_rows < 0 || n_kv_heads <= 0 || src_table_stride < 0 || dst_table_stride < 0 || idx_stride < 0)
+        return SPECVLM_EINVAL;
+    if ((v_src == nullptr) != (v_dst == nullptr)) return SPECVLM_EINVAL;
+    if (cu_idx && !row_idx) return SPECVLM_EINVAL;
+    if ((head_dim != 64 && head_dim != 128) || src_page_size % 16 || dst_page_size % 16) return SPECVLM_EUNSUPPORTED;
+    if (n_layers == 0 || batch == 0 || max_rows == 0) return SPECVLM_OK;
+    if (!k_src || !k_dst || !src_table || !dst_table) return SPECVLM_EINVAL;
+    if (!src_row && src_rows < batch) return SPECVLM_EINVAL;
+    const int64_t strides = src_layer_stride | src_page_stride | src_tok_stride | src_head_stride | dst_layer_stride | dst_page_stride |
+                            dst_tok_stride | dst_head_stride;
+    if ((strides & 7) || (((uintptr_t)k_src | (uintptr_t)v_src | (uintptr_t)k_dst | (uintptr_t)v_dst) & 15)) return SPECVLM_EUNSUPPORTED;
+    const int mats = v_src ? 2 : 1;
+    if (batch > 65535 || (int64_t)n_layers * mats > 65535 || n_kv_heads > (1 << 20)) return SPECVLM_EUNSUPPORTED;
+
+    CopyParams p;
+    p.k_src = (const __bf16*)k_src; p.v_src = (const __bf16*)v_src; p.k_dst = (__bf16*)k_dst; p.v_dst = (__bf16*)v_dst;
+    p.src = {src_layer_stride, src_page_stride, src_tok_stride, src_head_stride, src_table, src_table_stride, src_pages, src_page_size,
+             src_max_pages, reciprocal(src_page_size)};
+    p.dst = {dst_layer_stride, dst_page_stride, dst_tok_stride, dst_head_stride, dst_table, dst_table_stride, dst_pages, dst_page_size,
+             dst_max_pages, reciprocal(dst_page_size)};
+    p.src_row = src_row; p.n_rows = n_rows; p.src_start = src_start; p.dst_start = dst_start; p.row_idx = row_idx; p.cu_idx = cu_idx;
+    p.idx_stride = idx_stride; p.max_rows = max_rows; p.n_table_rows = src_rows; p.n_layers = n_layers; p.batch = batch; p.n_mats = mats;
+    p.head_pieces = head_dim / 8; p.pieces = n_kv_heads * p.head_pieces;
+    p.inv_head = reciprocal(p.head_pieces);
+    p.slices = (p.pieces + kCopyThreads - 1) / kCopyThreads;
+    const int per_row = p.pieces < kCopyThreads ? p.pieces : kCopyThreads, step = kCopyThreads / per_row * kCopyEach;
+    const bool in_place = k_src == k_dst || (v_src && v_src == v_dst);
+    p.row_blocks = in_place ? 1 : (max_rows + step - 1) / step;
+    if ((int64_t)p.row_blocks * p.slices > INT_MAX) return SPECVLM_EUNSUPPORTED;
+    const dim3 grid(p.row_blocks * p.slices, batch, n_layers * mats);
+    if (in_place) hipLaunchKernelGGL((pages_copy_kernel<true>), grid, dim3(kCopyThreads), 0, (hipStream_t)stream, p);
+    else          hipLaunchKernelGGL((pages_copy_kernel<false>), grid, dim3(kCopyThreads), 0, (hipStream_t)stream, p);
+    return launch_status();
+}
