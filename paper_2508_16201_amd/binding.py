@@ -563,6 +563,12 @@ def paged_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, pa
     q.shape[0] / batch queries, with it max_q_len says the most.  max_kv_len: the most that kv_lens may hold (the whole
     table's worth by default).  window > 0: a query sees that many tokens up to its own, and the first n_sinks.
     ancestor_mask int64/uint64 [sum q_len]: a draft tree's, as in tree_attn."""
+    got = (_calls or _load_calls()).paged_attn(q, k_pages, v_pages, page_table, kv_lens, softmax_scale, cu_q, max_q_len, max_kv_len, window, n_sinks,
+                                               ancestor_mask, out, want_lse, workspace)
+    if got is not None:
+        if type(got) is int:
+            _check("specvlm_paged_attn", got)
+        return got
     _on_device(q=q, k_pages=k_pages, v_pages=v_pages, page_table=page_table, kv_lens=kv_lens, cu_q=cu_q,
                ancestor_mask=ancestor_mask, out=out, workspace=workspace)
     _typed(torch.bfloat16, q=q, out=out)
@@ -621,6 +627,11 @@ def rope_append(k: Optional[torch.Tensor], v: Optional[torch.Tensor], k_pages: O
 
     kv_lens counts the new tokens.  positions int32 [tokens] where they are not the places in the cache.  q_out may be q.
     With k, v and the pages None only q is turned."""
+    got = (_calls or _load_calls()).rope_append(k, v, k_pages, v_pages, page_table, kv_lens, q, q_out, turns, interleaved, magnitude, positions, cu_q)
+    if got is not None:
+        if type(got) is int:
+            _check("specvlm_rope_append", got)
+        return None if got is True else got
     one = q if k is None else k
     if one is None:
         raise ValueError("neither q nor k")
@@ -672,6 +683,11 @@ def pages_assign(page_table: torch.Tensor, parent: torch.Tensor, keep_len: torch
     copy_rows[b] tokens from copy_start[b] on are to be copied from row parent[b] of the old table to row b of the new one
     (pages_copy), ref_counts says how many rows hold each page, status is 0, -1 (the row does not fit together) or -5 (too
     few pages are free)."""
+    got = (_calls or _load_calls()).pages_assign(page_table, parent, keep_len, new_len, n_pages, page_size, max_pages, window, n_sinks, out, workspace)
+    if got is not None:
+        if type(got) is int:
+            _check("specvlm_pages_assign", got)
+        return got
     _on_device(page_table=page_table, parent=parent, keep_len=keep_len, new_len=new_len, out=out, workspace=workspace)
     old_row, old_pages = _table("page_table", page_table)
     batch = parent.numel()
@@ -705,6 +721,12 @@ def pages_copy(k_src: torch.Tensor, v_src: Optional[torch.Tensor], src_table: to
     i < n_rows[b] (at most max_rows) token src_start[b] + (row_idx's i-th of the request, or i) of row src_row[b] (b) of
     src_table goes to token dst_start[b] + i of row b of dst_table.  Vectors are int32 [batch]; row_idx is [batch, entries],
     or one list cut by cu_idx [batch + 1] (n_rows may then be None).  Source and destination may be one pool if no row moves up."""
+    got = (_calls or _load_calls()).pages_copy(k_src, v_src, src_table, k_dst, v_dst, dst_table, n_rows, max_rows, src_row, src_start, dst_start,
+                                               row_idx, cu_idx)
+    if got is not None:
+        if type(got) is int:
+            _check("specvlm_pages_copy", got)
+        return
     _on_device(k_src=k_src, v_src=v_src, src_table=src_table, k_dst=k_dst, v_dst=v_dst, dst_table=dst_table, n_rows=n_rows, src_row=src_row,
                src_start=src_start, dst_start=dst_start, row_idx=row_idx, cu_idx=cu_idx)
     if (v_src is None) != (v_dst is None):

@@ -10,6 +10,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/headeronly/version.h>
 
@@ -30,11 +31,18 @@ decltype(&specvlm_gather_kv) c_gather_kv;
 decltype(&specvlm_decode_attn) c_decode_attn;
 decltype(&specvlm_tree_attn) c_tree_attn;
 decltype(&specvlm_decode_attn_workspace_bytes) c_attn_bytes;
+decltype(&specvlm_paged_attn) c_paged_attn;
+decltype(&specvlm_paged_attn_workspace_bytes) c_paged_bytes;
+decltype(&specvlm_rope_append) c_rope_append;
+decltype(&specvlm_pages_assign) c_pages_assign;
+decltype(&specvlm_pages_assign_workspace_bytes) c_assign_bytes;
+decltype(&specvlm_pages_copy) c_pages_copy;
 
 // A call's arguments.  What reads one that is not plain clears `plain` and gets nothing; a function looks at it before it uses what it read.
 struct Args {
     PyObject* const* o;
     bool plain = true;
+    int current = -1;
 
     bool none(int i) const { return o[i] == Py_None; }
     const at::Tensor* tensor(int i)
@@ -57,6 +65,44 @@ struct Args {
         if (!t || t->dim() == dims) return t;
         plain = false;
         return nullptr;
+    }
+    // what the paged functions ask of a tensor besides: its type, and that it lies on the current device
+    const at::Tensor* tensor(int i, int dims, at::ScalarType type)
+    {
+        const at::Tensor* const t = tensor(i, dims);
+        if (t && (t->scalar_type() != type || t->get_device() != device())) plain = false;
+        return plain ? t : nullptr;
+    }
+    int device()
+    {
+        if (current < 0) current = c10::hip::current_device();
+        return current;
+    }
+    const int32_t* vector(int i, int64_t n)          // contiguous int32 of n entries (null for None)
+    {
+        const at::Tensor* const t = none(i) ? nullptr : tensor(i, 1, at::kInt);
+        if (!t) return nullptr;
+        if (t->size(0) != n || !t->is_contiguous()) plain = false;
+        return (const int32_t*)t->data_ptr();
+    }
+    const at::Tensor* table(int i)                   // int32 with contiguous rows
+    {
+        const at::Tensor* const t = tensor(i, 2, at::kInt);
+        if (t && t->stride(1) != 1) plain = false;
+        return plain ? t : nullptr;
+    }
+    const at::Tensor* pool(int k, int v, int dims)   // the keys', whose shape and strides the values (or None) share
+    {
+        const at::Tensor *const kt = tensor(k, dims, at::kBFloat16), *const vt = none(v) ? nullptr : tensor(v, dims, at::kBFloat16);
+        if (plain && (kt->stride(dims - 1) != 1 || (vt && (vt->sizes() != kt->sizes() || vt->strides() != kt->strides())))) plain = false;
+        return plain ? kt : nullptr;
+    }
+    const void* words(int i, int64_t least)          // contiguous 64-bit integers, as many or more (null for None)
+    {
+        const at::Tensor* const t = none(i) ? nullptr : tensor(i);
+        if (!t) return nullptr;
+        if (t->scalar_type() != at::kLong || !t->is_contiguous() || t->numel() < least || t->get_device() != device()) plain = false;
+        return t->data_ptr();
     }
     void* ptr(int i)                     // (null for None)
     {
@@ -297,6 +343,121 @@ PyObject* decode_attn(Args& a)
     return want_lse ? pair(out.result(), THPVariable_Wrap(*lse)) : out.result();
 }
 
+// q, k_pages, v_pages, page_table, kv_lens, softmax_scale, cu_q, max_q_len, max_kv_len, window, n_sinks, ancestor_mask, out, want_lse, workspace
+PyObject* paged_attn(Args& a)
+{
+    const at::Tensor *const q = a.tensor(0, 3, at::kBFloat16), *const k = a.pool(1, 2, 4), *const table = a.table(3);
+    if (!a.plain || a.none(2) || a.none(4) || q->stride(2) != 1 || k->size(3) != q->size(2)) return nullptr;
+    const int64_t batch = table->size(0), tq = q->size(0), hq = q->size(1);
+    const int b = a.as_int(batch), h = a.as_int(hq), d = a.as_int(q->size(2)), pages = a.as_int(k->size(0)), ps = a.as_int(k->size(1)),
+              hkv = a.as_int(k->size(2)), width = a.as_int(table->size(1));
+    const int32_t *const lens = a.vector(4, batch), *const cu = a.vector(6, batch + 1);
+    if (batch <= 0 || (!cu && tq % batch)) return nullptr;
+    const int q_len = cu ? a.number(7) : a.as_int(tq / batch), kv_len = a.none(8) ? a.as_int((int64_t)width * ps) : a.number(8);
+    const float scale = (float)a.real(5);
+    const int window = a.number(9), sinks = a.number(10);
+    const uint64_t* const mask = (const uint64_t*)a.words(11, tq);
+    const bool want_lse = a.truth(13);
+    if (!a.none(12)) a.tensor(12, 3, at::kBFloat16);
+    const Out out(a, 12, [&] { return at::empty_like(*q); });
+    if (!a.plain || out.tensor().sizes() != q->sizes() || out.tensor().strides() != q->strides()) return nullptr;
+    std::optional<at::Tensor> lse;
+    if (want_lse) lse = make({tq, hq}, at::kFloat, *q);
+    const Workspace ws(a, 14, *q, [&] { return c_paged_bytes(b, q_len, h, hkv, d); });
+    if (!a.plain || (!a.none(14) && THPVariable_Unpack(a.o[14]).get_device() != a.device())) return nullptr;
+    const int status = call(c_paged_attn, q->data_ptr(), q->stride(0), q->stride(1), k->data_ptr(), THPVariable_Unpack(a.o[2]).data_ptr(), k->stride(0),
+                            k->stride(1), k->stride(2), pages, ps, (const int32_t*)table->data_ptr(), table->stride(0), width, lens, cu, b, q_len, kv_len, h,
+                            hkv, d, scale, window, sinks, mask, out.at, (float*)(lse ? lse->data_ptr() : nullptr), ws.at, ws.bytes);
+    if (status) return PyLong_FromLong(status);
+    return want_lse ? pair(out.result(), THPVariable_Wrap(*lse)) : out.result();
+}
+
+// k, v, k_pages, v_pages, page_table, kv_lens, q, q_out, turns, interleaved, magnitude, positions, cu_q
+PyObject* rope_append(Args& a)           // (with keys and values)
+{
+    const at::Tensor *const k = a.pool(0, 1, 3), *const pages = a.pool(2, 3, 4), *const table = a.table(4);
+    if (!a.plain || a.none(1) || a.none(3) || a.none(5)) return nullptr;
+    const at::Tensor *const q = a.none(6) ? nullptr : a.tensor(6, 3, at::kBFloat16), *const turns = a.none(8) ? nullptr : a.tensor(8, 1);
+    if (!a.plain || (!q && !a.none(7)) || (q && (q->size(0) != k->size(0) || q->size(2) != k->size(2) || q->stride(2) != 1))) return nullptr;
+    const int64_t batch = table->size(0), n = k->size(0);
+    const int b = a.as_int(batch), tokens = a.as_int(n), h = q ? a.as_int(q->size(1)) : 0, hkv = a.as_int(k->size(1)), d = a.as_int(k->size(2)),
+              ids = a.as_int(pages->size(0)), ps = a.as_int(pages->size(1)), width = a.as_int(table->size(1));
+    if (pages->size(2) != hkv || pages->size(3) != d) return nullptr;
+    const int32_t *const lens = a.vector(5, batch), *const at = a.vector(11, n), *const cu = a.vector(12, batch + 1);
+    const uint64_t* const table_of = (const uint64_t*)a.words(8, 0);
+    const int rot = turns ? a.as_int(2 * turns->numel()) : 0;
+    const bool interleaved = a.truth(9);
+    const float magnitude = (float)a.real(10);
+    std::optional<Out> out;
+    if (q) {
+        if (!a.none(7)) a.tensor(7, 3, at::kBFloat16);
+        out.emplace(a, 7, [&] { return at::empty_like(*q); });
+        if (!a.plain || out->tensor().sizes() != q->sizes() || out->tensor().stride(2) != 1) return nullptr;
+    }
+    if (!a.plain) return nullptr;
+    const int status = call(c_rope_append, q ? q->data_ptr() : nullptr, q ? q->stride(0) : 0, q ? q->stride(1) : 0, q ? out->at : nullptr,
+                            q ? out->tensor().stride(0) : 0, q ? out->tensor().stride(1) : 0, k->data_ptr(), THPVariable_Unpack(a.o[1]).data_ptr(), k->stride(0),
+                            k->stride(1), pages->data_ptr(), THPVariable_Unpack(a.o[3]).data_ptr(), pages->stride(0), pages->stride(1), pages->stride(2), ids, ps,
+                            (const int32_t*)table->data_ptr(), table->stride(0), width, lens, cu, b, tokens, at, table_of, rot, (int)interleaved, magnitude, h,
+                            hkv, d);
+    if (status) return PyLong_FromLong(status);
+    return q ? out->result() : Py_NewRef(Py_True);           // (a result that is none: done)
+}
+
+// page_table, parent, keep_len, new_len, n_pages, page_size, max_pages, window, n_sinks, out, workspace
+PyObject* pages_assign(Args& a)
+{
+    const at::Tensor* const old = a.table(0);
+    const at::Tensor* const given = a.none(9) ? nullptr : a.table(9);
+    const at::Tensor* const parent = a.tensor(1, 1, at::kInt);
+    if (!a.plain) return nullptr;
+    const int64_t batch = parent->size(0);
+    const int32_t *const from = a.vector(1, batch), *const keep = a.vector(2, batch), *const now = a.vector(3, batch);
+    const int b = a.as_int(batch), pages = a.number(4), ps = a.number(5), rows = a.as_int(old->size(0)), old_width = a.as_int(old->size(1)),
+              window = a.number(7), sinks = a.number(8);
+    const int width = a.none(6) ? given ? a.as_int(given->size(1)) : old_width : a.number(6);
+    if (!a.plain || !keep || !now || pages < 0 || (given && (given->size(0) != batch || given->size(1) != width))) return nullptr;
+    const Out out(a, 9, [&] { return make({batch, width}, at::kInt, *old); });
+    const Workspace ws(a, 10, *old, [&] { return c_assign_bytes(b, pages); });
+    if (!a.plain || (!a.none(10) && THPVariable_Unpack(a.o[10]).get_device() != a.device())) return nullptr;
+    // (one allocation for what is small: the parts are views of it)
+    const at::Tensor all = make({3 * batch + pages}, at::kInt, *old);
+    int32_t* const at = (int32_t*)all.data_ptr();
+    const int status = call(c_pages_assign, (const int32_t*)old->data_ptr(), old->stride(0), rows, old_width, from, keep, now, b, (int32_t*)out.at,
+                            out.tensor().stride(0), width, pages, ps, window, sinks, at, at + batch, at + 3 * batch, at + 2 * batch, ws.at, ws.bytes);
+    if (status) return PyLong_FromLong(status);
+    PyObject* const t = PyTuple_New(5);
+    if (!t) return nullptr;
+    PyTuple_SET_ITEM(t, 0, out.result());
+    PyTuple_SET_ITEM(t, 1, THPVariable_Wrap(all.narrow(0, 0, batch)));
+    PyTuple_SET_ITEM(t, 2, THPVariable_Wrap(all.narrow(0, batch, batch)));
+    PyTuple_SET_ITEM(t, 3, THPVariable_Wrap(all.narrow(0, 3 * batch, pages)));
+    PyTuple_SET_ITEM(t, 4, THPVariable_Wrap(all.narrow(0, 2 * batch, batch)));
+    return t;
+}
+
+// k_src, v_src, src_table, k_dst, v_dst, dst_table, n_rows, max_rows, src_row, src_start, dst_start, row_idx, cu_idx
+PyObject* pages_copy(Args& a)
+{
+    const at::Tensor *const src = a.pool(0, 1, 5), *const from = a.table(2), *const dst = a.pool(3, 4, 5), *const to = a.table(5);
+    if (!a.plain || a.none(1) != a.none(4) || src->size(0) != dst->size(0) || src->size(3) != dst->size(3) || src->size(4) != dst->size(4)) return nullptr;
+    const int64_t batch = to->size(0);
+    const int32_t *const n = a.vector(6, batch), *const row = a.vector(8, batch), *const src_start = a.vector(9, batch), *const dst_start = a.vector(10, batch);
+    const int most = a.number(7), b = a.as_int(batch), layers = a.as_int(src->size(0)), hkv = a.as_int(src->size(3)), d = a.as_int(src->size(4));
+    const int src_pages = a.as_int(src->size(1)), src_ps = a.as_int(src->size(2)), dst_pages = a.as_int(dst->size(1)), dst_ps = a.as_int(dst->size(2)),
+              rows = a.as_int(from->size(0)), src_width = a.as_int(from->size(1)), dst_width = a.as_int(to->size(1));
+    const at::Tensor* const idx = a.none(11) ? nullptr : a.tensor(11, a.none(12) ? 2 : 1, at::kInt);
+    const int32_t* const cu = a.vector(12, batch + 1);
+    if (!a.plain || (cu && !idx)) return nullptr;
+    if (idx && (cu ? !idx->is_contiguous() : idx->size(0) != batch || idx->size(1) < most || idx->stride(1) != 1)) return nullptr;
+    const int status = call(c_pages_copy, src->data_ptr(), a.none(1) ? nullptr : THPVariable_Unpack(a.o[1]).data_ptr(), src->stride(0), src->stride(1),
+                            src->stride(2), src->stride(3), src_pages, src_ps, (const int32_t*)from->data_ptr(), from->stride(0), rows, src_width, dst->data_ptr(),
+                            a.none(4) ? nullptr : THPVariable_Unpack(a.o[4]).data_ptr(), dst->stride(0), dst->stride(1), dst->stride(2), dst->stride(3), dst_pages,
+                            dst_ps, (const int32_t*)to->data_ptr(), to->stride(0), dst_width, layers, b, n, most, row, src_start, dst_start,
+                            (const int32_t*)(idx ? idx->data_ptr() : nullptr), idx && !cu ? idx->stride(0) : 0, cu, hkv, d);
+    return status ? PyLong_FromLong(status) : Py_NewRef(Py_True);
+}
+
 template <PyObject* (*F)(Args&), Py_ssize_t N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
@@ -320,7 +481,10 @@ struct { const char* name; void** at; } const functions[] = {
     {"specvlm_accept", (void**)&c_accept}, {"specvlm_accept_workspace_bytes", (void**)&c_accept_bytes}, {"specvlm_score", (void**)&c_score},
     {"specvlm_score_workspace_bytes", (void**)&c_score_bytes}, {"specvlm_select", (void**)&c_select}, {"specvlm_top_p_count", (void**)&c_top_p_count},
     {"specvlm_gather_kv", (void**)&c_gather_kv}, {"specvlm_decode_attn", (void**)&c_decode_attn}, {"specvlm_tree_attn", (void**)&c_tree_attn},
-    {"specvlm_decode_attn_workspace_bytes", (void**)&c_attn_bytes}};
+    {"specvlm_decode_attn_workspace_bytes", (void**)&c_attn_bytes}, {"specvlm_paged_attn", (void**)&c_paged_attn},
+    {"specvlm_paged_attn_workspace_bytes", (void**)&c_paged_bytes}, {"specvlm_rope_append", (void**)&c_rope_append},
+    {"specvlm_pages_assign", (void**)&c_pages_assign}, {"specvlm_pages_assign_workspace_bytes", (void**)&c_assign_bytes},
+    {"specvlm_pages_copy", (void**)&c_pages_copy}};
 
 // connect(version, address of every function by its name), once, before any call: the version is the library's, which has to be the one whose
 // header this was compiled with.
@@ -346,7 +510,7 @@ PyObject* connect(PyObject*, PyObject* const* args, Py_ssize_t n)
 PyMethodDef methods[] = {
     {"connect", (PyCFunction)(void (*)())connect, METH_FASTCALL, nullptr},
     SPECVLM_CALL(accept, 8), SPECVLM_CALL(score, 11), SPECVLM_CALL(select, 9), SPECVLM_CALL(top_p_count, 6), SPECVLM_CALL(gather_kv, 10),
-    SPECVLM_CALL(decode_attn, 13),
+    SPECVLM_CALL(decode_attn, 13), SPECVLM_CALL(paged_attn, 15), SPECVLM_CALL(rope_append, 13), SPECVLM_CALL(pages_assign, 11), SPECVLM_CALL(pages_copy, 13),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
