@@ -6,7 +6,7 @@
 // minimum over the rows that keep it of (-1 if it is a whole page there, else the row),  row b keeps its page iff first == b.
 // Free pages (kept by no row) go out lowest first to the lowest rows first: page of rank r to the row whose prefix sum of needs
 // holds r.  Everything is a sum, a minimum or a prefix sum of integers: the order of the atomics does not matter.
-// Bound: launches and round trips (four launches: clear, mark, plan, write); the table is read once, a count a page.
+// Bound: launches and round trips (one launch where a workgroup can do it, else four: clear, mark, plan, write).
 //
 // Copy.  Bound by HBM: 16 bytes a lane and row, several rows in flight.  Where source and destination are one pool the rows of a
 // request may lie in each other's way: a workgroup then has its columns of all the request's rows, and reads a run of them before
@@ -34,6 +34,7 @@ struct AssignParams {
 constexpr int kAssignThreads = 256;
 constexpr int kPlanThreads = 1024;
 constexpr int kPageBlock = 1024;                 // pages of a block, whose free ones are counted together
+constexpr int kSmallRows = kPlanThreads, kSmallPages = 12288, kSmallEntries = 1 << 14;     // what one workgroup takes
 
 // A row of the new table: pages [0, whole) whole, one more if `part`; pages [0, wanted) in the end.
 struct AssignRow { int parent, keep, whole, kept, wanted; bool valid; };
@@ -104,50 +105,55 @@ __device__ __forceinline__ int block_before(int x, int* total, int* s_wave)
     return before;
 }
 
-__global__ __launch_bounds__(kPlanThreads)
+// Free pages of every block; the last workgroup has the rows: what each needs, and the sum of the needs before it.
+__global__ __launch_bounds__(kAssignThreads)
 void assign_plan_kernel(const AssignParams p)
 {
-    __shared__ int s_wave[kPlanThreads / kWave];
-    int free = 0;
-    for (int base = 0; base < p.n_blocks; base += kPlanThreads / kWave) {
-        // a wave counts a block of pages
-        const int block = base + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-        int n = 0;
-        if (block < p.n_blocks) {
+    __shared__ int s_wave[kAssignThreads / kWave];
+    if ((int)blockIdx.x < p.n_blocks) {
+        int n = 0, all;
 #pragma unroll
-            for (int i = 0; i < kPageBlock / kWave; ++i) {
-                const int page = block * kPageBlock + i * kWave + lane;
-                n += page < p.n_pages && p.ref_counts[page] == 0;
-            }
+        for (int i = 0; i < kPageBlock / kAssignThreads; ++i) {
+            const int page = blockIdx.x * kPageBlock + i * kAssignThreads + threadIdx.x;
+            n += page < p.n_pages && p.ref_counts[page] == 0;
         }
-        int all;
-        const int before = block_before(n, &all, s_wave);
-        if (block < p.n_blocks && lane == 0) p.block_free[block] = free + before;
-        free += all;
+        block_before(n, &all, s_wave);
+        if (threadIdx.x == 0) p.block_free[blockIdx.x] = all;
+        return;
     }
     int needed = 0;
-    for (int base = 0; base < p.batch; base += kPlanThreads) {
+    for (int base = 0; base < p.batch; base += kAssignThreads) {
         const int b = base + threadIdx.x;
-        AssignRow r = {};
         int need = 0, all;
-        bool leaves = false;
         if (b < p.batch) {
-            r = assign_row(p, b);
+            const AssignRow r = assign_row(p, b);
             const int page = r.kept > r.whole ? assign_page(p, r, r.whole) : -1;
-            leaves = assign_leaves(p, page, b);
-            need = r.wanted - (page >= 0 && !leaves ? r.kept : r.whole);
+            need = r.wanted - (page >= 0 && !assign_leaves(p, page, b) ? r.kept : r.whole);
         }
         const int before = needed + block_before(need, &all, s_wave);
         needed += all;
-        if (b < p.batch) {
-            const bool fits = need == 0 || before + need <= free, copies = leaves && fits;
-            p.start[b] = before;
-            p.status[b] = !r.valid ? SPECVLM_EINVAL : fits ? SPECVLM_OK : SPECVLM_ENOPAGES;
-            p.copy_start[b] = copies ? r.whole * p.page_size : 0;
-            p.copy_rows[b] = copies ? r.keep - r.whole * p.page_size : 0;
-        }
+        if (b < p.batch) p.start[b] = before;
     }
-    if (threadIdx.x == 0) { p.start[p.batch] = needed; p.block_free[p.n_blocks] = free; }
+    if (threadIdx.x == 0) p.start[p.batch] = needed;
+}
+
+// What the plan says of a row.
+__device__ __forceinline__ void assign_tell(const AssignParams& p, const AssignRow& r, int b, bool leaves, bool fits)
+{
+    const bool copies = leaves && fits;
+    p.status[b] = !r.valid ? SPECVLM_EINVAL : fits ? SPECVLM_OK : SPECVLM_ENOPAGES;
+    p.copy_start[b] = copies ? r.whole * p.page_size : 0;
+    p.copy_rows[b] = copies ? r.keep - r.whole * p.page_size : 0;
+}
+// The row that gets the free page of this rank: the last that starts at or before it.
+__device__ __forceinline__ int assign_owner(const int32_t* start, int batch, int rank)
+{
+    int lo = 0, hi = batch;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] <= rank) lo = mid; else hi = mid;
+    }
+    return lo;
 }
 
 // The first workgroups hand out the free pages of a block each, the others write what the rows keep.
@@ -155,12 +161,25 @@ __global__ __launch_bounds__(kAssignThreads)
 void assign_write_kernel(const AssignParams p)
 {
     __shared__ int s_wave[kAssignThreads / kWave];
-    const int free = p.block_free[p.n_blocks];
-    if ((int)blockIdx.x < p.n_blocks) {
+    const bool hands_out = (int)blockIdx.x < p.n_blocks;
+    // free pages: all of them, and those of the blocks before
+    int before = 0, free = 0;
+    {
+        int n = 0, m = 0, all;
+        for (int i = threadIdx.x; i < p.n_blocks; i += kAssignThreads) {
+            const int f = p.block_free[i];
+            n += f;
+            m += i < (int)blockIdx.x ? f : 0;
+        }
+        block_before(n, &all, s_wave);
+        free = all;
+        if (hands_out) { block_before(m, &all, s_wave); before = all; }
+    }
+    if (hands_out) {
         constexpr int EACH = kPageBlock / kAssignThreads;
-        const int block = blockIdx.x, before = p.block_free[block], needed = p.start[p.batch];
+        const int needed = p.start[p.batch];
         if (before >= needed) return;
-        const int page0 = block * kPageBlock + threadIdx.x * EACH;
+        const int page0 = blockIdx.x * kPageBlock + threadIdx.x * EACH;
         bool is_free[EACH];
         int n = 0, all;
 #pragma unroll
@@ -171,16 +190,10 @@ void assign_write_kernel(const AssignParams p)
         int rank = before + block_before(n, &all, s_wave);
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            if (!is_free[i]) continue;
-            if (rank >= needed) break;
-            int lo = 0, hi = p.batch;                // the last row that starts at or before the rank
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (p.start[mid] <= rank) lo = mid; else hi = mid;
-            }
-            const int need = p.start[lo + 1] - p.start[lo];
-            if (p.start[lo] + need <= free) {
-                p.table[(int64_t)lo * p.row + assign_row(p, lo).wanted - need + rank - p.start[lo]] = page0 + i;
+            if (!is_free[i] || rank >= needed) continue;
+            const int b = assign_owner(p.start, p.batch, rank), first = p.start[b], need = p.start[b + 1] - first;
+            if (first + need <= free) {
+                p.table[(int64_t)b * p.row + assign_row(p, b).wanted - need + rank - first] = page0 + i;
                 p.ref_counts[page0 + i] = 1;
             }
             ++rank;
@@ -188,26 +201,81 @@ void assign_write_kernel(const AssignParams p)
         return;
     }
     const int w = blockIdx.x - p.n_blocks, b = w / p.row_chunks, i = (w % p.row_chunks) * kAssignThreads + threadIdx.x;
-    if (i >= p.max_pages) return;
     const AssignRow r = assign_row(p, b);
     const int need = p.start[b + 1] - p.start[b];
-    if (i >= r.wanted - need && i < r.wanted && p.start[b] + need <= free) {
-        // (handed out by the others; a page that the row leaves has one row less)
-        if (i == r.whole && r.kept > r.whole) {
+    const bool fits = need == 0 || p.start[b] + need <= free;
+    if (w % p.row_chunks == 0 && threadIdx.x == 0) {
+        const int page = r.kept > r.whole ? assign_page(p, r, r.whole) : -1;
+        const bool leaves = assign_leaves(p, page, b);
+        if (leaves) atomicSub(p.ref_counts + page, 1);
+        assign_tell(p, r, b, leaves, fits);
+    }
+    if (i >= p.max_pages) return;
+    const bool handed_out = i >= r.wanted - need && i < r.wanted;
+    if (handed_out && fits) return;
+    p.table[(int64_t)b * p.row + i] = i < r.kept && !handed_out ? assign_page(p, r, i) : -1;
+}
+
+// All of it in one workgroup, with the counts in LDS (bound: its round trips; us a call, four launches / this:  @SMALL@).
+__global__ __launch_bounds__(kPlanThreads)
+void assign_small_kernel(const AssignParams p)
+{
+    extern __shared__ int s_all[];
+    int* const refs = s_all;                          // [n_pages]
+    int* const first = refs + p.n_pages;              // [n_pages]
+    int* const start = first + p.n_pages;             // [batch + 1]
+    __shared__ int s_wave[kPlanThreads / kWave];
+    __shared__ AssignRow s_row[kSmallRows];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    constexpr int WAVES = kPlanThreads / kWave;
+    AssignRow mine = {};
+    if (tid < p.batch) s_row[tid] = mine = assign_row(p, tid);
+    for (int i = tid; i < p.n_pages; i += kPlanThreads) { refs[i] = 0; first[i] = INT_MAX; }
+    __syncthreads();
+    for (int b = wave; b < p.batch; b += WAVES) {
+        const AssignRow r = s_row[b];
+        for (int i = lane; i < r.kept; i += kWave) {
             const int page = assign_page(p, r, i);
-            if (page >= 0) atomicSub(p.ref_counts + page, 1);
-        }
-        return;
-    }
-    int page = -1;
-    if (i < r.kept) {
-        page = assign_page(p, r, i);
-        if (i == r.whole && assign_leaves(p, page, b)) {             // (no page was left for it)
-            atomicSub(p.ref_counts + page, 1);
-            page = -1;
+            if (page < 0) continue;
+            atomicAdd(refs + page, 1);
+            atomicMin(first + page, i < r.whole ? -1 : b);
         }
     }
-    p.table[(int64_t)b * p.row + i] = page;
+    __syncthreads();
+    // the rows' needs; the free pages of this thread's share of the pool
+    const int each = (p.n_pages + kPlanThreads - 1) / kPlanThreads, page0 = min(tid * each, p.n_pages), page1 = min(page0 + each, p.n_pages);
+    int n = 0, free, needed, need = 0, page = -1;
+    for (int i = page0; i < page1; ++i) n += refs[i] == 0;
+    if (mine.kept > mine.whole) page = assign_page(p, mine, mine.whole);
+    const bool leaves = page >= 0 && first[page] != tid;
+    need = mine.wanted - (page >= 0 && !leaves ? mine.kept : mine.whole);
+    int rank = block_before(n, &free, s_wave);
+    const int before = block_before(need, &needed, s_wave);
+    if (tid < p.batch) start[tid] = before;
+    if (tid == 0) start[p.batch] = needed;
+    __syncthreads();
+    if (tid < p.batch) assign_tell(p, mine, tid, leaves, need == 0 || before + need <= free);
+    for (int i = page0; i < page1 && rank < needed; ++i) {
+        if (refs[i] != 0) continue;
+        const int b = assign_owner(start, p.batch, rank), begin = start[b], wants = start[b + 1] - begin;
+        if (begin + wants <= free) {
+            p.table[(int64_t)b * p.row + s_row[b].wanted - wants + rank - begin] = i;
+            refs[i] = 1;                              // (nobody else looks at this page any more)
+        }
+        ++rank;
+    }
+    for (int b = wave; b < p.batch; b += WAVES) {
+        const AssignRow r = s_row[b];
+        const int wants = start[b + 1] - start[b];
+        const bool fits = wants == 0 || start[b] + wants <= free;
+        for (int i = lane; i < p.max_pages; i += kWave) {
+            const bool handed_out = i >= r.wanted - wants && i < r.wanted;
+            if (!(handed_out && fits)) p.table[(int64_t)b * p.row + i] = i < r.kept && !handed_out ? assign_page(p, r, i) : -1;
+        }
+    }
+    if (leaves) atomicSub(refs + page, 1);
+    __syncthreads();
+    for (int i = tid; i < p.n_pages; i += kPlanThreads) p.ref_counts[i] = refs[i];
 }
 
 // ------------------------------------------------------------------------------------------------------- copy ----
@@ -223,60 +291,119 @@ struct CopyParams {
     uint32_t inv_head;
 };
 
-constexpr int kCopyThreads = 256, kCopyEach = 4;     // rows of a thread that are in flight together
+constexpr int kCopyThreads = 256;
+constexpr int kCopyEach = 2;
+constexpr int kCopyTarget = 128 * kNumCu;       // workgroups of a launch
+constexpr int64_t kCopyStreamBytes = 64 << 20;  // from this size on a copy is not kept near (the caches that it would fill hold 4 and 256 MB)
 
-// Where row `token` begins, or -1: it has no page.
-__device__ __forceinline__ int64_t copy_row_at(const CopySide& s, int request, int64_t token)
+// The page of a token, and whether there may be one (else the first entry is read for nothing: no branch between the lookups).
+struct CopyToken { int column, row; bool in; };
+__device__ __forceinline__ CopyToken copy_token(const CopySide& s, int64_t token)
 {
-    if (token < 0 || token > INT_MAX) return -1;
-    const QuotRem at = divide((int)token, s.page_size, s.inv_page);
-    const int id = at.q < s.max_pages ? s.table[(int64_t)request * s.row + at.q] : -1;
-    return (uint32_t)id < (uint32_t)s.n_pages ? id * s.page + at.r * s.tok : -1;
+    CopyToken t;
+    t.in = token >= 0 && token <= INT_MAX;
+    const QuotRem at = divide(t.in ? (int)token : 0, s.page_size, s.inv_page);
+    t.in = t.in && at.q < s.max_pages;
+    t.column = t.in ? at.q : 0;
+    t.row = at.r;
+    return t;
 }
 
-// IN_PLACE: a workgroup goes over all rows of its request, in order.
-template <bool IN_PLACE>
+// EACH rows of a thread at once; their places are looked up once and serve every layer of K and V that the workgroup has.
+// IN_PLACE: a workgroup goes over all rows of its request, in order.  STREAM: what is copied is not kept near.
+//   1254 rows of 2 KB in 80 layers (822 MB):  kept near 168 us, not 141;  four rows of a thread 6 us more, 32 workgroups to a CU, with more
+//   layers each, 2 us more, 128 and none that share a lookup 50 us more.
+//   32 pages of 1 to 63 rows of 1 KB in 28 layers, in place:  stores kept near 38 us, not 28 (and loads that are not 35: forks of one row read
+//   one page);  4 rows in 28 layers of 8 requests 3.6 us, with four rows of a thread 3.9.
+template <bool IN_PLACE, bool STREAM>
 __global__ __launch_bounds__(kCopyThreads)
 void pages_copy_kernel(const CopyParams p)
 {
-    const int b = blockIdx.y, layer = blockIdx.z / p.n_mats, mat = blockIdx.z % p.n_mats;
+    constexpr int EACH = kCopyEach;
+    const int b = blockIdx.y;
     const int slice = blockIdx.x % p.slices, block = blockIdx.x / p.slices;
     const int first = p.cu_idx ? p.cu_idx[b] : 0;
     int n = p.max_rows;
     if (p.cu_idx) n = min(n, p.cu_idx[b + 1] - first);
     if (p.n_rows) n = min(n, p.n_rows[b]);
+    // the lanes lie over the pieces of a row, several rows at once where a row is short
+    const int per_row = min(p.pieces, kCopyThreads), rows = kCopyThreads / per_row, step = rows * EACH;
+    if (block * step >= n) return;
     const int from = p.src_row ? p.src_row[b] : b;
-    const bool there = from >= 0 && from < p.n_table_rows;
+    const bool there = from >= 0 && from < p.n_table_rows && p.src.max_pages > 0;
+    const int32_t* const src_table = p.src.table + (there ? from : 0) * p.src.row;
+    const int32_t* const dst_table = p.dst.table + b * p.dst.row;
     const int32_t* const idx = p.row_idx ? p.row_idx + (p.cu_idx ? (int64_t)first : b * p.idx_stride) : nullptr;
     const int64_t src0 = p.src_start ? p.src_start[b] : 0, dst0 = p.dst_start ? p.dst_start[b] : 0;
-    // the lanes lie over the pieces of a row, several rows at once where a row is short
-    const int per_row = min(p.pieces, kCopyThreads), rows = kCopyThreads / per_row;
     const int lane_row = threadIdx.x / per_row, piece = slice * kCopyThreads + threadIdx.x % per_row;
-    const bool on = lane_row < rows && piece < p.pieces;
+    const bool on = lane_row < rows && piece < p.pieces && p.dst.max_pages > 0;
     const QuotRem at = divide(piece, p.head_pieces, p.inv_head);
-    const __bf16* const src = (mat ? p.v_src : p.k_src) + layer * p.src.layer + at.q * p.src.head + at.r * 8;
-    __bf16* const dst = (mat ? p.v_dst : p.k_dst) + layer * p.dst.layer + at.q * p.dst.head + at.r * 8;
-    const int step = rows * kCopyEach;
     for (int i0 = block * step; i0 < n; i0 += IN_PLACE ? step : step * p.row_blocks) {
-        u32x4 x[kCopyEach];
-        int64_t to[kCopyEach];
+        int64_t to[EACH], of[EACH];                   // elements into a layer; -1: no such row
+        int token[EACH];
 #pragma unroll
-        for (int e = 0; e < kCopyEach; ++e) {
-            const int i = i0 + e * rows + lane_row;
-            to[e] = -1;
-            x[e] = u32x4{0u, 0u, 0u, 0u};
-            if (on && i < n) {
-                to[e] = copy_row_at(p.dst, b, dst0 + i);
-                const int64_t s = there ? copy_row_at(p.src, from, src0 + (idx ? idx[i] : i)) : -1;
-                if (to[e] >= 0 && s >= 0) x[e] = *reinterpret_cast<const u32x4*>(src + s);
+        for (int e = 0; e < EACH; ++e) {
+            const int i = min(i0 + e * rows + lane_row, n - 1);
+            token[e] = i;
+            if (idx && i0 + e * rows < n) token[e] = idx[i];
+        }
+        CopyToken s[EACH], d[EACH];
+        int s_id[EACH], d_id[EACH];
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            s[e] = copy_token(p.src, src0 + token[e]);
+            d[e] = copy_token(p.dst, dst0 + i0 + e * rows + lane_row);
+            s_id[e] = d_id[e] = -1;
+            if (i0 + e * rows < n) {
+                if (there) s_id[e] = src_table[s[e].column];
+                if (on) d_id[e] = dst_table[d[e].column];
             }
         }
-        if constexpr (IN_PLACE) __syncthreads();
 #pragma unroll
-        for (int e = 0; e < kCopyEach; ++e)
-            if (to[e] >= 0) *reinterpret_cast<u32x4*>(dst + to[e]) = x[e];
+        for (int e = 0; e < EACH; ++e) {
+            const bool live = on && i0 + e * rows + lane_row < n && d[e].in && (uint32_t)d_id[e] < (uint32_t)p.dst.n_pages;
+            to[e] = live ? d_id[e] * p.dst.page + d[e].row * p.dst.tok + at.q * p.dst.head + at.r * 8 : -1;
+            of[e] = live && s[e].in && (uint32_t)s_id[e] < (uint32_t)p.src.n_pages
+                        ? s_id[e] * p.src.page + s[e].row * p.src.tok + at.q * p.src.head + at.r * 8 : -1;
+        }
+        for (int z = blockIdx.z; z < p.n_layers * p.n_mats; z += gridDim.z) {
+            const int layer = p.n_mats == 2 ? z >> 1 : z;
+            const bool is_v = p.n_mats == 2 && (z & 1);
+            const __bf16* const src = (is_v ? p.v_src : p.k_src) + layer * p.src.layer;
+            __bf16* const dst = (is_v ? p.v_dst : p.k_dst) + layer * p.dst.layer;
+            u32x4 x[EACH];
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                x[e] = u32x4{0u, 0u, 0u, 0u};
+                if (of[e] >= 0) {
+                    if constexpr (STREAM && !IN_PLACE) x[e] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + of[e]));
+                    else x[e] = *reinterpret_cast<const u32x4*>(src + of[e]);
+                }
+            }
+            if constexpr (IN_PLACE) __syncthreads();
+#pragma unroll
+            for (int e = 0; e < EACH; ++e)
+                if (to[e] >= 0) {
+                    if constexpr (STREAM) __builtin_nontemporal_store(x[e], reinterpret_cast<u32x4*>(dst + to[e]));
+                    else *reinterpret_cast<u32x4*>(dst + to[e]) = x[e];
+                }
+        }
         if constexpr (IN_PLACE) __syncthreads();
     }
+}
+
+template <bool IN_PLACE, bool STREAM>
+static int launch_copy(CopyParams& p, hipStream_t stream)
+{
+    const int per_row = p.pieces < kCopyThreads ? p.pieces : kCopyThreads, step = kCopyThreads / per_row * kCopyEach;
+    p.row_blocks = IN_PLACE ? 1 : (p.max_rows + step - 1) / step;
+    if ((int64_t)p.row_blocks * p.slices > INT_MAX) return SPECVLM_EUNSUPPORTED;
+    // layers of K and V that share a workgroup, and its lookups: as many as leave workgroups enough
+    const int64_t each = (int64_t)p.row_blocks * p.slices * p.batch;
+    int64_t z = (kCopyTarget + each - 1) / each;
+    if (z > p.n_layers * p.n_mats) z = p.n_layers * p.n_mats;
+    hipLaunchKernelGGL((pages_copy_kernel<IN_PLACE, STREAM>), dim3(p.row_blocks * p.slices, p.batch, (int)z), dim3(kCopyThreads), 0, stream, p);
+    return launch_status();
 }
 
 }  // namespace specvlm
@@ -326,13 +453,19 @@ extern "C" int specvlm_pages_assign(
     p.row_chunks = chunks;
     hipStream_t s = (hipStream_t)stream;
     int rc;
+    if (batch <= kSmallRows && n_pages <= kSmallPages && (int64_t)batch * most <= kSmallEntries) {
+        constexpr int kMostLds = (2 * kSmallPages + kSmallRows + 1) * (int)sizeof(int);
+        if ((rc = allow_lds<&assign_small_kernel>(kMostLds)) != SPECVLM_OK) return rc;
+        hipLaunchKernelGGL(assign_small_kernel, dim3(1), dim3(kPlanThreads), (2 * n_pages + batch + 1) * sizeof(int), s, p);
+        return launch_status();
+    }
     if (n_pages) {
         hipLaunchKernelGGL(assign_clear_kernel, dim3((n_pages + kAssignThreads - 1) / kAssignThreads), dim3(kAssignThreads), 0, s, p);
         if ((rc = launch_status()) != SPECVLM_OK) return rc;
         hipLaunchKernelGGL(assign_mark_kernel, dim3(batch * chunks), dim3(kAssignThreads), 0, s, p);
         if ((rc = launch_status()) != SPECVLM_OK) return rc;
     }
-    hipLaunchKernelGGL(assign_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p);
+    hipLaunchKernelGGL(assign_plan_kernel, dim3(p.n_blocks + 1), dim3(kAssignThreads), 0, s, p);
     if ((rc = launch_status()) != SPECVLM_OK) return rc;
     hipLaunchKernelGGL(assign_write_kernel, dim3(p.n_blocks + batch * chunks), dim3(kAssignThreads), 0, s, p);
     return launch_status();
@@ -373,12 +506,9 @@ extern "C" int specvlm_pages_copy(
     p.head_pieces = head_dim / 8; p.pieces = n_kv_heads * p.head_pieces;
     p.inv_head = reciprocal(p.head_pieces);
     p.slices = (p.pieces + kCopyThreads - 1) / kCopyThreads;
-    const int per_row = p.pieces < kCopyThreads ? p.pieces : kCopyThreads, step = kCopyThreads / per_row * kCopyEach;
     const bool in_place = k_src == k_dst || (v_src && v_src == v_dst);
-    p.row_blocks = in_place ? 1 : (max_rows + step - 1) / step;
-    if ((int64_t)p.row_blocks * p.slices > INT_MAX) return SPECVLM_EUNSUPPORTED;
-    const dim3 grid(p.row_blocks * p.slices, batch, n_layers * mats);
-    if (in_place) hipLaunchKernelGGL((pages_copy_kernel<true>), grid, dim3(kCopyThreads), 0, (hipStream_t)stream, p);
-    else          hipLaunchKernelGGL((pages_copy_kernel<false>), grid, dim3(kCopyThreads), 0, (hipStream_t)stream, p);
-    return launch_status();
+    hipStream_t s = (hipStream_t)stream;
+    if (in_place) return launch_copy<true, true>(p, s);
+    const bool large = 16.0 * p.pieces * max_rows * batch * n_layers * mats >= kCopyStreamBytes;
+    return large ? launch_copy<false, true>(p, s) : launch_copy<false, false>(p, s);
 }
