@@ -34,7 +34,10 @@ struct AssignParams {
 constexpr int kAssignThreads = 256;
 constexpr int kPlanThreads = 1024;
 constexpr int kPageBlock = 1024;                 // pages of a block, whose free ones are counted together
-constexpr int kSmallRows = kPlanThreads, kSmallPages = 12288, kSmallEntries = 1 << 14;     // what one workgroup takes
+// What one workgroup takes: a wave goes over a row, 64 entries at a time, and over every sixteenth row.  Us a call, four launches / one, by
+// rows, pages a row, pages of the pool:  1 x 100 of 1000 9.75 / 5.0;  8 x 129 of 4096 12.5 / 6.4;  16 x 500 of 6100 13.4 / 9.4;  32 x 240 of 6100 13.5 /
+// 10.0;  128 x 40 of 6100 14.4 / 13.4;  but 64 x 250 of 12200 14.1 / 16.9, 120 x 16 of 12200 14.1 / 17.8, 2 x 3900 of 6100 11.5 / 17.6, 250 x 48 15.2 / 23.6.
+constexpr int kSmallPages = 8192, kSmallTrips = 8, kSmallRows = kSmallTrips * kPlanThreads / kWave;
 
 // A row of the new table: pages [0, whole) whole, one more if `part`; pages [0, wanted) in the end.
 struct AssignRow { int parent, keep, whole, kept, wanted; bool valid; };
@@ -162,19 +165,15 @@ void assign_write_kernel(const AssignParams p)
 {
     __shared__ int s_wave[kAssignThreads / kWave];
     const bool hands_out = (int)blockIdx.x < p.n_blocks;
-    // free pages: all of them, and those of the blocks before
+    // free pages: all of them, and those of the blocks before (each wave for itself: no barrier)
     int before = 0, free = 0;
-    {
-        int n = 0, m = 0, all;
-        for (int i = threadIdx.x; i < p.n_blocks; i += kAssignThreads) {
-            const int f = p.block_free[i];
-            n += f;
-            m += i < (int)blockIdx.x ? f : 0;
-        }
-        block_before(n, &all, s_wave);
-        free = all;
-        if (hands_out) { block_before(m, &all, s_wave); before = all; }
+    for (int i = threadIdx.x & 63; i < p.n_blocks; i += kWave) {
+        const int f = p.block_free[i];
+        free += f;
+        before += i < (int)blockIdx.x ? f : 0;
     }
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) { free += __shfl_xor(free, d); before += __shfl_xor(before, d); }
     if (hands_out) {
         constexpr int EACH = kPageBlock / kAssignThreads;
         const int needed = p.start[p.batch];
@@ -216,7 +215,7 @@ void assign_write_kernel(const AssignParams p)
     p.table[(int64_t)b * p.row + i] = i < r.kept && !handed_out ? assign_page(p, r, i) : -1;
 }
 
-// All of it in one workgroup, with the counts in LDS (bound: its round trips; us a call, four launches / this:  @SMALL@).
+// All of it in one workgroup, with the counts in LDS (bound: its round trips; kSmallPages has both sides' times).
 __global__ __launch_bounds__(kPlanThreads)
 void assign_small_kernel(const AssignParams p)
 {
@@ -453,7 +452,9 @@ extern "C" int specvlm_pages_assign(
     p.row_chunks = chunks;
     hipStream_t s = (hipStream_t)stream;
     int rc;
-    if (batch <= kSmallRows && n_pages <= kSmallPages && (int64_t)batch * most <= kSmallEntries) {
+    constexpr int kWaves = kPlanThreads / kWave;
+    if (n_pages <= kSmallPages && batch <= kSmallRows && most <= kSmallTrips * kWave &&
+        (batch + kWaves - 1) / kWaves * ((most + kWave - 1) / kWave) <= kSmallTrips) {
         constexpr int kMostLds = (2 * kSmallPages + kSmallRows + 1) * (int)sizeof(int);
         if ((rc = allow_lds<&assign_small_kernel>(kMostLds)) != SPECVLM_OK) return rc;
         hipLaunchKernelGGL(assign_small_kernel, dim3(1), dim3(kPlanThreads), (2 * n_pages + batch + 1) * sizeof(int), s, p);

@@ -6,7 +6,7 @@
 // turn, exactly: at position 2^20 a product in 32-bit floating point would be off by 2^20 * 2^-24 rad.  The upper 32 bits of
 // it go to the sine and the cosine.  The products are fp32 and rounded to bf16 once.
 //
-// Bound: every element is read once and written once, HBM for a prompt, the launch for a block.  A lane keeps the sines
+// Bound: every element is read once and written once, HBM for a prompt (5.7 TB/s at 151 MB), the launch for a block (3.3 us for 48 tokens).  A lane keeps the sines
 // and cosines of its eight pairs (two 16-byte pieces of a row) and takes them to row after row of the token.
 #include "common.h"
 
@@ -37,8 +37,26 @@ struct RopeParams {
 };
 
 constexpr int kRopeWaves = 4;
+constexpr int64_t kRopeStreamBytes = 128 << 20;      // read and written
 
-template <int D>
+// Sine and cosine of phase * 2^-32 turns.  The quarter turn nearest is taken off in integers; what is left, at most an eighth of a turn, goes
+// into the Taylor polynomials (first terms left out: x^11 / 11! and x^12 / 12!, below 2^-29 of 1).
+__device__ __forceinline__ void turn_sincos(uint32_t phase, float* sine, float* cosine)
+{
+    const uint32_t quarter = (phase + 0x20000000u) >> 30;
+    const float x = (float)(int32_t)(phase - (quarter << 30)) * 1.46291807926715968105e-9f;      // 2 pi / 2^32
+    const float z = x * x;
+    const float s = fmaf(x * z, fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), x);
+    const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
+    const bool swapped = quarter & 1u;
+    const float a = swapped ? c : s, b = swapped ? s : c;
+    *sine = quarter & 2u ? -a : a;
+    *cosine = (quarter + 1u) & 2u ? -b : b;
+}
+
+// STREAM: results are not kept near, for they would not all stay there (8190 tokens of 28/4 heads of 128, 151 MB 33.4 us kept, 26.4 not;  4096 of
+// 64/8, 168 MB 36.6 / 29.3;  2048, 84 MB 16.5 / 17.3, and what reads them next finds them).
+template <int D, bool STREAM>
 __global__ __launch_bounds__(kRopeWaves * kWave)
 void rope_append_kernel(const RopeParams p)
 {
@@ -75,7 +93,7 @@ void rope_append_kernel(const RopeParams p)
         for (int i = 0; i < 8; ++i) {
             const uint64_t phase = p.turns[8 * u + i] * (uint64_t)(int64_t)pos;
             float s, c;
-            sincospif((float)(int32_t)(phase >> 32) * 0x1p-31f, &s, &c);        // (in half turns)
+            turn_sincos((uint32_t)(phase >> 32), &s, &c);
             cs[i] = c * p.magnitude;
             sn[i] = s * p.magnitude;
         }
@@ -115,8 +133,13 @@ void rope_append_kernel(const RopeParams p)
             x = __builtin_convertvector(na, bf16x8);
             y = __builtin_convertvector(nc, bf16x8);
         }
-        *reinterpret_cast<bf16x8*>(dst + lo) = x;
-        *reinterpret_cast<bf16x8*>(dst + hi) = y;
+        if constexpr (STREAM) {
+            __builtin_nontemporal_store(__builtin_bit_cast(u32x4, x), reinterpret_cast<u32x4*>(dst + lo));
+            __builtin_nontemporal_store(__builtin_bit_cast(u32x4, y), reinterpret_cast<u32x4*>(dst + hi));
+        } else {
+            *reinterpret_cast<bf16x8*>(dst + lo) = x;
+            *reinterpret_cast<bf16x8*>(dst + hi) = y;
+        }
     }
 }
 
@@ -131,7 +154,9 @@ static int launch_rope(RopeParams& p, int n_tokens, hipStream_t stream)
     p.inv_parts = reciprocal(p.parts);
     if ((int64_t)n_tokens * p.parts > 0x7fffffff - kRopeWaves) return SPECVLM_EUNSUPPORTED;
     p.n_waves = n_tokens * p.parts;
-    hipLaunchKernelGGL((rope_append_kernel<D>), dim3((p.n_waves + kRopeWaves - 1) / kRopeWaves), dim3(kRopeWaves * kWave), 0, stream, p);
+    const dim3 grid((p.n_waves + kRopeWaves - 1) / kRopeWaves), block(kRopeWaves * kWave);
+    if ((int64_t)n_tokens * p.rows * D * 4 >= kRopeStreamBytes) hipLaunchKernelGGL((rope_append_kernel<D, true>), grid, block, 0, stream, p);
+    else                                                        hipLaunchKernelGGL((rope_append_kernel<D, false>), grid, block, 0, stream, p);
     return launch_status();
 }
 

@@ -136,6 +136,12 @@ def test_rope_of_a_long_prompt(B):
     check_rope(B, 14, [2100, 1700], [2100, 1600], (28, 4, 128), 16, 128, interleaved=True)
 
 
+def test_rope_of_a_prompt_that_is_not_kept_near(B):
+    n = 3400
+    assert n * (64 + 2 * 8) * 128 * 4 >= 128 << 20
+    check_rope(B, 15, [n + 100], [n], (64, 8, 128), 64, 96)
+
+
 def test_rope_strides(B):
     n, hq, hkv, d, ps = 5, 6, 2, 64, 16
     fused = rnd_bits((n, hq + 2 * hkv, d), 15)                           # q, k and v of a token side by side, as one projection leaves them
@@ -344,6 +350,12 @@ def test_copy_counts_and_rows_that_are_off(B):
     check_copy(B, 5, 2, (2, 64), [64, 64], [64, 64, 64, 64], 16, 16, [40, 20, -3, 2], [0, 60, 0, 0], [10, 5, 0, 50], src_row=[0, 1, 0, 2], max_rows=30, break_tables=broken)
     check_copy(B, 6, 2, (2, 64), [64, 64], [64, 64], 16, 16, [3, 3], [0, 0], [0, 0], idx=[[-5, 70, 3], [2 ** 31 - 1, 63, 64]], max_rows=3)
     check_copy(B, 7, 2, (2, 64), [64, 64], [64, 64], 16, 16, [3, 3], [2 ** 31 - 1, -2], [-1, 2 ** 31 - 2])
+
+
+def test_copy_that_is_not_kept_near(B):
+    idx = [np.arange(0, 1000)[np.random.default_rng(3).random(1000) < 0.9]]
+    assert 2 * 2 * 8 * 128 * 20 * len(idx[0]) >= 64 << 20
+    check_copy(B, 9, 20, (8, 128), [1000], [1000], 16, 64, [len(idx[0])], None, [7], idx=idx)
 
 
 def test_copy_keys_alone_without_starts(B):
