@@ -7,7 +7,8 @@
 // each (16 bits), the output is rounded once.
 //
 // Bound.  Every visible K and V row is read once for up to 64 query rows of a kv head: HBM for long caches, launches and
-// round trips for short ones.
+// round trips for short ones.  More rows than 64 are groups that read the keys again, from the L2, which is their bound: 208 rows (trees of 26 nodes of
+// 64/8 heads) load 520 MB of it in 52 of 62 us.
 //
 // Pages.  A page holds a multiple of 16 keys, so 16 consecutive keys starting at a multiple of 16 lie in one page and
 // one scalar table lookup serves them: the address of a wave-wide load is a scalar base plus a lane offset that never
@@ -22,7 +23,11 @@
 // results that the second launch joins.
 //
 // A workgroup has MB*KS compute waves (row block mb, every KS-th 32-key chunk of a tile) and NLD loader waves that only issue
-// direct-to-LDS loads into a ring of NS tiles (see decode_attn.hip for the matrix formulation and the swizzles).
+// direct-to-LDS loads into a ring of NS tiles (see decode_attn.hip for the matrix formulation and the swizzles).  The two roles plan for
+// themselves, each its own way to its first instruction that matters:  a launch's 6 us over one tile were mostly instructions that it met
+// for the first time.
+#include <type_traits>
+
 #include "attn_tile.h"
 
 namespace specvlm {
@@ -44,7 +49,7 @@ struct PagedParams {
     int n_pages, page_size;
     int batch, q_len, kv_len, n_q_heads, n_kv_heads, group;
     int window, n_sinks;
-    uint32_t inv_page, inv_heads, inv_all_heads, inv_group, inv_rgroups;
+    uint32_t inv_page, inv_heads, inv_all_heads, inv_group, inv_rgroups, inv_groups;
     float scale_log2;
     int n_rgroups, rows_pad, max_groups;
     float* part_o;           // [(groups + batch) * H_kv][rows_pad][D] unnormalised partial outputs
@@ -52,8 +57,13 @@ struct PagedParams {
 };
 
 constexpr int kTileKeys = 64;
+constexpr int kRing = 3;                 // tiles of a ring (four: 0.4 us more a call, no faster for long caches)
 constexpr int kMinRun = 2;               // tiles a group takes at least
 constexpr int kTargetGroups = 256;       // workgroups of a launch
+constexpr int kMostBlocks = 4;           // row blocks of a workgroup: two compute waves on each SIMD
+
+// A word that all lanes of a wave read, of memory that nothing writes meanwhile: by a scalar load.
+__device__ __forceinline__ int uniform_load(const int32_t* at, int i) { return ((const SPECVLM_AS4 int32_t*)(uintptr_t)at)[i]; }
 
 // The keys of a request in the order of the sweep: place x < sinks is key x, the others key x + skip; n places.  Both are multiples of 16.
 struct PagedView { int sinks, skip, n; };
@@ -70,6 +80,17 @@ __device__ __forceinline__ int paged_tiles(const PagedParams& p, int b)
 {
     const int ql = p.cu_q ? p.cu_q[b + 1] - p.cu_q[b] : p.q_len;
     return (paged_view(p, ql, p.kv_lens[b]).n + kTileKeys - 1) / kTileKeys;
+}
+
+// The same for a request that all lanes have in common, and its first query.
+struct PagedRequest { int q0, ql, kvl; };
+__device__ __forceinline__ PagedRequest paged_request(const PagedParams& p, int b)
+{
+    PagedRequest r;
+    r.kvl = uniform_load(p.kv_lens, b);
+    r.q0 = p.cu_q ? uniform_load(p.cu_q, b) : b * p.q_len;
+    r.ql = p.cu_q ? uniform_load(p.cu_q, b + 1) - r.q0 : p.q_len;
+    return r;
 }
 
 __device__ __forceinline__ int wave_prefix(int x, int lane)            // sum over the lanes up to this one
@@ -90,20 +111,70 @@ __device__ __forceinline__ int wave_total(int x)
 // Tiles of the whole batch (all lanes of a wave together).
 __device__ __forceinline__ int paged_total(const PagedParams& p, int lane)
 {
-    if (p.batch == 1) return paged_tiles(p, 0);
     int n = 0;
     for (int c = 0; c < p.batch; c += kWave) n += c + lane < p.batch ? paged_tiles(p, c + lane) : 0;
     return wave_total(n);
 }
 // Tiles that a group takes.
-__device__ __forceinline__ int paged_run(const PagedParams& p, int total) { return max(kMinRun, (total + p.max_groups - 1) / p.max_groups); }
+__device__ __forceinline__ int paged_run(const PagedParams& p, int total) { return max(kMinRun, divide(total + p.max_groups - 1, p.max_groups, p.inv_groups).q); }
 
-template <int D, int MB, int KS, int NS, int NLD, bool STREAM>
-__global__ __launch_bounds__((MB * KS + NLD) * kWave)
+// Places [x0, x0 + 16) of the sweep that hold keys k0.. : bit i is set if a query row sees key k0 + i.  before: keys before the block; seen: the
+// row's mask of the block; hidden_to: the last key that the window hides (-1: none).
+__device__ __forceinline__ uint32_t low_bits(int n) { return (1u << min(max(n, 0), 16)) - 1u; }
+__device__ __forceinline__ uint32_t paged_sees(int k0, int before, int kvl, uint64_t seen, int hidden_to, int n_sinks)
+{
+    const int at = k0 - before;                               // the block's key that k0 is
+    const uint64_t block = at >= 0 ? (at < 64 ? seen >> at : 0) : (at > -16 ? seen << -at : 0);
+    const uint32_t window = low_bits(hidden_to + 1 - k0) & ~low_bits(n_sinks - k0);
+    return ((uint32_t)block | low_bits(-at)) & low_bits(kvl - k0) & ~window;
+}
+
+// The runs of group j, request by request: f(request's number, request, first tile, end, whether that is all of it).  All waves of the
+// workgroup pass here, and a barrier between two of them.
+template <class F>
+__device__ __forceinline__ void paged_walk(const PagedParams& p, int lane, int j, F&& f)
+{
+    // one request: its tiles are the numbering;  more: a prefix sum over the requests, 64 at a time
+    int total, tiles = 0, upto = 0, base = 0;                     // (upto: tiles up to and with the lane's request; base: with all 64)
+    PagedRequest rq = {};
+    if (p.batch == 1) {
+        rq = paged_request(p, 0);
+        total = base = (paged_view(p, rq.ql, rq.kvl).n + kTileKeys - 1) / kTileKeys;
+    } else {
+        total = paged_total(p, lane);
+    }
+    const int run = paged_run(p, total);
+    int x = j * run, c64 = -kWave;
+    const int x_end = min(total, x + run);
+    while (x < x_end) {
+        int b = 0, first = 0, last = total;
+        if (p.batch > 1) {
+            while (x >= base) {
+                c64 += kWave;
+                tiles = c64 + lane < p.batch ? paged_tiles(p, c64 + lane) : 0;
+                upto = base + wave_prefix(tiles, lane);
+                base = __builtin_amdgcn_readlane(upto, kWave - 1);
+            }
+            const int at = __builtin_ctzll(__ballot(upto > x));              // the request that holds tile x
+            last = __builtin_amdgcn_readlane(upto, at);
+            first = last - __builtin_amdgcn_readlane(tiles, at);
+            b = c64 + at;
+            rq = paged_request(p, b);
+        }
+        const int to = min(last, x_end);
+        f(b, rq, x - first, to - first, x == first && to == last);
+        x = to;
+        if (x < x_end) __syncthreads();          // the next piece reuses the ring and the exchange buffer
+    }
+}
+
+// MB: row blocks of 16, one to a compute wave.
+template <int D, int MB, int NLD>
+__global__ __launch_bounds__((MB * 2 + NLD) * kWave)
 void paged_split_kernel(const PagedParams p)
 {
-    constexpr int TK = kTileKeys;
-    constexpr int NW = MB * KS;                  // compute waves (the loader waves come after them)
+    constexpr int TK = kTileKeys, KS = TK / kChunkKeys, NS = kRing;
+    constexpr int NW = MB * KS;                  // compute waves (row block, key split); the loader waves come after them
     constexpr int DJ = D / 16, KK = D / 32, CH = D / 8, ROW_BYTES = D * 2;
     constexpr int KEYS_PER_LOAD = kWave / CH;    // key rows of one wave-wide load (4 or 8)
     constexpr int TILE_BYTES = TK * ROW_BYTES;   // one of K or V
@@ -112,170 +183,169 @@ void paged_split_kernel(const PagedParams p)
     constexpr int GPW = LPW * KEYS_PER_LOAD / 16;        // groups of 16 keys of a loader wave
     constexpr int LPG = 16 / KEYS_PER_LOAD;      // loads per group
     constexpr int LDS_STRIDE = D + 4;
-    static_assert(TK / kChunkKeys == KS, "one chunk of a tile per key-split wave");
-    static_assert(NLD == 2 || NLD == 4, "loader waves");
+    static_assert(NLD == 2 || NLD == 4, "loader waves: half for K, half for V");
+    static_assert(NS >= 3 && NS <= 4, "ring depth");
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool is_loader = wave >= NW;
     const int lw = wave - NW;                    // loader index
-    const int mb = wave % MB, ks = wave / MB;    // (compute waves)
+    const int mb = wave % MB, ks = wave / MB;    // (compute waves) row block, chunk of a tile
     const int r = lane & 15, c = lane >> 4;
 
-    extern __shared__ __align__(16) unsigned char smem[];        // stage s: K tile at s*2*TILE_BYTES, V tile right after it
+    extern __shared__ __align__(1024) unsigned char smem[];      // stage s: K tile at s*2*TILE_BYTES, V tile right after it
     uint32_t* const s_ok = reinterpret_cast<uint32_t*>(smem + NS * 2 * TILE_BYTES);     // per stage a byte per 16 keys: their page is there
 
     const QuotRem head = divide(blockIdx.x, p.n_kv_heads, p.inv_heads), rows_of = divide(head.q, p.n_rgroups, p.inv_rgroups);
     const int g = head.r, row0 = rows_of.r * (MB * 16), j = rows_of.q;
 
-    // loader: this wave's matrix, its first group of a tile, and the lane offsets of the loads of a group
-    const bool is_v = lw >= NLD / 2;
-    const int group0 = (lw % (NLD / 2)) * GPW;
-    const char* const mat = reinterpret_cast<const char*>((is_v ? p.v : p.k) + (int64_t)g * p.head);
-    uint32_t lane_off[LPG];
+    if (is_loader) {
+        // this wave's matrix, its first group of a tile, and the lane offsets of the loads of a group
+        const bool is_v = lw >= NLD / 2;
+        const int group0 = (lw % (NLD / 2)) * GPW;
+        const char* const mat = reinterpret_cast<const char*>((is_v ? p.v : p.k) + (int64_t)g * p.head);
+        uint32_t lane_off[LPG];
 #pragma unroll
-    for (int i = 0; i < LPG; ++i) {
-        const int kl = i * KEYS_PER_LOAD + lane / CH;             // key inside the group
-        const int swz = is_v ? v_swizzle<D>(kl) : (D == 128 ? kl : kl >> 1);
-        lane_off[i] = (uint32_t)kl * (uint32_t)(p.tok * 2) + (uint32_t)((lane % CH) ^ swz) * 16u;
+        for (int i = 0; i < LPG; ++i) {
+            const int kl = i * KEYS_PER_LOAD + lane / CH;             // key inside the group
+            const int swz = is_v ? v_swizzle<D>(kl) : (D == 128 ? kl : kl >> 1);
+            lane_off[i] = (uint32_t)kl * (uint32_t)(p.tok * 2) + (uint32_t)((lane % CH) ^ swz) * 16u;
+        }
+        paged_walk(p, lane, j, [&](const int b, const PagedRequest& rq, const int t_begin, const int t_end, bool) {
+            const PagedView view = paged_view(p, rq.ql, rq.kvl);
+            const int n = view.n, n_tiles = t_end - t_begin;      // >= 1
+            if (row0 >= p.group * rq.ql) return;
+            const SPECVLM_AS4 int32_t* const table = (const SPECVLM_AS4 int32_t*)(uintptr_t)(p.table + (int64_t)b * p.table_row);
+            int id[GPW], row[GPW];                                    // pages of the next tile's groups, and the rows in them
+            auto look_up = [&](int tile) {
+#pragma unroll
+                for (int i = 0; i < GPW; ++i) {
+                    // (places behind the last are masked in the compute: its group of 16 is loaded again)
+                    const int x = min(tile * TK + (group0 + i) * 16, (n - 1) & ~15);
+                    const QuotRem at = divide(x < view.sinks ? x : x + view.skip, p.page_size, p.inv_page);
+                    id[i] = table[at.q];
+                    row[i] = at.r;
+                }
+            };
+            auto issue_tile = [&](int stage) {
+                unsigned char* const st = smem + stage * (2 * TILE_BYTES) + (is_v ? TILE_BYTES : 0) + group0 * 16 * ROW_BYTES;
+                uint32_t ok = 0;
+#pragma unroll
+                for (int i = 0; i < GPW; ++i) {
+                    // (a page that is not one of the pool's is not read: the pool's first is, and its keys are masked)
+                    const bool there = (uint32_t)id[i] < (uint32_t)p.n_pages;
+                    ok |= (there ? 1u : 0u) << (8 * i);
+                    const char* const src = mat + 2 * ((there ? id[i] : 0) * p.page + row[i] * p.tok);
+#pragma unroll
+                    for (int l = 0; l < LPG; ++l)
+                        __builtin_amdgcn_global_load_lds((const SPECVLM_AS1 void*)(src + lane_off[l]),
+                                                         (SPECVLM_AS3 void*)(st + (i * LPG + l) * 1024), 16, 0, 2);
+                }
+                if (!is_v && lane == 0) {
+                    if constexpr (GPW == 4) s_ok[stage] = ok;
+                    else reinterpret_cast<uint16_t*>(s_ok + stage)[lw] = (uint16_t)ok;
+                }
+            };
+            const int n_load = n_tiles > NS - 1 ? n_tiles : NS - 1;   // (a run shorter than the ring loads its last tile again)
+            int i = 1 - NS, stage = 0;
+            look_up(t_begin);
+            do {
+                if (i >= 0) {
+                    const int younger = min(NS - 2, n_load - 1 - i);  // tiles in flight behind tile i
+                    wait_vmcnt<(NS - 2) * LPW>();
+                    if constexpr (NS >= 4) { if (younger <= 1) wait_vmcnt<1 * LPW>(); }
+                    if (younger <= 0) wait_vmcnt<0>();
+                    __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the bytes of s_ok are written
+                    stage_barrier();                                  // tile i landed for everyone; the stage of tile i-1 is free
+                }
+                if (i + NS - 1 < n_load) {
+                    issue_tile(stage);
+                    look_up(t_begin + min(i + NS, n_tiles - 1));
+                    stage = stage == NS - 1 ? 0 : stage + 1;
+                }
+            } while (++i < n_tiles);
+            wait_vmcnt<0>();                                          // (spare copies may still be landing)
+            __syncthreads();                                      // the exchange of the others
+            __syncthreads();
+        });
+        return;
     }
+
     const float sc = fmaxf(p.scale_log2, 1e-30f);                 // (a zero scale as a vanishing one: -inf stays -inf)
 
     // Tiles [t_begin, t_end) of request b; the result goes to partial slot slot0 + row, or straight to the output.
-    auto piece = [&](const int b, const int t_begin, const int t_end, const int64_t slot0, const bool direct) {
-    const int q0 = p.cu_q ? p.cu_q[b] : b * p.q_len, ql = p.cu_q ? p.cu_q[b + 1] - q0 : p.q_len, kvl = p.kv_lens[b];
-    const PagedView view = paged_view(p, ql, kvl);
-    const int n_rows = p.group * ql, n = view.n;
-    if (row0 >= n_rows) return;
-    const int n_tiles = t_end - t_begin;                          // >= 1
-
-    float m_run = -INFINITY, l_run = 0.f;
-    floatx4 o_acc[DJ];
+    paged_walk(p, lane, j, [&](const int b, const PagedRequest& rq, const int t_begin, const int t_end, const bool direct) {
+        const PagedView view = paged_view(p, rq.ql, rq.kvl);
+        const int kvl = rq.kvl, before = kvl - rq.ql, n_rows = p.group * rq.ql, n = view.n;
+        if (row0 >= n_rows) return;
+        const int n_tiles = t_end - t_begin;
+        const int64_t slot0 = (int64_t)((j + b) * p.n_kv_heads + g) * p.rows_pad;
+        float m_run = -INFINITY, l_run = 0.f;
+        floatx4 o_acc[DJ];
 #pragma unroll
-    for (int jj = 0; jj < DJ; ++jj) o_acc[jj] = floatx4{0.f, 0.f, 0.f, 0.f};
-
-    if (is_loader) {
-        const SPECVLM_AS4 int32_t* const table = (const SPECVLM_AS4 int32_t*)(uintptr_t)(p.table + (int64_t)b * p.table_row);
-        int id[GPW], row[GPW];                                    // pages of the next tile's groups, and the rows in them
-        auto look_up = [&](int tile) {
-#pragma unroll
-            for (int i = 0; i < GPW; ++i) {
-                // (places behind the last are masked in the compute: its group of 16 is loaded again)
-                const int x = min(tile * TK + (group0 + i) * 16, (n - 1) & ~15);
-                const QuotRem at = divide(x < view.sinks ? x : x + view.skip, p.page_size, p.inv_page);
-                id[i] = table[at.q];
-                row[i] = at.r;
-            }
-        };
-        auto issue_tile = [&](int stage) {
-            unsigned char* const st = smem + stage * (2 * TILE_BYTES) + (is_v ? TILE_BYTES : 0) + group0 * 16 * ROW_BYTES;
-            uint32_t ok = 0;
-#pragma unroll
-            for (int i = 0; i < GPW; ++i) {
-                // (a page that is not one of the pool's is not read: the pool's first is, and its keys are masked)
-                const bool there = (uint32_t)id[i] < (uint32_t)p.n_pages;
-                ok |= (there ? 1u : 0u) << (8 * i);
-                const char* const src = mat + 2 * ((there ? id[i] : 0) * p.page + row[i] * p.tok);
-#pragma unroll
-                for (int l = 0; l < LPG; ++l)
-                    __builtin_amdgcn_global_load_lds((const SPECVLM_AS1 void*)(src + lane_off[l]),
-                                                     (SPECVLM_AS3 void*)(st + (i * LPG + l) * 1024), 16, 0, STREAM ? 2 : 0);
-            }
-            if (!is_v && lane == 0) {
-                if constexpr (GPW == 4) s_ok[stage] = ok;
-                else reinterpret_cast<uint16_t*>(s_ok + stage)[lw] = (uint16_t)ok;
-            }
-        };
-        const int n_load = n_tiles > NS - 1 ? n_tiles : NS - 1;   // (a run shorter than the ring loads its last tile again)
-        look_up(t_begin);
-#pragma unroll
-        for (int s = 0; s < NS - 1; ++s) {
-            issue_tile(s);
-            look_up(t_begin + min(s + 1, n_tiles - 1));
-        }
-        int i = 0;
-        do {
-            const int younger = min(NS - 2, n_load - 1 - i);      // tiles in flight behind tile i
-            wait_vmcnt<(NS - 2) * LPW>();
-            if constexpr (NS >= 4) { if (younger <= 1) wait_vmcnt<1 * LPW>(); }
-            if constexpr (NS >= 3) { if (younger <= 0) wait_vmcnt<0>(); }
-            __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the bytes of s_ok are written
-            stage_barrier();                                      // tile i landed for everyone; stage (i-1)%NS is free
-            if (i + NS - 1 < n_load) {
-                issue_tile((i + NS - 1) % NS);
-                look_up(t_begin + min(i + NS, n_tiles - 1));
-            }
-        } while (++i < n_tiles);
-        wait_vmcnt<0>();                                          // (spare copies may still be landing)
-    } else {
+        for (int jj = 0; jj < DJ; ++jj) o_acc[jj] = floatx4{0.f, 0.f, 0.f, 0.f};
         bf16x8 qf[KK];
         const int row = row0 + mb * 16 + r;
-        const QuotRem at = divide(row < n_rows ? row : 0, p.group, p.inv_group);     // (padding rows take row 0: never stored)
-        const int t_blk = at.q;
-        const __bf16* qp = p.q + (int64_t)(q0 + t_blk) * p.q_tok + (int64_t)(g * p.group + at.r) * p.q_head + c * 8;
+        const QuotRem q_at = divide(row < n_rows ? row : 0, p.group, p.inv_group);   // (padding rows take row 0: never stored)
+        const int t_blk = q_at.q;
+        const __bf16* qp = p.q + (int64_t)(rq.q0 + t_blk) * p.q_tok + (int64_t)(g * p.group + q_at.r) * p.q_head + c * 8;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(qp + kk * 32);
         // places [n_sinks, edge) hold keys that the window hides from some query
         const int edge = p.window ? kvl - p.window - view.skip : 0;
-        int i = 0;
-        do {
+        // where this lane reads in a stage: its keys' rows and its value rows.  A row's swizzle is an XOR of the piece's number, and so are the
+        // kk-th quarter of a key and the jj-th pair of pieces of a value row, whose bits of the address are the row's own
+        const uint32_t lds0 = (uint32_t)(uintptr_t)(SPECVLM_AS3 unsigned char*)smem;
+        const int v_row = ks * kChunkKeys + 4 * c + (r >> 2);                   // (16 rows on the swizzles are the same)
+        const uint32_t k_base = lds0 + (ks * kChunkKeys + r) * ROW_BYTES + (c ^ ((D == 128) ? (r & 15) : ((r >> 1) & 7))) * 16;
+        const uint32_t v_base = lds0 + TILE_BYTES + v_row * ROW_BYTES + (r & 3) * 8 + (v_swizzle<D>(v_row) >> 1) * 32;
+        bool fresh = true;                                        // some row has seen nothing yet
+        uint32_t at_stage = 0;
+        int base = t_begin * TK + ks * kChunkKeys;
+        for (int i = 0; i < n_tiles; ++i, base += TK, at_stage = at_stage == (NS - 1) * 2 * TILE_BYTES ? 0 : at_stage + 2 * TILE_BYTES) {
             stage_barrier();
-            const unsigned char* const kt = smem + (i % NS) * (2 * TILE_BYTES);
-            const unsigned char* const vt = kt + TILE_BYTES;
-            const int base = (t_begin + i) * TK + ks * kChunkKeys;
             if (base >= n) continue;
-            const uint32_t ok = (uint32_t)__builtin_amdgcn_readfirstlane(s_ok[i % NS]) >> (16 * ks);
+            const uint32_t ok = (uint32_t)__builtin_amdgcn_readfirstlane(s_ok[at_stage / (2 * TILE_BYTES)]) >> (16 * ks);
             // ---- S^T = K Q^T for 32 keys ----
             floatx4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
-                const int x = kk * 4 + c;
-                const int key0 = ks * kChunkKeys + r;
-                const int sw = (D == 128) ? (r & 15) : ((r >> 1) & 7);          // (the same for row r + 16)
-                const u32x4 k0 = *reinterpret_cast<const u32x4*>(kt + key0 * ROW_BYTES + ((x ^ sw) * 16));
-                const u32x4 k1 = *reinterpret_cast<const u32x4*>(kt + (key0 + 16) * ROW_BYTES + ((x ^ sw) * 16));
+                const SPECVLM_AS3 u32x4* const at = (const SPECVLM_AS3 u32x4*)(k_base + at_stage ^ kk * 64);
+                const u32x4 k0 = at[0], k1 = at[16 * ROW_BYTES / 16];
                 s0 = mfma16(__builtin_bit_cast(bf16x8, k0), qf[kk], s0);
                 s1 = mfma16(__builtin_bit_cast(bf16x8, k1), qf[kk], s1);
             }
+            // ---- V^T fragments of the lane's keys (4c+e and 16+4c+e) by the transposing LDS read ----
+            bf16x8 vf[DJ];
+#pragma unroll
+            for (int jj = 0; jj < DJ; ++jj) {
+                typedef short s16x4 __attribute__((ext_vector_type(4)));
+                SPECVLM_AS3 s16x4* const at = (SPECVLM_AS3 s16x4*)(v_base + at_stage ^ jj * 32);
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at);
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at + 16 * ROW_BYTES / 8);
+                vf[jj] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+            const bool need_mask = (ok & 0xffffu) != 0x0101u || base + kChunkKeys > n - rq.ql || (base < edge && base + kChunkKeys > p.n_sinks);
             float s[8];
 #pragma unroll
             for (int e = 0; e < 4; ++e) { s[e] = s0[e]; s[4 + e] = s1[e]; }
-            // ---- V^T fragments of the lane's keys (4c+e and 16+4c+e) by the transposing LDS read ----
-            bf16x8 vf[DJ];
-            {
-                const int kl = ks * kChunkKeys + 4 * c + (r >> 2);
-                const int pair_swz = v_swizzle<D>(kl) >> 1;                     // same for kl + 16
-                const unsigned char* const vrow = vt + kl * ROW_BYTES + (r & 3) * 8;
-#pragma unroll
-                for (int jj = 0; jj < DJ; ++jj) {
-                    typedef short s16x4 __attribute__((ext_vector_type(4)));
-                    const unsigned char* const src = vrow + (jj ^ pair_swz) * 32;
-                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SPECVLM_AS3 s16x4*)src);
-                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SPECVLM_AS3 s16x4*)(src + 16 * ROW_BYTES));
-                    vf[jj] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-                }
-            }
-            const bool need_mask = (ok & 0xffffu) != 0x0101u || base + kChunkKeys > n - ql || (base < edge && base + kChunkKeys > p.n_sinks);
+            uint32_t sees = 0;                                    // (with need_mask) bits 0..3 and 16..19: the lane's keys that its row sees
             if (need_mask) {
                 // block key b is visible where bit b is set: 0..t in a chain, the caller's ancestors in a tree
-                const uint64_t row_mask = p.block_mask ? p.block_mask[q0 + t_blk] : ((2ull << t_blk) - 1ull);
-                const uint32_t mask_lo = (uint32_t)row_mask, mask_hi = (uint32_t)(row_mask >> 32);
-                const int hidden_to = p.window ? kvl - ql + t_blk - p.window : -1;          // the window's last hidden key
+                const uint64_t seen = p.block_mask ? p.block_mask[rq.q0 + t_blk] : ((2ull << t_blk) - 1ull);
+                const int hidden_to = p.window ? before + t_blk - p.window : -1;
+                const int x1 = base + 16, ka = base < view.sinks ? base : base + view.skip, kb = x1 < view.sinks ? x1 : x1 + view.skip;
+                const uint32_t lo = (ok & 1u) ? paged_sees(ka, before, kvl, seen, hidden_to, p.n_sinks) : 0u;
+                const uint32_t hi = (ok & 0x100u) ? paged_sees(kb, before, kvl, seen, hidden_to, p.n_sinks) : 0u;
+                sees = (lo | hi << 16) >> (4 * c);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int x0 = base + (e < 4 ? 0 : 16), key = (x0 < view.sinks ? x0 : x0 + view.skip) + 4 * c + (e & 3);
-                    const int bk = key - (kvl - ql);                                    // (negative: a context key)
-                    const uint32_t bit = (((bk & 32) ? mask_hi : mask_lo) >> (bk & 31)) & 1u;
-                    const bool hidden = (((ok >> (e < 4 ? 0 : 8)) & 1u) == 0u) | (key >= kvl) | ((key <= hidden_to) & (key >= p.n_sinks)) |
-                                        ((bk >= 0) & (bit == 0u));
-                    s[e] = hidden ? -INFINITY : s[e];
-                }
+                for (int e = 0; e < 8; ++e) s[e] = (sees >> (e < 4 ? e : e + 12)) & 1u ? s[e] : -INFINITY;
             }
             // Away from the masks the exponentials are taken against the reference that the earlier chunks left, and the
             // maximum is tracked only where a lane's sum does not stay moderate (see decode_attn.hip).
             floatx8 pv;
             bool settled = false;
-            if (!need_mask && !__any(!(m_run > -INFINITY))) {
+            if (!need_mask && !fresh) {
                 float psum = 0.f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) { pv[e] = fast_exp2(fmaf(s[e], sc, -m_run)); psum += pv[e]; }
@@ -301,124 +371,110 @@ void paged_split_kernel(const PagedParams p)
                     for (int jj = 0; jj < DJ; ++jj) o_acc[jj] *= alpha;
                 }
             }
-            // the probabilities as two bf16 each: rounded to one, their error (2^-9 of each term) was as large as the output's own
-            // rounding, and the result 1.45 times as far from the sums in 64 bits as one that is only rounded at the end
-            const bf16x8 pf = __builtin_convertvector(pv, bf16x8);
-            const bf16x8 pf_rest = __builtin_convertvector(pv - __builtin_convertvector(pf, floatx8), bf16x8);
+            if (need_mask || fresh) fresh = __any(!(m_run > -INFINITY));
             if (need_mask) {
                 // A value that is no number (an infinity, rows never written) belongs only to the rows that see its key, and 0
-                // times it is no zero: it is left out of the product, and the rows get it by how many such values they see.
-                bool odd = false;
+                // times it is no zero (by which the products with 0 find it): it is left out of the product, and the rows get it by
+                // how many such values they see.
+                const floatx4 none = {0.f, 0.f, 0.f, 0.f};
+                floatx4 odd = none;
 #pragma unroll
-                for (int jj = 0; jj < DJ; ++jj) {
-                    const u32x4 w = __builtin_bit_cast(u32x4, vf[jj]);
+                for (int jj = 0; jj < DJ; ++jj) odd = mfma16(vf[jj], __builtin_bit_cast(bf16x8, u32x4{}), odd);
+                if (__builtin_expect(__any(!(odd[0] + odd[1] + odd[2] + odd[3] == 0.f)), 0)) {
+                    u32x4 seen;                                   // bf16 0 or 1
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) odd |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
-                }
-                if (__any(odd)) {
-                    typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
-                    u16x8 sees;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) sees[e] = s[e] == -INFINITY ? 0 : 0x3f80;       // bf16 0 or 1
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t two = sees >> (e < 2 ? 2 * e : 2 * e + 12);
+                        seen[e] = (two & 1u) * 0x3f80u | (two & 2u) * (0x3f800000u / 2);
+                    }
 #pragma unroll
                     for (int jj = 0; jj < DJ; ++jj) {
-                        u16x8 w = __builtin_bit_cast(u16x8, vf[jj]), up, down, nan;
+                        u32x4 w = __builtin_bit_cast(u32x4, vf[jj]), up, down, nan;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            up[e] = w[e] == 0x7f80 ? 0x3f80 : 0;
-                            down[e] = w[e] == 0xff80 ? 0x3f80 : 0;
-                            nan[e] = (w[e] & 0x7fff) > 0x7f80 ? 0x3f80 : 0;
-                            w[e] = (w[e] & 0x7f80) == 0x7f80 ? 0 : w[e];
+                        for (int e = 0; e < 4; ++e) {             // (two halves a word: a carry into bit 15 says that a size is an infinity's or more, or more than one)
+                            const uint32_t size = w[e] & 0x7fff7fffu, odd2 = (size + 0x00800080u) >> 15 & 0x00010001u;
+                            nan[e] = (size + 0x007f007fu) >> 15 & 0x00010001u;
+                            down[e] = (odd2 ^ nan[e]) & w[e] >> 15;
+                            up[e] = odd2 ^ nan[e] ^ down[e];
+                            w[e] &= ~(odd2 * 0xffffu);
                         }
                         vf[jj] = __builtin_bit_cast(bf16x8, w);
-                        const floatx4 none = {0.f, 0.f, 0.f, 0.f};
-                        const bf16x8 see = __builtin_bit_cast(bf16x8, sees);
-                        const floatx4 n_up = mfma16(__builtin_bit_cast(bf16x8, up), see, none);
-                        const floatx4 n_down = mfma16(__builtin_bit_cast(bf16x8, down), see, none);
-                        const floatx4 n_nan = mfma16(__builtin_bit_cast(bf16x8, nan), see, none);
+                        const auto count = [&](u32x4 x) {
+                            return mfma16(__builtin_bit_cast(bf16x8, x * 0x3f80u), __builtin_bit_cast(bf16x8, seen), none);
+                        };
+                        const floatx4 n_up = count(up), n_down = count(down), n_nan = count(nan);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             if (n_up[e] > 0.f) o_acc[jj][e] += INFINITY;
                             if (n_down[e] > 0.f) o_acc[jj][e] += -INFINITY;
                             if (n_nan[e] > 0.f) o_acc[jj][e] = NAN;
                         }
+                        __builtin_amdgcn_sched_barrier(0);        // (one after the other: the registers of all at once would be the kernel's most)
                     }
                 }
             }
-            // ---- O^T += V^T P^T ----
+            // ---- O^T += V^T P^T, the probabilities as two bf16 each: rounded to one, their error (2^-9 of each term) was as large as the
+            // output's own rounding, and the result 1.45 times as far from the sums in 64 bits as one that is only rounded at the end ----
+            const bf16x8 pf = __builtin_convertvector(pv, bf16x8);
+            const u32x4 two = __builtin_bit_cast(u32x4, pf);
+            floatx8 rest;
 #pragma unroll
-            for (int jj = 0; jj < DJ; ++jj) o_acc[jj] = mfma16(vf[jj], pf, mfma16(vf[jj], pf_rest, o_acc[jj]));
-        } while (++i < n_tiles);
-    }
-
-    // ---- the KS waves of a row block exchange their results through LDS; wave ks then owns D/KS columns of its 16 rows ----
-    constexpr int SLICE = D / KS, CPL = SLICE / 4;
-    l_run = quad_sum(l_run);
-    const int row = row0 + mb * 16 + r;
-    __syncthreads();                             // every wave is done with the ring
-    float* sm_m = reinterpret_cast<float*>(smem);            // [NW][16]
-    float* sm_l = sm_m + NW * 16;                            // [NW][16]
-    float* sm_o = sm_l + NW * 16;                            // [NW][16][LDS_STRIDE]
-    if (!is_loader) {
-        if (c == 0) { sm_m[wave * 16 + r] = m_run; sm_l[wave * 16 + r] = l_run; }
-        float* buf = sm_o + (wave * 16 + r) * LDS_STRIDE + 4 * c;
+            for (int e = 0; e < 4; ++e) {
+                rest[2 * e] = pv[2 * e] - __uint_as_float(two[e] << 16);
+                rest[2 * e + 1] = pv[2 * e + 1] - __uint_as_float(two[e] & 0xffff0000u);
+            }
+            const bf16x8 pf_rest = __builtin_convertvector(rest, bf16x8);
 #pragma unroll
-        for (int jj = 0; jj < DJ; ++jj) *reinterpret_cast<floatx4*>(buf + 16 * jj) = o_acc[jj];
-    }
-    __syncthreads();
-    if (is_loader || row >= n_rows) return;
-    float m_x[KS], m_all = -INFINITY, l_all = 0.f;
+            for (int jj = 0; jj < DJ; ++jj) o_acc[jj] = mfma16(vf[jj], pf, o_acc[jj]);
 #pragma unroll
-    for (int kx = 0; kx < KS; ++kx) { m_x[kx] = sm_m[(kx * MB + mb) * 16 + r]; m_all = fmaxf(m_all, m_x[kx]); }
-    const float m_ref = (m_all == -INFINITY) ? 0.f : m_all;
-#pragma unroll
-    for (int kx = 0; kx < KS; ++kx) { m_x[kx] = fast_exp2(m_x[kx] - m_ref); l_all += m_x[kx] * sm_l[(kx * MB + mb) * 16 + r]; }
-    const int col0 = ks * SLICE + c * CPL;
-    floatx4 acc[CPL / 4];
-#pragma unroll
-    for (int qd = 0; qd < CPL / 4; ++qd) acc[qd] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int kx = 0; kx < KS; ++kx) {
-        const float* buf = sm_o + ((kx * MB + mb) * 16 + r) * LDS_STRIDE + col0;
-#pragma unroll
-        for (int qd = 0; qd < CPL / 4; ++qd) acc[qd] += m_x[kx] * *reinterpret_cast<const floatx4*>(buf + 4 * qd);
-    }
-    if (direct) {
-        const QuotRem at = divide(row, p.group, p.inv_group);
-        const int t = at.q, h = g * p.group + at.r;
-        const float inv = l_all == 0.f ? 0.f : 1.f / l_all;                   // (a row that sees nothing: 0)
-        __bf16* op = p.out + (int64_t)(q0 + t) * p.q_tok + (int64_t)h * p.q_head + col0;
-#pragma unroll
-        for (int qd = 0; qd < CPL / 4; ++qd)
-            *reinterpret_cast<bf16x4*>(op + 4 * qd) = __builtin_convertvector(acc[qd] * inv, bf16x4);
-        if (p.lse && c == 0 && ks == 0)
-            p.lse[(int64_t)(q0 + t) * p.n_q_heads + h] = (m_all + fast_log2(l_all)) * kLn2;
-    } else {
-        float* po = p.part_o + (slot0 + row) * D + col0;
-#pragma unroll
-        for (int qd = 0; qd < CPL / 4; ++qd) *reinterpret_cast<floatx4*>(po + 4 * qd) = acc[qd];
-        if (c == 0 && ks == 0) { p.part_ml[(slot0 + row) * 2] = m_all; p.part_ml[(slot0 + row) * 2 + 1] = l_all; }
-    }
-    };   // piece
-
-    const auto slot_of = [&](int b) { return (int64_t)((j + b) * p.n_kv_heads + g) * p.rows_pad; };
-    const int total = paged_total(p, lane), run = paged_run(p, total);
-    int x = __builtin_amdgcn_readfirstlane(j * run);
-    const int x_end = min(total, x + run);
-    int base = 0;                                // tiles of the requests before the 64 at hand
-    for (int c64 = 0; x < x_end; c64 += kWave) {
-        const int tiles = p.batch == 1 ? total : c64 + lane < p.batch ? paged_tiles(p, c64 + lane) : 0;
-        const int upto = p.batch == 1 ? total : base + wave_prefix(tiles, lane);
-        base = __builtin_amdgcn_readlane(upto, kWave - 1);
-        while (x < min(x_end, base)) {
-            const int at = __builtin_ctzll(__ballot(upto > x));              // the request that holds tile x
-            const int last = __builtin_amdgcn_readlane(upto, at), n = __builtin_amdgcn_readlane(tiles, at), first = last - n;
-            const int to = min(last, x_end);
-            piece(c64 + at, x - first, to - first, slot_of(c64 + at), x == first && to == last);
-            x = to;
-            __syncthreads();                     // the next piece reuses the ring and the exchange buffer
+            for (int jj = 0; jj < DJ; ++jj) o_acc[jj] = mfma16(vf[jj], pf_rest, o_acc[jj]);
         }
-    }
+
+        // ---- the KS waves of a row block exchange their results through LDS; wave ks then owns D/KS columns of its rows ----
+        constexpr int SLICE = D / KS, CPL = SLICE / 4;
+        __syncthreads();                             // every wave is done with the ring
+        float* sm_m = reinterpret_cast<float*>(smem);            // [KS][MB][16]
+        float* sm_l = sm_m + KS * MB * 16;                       // [KS][MB][16]
+        float* sm_o = sm_l + KS * MB * 16;                       // [KS][MB][16][LDS_STRIDE]
+        const int at = (ks * MB + mb) * 16 + r;
+        const float l = quad_sum(l_run);
+        if (c == 0) { sm_m[at] = m_run; sm_l[at] = l; }
+#pragma unroll
+        for (int jj = 0; jj < DJ; ++jj) *reinterpret_cast<floatx4*>(sm_o + at * LDS_STRIDE + 4 * c + 16 * jj) = o_acc[jj];
+        __syncthreads();
+        if (row >= n_rows) return;
+        float m_x[KS], m_all = -INFINITY, l_all = 0.f;
+#pragma unroll
+        for (int kx = 0; kx < KS; ++kx) { m_x[kx] = sm_m[(kx * MB + mb) * 16 + r]; m_all = fmaxf(m_all, m_x[kx]); }
+        const float m_ref = (m_all == -INFINITY) ? 0.f : m_all;
+#pragma unroll
+        for (int kx = 0; kx < KS; ++kx) { m_x[kx] = fast_exp2(m_x[kx] - m_ref); l_all += m_x[kx] * sm_l[(kx * MB + mb) * 16 + r]; }
+        const int col0 = ks * SLICE + c * CPL;
+        floatx4 acc[CPL / 4];
+#pragma unroll
+        for (int qd = 0; qd < CPL / 4; ++qd) acc[qd] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kx = 0; kx < KS; ++kx) {
+            const float* buf = sm_o + ((kx * MB + mb) * 16 + r) * LDS_STRIDE + col0;
+#pragma unroll
+            for (int qd = 0; qd < CPL / 4; ++qd) acc[qd] += m_x[kx] * *reinterpret_cast<const floatx4*>(buf + 4 * qd);
+        }
+        if (direct) {
+            const int t = t_blk, h = g * p.group + q_at.r;
+            const float inv = l_all == 0.f ? 0.f : 1.f / l_all;                   // (a row that sees nothing: 0)
+            __bf16* op = p.out + (int64_t)(rq.q0 + t) * p.q_tok + (int64_t)h * p.q_head + col0;
+#pragma unroll
+            for (int qd = 0; qd < CPL / 4; ++qd)
+                *reinterpret_cast<bf16x4*>(op + 4 * qd) = __builtin_convertvector(acc[qd] * inv, bf16x4);
+            if (p.lse && c == 0 && ks == 0)
+                p.lse[(int64_t)(rq.q0 + t) * p.n_q_heads + h] = (m_all + fast_log2(l_all)) * kLn2;
+        } else {
+            float* po = p.part_o + (slot0 + row) * D + col0;
+#pragma unroll
+            for (int qd = 0; qd < CPL / 4; ++qd) *reinterpret_cast<floatx4*>(po + 4 * qd) = acc[qd];
+            if (c == 0 && ks == 0) { p.part_ml[(slot0 + row) * 2] = m_all; p.part_ml[(slot0 + row) * 2 + 1] = l_all; }
+        }
+    });
 }
 
 // Joins the pieces of the requests that were cut (one that was not is in its place already).  GP groups of threads share a row's
@@ -433,12 +489,11 @@ void paged_join_kernel(const PagedParams p)
     const int nbh = p.batch * p.n_kv_heads;
     const QuotRem at = divide(blockIdx.x, nbh, p.inv_all_heads), head = divide(at.r, p.n_kv_heads, p.inv_heads);
     const int b = head.q, g = head.r, lane = threadIdx.x & 63;
-    const int q0 = p.cu_q ? p.cu_q[b] : b * p.q_len, ql = p.cu_q ? p.cu_q[b + 1] - q0 : p.q_len;
-    const int n_rows = p.group * ql, row0 = at.q * ROWS;
-    if (row0 >= n_rows) return;
-    int first = 0, total = 0;
-    if (p.batch == 1) total = paged_tiles(p, 0);
-    else {
+    const PagedRequest rq = paged_request(p, b);
+    const int n_rows = p.group * rq.ql, row0 = at.q * ROWS, tiles = (paged_view(p, rq.ql, rq.kvl).n + kTileKeys - 1) / kTileKeys;
+    if (row0 >= n_rows || tiles == 0) return;
+    int first = 0, total = tiles;
+    if (p.batch > 1) {
         int before = 0, all = 0;
         for (int c = 0; c < p.batch; c += kWave) {
             const int t = c + lane < p.batch ? paged_tiles(p, c + lane) : 0;
@@ -447,8 +502,7 @@ void paged_join_kernel(const PagedParams p)
         }
         total = wave_total(all); first = wave_total(before);
     }
-    const int tiles = paged_tiles(p, b), run = paged_run(p, total);
-    if (tiles == 0) return;
+    const int run = paged_run(p, total);
     const int j0 = first / run, live = (first + tiles - 1) / run - j0 + 1;
     if (live == 1) return;
     const int sub = threadIdx.x / TPR, grp = sub % GP, lr = sub / GP, col = (threadIdx.x % TPR) * 4, row = row0 + lr;
@@ -500,8 +554,8 @@ void paged_join_kernel(const PagedParams p)
     acc *= l == 0.f ? 0.f : 1.f / l;
     const QuotRem out_at = divide(row, p.group, p.inv_group);
     const int t = out_at.q, h = g * p.group + out_at.r;
-    *reinterpret_cast<bf16x4*>(p.out + (int64_t)(q0 + t) * p.q_tok + (int64_t)h * p.q_head + col) = __builtin_convertvector(acc, bf16x4);
-    if (p.lse && col == 0) p.lse[(int64_t)(q0 + t) * p.n_q_heads + h] = (m + fast_log2(l)) * kLn2;
+    *reinterpret_cast<bf16x4*>(p.out + (int64_t)(rq.q0 + t) * p.q_tok + (int64_t)h * p.q_head + col) = __builtin_convertvector(acc, bf16x4);
+    if (p.lse && col == 0) p.lse[(int64_t)(rq.q0 + t) * p.n_q_heads + h] = (m + fast_log2(l)) * kLn2;
 }
 
 // ---------------------------------------------------------------- host side ----
@@ -510,7 +564,9 @@ struct PagedPlan { int n_rgroups, mb, rows_pad, max_groups; };
 static PagedPlan paged_plan(int q_len, int n_q_heads, int n_kv_heads)
 {
     PagedPlan s;
-    attn_row_groups(n_q_heads / n_kv_heads * q_len, &s.n_rgroups, &s.mb);
+    const int blocks = (n_q_heads / n_kv_heads * q_len + 15) / 16;
+    s.n_rgroups = (blocks + kMostBlocks - 1) / kMostBlocks;
+    s.mb = (blocks + s.n_rgroups - 1) / s.n_rgroups;
     s.rows_pad = s.n_rgroups * s.mb * 16;
     s.max_groups = kTargetGroups / (n_kv_heads * s.n_rgroups);
     if (s.max_groups < 1) s.max_groups = 1;
@@ -520,13 +576,13 @@ static PagedPlan paged_plan(int q_len, int n_q_heads, int n_kv_heads)
 template <int D, int MB, int NLD>
 static int launch_paged(const PagedParams& p, hipStream_t stream)
 {
-    constexpr int KS = 2, NS = 3, NW = MB * KS;
-    constexpr size_t ring = (size_t)NS * 2 * kTileKeys * D * 2 + 64;
-    constexpr size_t exchange = sizeof(float) * (size_t)(2 * NW * 16 + NW * 16 * (D + 4));
+    constexpr int NW = MB * 2;
+    constexpr size_t ring = (size_t)kRing * 2 * kTileKeys * D * 2 + 64;
+    constexpr size_t exchange = sizeof(float) * (size_t)(2 * 2 * MB * 16 + 2 * MB * 16 * (D + 4));
     constexpr size_t lds = ring > exchange ? ring : exchange;
     if (lds > 64 * 1024)
-        if (const int rc = allow_lds<&paged_split_kernel<D, MB, KS, NS, NLD, true>>((int)lds)) return rc;
-    hipLaunchKernelGGL((paged_split_kernel<D, MB, KS, NS, NLD, true>), dim3(p.max_groups * p.n_rgroups * p.n_kv_heads),
+        if (const int rc = allow_lds<&paged_split_kernel<D, MB, NLD>>((int)lds)) return rc;
+    hipLaunchKernelGGL((paged_split_kernel<D, MB, NLD>), dim3(p.max_groups * p.n_rgroups * p.n_kv_heads),
                        dim3((NW + NLD) * kWave), lds, stream, p);
     return launch_status();
 }
@@ -536,15 +592,22 @@ static int launch_paged_d(const PagedParams& p, int mb, hipStream_t stream)
 {
     int rc = SPECVLM_EUNSUPPORTED;
     switch (mb) {
-        case 1: rc = launch_paged<D, 1, 2>(p, stream); break;
+        case 1: rc = launch_paged<D, 1, 4>(p, stream); break;
         case 2: rc = launch_paged<D, 2, 4>(p, stream); break;
-        case 3: rc = launch_paged<D, 3, 2>(p, stream); break;
+        case 3: rc = launch_paged<D, 3, 2>(p, stream); break;     // (four loader waves: one request of 128 keys 8.2 us, not 7.9, long ones the same)
         case 4: rc = launch_paged<D, 4, 4>(p, stream); break;
     }
     if (rc != SPECVLM_OK) return rc;
-    constexpr int GP = 8, ROWS = 256 / (D / 4 * GP);
     const int rows = p.group * p.q_len;
-    hipLaunchKernelGGL((paged_join_kernel<D, GP>), dim3((rows + ROWS - 1) / ROWS * p.batch * p.n_kv_heads), dim3(256), 0, stream, p);
+    const auto join = [&](auto gp) {
+        constexpr int GP = decltype(gp)::value, ROWS = 256 / (D / 4 * GP);
+        hipLaunchKernelGGL((paged_join_kernel<D, GP>), dim3((rows + ROWS - 1) / ROWS * p.batch * p.n_kv_heads), dim3(256), 0, stream, p);
+    };
+    // few rows: eight groups of threads share a row's pieces;  where the rows fill the chip two do, in a quarter of the workgroups.  Us a call, eight /
+    // two:  64/8 heads, 12806 keys, 8 queries 18.1 / 19.4;  14/2 heads, one, 1511 keys 7.3 / 8.0;  but 64 requests of up to 1000 keys, 28/4 heads 22.2 / 21.1,
+    // windows of 12 requests, 4 queries, 40/8 heads 43.1 / 41.5, trees of 208 rows, four requests, the join alone 11 / 5.2.
+    if ((int64_t)rows * p.batch * p.n_kv_heads < 1024) join(std::integral_constant<int, 8>{});
+    else                                               join(std::integral_constant<int, 2>{});
     return launch_status();
 }
 
@@ -597,7 +660,7 @@ extern "C" int specvlm_paged_attn(
     p.n_q_heads = n_q_heads; p.n_kv_heads = n_kv_heads; p.group = n_q_heads / n_kv_heads;
     p.window = window; p.n_sinks = n_sinks;
     p.inv_page = reciprocal(page_size); p.inv_heads = reciprocal(n_kv_heads); p.inv_all_heads = reciprocal(batch * n_kv_heads);
-    p.inv_group = reciprocal(p.group); p.inv_rgroups = reciprocal(s.n_rgroups);
+    p.inv_group = reciprocal(p.group); p.inv_rgroups = reciprocal(s.n_rgroups); p.inv_groups = reciprocal(s.max_groups);
     p.scale_log2 = softmax_scale * kLog2e;
     p.n_rgroups = s.n_rgroups; p.rows_pad = s.rows_pad; p.max_groups = s.max_groups;
     const size_t slots = ((size_t)s.max_groups + batch) * n_kv_heads * s.rows_pad;
