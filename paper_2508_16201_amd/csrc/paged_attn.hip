@@ -20,7 +20,8 @@
 // request; group j (a workgroup for each kv head and row group) takes a run of equal length, which every workgroup
 // finds by a prefix sum over the lengths, 64 requests at a time in the lanes of a wave.  A captured launch so stays
 // balanced as the caches grow.  A request that one group covers is written out directly; the others leave partial
-// results that the second launch joins.
+// results that the second launch joins.  Short caches take one launch in which a workgroup has a request's keys of a head
+// whole (paged_takes_whole has the line).
 //
 // A workgroup has MB*KS compute waves (row block mb, every KS-th 32-key chunk of a tile) and NLD loader waves that only issue
 // direct-to-LDS loads into a ring of NS tiles (see decode_attn.hip for the matrix formulation and the swizzles).  The two roles plan for
@@ -168,12 +169,24 @@ __device__ __forceinline__ void paged_walk(const PagedParams& p, int lane, int j
     }
 }
 
-// MB: row blocks of 16, one to a compute wave.
-template <int D, int MB, int NLD>
-__global__ __launch_bounds__((MB * 2 + NLD) * kWave)
+// Waits until at most `younger` tiles of LPW loads each are on the way.
+template <int LPW, int MOST>
+__device__ __forceinline__ void wait_tiles(int younger)
+{
+    if constexpr (MOST > 0) {
+        if (younger < MOST) return wait_tiles<LPW, MOST - 1>(younger);
+    }
+    wait_vmcnt<MOST * LPW>();
+}
+
+// MB: row blocks of 16, one to a compute wave.  KS: chunks of 32 keys of a tile, a wave for each.  NS: tiles of the ring.  NLD: loader waves.
+// WHOLE: a workgroup has all keys of its request, and there is no plan.
+template <int D, int MB, int KS, int NS, int NLD, bool WHOLE>
+__global__ __launch_bounds__((MB * KS + NLD) * kWave)
 void paged_split_kernel(const PagedParams p)
 {
-    constexpr int TK = kTileKeys, KS = TK / kChunkKeys, NS = kRing;
+    constexpr int TK = KS * kChunkKeys;
+    static_assert(WHOLE || TK == kTileKeys, "what the plan counts");
     constexpr int NW = MB * KS;                  // compute waves (row block, key split); the loader waves come after them
     constexpr int DJ = D / 16, KK = D / 32, CH = D / 8, ROW_BYTES = D * 2;
     constexpr int KEYS_PER_LOAD = kWave / CH;    // key rows of one wave-wide load (4 or 8)
@@ -184,7 +197,7 @@ void paged_split_kernel(const PagedParams p)
     constexpr int LPG = 16 / KEYS_PER_LOAD;      // loads per group
     constexpr int LDS_STRIDE = D + 4;
     static_assert(NLD == 2 || NLD == 4, "loader waves: half for K, half for V");
-    static_assert(NS >= 3 && NS <= 4, "ring depth");
+    static_assert(GPW == 2 || GPW == 4, "their pages' bytes are one word or half of one");
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -194,10 +207,19 @@ void paged_split_kernel(const PagedParams p)
     const int r = lane & 15, c = lane >> 4;
 
     extern __shared__ __align__(1024) unsigned char smem[];      // stage s: K tile at s*2*TILE_BYTES, V tile right after it
-    uint32_t* const s_ok = reinterpret_cast<uint32_t*>(smem + NS * 2 * TILE_BYTES);     // per stage a byte per 16 keys: their page is there
+    unsigned char* const s_ok = smem + NS * 2 * TILE_BYTES;       // per stage eight bytes, one for 16 keys: their page is there
 
     const QuotRem head = divide(blockIdx.x, p.n_kv_heads, p.inv_heads), rows_of = divide(head.q, p.n_rgroups, p.inv_rgroups);
-    const int g = head.r, row0 = rows_of.r * (MB * 16), j = rows_of.q;
+    const int g = head.r, row0 = rows_of.r * (MB * 16), j = rows_of.q;       // (j: group of workgroups, or request)
+    const auto work = [&](auto&& f) {
+        if constexpr (WHOLE) {
+            const PagedRequest rq = paged_request(p, j);
+            const int n = paged_view(p, rq.ql, rq.kvl).n;
+            if (n > 0) f(j, rq, 0, (n + TK - 1) / TK, true);
+        } else {
+            paged_walk(p, lane, j, f);
+        }
+    };
 
     if (is_loader) {
         // this wave's matrix, its first group of a tile, and the lane offsets of the loads of a group
@@ -211,7 +233,7 @@ void paged_split_kernel(const PagedParams p)
             const int swz = is_v ? v_swizzle<D>(kl) : (D == 128 ? kl : kl >> 1);
             lane_off[i] = (uint32_t)kl * (uint32_t)(p.tok * 2) + (uint32_t)((lane % CH) ^ swz) * 16u;
         }
-        paged_walk(p, lane, j, [&](const int b, const PagedRequest& rq, const int t_begin, const int t_end, bool) {
+        work([&](const int b, const PagedRequest& rq, const int t_begin, const int t_end, bool) {
             const PagedView view = paged_view(p, rq.ql, rq.kvl);
             const int n = view.n, n_tiles = t_end - t_begin;      // >= 1
             if (row0 >= p.group * rq.ql) return;
@@ -242,29 +264,24 @@ void paged_split_kernel(const PagedParams p)
                                                          (SPECVLM_AS3 void*)(st + (i * LPG + l) * 1024), 16, 0, 2);
                 }
                 if (!is_v && lane == 0) {
-                    if constexpr (GPW == 4) s_ok[stage] = ok;
-                    else reinterpret_cast<uint16_t*>(s_ok + stage)[lw] = (uint16_t)ok;
+                    if constexpr (GPW == 4) *reinterpret_cast<uint32_t*>(s_ok + 8 * stage + group0) = ok;
+                    else *reinterpret_cast<uint16_t*>(s_ok + 8 * stage + group0) = (uint16_t)ok;
                 }
             };
-            const int n_load = n_tiles > NS - 1 ? n_tiles : NS - 1;   // (a run shorter than the ring loads its last tile again)
             int i = 1 - NS, stage = 0;
             look_up(t_begin);
             do {
                 if (i >= 0) {
-                    const int younger = min(NS - 2, n_load - 1 - i);  // tiles in flight behind tile i
-                    wait_vmcnt<(NS - 2) * LPW>();
-                    if constexpr (NS >= 4) { if (younger <= 1) wait_vmcnt<1 * LPW>(); }
-                    if (younger <= 0) wait_vmcnt<0>();
+                    wait_tiles<LPW, NS - 2>(n_tiles - 1 - i);          // (the tiles behind tile i that are on the way)
                     __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the bytes of s_ok are written
                     stage_barrier();                                  // tile i landed for everyone; the stage of tile i-1 is free
                 }
-                if (i + NS - 1 < n_load) {
+                if (i + NS - 1 < n_tiles) {
                     issue_tile(stage);
                     look_up(t_begin + min(i + NS, n_tiles - 1));
                     stage = stage == NS - 1 ? 0 : stage + 1;
                 }
             } while (++i < n_tiles);
-            wait_vmcnt<0>();                                          // (spare copies may still be landing)
             __syncthreads();                                      // the exchange of the others
             __syncthreads();
         });
@@ -274,7 +291,7 @@ void paged_split_kernel(const PagedParams p)
     const float sc = fmaxf(p.scale_log2, 1e-30f);                 // (a zero scale as a vanishing one: -inf stays -inf)
 
     // Tiles [t_begin, t_end) of request b; the result goes to partial slot slot0 + row, or straight to the output.
-    paged_walk(p, lane, j, [&](const int b, const PagedRequest& rq, const int t_begin, const int t_end, const bool direct) {
+    work([&](const int b, const PagedRequest& rq, const int t_begin, const int t_end, const bool direct) {
         const PagedView view = paged_view(p, rq.ql, rq.kvl);
         const int kvl = rq.kvl, before = kvl - rq.ql, n_rows = p.group * rq.ql, n = view.n;
         if (row0 >= n_rows) return;
@@ -305,7 +322,7 @@ void paged_split_kernel(const PagedParams p)
         for (int i = 0; i < n_tiles; ++i, base += TK, at_stage = at_stage == (NS - 1) * 2 * TILE_BYTES ? 0 : at_stage + 2 * TILE_BYTES) {
             stage_barrier();
             if (base >= n) continue;
-            const uint32_t ok = (uint32_t)__builtin_amdgcn_readfirstlane(s_ok[at_stage / (2 * TILE_BYTES)]) >> (16 * ks);
+            const uint32_t ok = (uint32_t)__builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint16_t*>(s_ok + at_stage / (TILE_BYTES / 4) + 2 * ks));
             // ---- S^T = K Q^T for 32 keys ----
             floatx4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -325,7 +342,7 @@ void paged_split_kernel(const PagedParams p)
                 const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at + 16 * ROW_BYTES / 8);
                 vf[jj] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
             }
-            const bool need_mask = (ok & 0xffffu) != 0x0101u || base + kChunkKeys > n - rq.ql || (base < edge && base + kChunkKeys > p.n_sinks);
+            const bool need_mask = ok != 0x0101u || base + kChunkKeys > n - rq.ql || (base < edge && base + kChunkKeys > p.n_sinks);
             float s[8];
 #pragma unroll
             for (int e = 0; e < 4; ++e) { s[e] = s0[e]; s[4 + e] = s1[e]; }
@@ -573,29 +590,62 @@ static PagedPlan paged_plan(int q_len, int n_q_heads, int n_kv_heads)
     return s;
 }
 
-template <int D, int MB, int NLD>
+template <int D, int MB, int KS, int NS, int NLD, bool WHOLE>
 static int launch_paged(const PagedParams& p, hipStream_t stream)
 {
-    constexpr int NW = MB * 2;
-    constexpr size_t ring = (size_t)kRing * 2 * kTileKeys * D * 2 + 64;
-    constexpr size_t exchange = sizeof(float) * (size_t)(2 * 2 * MB * 16 + 2 * MB * 16 * (D + 4));
+    constexpr int NW = MB * KS;
+    constexpr size_t ring = (size_t)NS * (2 * KS * kChunkKeys * D * 2 + 8);
+    constexpr size_t exchange = sizeof(float) * (size_t)(NW * 16 * (D + 4 + 2));
     constexpr size_t lds = ring > exchange ? ring : exchange;
     if (lds > 64 * 1024)
-        if (const int rc = allow_lds<&paged_split_kernel<D, MB, NLD>>((int)lds)) return rc;
-    hipLaunchKernelGGL((paged_split_kernel<D, MB, NLD>), dim3(p.max_groups * p.n_rgroups * p.n_kv_heads),
+        if (const int rc = allow_lds<&paged_split_kernel<D, MB, KS, NS, NLD, WHOLE>>((int)lds)) return rc;
+    hipLaunchKernelGGL((paged_split_kernel<D, MB, KS, NS, NLD, WHOLE>), dim3((WHOLE ? p.batch : p.max_groups) * p.n_rgroups * p.n_kv_heads),
                        dim3((NW + NLD) * kWave), lds, stream, p);
     return launch_status();
 }
 
-template <int D>
-static int launch_paged_d(const PagedParams& p, int mb, hipStream_t stream)
+// Whether a workgroup takes a request whole: one launch and no plan, but no more than a CU's share of the memory and two or four waves at
+// work.  `places` is the most that a request's sweep can have.  Us a call, equal runs and join / whole, ragged batches:
+//   size 64, 14/2 heads:   one request, 512 keys 7.2 / 5.6, 1024 7.0 / 7.8 (42 rows, 512 8.3 / 7.5, 1024 8.4 / 10.5);  2 of 1024 8.4 / 7.8;  8 of 1024 9.7 / 8.0,
+//     2048 10.5 / 13.2;  32 of 1024 11.0 / 8.6, 2048 12.3 / 13.9;  64 of 2048 15.3 / 14.4
+//   size 128, 28/4 heads:  one request, 256 keys 7.4 / 5.5, 512 7.5 / 7.6, 1024 7.5 / 12.8;  8 of 512 11.3 / 8.6, 1024 11.6 / 13.8;  32 of 1024 16.7 / 15.1
+//   size 128, 64/8 heads:  8 of 512 11.4 / 8.8, 1024 12.4 / 14.5, 6 queries 16.4 / 16.2;  32 of 1024 20.6 / 17.5, 2048 29.8 / 31.2, 6 queries 40.3 / 33.0
+static bool paged_takes_whole(int batch, int n_kv_heads, int n_rgroups, int head_dim, int64_t places)
 {
+    const int64_t wgs = (int64_t)batch * n_kv_heads * n_rgroups;
+    const int eighths = batch == 1 ? 8 : wgs < 64 ? 11 : wgs < 128 ? 14 : wgs < 256 ? 20 : 32;
+    return places * 8 <= (head_dim == 64 ? 768 : 448) * eighths;
+}
+static int64_t paged_most_places(int q_len, int kv_len, int window, int n_sinks)
+{
+    const int64_t seen = window ? (int64_t)window + q_len + 14 + ((n_sinks + 15ll) & ~15ll) : kv_len;
+    return seen < kv_len ? seen : kv_len;
+}
+
+template <int D>
+static int launch_paged_d(const PagedParams& p, int mb, bool whole, hipStream_t stream)
+{
+    if (whole) {
+        if constexpr (D == 64) switch (mb) {
+            case 1: return launch_paged<D, 1, 4, 3, 4, true>(p, stream);
+            case 2: return launch_paged<D, 2, 4, 3, 4, true>(p, stream);
+            case 3: return launch_paged<D, 3, 4, 3, 4, true>(p, stream);
+            case 4: return launch_paged<D, 4, 2, 4, 4, true>(p, stream);
+        }
+        else switch (mb) {
+            case 1: return launch_paged<D, 1, 2, 3, 4, true>(p, stream);
+            case 2: return launch_paged<D, 2, 2, 3, 4, true>(p, stream);
+            case 3: return launch_paged<D, 3, 2, 3, 2, true>(p, stream);
+            case 4: return launch_paged<D, 4, 2, 3, 4, true>(p, stream);
+        }
+        return SPECVLM_EUNSUPPORTED;
+    }
     int rc = SPECVLM_EUNSUPPORTED;
     switch (mb) {
-        case 1: rc = launch_paged<D, 1, 4>(p, stream); break;
-        case 2: rc = launch_paged<D, 2, 4>(p, stream); break;
-        case 3: rc = launch_paged<D, 3, 2>(p, stream); break;     // (four loader waves: one request of 128 keys 8.2 us, not 7.9, long ones the same)
-        case 4: rc = launch_paged<D, 4, 4>(p, stream); break;
+        case 1: rc = launch_paged<D, 1, 2, kRing, 4, false>(p, stream); break;
+        case 2: rc = launch_paged<D, 2, 2, kRing, 4, false>(p, stream); break;
+        case 3: rc = launch_paged<D, 3, 2, kRing, 2, false>(p, stream); break;     // (four loader waves: one request of 128 keys 8.2 us, not 7.9, long ones the same)
+        case 4: rc = launch_paged<D, 4, 2, kRing, 4, false>(p, stream); break;
     }
     if (rc != SPECVLM_OK) return rc;
     const int rows = p.group * p.q_len;
@@ -646,6 +696,7 @@ extern "C" int specvlm_paged_attn(
     // (a lane's offset inside 16 keys has 32 bits; tiles and places of the sweep are ints)
     if (tok_stride < 0 || tok_stride >= ((int64_t)1 << 26) || kv_len > (1 << 30)) return SPECVLM_EUNSUPPORTED;
     if ((int64_t)batch * ((kv_len + kTileKeys - 1) / kTileKeys) >= ((int64_t)1 << 30)) return SPECVLM_EUNSUPPORTED;
+    if ((int64_t)batch * q_len >= ((int64_t)1 << 31) / n_q_heads) return SPECVLM_EUNSUPPORTED;        // (a launch's workgroups)
     const PagedPlan s = paged_plan(q_len, n_q_heads, n_kv_heads);
     const size_t need = specvlm_paged_attn_workspace_bytes(batch, q_len, n_q_heads, n_kv_heads, head_dim);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return SPECVLM_EWORKSPACE;
@@ -666,5 +717,6 @@ extern "C" int specvlm_paged_attn(
     const size_t slots = ((size_t)s.max_groups + batch) * n_kv_heads * s.rows_pad;
     p.part_o = (float*)workspace;
     p.part_ml = (float*)((char*)workspace + align256(slots * head_dim * sizeof(float)));
-    return head_dim == 128 ? launch_paged_d<128>(p, s.mb, (hipStream_t)stream) : launch_paged_d<64>(p, s.mb, (hipStream_t)stream);
+    const bool whole = paged_takes_whole(batch, n_kv_heads, s.n_rgroups, head_dim, paged_most_places(q_len, kv_len, window, n_sinks));
+    return head_dim == 128 ? launch_paged_d<128>(p, s.mb, whole, (hipStream_t)stream) : launch_paged_d<64>(p, s.mb, whole, (hipStream_t)stream);
 }

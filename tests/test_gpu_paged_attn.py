@@ -51,6 +51,8 @@ def i32(x):
 
 
 def check(B, q, k, v, table, kv_lens, q_lens, scale, *, head_major=False, window=0, n_sinks=0, masks=None, ragged=None, max_kv_len=None, **kw):
+    """The call against the plain implementation: as it is, and unless the caller has a bound, with room for long caches, which
+    takes launches that share a request's keys among workgroups."""
     ragged = len(set(q_lens)) > 1 if ragged is None else ragged
     more = dict(kw)
     if ragged:
@@ -58,22 +60,24 @@ def check(B, q, k, v, table, kv_lens, q_lens, scale, *, head_major=False, window
     if masks is not None:
         more["ancestor_mask"] = torch.from_numpy(np.asarray(masks, dtype=np.uint64).view(np.int64)).cuda()
     qd = dev_bf16(q)
-    out = torch.full_like(qd, 7.0)
-    got, lse = B.paged_attn(qd, on_gpu(k, head_major), on_gpu(v, head_major), i32(table), i32(kv_lens), scale, window=window, n_sinks=n_sinks,
-                            out=out, want_lse=True, max_kv_len=max_kv_len, **more)
-    torch.cuda.synchronize()
-    assert got is out
     want, want_lse, tol, tol_lse, written = R.paged_attention(R.values(q), R.values(k), R.values(v), table, kv_lens, q_lens, scale, window, n_sinks,
                                                               masks, max_kv_len)
-    got, lse = host_f64(got), host_f64(lse)
-    assert (got[~written] == 7.0).all()
-    err = np.abs(got - want)[written]
-    assert np.isfinite(got[written]).all()
-    assert (err <= tol[written]).all(), (err - tol[written]).max()
-    none = np.isinf(want_lse) & written[:, None]
-    assert (lse[none] == -np.inf).all()
-    some = ~none & written[:, None]
-    assert (np.abs(lse[some] - want_lse[some]) <= tol_lse[some]).all()
+    wide = np.concatenate([table, np.full((len(table), -(-8192 // k.shape[1])), -1, dtype=np.int32)], axis=1)
+    for entries in ([table] if max_kv_len else [wide, table]):
+        out = torch.full_like(qd, 7.0)
+        got, lse = B.paged_attn(qd, on_gpu(k, head_major), on_gpu(v, head_major), i32(entries), i32(kv_lens), scale, window=window, n_sinks=n_sinks,
+                                out=out, want_lse=True, max_kv_len=max_kv_len, **more)
+        torch.cuda.synchronize()
+        assert got is out
+        got, lse = host_f64(got), host_f64(lse)
+        assert (got[~written] == 7.0).all()
+        err = np.abs(got - want)[written]
+        assert np.isfinite(got[written]).all()
+        assert (err <= tol[written]).all(), (err - tol[written]).max()
+        none = np.isinf(want_lse) & written[:, None]
+        assert (lse[none] == -np.inf).all()
+        some = ~none & written[:, None]
+        assert (np.abs(lse[some] - want_lse[some]) <= tol_lse[some]).all()
     return got
 
 
@@ -161,6 +165,14 @@ def test_window_and_sinks(B, window, n_sinks):
     check(B, q, k, v, table, kv_lens, q_lens, 0.088, window=window, n_sinks=n_sinks)
 
 
+@pytest.mark.parametrize("heads", [(14, 2, 64), (8, 2, 128)])
+@pytest.mark.parametrize("window,n_sinks", [(900, 0), (1500, 4), (2000, 130)])
+def test_window_that_is_shared_among_workgroups(B, heads, window, n_sinks):
+    kv_lens, q_lens = [2600], [5]
+    q, k, v, table = build(window, kv_lens, q_lens, heads, 16)
+    check(B, q, k, v, table, kv_lens, q_lens, heads[2] ** -0.5, window=window, n_sinks=n_sinks)
+
+
 @pytest.mark.parametrize("ps", [16, 48, 256])
 def test_window_over_freed_pages(B, ps):
     """What lies between the first keys and the window is in no page any more."""
@@ -191,34 +203,36 @@ def test_values_that_a_row_does_not_see_do_not_reach_it(B):
     heads, kv_lens, q_lens = (8, 2, 128), [200, 90], [6, 6]
     q, k, v, table = build(17, kv_lens, q_lens, heads, 16)
     masks = np.array([1, 3, 5, 9, 17, 33] * 2, dtype=np.uint64)         # node i sees the root and itself
-    clean = check(B, q, k, v, table, kv_lens, q_lens, 0.088, masks=masks)
-    dirty = [x.copy() for x in (k, v)]
-    for b, n in enumerate(kv_lens):
-        for node, what in ((1, 0x7fc0), (3, 0x7f80), (5, 0xff80)):
-            j = n - 6 + node
-            for x in dirty:
-                x[table[b, j // 16], j % 16] = what
-    run = lambda kk, vv: B.paged_attn(dev_bf16(q), dev_bf16(kk), dev_bf16(vv), i32(table), i32(kv_lens), 0.088,
-                                      ancestor_mask=torch.from_numpy(masks.view(np.int64)).cuda())
-    got = host_f64(run(*dirty))
-    for row in (0, 2, 4, 6, 8, 10):
-        assert np.array_equal(got[row], clean[row]), row
-    for row in (1, 3, 5, 7, 9, 11):
-        assert not np.isfinite(got[row]).any(), row
-    got = host_f64(run(k, dirty[1]))                                    # the values alone: what they are comes out
-    assert np.isnan(got[[1, 7]]).all() and (got[[3, 9]] == np.inf).all() and (got[[5, 11]] == -np.inf).all()
-    # behind the window, some of which the block's first query still sees
-    window = 20
-    base = check(B, q, k, v, table, kv_lens, q_lens, 0.088, window=window, n_sinks=3)
-    dirty = [x.copy() for x in (k, v)]
-    for b, n in enumerate(kv_lens):
-        for j in [3, 15, 16] + list(range(n - 6 - window - 10, n - 6 - window + 1)) + [n - 6 - window + 2]:
-            for x in dirty:
-                x[table[b, j // 16], j % 16] = 0x7f80
-    got = host_f64(B.paged_attn(dev_bf16(q), dev_bf16(dirty[0]), dev_bf16(dirty[1]), i32(table), i32(kv_lens), 0.088, window=window, n_sinks=3))
-    for b in range(2):
-        assert not np.isfinite(got[6 * b]).any() and not np.isfinite(got[6 * b + 1]).any()
-        assert np.array_equal(got[6 * b + 2:6 * b + 6], base[6 * b + 2:6 * b + 6])
+    wide = np.concatenate([table, np.full((2, 600), -1, dtype=np.int32)], axis=1)
+    mask = torch.from_numpy(masks.view(np.int64)).cuda()
+    for entries in (table, wide):
+        run = lambda kk, vv, **more: host_f64(B.paged_attn(dev_bf16(q), dev_bf16(kk), dev_bf16(vv), i32(entries), i32(kv_lens), 0.088, **more))
+        clean = run(k, v, ancestor_mask=mask)
+        dirty = [x.copy() for x in (k, v)]
+        for b, n in enumerate(kv_lens):
+            for node, what in ((1, 0x7fc0), (3, 0x7f80), (5, 0xff80)):
+                j = n - 6 + node
+                for x in dirty:
+                    x[table[b, j // 16], j % 16] = what
+        got = run(*dirty, ancestor_mask=mask)
+        for row in (0, 2, 4, 6, 8, 10):
+            assert np.array_equal(got[row], clean[row]), row
+        for row in (1, 3, 5, 7, 9, 11):
+            assert not np.isfinite(got[row]).any(), row
+        got = run(k, dirty[1], ancestor_mask=mask)                           # the values alone: what they are comes out
+        assert np.isnan(got[[1, 7]]).all() and (got[[3, 9]] == np.inf).all() and (got[[5, 11]] == -np.inf).all()
+        # behind the window, some of which the block's first query still sees
+        window = 20
+        base = run(k, v, window=window, n_sinks=3)
+        dirty = [x.copy() for x in (k, v)]
+        for b, n in enumerate(kv_lens):
+            for j in [3, 15, 16] + list(range(n - 6 - window - 10, n - 6 - window + 1)) + [n - 6 - window + 2]:
+                for x in dirty:
+                    x[table[b, j // 16], j % 16] = 0x7f80
+        got = run(*dirty, window=window, n_sinks=3)
+        for b in range(2):
+            assert not np.isfinite(got[6 * b]).any() and not np.isfinite(got[6 * b + 1]).any()
+            assert np.array_equal(got[6 * b + 2:6 * b + 6], base[6 * b + 2:6 * b + 6])
 
 
 def test_scale_zero_and_large(B):
@@ -255,7 +269,7 @@ def test_strides(B):
     qd = qb[:, 1:9, 64:]
     qd.copy_(dev_bf16(q))
     out = torch.zeros_like(qb)[:, 1:9, 64:]
-    B.paged_attn(qd, kd, vd, wide[:, 4:4 + table.shape[1]], i32(kv_lens), 0.125, out=out)
+    B.paged_attn(qd, kd, vd, wide[:, 4:4 + table.shape[1]], i32(kv_lens), 0.125, out=out)           # (wide: rows of the table have a stride)
     plain = check(B, q, k, v, table, kv_lens, q_lens, 0.125)
     assert np.array_equal(host_f64(out), plain)
 
