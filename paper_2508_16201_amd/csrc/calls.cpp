@@ -418,21 +418,31 @@ PyObject* pages_assign(Args& a)
     const int width = a.none(6) ? given ? a.as_int(given->size(1)) : old_width : a.number(6);
     if (!a.plain || !keep || !now || pages < 0 || (given && (given->size(0) != batch || given->size(1) != width))) return nullptr;
     const Out out(a, 9, [&] { return make({batch, width}, at::kInt, *old); });
-    const Workspace ws(a, 10, *old, [&] { return c_assign_bytes(b, pages); });
-    if (!a.plain || (!a.none(10) && THPVariable_Unpack(a.o[10]).get_device() != a.device())) return nullptr;
-    // (one allocation for what is small: the parts are views of it)
-    const at::Tensor all = make({3 * batch + pages}, at::kInt, *old);
-    int32_t* const at = (int32_t*)all.data_ptr();
+    if (!a.plain) return nullptr;
+    // (one allocation for what is small, and for the workspace before it: the parts are views of it, which autograd has no part in)
+    const at::AutoDispatchBelowADInplaceOrView guard;
+    const int64_t own = a.none(10) ? (int64_t)((c_assign_bytes(b, pages) + 255) / 256 * 64) : 0;
+    const at::Tensor all = make({own + 3 * batch + pages}, at::kInt, *old);
+    int32_t* const at = (int32_t*)all.data_ptr() + own;
+    void* ws = all.data_ptr();
+    size_t ws_bytes = (size_t)own * sizeof(int32_t);
+    if (!a.none(10)) {
+        const at::Tensor* const given_ws = a.tensor(10);
+        if (!given_ws || given_ws->get_device() != a.device()) return nullptr;
+        ws = given_ws->data_ptr();
+        ws_bytes = (size_t)given_ws->numel();
+    }
     const int status = call(c_pages_assign, (const int32_t*)old->data_ptr(), old->stride(0), rows, old_width, from, keep, now, b, (int32_t*)out.at,
-                            out.tensor().stride(0), width, pages, ps, window, sinks, at, at + batch, at + 3 * batch, at + 2 * batch, ws.at, ws.bytes);
+                            out.tensor().stride(0), width, pages, ps, window, sinks, at, at + batch, at + 3 * batch, at + 2 * batch, ws, ws_bytes);
     if (status) return PyLong_FromLong(status);
+    const auto part = [&](int64_t first, int64_t n) { return THPVariable_Wrap(at::as_strided(all, {n}, {1}, own + first)); };
     PyObject* const t = PyTuple_New(5);
     if (!t) return nullptr;
     PyTuple_SET_ITEM(t, 0, out.result());
-    PyTuple_SET_ITEM(t, 1, THPVariable_Wrap(all.narrow(0, 0, batch)));
-    PyTuple_SET_ITEM(t, 2, THPVariable_Wrap(all.narrow(0, batch, batch)));
-    PyTuple_SET_ITEM(t, 3, THPVariable_Wrap(all.narrow(0, 3 * batch, pages)));
-    PyTuple_SET_ITEM(t, 4, THPVariable_Wrap(all.narrow(0, 2 * batch, batch)));
+    PyTuple_SET_ITEM(t, 1, part(0, batch));
+    PyTuple_SET_ITEM(t, 2, part(batch, batch));
+    PyTuple_SET_ITEM(t, 3, part(3 * batch, pages));
+    PyTuple_SET_ITEM(t, 4, part(2 * batch, batch));
     return t;
 }
 
