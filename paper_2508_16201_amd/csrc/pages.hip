@@ -87,6 +87,7 @@ void assign_mark_kernel(const AssignParams p)
 }
 
 // Prefix sum over the workgroup's threads: what is before the thread's x, and the total.
+template <int THREADS>
 __device__ __forceinline__ int block_before(int x, int* total, int* s_wave)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -100,7 +101,8 @@ __device__ __forceinline__ int block_before(int x, int* total, int* s_wave)
     if (lane == kWave - 1) s_wave[wave] = upto;
     __syncthreads();
     int before = upto - x, all = 0;
-    for (int i = 0; i < (int)blockDim.x / kWave; ++i) {
+#pragma unroll
+    for (int i = 0; i < THREADS / kWave; ++i) {
         if (i < wave) before += s_wave[i];
         all += s_wave[i];
     }
@@ -120,7 +122,7 @@ void assign_plan_kernel(const AssignParams p)
             const int page = blockIdx.x * kPageBlock + i * kAssignThreads + threadIdx.x;
             n += page < p.n_pages && p.ref_counts[page] == 0;
         }
-        block_before(n, &all, s_wave);
+        block_before<kAssignThreads>(n, &all, s_wave);
         if (threadIdx.x == 0) p.block_free[blockIdx.x] = all;
         return;
     }
@@ -133,7 +135,7 @@ void assign_plan_kernel(const AssignParams p)
             const int page = r.kept > r.whole ? assign_page(p, r, r.whole) : -1;
             need = r.wanted - (page >= 0 && !assign_leaves(p, page, b) ? r.kept : r.whole);
         }
-        const int before = needed + block_before(need, &all, s_wave);
+        const int before = needed + block_before<kAssignThreads>(need, &all, s_wave);
         needed += all;
         if (b < p.batch) p.start[b] = before;
     }
@@ -186,7 +188,7 @@ void assign_write_kernel(const AssignParams p)
             is_free[i] = page0 + i < p.n_pages && p.ref_counts[page0 + i] == 0;
             n += is_free[i];
         }
-        int rank = before + block_before(n, &all, s_wave);
+        int rank = before + block_before<kAssignThreads>(n, &all, s_wave);
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             if (!is_free[i] || rank >= needed) continue;
@@ -248,8 +250,8 @@ void assign_small_kernel(const AssignParams p)
     if (mine.kept > mine.whole) page = assign_page(p, mine, mine.whole);
     const bool leaves = page >= 0 && first[page] != tid;
     need = mine.wanted - (page >= 0 && !leaves ? mine.kept : mine.whole);
-    int rank = block_before(n, &free, s_wave);
-    const int before = block_before(need, &needed, s_wave);
+    int rank = block_before<kPlanThreads>(n, &free, s_wave);
+    const int before = block_before<kPlanThreads>(need, &needed, s_wave);
     if (tid < p.batch) start[tid] = before;
     if (tid == 0) start[p.batch] = needed;
     __syncthreads();
@@ -286,7 +288,7 @@ struct CopyParams {
     const int32_t *src_row, *n_rows, *src_start, *dst_start, *row_idx, *cu_idx;
     int64_t idx_stride;
     int max_rows, n_table_rows, n_layers, batch, n_mats;
-    int pieces, head_pieces, slices, row_blocks;     // 16-byte pieces of a row and of a head; workgroups that share them; workgroups over the rows
+    int pieces, head_pieces, slice, slices, row_blocks;      // 16-byte pieces of a row, of a head, of a workgroup; workgroups that share a row; workgroups over the rows
     uint32_t inv_head;
 };
 
@@ -313,7 +315,8 @@ __device__ __forceinline__ CopyToken copy_token(const CopySide& s, int64_t token
 //   1254 rows of 2 KB in 80 layers (822 MB):  kept near 168 us, not 141;  four rows of a thread 6 us more, 32 workgroups to a CU, with more
 //   layers each, 2 us more, 128 and none that share a lookup 50 us more.
 //   32 pages of 1 to 63 rows of 1 KB in 28 layers, in place:  stores kept near 38 us, not 28 (and loads that are not 35: forks of one row read
-//   one page);  4 rows in 28 layers of 8 requests 3.6 us, with four rows of a thread 3.9.
+//   one page);  a workgroup with whole rows, one run after the other, 31.6 us, with 16 pieces of each 25.1;  up to 5 rows in 28 layers of 8 requests
+//   3.5 us, with four rows of a thread 3.9.
 template <bool IN_PLACE, bool STREAM>
 __global__ __launch_bounds__(kCopyThreads)
 void pages_copy_kernel(const CopyParams p)
@@ -326,7 +329,7 @@ void pages_copy_kernel(const CopyParams p)
     if (p.cu_idx) n = min(n, p.cu_idx[b + 1] - first);
     if (p.n_rows) n = min(n, p.n_rows[b]);
     // the lanes lie over the pieces of a row, several rows at once where a row is short
-    const int per_row = min(p.pieces, kCopyThreads), rows = kCopyThreads / per_row, step = rows * EACH;
+    const int per_row = p.slice, rows = kCopyThreads / per_row, step = rows * EACH;
     if (block * step >= n) return;
     const int from = p.src_row ? p.src_row[b] : b;
     const bool there = from >= 0 && from < p.n_table_rows && p.src.max_pages > 0;
@@ -334,7 +337,7 @@ void pages_copy_kernel(const CopyParams p)
     const int32_t* const dst_table = p.dst.table + b * p.dst.row;
     const int32_t* const idx = p.row_idx ? p.row_idx + (p.cu_idx ? (int64_t)first : b * p.idx_stride) : nullptr;
     const int64_t src0 = p.src_start ? p.src_start[b] : 0, dst0 = p.dst_start ? p.dst_start[b] : 0;
-    const int lane_row = threadIdx.x / per_row, piece = slice * kCopyThreads + threadIdx.x % per_row;
+    const int lane_row = threadIdx.x / per_row, piece = slice * per_row + threadIdx.x % per_row;
     const bool on = lane_row < rows && piece < p.pieces && p.dst.max_pages > 0;
     const QuotRem at = divide(piece, p.head_pieces, p.inv_head);
     for (int i0 = block * step; i0 < n; i0 += IN_PLACE ? step : step * p.row_blocks) {
@@ -394,7 +397,11 @@ void pages_copy_kernel(const CopyParams p)
 template <bool IN_PLACE, bool STREAM>
 static int launch_copy(CopyParams& p, hipStream_t stream)
 {
-    const int per_row = p.pieces < kCopyThreads ? p.pieces : kCopyThreads, step = kCopyThreads / per_row * kCopyEach;
+    p.slice = p.pieces < kCopyThreads ? p.pieces : kCopyThreads;
+    // in place a workgroup goes over its rows one run after the other: columns are shared out until a run has all of them, or is one of 16 pieces
+    while (IN_PLACE && p.slice > 16 && kCopyThreads / p.slice * kCopyEach < p.max_rows) p.slice = p.slice / 2 > 16 ? p.slice / 2 : 16;
+    p.slices = (p.pieces + p.slice - 1) / p.slice;
+    const int step = kCopyThreads / p.slice * kCopyEach;
     p.row_blocks = IN_PLACE ? 1 : (p.max_rows + step - 1) / step;
     if ((int64_t)p.row_blocks * p.slices > INT_MAX) return SPECVLM_EUNSUPPORTED;
     // layers of K and V that share a workgroup, and its lookups: as many as leave workgroups enough
@@ -506,7 +513,6 @@ extern "C" int specvlm_pages_copy(
     p.idx_stride = idx_stride; p.max_rows = max_rows; p.n_table_rows = src_rows; p.n_layers = n_layers; p.batch = batch; p.n_mats = mats;
     p.head_pieces = head_dim / 8; p.pieces = n_kv_heads * p.head_pieces;
     p.inv_head = reciprocal(p.head_pieces);
-    p.slices = (p.pieces + kCopyThreads - 1) / kCopyThreads;
     const bool in_place = k_src == k_dst || (v_src && v_src == v_dst);
     hipStream_t s = (hipStream_t)stream;
     if (in_place) return launch_copy<true, true>(p, s);
