@@ -480,8 +480,8 @@ int specvlm_rope_append(
  *   old_table   int32 [old_rows, old_max_pages], rows old_stride apart; an entry that is no
  *               page of the pool stays -1
  *   page_table  int32 [batch, max_pages], rows table_stride apart (>= max_pages); every entry is
- *               written, -1 behind the last page.  Must not overlap old_table.
- *   ref_counts  int32 [n_pages]: rows of the new table that hold each page
+ *               written, -1 behind the last page.  Must not overlap old_table (SPECVLM_EINVAL).
+ *   ref_counts  int32 [n_pages]: rows of the new table that hold each page (with batch 0, none)
  *   status      int32 [batch]: SPECVLM_OK; SPECVLM_EINVAL for a row that does not fit together
  *               (parent outside [-1, old_rows), keep_len > new_len, negative, kept tokens of
  *               nothing, more pages than a table has), which gets none; SPECVLM_ENOPAGES for a
@@ -522,6 +522,7 @@ int specvlm_pages_assign(
  * request may then overlap if its indices ascend and no row moves to a later token of the
  * same table row.  No request's destination may be another's source or destination.  Pools that are not
  * the same must not overlap.
+ * Limits: batch <= 65535, max_rows <= 2^30.
  * -------------------------------------------------------------------------- */
 int specvlm_pages_copy(
     const void* k_src, const void* v_src, int64_t src_layer_stride, int64_t src_page_stride, int64_t src_tok_stride, int64_t src_head_stride,

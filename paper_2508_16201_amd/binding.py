@@ -612,6 +612,8 @@ ROPE_SCALINGS = {None: 0, "linear": 1, "base": 2, "by-parts": 3}
 def rope_turns(rot_dim: int, base: float, *, scaling: Optional[str] = None, factor: float = 1.0, original_len: float = 0.0,
                beta_fast: float = 32.0, beta_slow: float = 1.0, device=None) -> torch.Tensor:
     """The frequencies of rotary positions for rope_append: int64 [rot_dim / 2], turns a position in units of 2^-64."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {list(ROPE_SCALINGS)}")
     turns = np.zeros(max(rot_dim, 0) // 2, dtype=np.uint64)
     spec = _RopeSpec(ROPE_SCALINGS[scaling], base, factor, original_len, beta_fast, beta_slow)
     _check("specvlm_rope_turns", lib().specvlm_rope_turns(rot_dim, C.byref(spec), turns.ctypes.data))
@@ -743,6 +745,8 @@ def pages_copy(k_src: torch.Tensor, v_src: Optional[torch.Tensor], src_table: to
     if cu_idx is not None:
         _int32s(batch + 1, cu_idx=cu_idx)
         _int32s(None, row_idx=row_idx)
+        if row_idx is not None and row_idx.numel() == 0:        # (lists of which each is empty)
+            return
     elif row_idx is not None:
         if row_idx.dim() != 2 or row_idx.shape[0] != batch or row_idx.shape[1] < max_rows or (row_idx.shape[1] > 1 and row_idx.stride(1) != 1):
             raise ValueError("row_idx must be [batch, at least max_rows] with contiguous rows")

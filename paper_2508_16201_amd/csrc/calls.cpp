@@ -458,7 +458,7 @@ PyObject* pages_copy(Args& a)
               rows = a.as_int(from->size(0)), src_width = a.as_int(from->size(1)), dst_width = a.as_int(to->size(1));
     const at::Tensor* const idx = a.none(11) ? nullptr : a.tensor(11, a.none(12) ? 2 : 1, at::kInt);
     const int32_t* const cu = a.vector(12, batch + 1);
-    if (!a.plain || (cu && !idx)) return nullptr;
+    if (!a.plain || (cu && (!idx || idx->numel() == 0))) return nullptr;
     if (idx && (cu ? !idx->is_contiguous() : idx->size(0) != batch || idx->size(1) < most || idx->stride(1) != 1)) return nullptr;
     const int status = call(c_pages_copy, src->data_ptr(), a.none(1) ? nullptr : THPVariable_Unpack(a.o[1]).data_ptr(), src->stride(0), src->stride(1),
                             src->stride(2), src->stride(3), src_pages, src_ps, (const int32_t*)from->data_ptr(), from->stride(0), rows, src_width, dst->data_ptr(),

@@ -71,7 +71,9 @@ __global__ __launch_bounds__(kAssignThreads)
 void assign_clear_kernel(const AssignParams p)
 {
     const int i = blockIdx.x * kAssignThreads + threadIdx.x;
-    if (i < p.n_pages) { p.ref_counts[i] = 0; p.first[i] = INT_MAX; }
+    if (i >= p.n_pages) return;
+    p.ref_counts[i] = 0;
+    if (p.batch) p.first[i] = INT_MAX;                // (no rows: no workspace)
 }
 
 __global__ __launch_bounds__(kAssignThreads)
@@ -403,7 +405,7 @@ static int launch_copy(CopyParams& p, hipStream_t stream)
     p.slices = (p.pieces + p.slice - 1) / p.slice;
     const int step = kCopyThreads / p.slice * kCopyEach;
     p.row_blocks = IN_PLACE ? 1 : (p.max_rows + step - 1) / step;
-    if ((int64_t)p.row_blocks * p.slices > INT_MAX) return SPECVLM_EUNSUPPORTED;
+    if ((int64_t)p.row_blocks * p.slices > (int64_t)UINT32_MAX / kCopyThreads) return SPECVLM_EUNSUPPORTED;      // (a launch's threads)
     // layers of K and V that share a workgroup, and its lookups: as many as leave workgroups enough
     const int64_t each = (int64_t)p.row_blocks * p.slices * p.batch;
     int64_t z = (kCopyTarget + each - 1) / each;
@@ -415,6 +417,17 @@ static int launch_copy(CopyParams& p, hipStream_t stream)
 }  // namespace specvlm
 
 using namespace specvlm;
+
+// Whether two tables have a byte in common (columns of one table, cut side by side, have none).
+static bool tables_overlap(const int32_t* a, int64_t a_stride, int a_rows, int a_width, const int32_t* b, int64_t b_stride, int b_rows, int b_width)
+{
+    if (a_rows == 0 || a_width == 0 || b_rows == 0 || b_width == 0) return false;
+    const int64_t from_a = ((int64_t)(uintptr_t)b - (int64_t)(uintptr_t)a) / (int64_t)sizeof(int32_t);
+    if (from_a >= (a_rows - 1) * a_stride + a_width || -from_a >= (b_rows - 1) * b_stride + b_width) return false;
+    if (a_stride != b_stride || a_stride <= 0 || (a_rows == 1 && b_rows == 1)) return true;
+    const int64_t column = ((from_a % a_stride) + a_stride) % a_stride;
+    return column < a_width || column + b_width > a_stride;
+}
 
 static int assign_blocks(int n_pages) { return (n_pages + kPageBlock - 1) / kPageBlock; }
 
@@ -436,10 +449,18 @@ extern "C" int specvlm_pages_assign(
         old_stride < 0)
         return SPECVLM_EINVAL;
     if (page_size % 16) return SPECVLM_EUNSUPPORTED;
-    if (batch == 0) return SPECVLM_OK;
+    if (batch == 0) {                                 // (nobody holds a page)
+        if (n_pages == 0) return SPECVLM_OK;
+        if (!ref_counts) return SPECVLM_EINVAL;
+        AssignParams p = {};
+        p.ref_counts = ref_counts; p.n_pages = n_pages;
+        hipLaunchKernelGGL(assign_clear_kernel, dim3((n_pages - 1) / kAssignThreads + 1), dim3(kAssignThreads), 0, (hipStream_t)stream, p);
+        return launch_status();
+    }
     if (!parent || !keep_len || !new_len || !copy_start || !copy_rows || !status || (!ref_counts && n_pages > 0)) return SPECVLM_EINVAL;
     if ((!old_table && old_rows > 0 && old_max_pages > 0) || (!page_table && max_pages > 0)) return SPECVLM_EINVAL;
     if (batch > 1 && table_stride < max_pages) return SPECVLM_EINVAL;                  // (rows that overlap)
+    if (tables_overlap(old_table, old_stride, old_rows, old_max_pages, page_table, table_stride, batch, max_pages)) return SPECVLM_EINVAL;
     const int most = old_max_pages > max_pages ? old_max_pages : max_pages;
     const int chunks = most ? (most + kAssignThreads - 1) / kAssignThreads : 1;
     if ((int64_t)batch * max_pages > INT_MAX / 2 || (int64_t)batch * chunks + assign_blocks(n_pages) > INT_MAX / 2) return SPECVLM_EUNSUPPORTED;
@@ -501,7 +522,7 @@ extern "C" int specvlm_pages_copy(
                             dst_tok_stride | dst_head_stride;
     if ((strides & 7) || (((uintptr_t)k_src | (uintptr_t)v_src | (uintptr_t)k_dst | (uintptr_t)v_dst) & 15)) return SPECVLM_EUNSUPPORTED;
     const int mats = v_src ? 2 : 1;
-    if (batch > 65535 || (int64_t)n_layers * mats > 65535 || n_kv_heads > (1 << 20)) return SPECVLM_EUNSUPPORTED;
+    if (batch > 65535 || (int64_t)n_layers * mats > 65535 || n_kv_heads > (1 << 20) || max_rows > (1 << 30)) return SPECVLM_EUNSUPPORTED;
 
     CopyParams p;
     p.k_src = (const __bf16*)k_src; p.v_src = (const __bf16*)v_src; p.k_dst = (__bf16*)k_dst; p.v_dst = (__bf16*)v_dst;

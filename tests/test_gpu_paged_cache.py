@@ -524,3 +524,37 @@ def test_a_window_that_moves_on(B):
 def test_assign_from_no_rows(B):
     """The first table of a program: nothing to go on from."""
     check_assign(B, np.zeros((0, 2), dtype=np.int32), [-1, -1], [0, 0], [20, 1], 5, 16)
+
+
+def test_assign_for_no_rows(B):
+    """The last request ended: every page is free, and the counts say so."""
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    junk = torch.full((1 << 20,), 7, dtype=torch.int32, device="cuda")
+    del junk                                                                             # (what the next allocations find)
+    table, start, rows, refs, status = B.pages_assign(i32([[0, 1]]), none, none, none, 700, 16)
+    assert table.shape == (0, 2) and start.numel() == rows.numel() == status.numel() == 0
+    assert refs.shape == (700,) and not refs.any()
+
+
+def test_assign_refuses_a_table_over_the_old_one(B):
+    both = torch.full((2, 6), -1, dtype=torch.int32, device="cuda")
+    old, one = both[:, :3], i32([0, 1])
+    for out in (old, both[:, 2:5], both[:, 1:4]):
+        with pytest.raises(B.SpecVLMError) as e:
+            B.pages_assign(old, one, i32([0, 0]), i32([5, 20]), 9, 16, out=out)
+        assert e.value.status == -1
+    B.pages_assign(old, one, i32([0, 0]), i32([5, 20]), 9, 16, out=both[:, 3:])          # side by side
+    assert both.tolist() == [[-1, -1, -1, 0, -1, -1], [-1, -1, -1, 1, 2, -1]]
+
+
+def test_copy_of_empty_lists(B):
+    k = torch.ones((2, 4, 16, 2, 64), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    t = i32([[0, 1], [2, 3]])
+    B.pages_copy(v, v, t, k, k, t, None, 8, row_idx=torch.zeros(0, dtype=torch.int32, device="cuda"), cu_idx=i32([0, 0, 0]))
+    assert (k == 1).all()
+
+
+def test_turns_of_an_unknown_scaling(B):
+    with pytest.raises(ValueError):
+        B.rope_turns(64, 1e4, scaling="cubic")

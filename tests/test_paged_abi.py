@@ -27,7 +27,7 @@ ROPE = dict(q=AT, q_tok_stride=1792, q_head_stride=128, q_out=AT, out_tok_stride
             kv_head_stride=128, k_pages=AT, v_pages=AT, page_stride=16 * 512, tok_stride=512, head_stride=128, n_pages=100, page_size=16,
             page_table=AT, table_stride=50, max_pages=50, kv_lens=AT, batch=3, n_tokens=6, turns=AT, rot_dim=128, magnitude=1.0, n_q_heads=28,
             n_kv_heads=4, head_dim=128)
-ASSIGN = dict(old_table=AT, old_stride=50, old_rows=3, old_max_pages=50, parent=AT, keep_len=AT, new_len=AT, batch=3, page_table=AT, table_stride=50,
+ASSIGN = dict(old_table=AT, old_stride=50, old_rows=3, old_max_pages=50, parent=AT, keep_len=AT, new_len=AT, batch=3, page_table=2 * AT, table_stride=50,
               max_pages=50, n_pages=100, page_size=16, copy_start=AT, copy_rows=AT, ref_counts=AT, status=AT, workspace=AT, workspace_bytes=1 << 40)
 COPY = dict(k_src=AT, v_src=AT, src_layer_stride=819200, src_page_stride=8192, src_tok_stride=512, src_head_stride=128, src_pages=100, src_page_size=16,
             src_table=AT, src_table_stride=50, src_rows=3, src_max_pages=50, k_dst=2 * AT, v_dst=2 * AT, dst_layer_stride=819200, dst_page_stride=8192,
@@ -59,16 +59,25 @@ REFUSED = [
     *[("specvlm_pages_assign", {k: -1}, -1) for k in ("old_rows", "old_max_pages", "batch", "max_pages", "n_pages", "window", "n_sinks", "old_stride")],
     ("specvlm_pages_assign", {"page_size": 0}, -1), ("specvlm_pages_assign", {"page_size": 40}, -2), ("specvlm_pages_assign", {"table_stride": 49}, -1),
     ("specvlm_pages_assign", {"workspace": None}, -3), ("specvlm_pages_assign", {"workspace_bytes": 300}, -3), ("specvlm_pages_assign", {"workspace": AT + 4}, -3),
+    # the new table over the old one: the same, a row on, from behind, into the last row, one row each;  but columns of one table side by side are two
+    *[("specvlm_pages_assign", {"page_table": AT + 4 * at}, -1) for at in (0, 50, 37, -149, 149)],
+    ("specvlm_pages_assign", {"page_table": AT + 4 * 150}, 0), ("specvlm_pages_assign", {"page_table": AT - 4 * 150}, 0),
+    ("specvlm_pages_assign", {"page_table": AT + 4 * 50, "old_stride": 100, "table_stride": 100}, 0),
+    ("specvlm_pages_assign", {"page_table": AT + 4 * 49, "old_stride": 100, "table_stride": 100}, -1),
+    ("specvlm_pages_assign", {"page_table": AT - 4 * 40, "old_stride": 100, "table_stride": 100}, -1),
+    ("specvlm_pages_assign", {"page_table": AT + 4 * 50, "old_stride": 100, "table_stride": 101}, -1),
+    ("specvlm_pages_assign", {"page_table": AT, "old_rows": 0}, 0), ("specvlm_pages_assign", {"batch": 0, "ref_counts": None}, -1),
     *[("specvlm_pages_copy", {k: None}, -1) for k in ("k_src", "k_dst", "v_src", "v_dst", "src_table", "dst_table")],
     *[("specvlm_pages_copy", {k: -1}, -1) for k in ("src_pages", "src_rows", "src_max_pages", "dst_pages", "dst_max_pages", "n_layers", "batch", "max_rows",
                                                      "src_table_stride", "dst_table_stride", "idx_stride")],
     ("specvlm_pages_copy", {"cu_idx": AT}, -1), ("specvlm_pages_copy", {"src_rows": 2}, -1), ("specvlm_pages_copy", {"n_kv_heads": 0}, -1),
     ("specvlm_pages_copy", {"head_dim": 32}, -2), ("specvlm_pages_copy", {"src_page_size": 20}, -2), ("specvlm_pages_copy", {"dst_page_size": 20}, -2),
     ("specvlm_pages_copy", {"dst_tok_stride": 20}, -2), ("specvlm_pages_copy", {"k_src": AT + 8}, -2), ("specvlm_pages_copy", {"batch": 65536, "src_rows": 65536}, -2),
-    ("specvlm_pages_copy", {"n_layers": 40000}, -2),
+    ("specvlm_pages_copy", {"n_layers": 40000}, -2), ("specvlm_pages_copy", {"max_rows": (1 << 30) + 1}, -2),
+    ("specvlm_pages_copy", {"max_rows": 1 << 30}, -2), ("specvlm_pages_copy", {"max_rows": 1 << 30, "k_dst": AT, "v_dst": AT}, 0),
 ]
 NOTHING = [("specvlm_paged_attn", {"batch": 0}), ("specvlm_paged_attn", {"q_len": 0}), ("specvlm_rope_append", {"batch": 0}), ("specvlm_rope_append", {"n_tokens": 0}),
-           ("specvlm_rope_append", {"q": None, "k": None, "v": None}), ("specvlm_pages_assign", {"batch": 0}), ("specvlm_pages_copy", {"batch": 0}),
+           ("specvlm_rope_append", {"q": None, "k": None, "v": None}), ("specvlm_pages_assign", {"batch": 0, "n_pages": 0}), ("specvlm_pages_copy", {"batch": 0}),
            ("specvlm_pages_copy", {"n_layers": 0}), ("specvlm_pages_copy", {"max_rows": 0})]
 
 
@@ -87,6 +96,8 @@ def test_launches(tmp_path):
                       ("specvlm_rope_append", {**ROPE, "q": None, "q_out": None}), ("specvlm_rope_append", {**ROPE, "k": None, "v": None})], tmp_path)
     assert [status for status, _ in got] == [0] * 5
     assert [len(launched) for _, launched in got] == [1] * 5
+    (status, launched), = L.launches([("specvlm_pages_assign", {**ASSIGN, "batch": 0, "workspace": None})], tmp_path)
+    assert status == 0 and len(launched) == 1                                          # no rows: nobody holds a page
     assert "true" in got[2][1][0][0] and "false" in got[1][1][0][0]                     # one pool: in order
 
 
