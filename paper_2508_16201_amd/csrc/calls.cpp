@@ -1,6 +1,8 @@
 // The short calls of binding.py in native code.  Calls of a few microseconds of GPU time were bound by the host, and up to half of
 // that was Python taking tensors apart (us of host time a call, its launches of 2.65 each included, in Python / here):  greedy and sampling
-// acceptance 8.2 / 5.35, scores of one small layer 12.3 / 8.5, selection and gather 14.45 / 8.0, attention of a ragged batch 14.5 / 9.7.
+// acceptance 8.2 / 5.35, scores of one small layer 12.3 / 8.5, selection and gather 14.45 / 8.0, attention of a ragged batch 14.5 / 9.7.  Calls over paged
+// caches one behind the other, what the GPU takes included:  a block's rows turned and appended 15 / 4.5, accepted rows moved 16.7 / 4.6, one token's
+// attention 17.4 / 9.75 (two launches).
 //
 // Every function here takes the arguments of its namesake in binding.py by position and serves the plain call: tensors of torch's
 // own types in the memory of a GPU, numbers of Python's and NumPy's types, arguments that fit together.  It returns that function's
