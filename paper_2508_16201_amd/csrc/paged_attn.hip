@@ -20,8 +20,8 @@
 // request; group j (a workgroup for each kv head and row group) takes a run of equal length, which every workgroup
 // finds by a prefix sum over the lengths, 64 requests at a time in the lanes of a wave.  A captured launch so stays
 // balanced as the caches grow.  A request that one group covers is written out directly; the others leave partial
-// results that the second launch joins.  Short caches take one launch in which a workgroup has a request's keys of a head
-// whole (paged_takes_whole has the line).
+// results that the second launch joins.  Short caches take one launch: a workgroup has a request's keys of a head whole (paged_takes_whole has the
+// line), and where those would be few workgroups a slice of its value columns (paged_short_kernel, paged_short_chunks).
 //
 // A workgroup has MB*KS compute waves (row block mb, every KS-th 32-key chunk of a tile) and NLD loader waves that only issue
 // direct-to-LDS loads into a ring of NS tiles (see decode_attn.hip for the matrix formulation and the swizzles).  The two roles plan for
@@ -53,6 +53,9 @@ struct PagedParams {
     uint32_t inv_page, inv_heads, inv_all_heads, inv_group, inv_rgroups, inv_groups;
     float scale_log2;
     int n_rgroups, rows_pad, max_groups;
+    int n_units;             // (paged_short_kernel) requests' kv heads' blocks of 16 rows
+    int last_units;          // of them, what is left of the last eight (1 to 8)
+    uint32_t inv_last;
     float* part_o;           // [(groups + batch) * H_kv][rows_pad][D] unnormalised partial outputs
     float* part_ml;          // [(groups + batch) * H_kv][rows_pad][2] running maximum in log2 units, sum
 };
@@ -177,6 +180,48 @@ __device__ __forceinline__ void wait_tiles(int younger)
         if (younger < MOST) return wait_tiles<LPW, MOST - 1>(younger);
     }
     wait_vmcnt<MOST * LPW>();
+}
+
+// A value that is no number (an infinity, rows never written) belongs only to the rows that see its key, and 0 times it is no zero (by which the
+// products with 0 find it): it is left out of the product, and the rows get it by how many such values they see.  sees: bits 0..3 and 16..19,
+// the lane's keys that its row sees.
+template <int DJ>
+__device__ __forceinline__ void take_odd_values(bf16x8 (&vf)[DJ], uint32_t sees, floatx4 (&o_acc)[DJ])
+{
+    const floatx4 none = {0.f, 0.f, 0.f, 0.f};
+    floatx4 odd = none;
+#pragma unroll
+    for (int jj = 0; jj < DJ; ++jj) odd = mfma16(vf[jj], __builtin_bit_cast(bf16x8, u32x4{}), odd);
+    if (__builtin_expect(__any(!(odd[0] + odd[1] + odd[2] + odd[3] == 0.f)), 0)) {
+        u32x4 seen;                                   // bf16 0 or 1
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t two = sees >> (e < 2 ? 2 * e : 2 * e + 12);
+            seen[e] = (two & 1u) * 0x3f80u | (two & 2u) * (0x3f800000u / 2);
+        }
+#pragma unroll
+        for (int jj = 0; jj < DJ; ++jj) {
+            u32x4 w = __builtin_bit_cast(u32x4, vf[jj]), up, down, nan;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {             // (two halves a word: a carry into bit 15 says that a size is an infinity's or more, or more than one)
+                const uint32_t size = w[e] & 0x7fff7fffu, odd2 = (size + 0x00800080u) >> 15 & 0x00010001u;
+                nan[e] = (size + 0x007f007fu) >> 15 & 0x00010001u;
+                down[e] = (odd2 ^ nan[e]) & w[e] >> 15;
+                up[e] = odd2 ^ nan[e] ^ down[e];
+                w[e] &= ~(odd2 * 0xffffu);
+            }
+            vf[jj] = __builtin_bit_cast(bf16x8, w);
+            const auto count = [&](u32x4 x) { return mfma16(__builtin_bit_cast(bf16x8, x * 0x3f80u), __builtin_bit_cast(bf16x8, seen), none); };
+            const floatx4 n_up = count(up), n_down = count(down), n_nan = count(nan);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (n_up[e] > 0.f) o_acc[jj][e] += INFINITY;
+                if (n_down[e] > 0.f) o_acc[jj][e] += -INFINITY;
+                if (n_nan[e] > 0.f) o_acc[jj][e] = NAN;
+            }
+            __builtin_amdgcn_sched_barrier(0);        // (one after the other: the registers of all at once would be the kernel's most)
+        }
+    }
 }
 
 // MB: row blocks of 16, one to a compute wave.  KS: chunks of 32 keys of a tile, a wave for each.  NS: tiles of the ring.  NLD: loader waves.
@@ -390,45 +435,7 @@ void paged_split_kernel(const PagedParams p)
             }
             if (need_mask || fresh) fresh = __any(!(m_run > -INFINITY));
             if (need_mask) {
-                // A value that is no number (an infinity, rows never written) belongs only to the rows that see its key, and 0
-                // times it is no zero (by which the products with 0 find it): it is left out of the product, and the rows get it by
-                // how many such values they see.
-                const floatx4 none = {0.f, 0.f, 0.f, 0.f};
-                floatx4 odd = none;
-#pragma unroll
-                for (int jj = 0; jj < DJ; ++jj) odd = mfma16(vf[jj], __builtin_bit_cast(bf16x8, u32x4{}), odd);
-                if (__builtin_expect(__any(!(odd[0] + odd[1] + odd[2] + odd[3] == 0.f)), 0)) {
-                    u32x4 seen;                                   // bf16 0 or 1
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t two = sees >> (e < 2 ? 2 * e : 2 * e + 12);
-                        seen[e] = (two & 1u) * 0x3f80u | (two & 2u) * (0x3f800000u / 2);
-                    }
-#pragma unroll
-                    for (int jj = 0; jj < DJ; ++jj) {
-                        u32x4 w = __builtin_bit_cast(u32x4, vf[jj]), up, down, nan;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {             // (two halves a word: a carry into bit 15 says that a size is an infinity's or more, or more than one)
-                            const uint32_t size = w[e] & 0x7fff7fffu, odd2 = (size + 0x00800080u) >> 15 & 0x00010001u;
-                            nan[e] = (size + 0x007f007fu) >> 15 & 0x00010001u;
-                            down[e] = (odd2 ^ nan[e]) & w[e] >> 15;
-                            up[e] = odd2 ^ nan[e] ^ down[e];
-                            w[e] &= ~(odd2 * 0xffffu);
-                        }
-                        vf[jj] = __builtin_bit_cast(bf16x8, w);
-                        const auto count = [&](u32x4 x) {
-                            return mfma16(__builtin_bit_cast(bf16x8, x * 0x3f80u), __builtin_bit_cast(bf16x8, seen), none);
-                        };
-                        const floatx4 n_up = count(up), n_down = count(down), n_nan = count(nan);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            if (n_up[e] > 0.f) o_acc[jj][e] += INFINITY;
-                            if (n_down[e] > 0.f) o_acc[jj][e] += -INFINITY;
-                            if (n_nan[e] > 0.f) o_acc[jj][e] = NAN;
-                        }
-                        __builtin_amdgcn_sched_barrier(0);        // (one after the other: the registers of all at once would be the kernel's most)
-                    }
-                }
+                take_odd_values(vf, sees, o_acc);
             }
             // ---- O^T += V^T P^T, the probabilities as two bf16 each: rounded to one, their error (2^-9 of each term) was as large as the
             // output's own rounding, and the result 1.45 times as far from the sums in 64 bits as one that is only rounded at the end ----
@@ -492,6 +499,203 @@ void paged_split_kernel(const PagedParams p)
             if (c == 0 && ks == 0) { p.part_ml[(slot0 + row) * 2] = m_all; p.part_ml[(slot0 + row) * 2 + 1] = l_all; }
         }
     });
+}
+
+// Short caches of few heads and requests.  A workgroup has 16 query rows and 16 value COLUMNS over all keys: the column slices compute the same logits, and
+// in return there are no partial results and one launch.  Sixteen waves have CH chunks of 32 places each and issue all their loads, through registers,
+// before they wait for the first (the bytes in flight are then not bound by a ring in LDS: 1511 keys of size 64 in whole workgroups 10 us, here 6.8).  All logits of
+// a wave are there before its maximum is taken, so nothing is rescaled; the waves meet once, at the end.  Without a window the pages are looked up while the
+// lengths are on their way.  Tried: chunks dealt to the waves in turn (700 keys of size 64 5.6 us, not 5.1: more lines for masked places), helper workgroups
+// that touch the rows for the XCD's L2 (size 128, 1000 keys 8.8 / 7.9, where the split takes 7.5; 512 and size 64 the same).
+template <int D, int CH>
+__global__ __launch_bounds__(16 * kWave)
+void paged_short_kernel(const PagedParams p)
+{
+    constexpr int NW = 16, COLS = 16, SLICES = D / COLS, KK = D / 32, KP = D / 8, KPL = kWave / KP, LPG = 16 / KPL, KL = 2 * LPG;
+    constexpr int ROW_BYTES = D * 2, K_BYTES = kChunkKeys * ROW_BYTES, WAVE_LDS = K_BYTES + kChunkKeys * COLS * 2;
+    extern __shared__ __align__(16) unsigned char smem[];
+    float (*s_m)[NW] = reinterpret_cast<float (*)[NW]>(smem + NW * WAVE_LDS);
+    float (*s_l)[NW] = s_m + 16;
+    // (the parameters together: fetched where each is first used, one wait after the other, 8 requests of 500 keys took 7.1 us, not 6.9)
+    __asm__ volatile("" :: "s"(p.q), "s"(p.k), "s"(p.v), "s"(p.q_tok), "s"(p.q_head), "s"(p.page), "s"(p.tok), "s"(p.head), "s"(p.table), "s"(p.table_row),
+                     "s"(p.kv_lens), "s"(p.cu_q), "s"(p.n_pages), "s"(p.page_size), "s"(p.q_len), "s"(p.kv_len), "s"(p.n_kv_heads), "s"(p.group),
+                     "s"(p.window), "s"(p.n_sinks), "s"(p.inv_page), "s"(p.inv_heads), "s"(p.inv_group), "s"(p.inv_rgroups), "s"(p.n_rgroups));
+    __asm__ volatile("" :: "s"(p.scale_log2), "s"(p.block_mask), "s"(p.n_units), "s"(p.last_units), "s"(p.inv_last));
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, c = lane >> 4;
+    // ids go round the XCDs: the slices of a unit lie 8 apart (or as many as are left) and share an L2 where there are units enough (8 requests of 1024
+    // keys, 14/2 heads 7.6 us with a request's heads side by side, 6.6 here)
+    const int eights = blockIdx.x / (kNumXcd * SLICES), in = blockIdx.x % (kNumXcd * SLICES);
+    QuotRem at_unit = {in / kNumXcd, in % kNumXcd};
+    if (kNumXcd * (eights + 1) > p.n_units) at_unit = divide(in, p.last_units, p.inv_last);
+    const int slice = at_unit.q, unit = kNumXcd * eights + at_unit.r;
+    const QuotRem head = divide(unit, p.n_kv_heads, p.inv_heads), block = divide(head.q, p.n_rgroups, p.inv_rgroups);
+    const int g = head.r, rb = block.r, b = block.q;
+    const int x0 = wave * (CH * kChunkKeys);
+    const SPECVLM_AS4 int32_t* const table = (const SPECVLM_AS4 int32_t*)(uintptr_t)(p.table + (int64_t)b * p.table_row);
+    const PagedRequest rq = paged_request(p, b);
+    const PagedView view = paged_view(p, rq.ql, rq.kvl);
+    // the pages, which without a window do not wait for the lengths (places behind the last are masked)
+    int id[2 * CH], at_row[2 * CH];
+#pragma unroll
+    for (int i = 0; i < 2 * CH; ++i) {
+        int key;
+        if (p.window == 0) key = min(x0 + 16 * i, (p.kv_len - 1) & ~15);
+        else { const int x = max(min(x0 + 16 * i, (view.n - 1) & ~15), 0); key = x < view.sinks ? x : x + view.skip; }
+        const QuotRem at = divide(key, p.page_size, p.inv_page);
+        id[i] = table[at.q];
+        at_row[i] = at.r;
+    }
+    const int kvl = rq.kvl, before = kvl - rq.ql, n_rows = p.group * rq.ql, n = view.n;
+    if (n == 0 || rb * 16 >= n_rows) return;
+    const int row = rb * 16 + r;
+    const QuotRem q_at = divide(row < n_rows ? row : 0, p.group, p.inv_group);       // (padding rows take row 0: never stored)
+    const int t_blk = q_at.q;
+    unsigned char* const k_lds = smem + wave * WAVE_LDS;
+    unsigned char* const v_lds = k_lds + K_BYTES;
+    float m = -INFINITY, l = 0.f;
+    floatx4 o_acc[1] = {floatx4{0.f, 0.f, 0.f, 0.f}};
+    if (x0 < n) {
+        bf16x8 qf[KK];
+        u32x4 kraw[CH][KL], vraw[CH];
+        const __bf16* qp = p.q + (int64_t)(rq.q0 + t_blk) * p.q_tok + (int64_t)(g * p.group + q_at.r) * p.q_head + c * 8;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(qp + kk * 32);
+        const char* const kmat = reinterpret_cast<const char*>(p.k + (int64_t)g * p.head);
+        const char* const vmat = reinterpret_cast<const char*>(p.v + (int64_t)g * p.head + slice * COLS);
+        uint32_t k_off[LPG];
+#pragma unroll
+        for (int i = 0; i < LPG; ++i) k_off[i] = (uint32_t)(i * KPL + lane / KP) * (uint32_t)(p.tok * 2) + (uint32_t)(lane % KP) * 16u;
+        const uint32_t v_off = (uint32_t)(lane / 2 % 16) * (uint32_t)(p.tok * 2) + (uint32_t)(lane % 2) * 16u;
+        uint32_t ok = 0;
+        int64_t page_at[2 * CH];
+#pragma unroll
+        for (int i = 0; i < 2 * CH; ++i) {
+            const bool there = (uint32_t)id[i] < (uint32_t)p.n_pages;
+            ok |= (there ? 1u : 0u) << i;
+            page_at[i] = 2 * ((there ? id[i] : 0) * p.page + at_row[i] * p.tok);
+        }
+#pragma unroll
+        for (int ch = 0; ch < CH; ++ch)
+#pragma unroll
+            for (int i = 0; i < KL; ++i) kraw[ch][i] = *reinterpret_cast<const u32x4*>(kmat + page_at[2 * ch + i / LPG] + k_off[i % LPG]);
+#pragma unroll
+        for (int ch = 0; ch < CH; ++ch) {
+            const int64_t first = page_at[2 * ch], second = page_at[2 * ch + 1] - first;
+            vraw[ch] = *reinterpret_cast<const u32x4*>(vmat + first + ((lane < 32 ? 0 : second) + v_off));
+        }
+        const float sc = fmaxf(p.scale_log2, 1e-30f);
+        const int edge = p.window ? kvl - p.window - view.skip : 0;
+        const uint64_t row_mask = p.block_mask ? p.block_mask[rq.q0 + t_blk] : ((2ull << t_blk) - 1ull);
+        const int hidden_to = p.window ? before + t_blk - p.window : -1;
+        float s[CH][8], mx = -INFINITY;
+        uint32_t sees[CH];
+#pragma unroll
+        for (int ch = 0; ch < CH; ++ch) {
+#pragma unroll
+            for (int i = 0; i < KL; ++i) {
+                const int kl = i * KPL + lane / KP, swz = (D == 128) ? (kl & 15) : ((kl >> 1) & 7);
+                *reinterpret_cast<u32x4*>(k_lds + kl * ROW_BYTES + (((lane % KP) ^ swz) * 16)) = kraw[ch][i];
+            }
+            floatx4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                const int x = (kk * 4 + c) ^ ((D == 128) ? r : (r >> 1));
+                const u32x4 k0 = *reinterpret_cast<const u32x4*>(k_lds + r * ROW_BYTES + x * 16);
+                const u32x4 k1 = *reinterpret_cast<const u32x4*>(k_lds + (r + 16) * ROW_BYTES + x * 16);
+                s0 = mfma16(__builtin_bit_cast(bf16x8, k0), qf[kk], s0);
+                s1 = mfma16(__builtin_bit_cast(bf16x8, k1), qf[kk], s1);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { s[ch][e] = s0[e]; s[ch][4 + e] = s1[e]; }
+            const int base = x0 + ch * kChunkKeys;
+            sees[ch] = 0x000f000fu;
+            if ((ok >> (2 * ch) & 3u) != 3u || base + kChunkKeys > n - rq.ql || (base < edge && base + kChunkKeys > p.n_sinks)) {
+                uint32_t lo = 0, hi = 0;
+                if (base < n) {
+                    const int x1 = base + 16, ka = base < view.sinks ? base : base + view.skip, kb = x1 < view.sinks ? x1 : x1 + view.skip;
+                    if (ok >> (2 * ch) & 1u) lo = paged_sees(ka, before, kvl, row_mask, hidden_to, p.n_sinks);
+                    if (ok >> (2 * ch) & 2u) hi = paged_sees(kb, before, kvl, row_mask, hidden_to, p.n_sinks);
+                }
+                sees[ch] = (lo | hi << 16) >> (4 * c) & 0x000f000fu;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[ch][e] = (sees[ch] >> (e < 4 ? e : e + 12)) & 1u ? s[ch][e] : -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) mx = fmaxf(mx, s[ch][e]);
+        }
+        m = quad_max(mx) * sc;
+        const float m_ref = (m == -INFINITY) ? 0.f : m;
+        const uint32_t v_addr = (uint32_t)(uintptr_t)(SPECVLM_AS3 const void*)(v_lds + (4 * c + (r >> 2)) * (COLS * 2) + (r & 3) * 8);
+#pragma unroll
+        for (int ch = 0; ch < CH; ++ch) {
+            floatx8 pv, rest;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { pv[e] = fast_exp2(fmaf(s[ch][e], sc, -m_ref)); l += pv[e]; }
+            const bf16x8 pf = __builtin_convertvector(pv, bf16x8);
+            const u32x4 two = __builtin_bit_cast(u32x4, pf);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                rest[2 * e] = pv[2 * e] - __uint_as_float(two[e] << 16);
+                rest[2 * e + 1] = pv[2 * e + 1] - __uint_as_float(two[e] & 0xffff0000u);
+            }
+            const bf16x8 pf_rest = __builtin_convertvector(rest, bf16x8);
+            *reinterpret_cast<u32x4*>(v_lds + lane * 16) = vraw[ch];
+            __asm__ volatile("" ::: "memory");
+            u32x2 lo = lds_read_tr16<0>(v_addr), hi = lds_read_tr16<16 * COLS * 2>(v_addr);
+            __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __asm__ volatile("" : "+v"(lo), "+v"(hi));
+            bf16x8 vf[1] = {__builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3))};
+            if (__any(sees[ch] != 0x000f000fu)) take_odd_values(vf, sees[ch], o_acc);
+            o_acc[0] = mfma16(vf[0], pf, o_acc[0]);
+            o_acc[0] = mfma16(vf[0], pf_rest, o_acc[0]);
+        }
+        l = quad_sum(l);
+    }
+    // ---- the waves meet: lane (r, c) holds columns 4c .. 4c + 3 of row r; four lanes a piece sum the waves' results, a quarter of them each ----
+    constexpr int LANES = 4, EACH = NW / LANES, PIECES = COLS / 4, SKEW = 256 / LANES;
+    static_assert(16 * COLS * 4 + NW * SKEW <= WAVE_LDS, "a wave's result takes the place of its buffers");
+    reinterpret_cast<floatx4*>(k_lds + wave * SKEW)[r * PIECES + (c ^ (r & 3))] = o_acc[0];
+    if (c == 0) { s_m[r][wave] = m; s_l[r][wave] = l; }
+    __syncthreads();
+    const int w = threadIdx.x % LANES, orow = threadIdx.x / LANES / PIECES, piece = threadIdx.x / LANES % PIECES, grow = rb * 16 + orow;
+    if (grow >= n_rows || threadIdx.x >= kWave * LANES) return;
+    float m_w[EACH], l_w[EACH];
+    floatx4 o_w[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        m_w[i] = s_m[orow][w + LANES * i];
+        l_w[i] = s_l[orow][w + LANES * i];
+        o_w[i] = reinterpret_cast<const floatx4*>(smem + (w + LANES * i) * (WAVE_LDS + SKEW))[orow * PIECES + (piece ^ (orow & 3))];
+    }
+    const auto over_lanes = [](float x, auto op) {
+        x = op(x, row_move<0xB1>(x));
+        return op(x, row_move<0x4E>(x));
+    };
+    const auto sum = [](float a, float b) { return a + b; };
+    float m_all = m_w[0], l_all = 0.f;
+#pragma unroll
+    for (int i = 1; i < EACH; ++i) m_all = fmaxf(m_all, m_w[i]);
+    m_all = over_lanes(m_all, [](float a, float b) { return fmaxf(a, b); });
+    const float ref = (m_all == -INFINITY) ? 0.f : m_all;
+    floatx4 tot = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const float f = fast_exp2(m_w[i] - ref);             // 0 for a wave without keys
+        tot += f * o_w[i];
+        l_all += f * l_w[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) tot[i] = over_lanes(tot[i], sum);
+    l_all = over_lanes(l_all, sum);
+    if (w != 0) return;
+    const QuotRem out_at = divide(grow, p.group, p.inv_group);
+    const int t = out_at.q, h = g * p.group + out_at.r;
+    tot *= l_all == 0.f ? 0.f : 1.f / l_all;                 // (a row that sees nothing: 0)
+    *reinterpret_cast<bf16x4*>(p.out + (int64_t)(rq.q0 + t) * p.q_tok + (int64_t)h * p.q_head + slice * COLS + 4 * piece) =
+        __builtin_convertvector(tot, bf16x4);
+    if (p.lse && slice == 0 && piece == 0) p.lse[(int64_t)(rq.q0 + t) * p.n_q_heads + h] = (m_all + fast_log2(l_all)) * kLn2;
 }
 
 // Joins the pieces of the requests that were cut (one that was not is in its place already).  GP groups of threads share a row's
@@ -622,9 +826,50 @@ static int64_t paged_most_places(int q_len, int kv_len, int window, int n_sinks)
     return seen < kv_len ? seen : kv_len;
 }
 
-template <int D>
-static int launch_paged_d(const PagedParams& p, int mb, bool whole, hipStream_t stream)
+// Chunks of a wave of paged_short_kernel, or 0: not this one.  It takes one round of workgroups (slices of a unit wait for nobody, but two rounds of them read
+// everything twice), and as many keys as its waves hold.  Us a call, the best of the others / this:
+//   size 64, 14/2 heads:   one request, 256 keys 4.5 / 3.7, 512 5.6 / 4.3, 1024 6.9 / 5.6, 1511 7.2 / 6.8 (42 rows 8.7 / 7.2);  8 of 1024 8.3 / 6.6, 1511 9.2 / 9.0;
+//     32 of 500 6.4 / 5.7, 1024 9.1 / 7.8;  but 64 of 100 4.4 / 6.9, 16 of 512 of 42 rows 7.8 / 10.2
+//   size 128, 28/4 heads:  one request, 512 keys 7.4 / 5.4, 700 7.2 / 7.1, 1024 7.5 / 8.8, 42 rows 600 9.1 / 6.8, 1000 9.3 / 9.0;  8 of 500 8.8 / 6.9, 800 11.8 /
+//     9.0;  but 16 of 500 9.4 / 12.4, 250 6.5 / 9.5
+//   size 128, 64/8 heads:  2 of 512 8.6 / 6.5, 800 11.1 / 8.5, 4 of 512 8.8 / 7.0
+// (A single block of query rows of a request alone has the cheapest plan: there the line is lower.)
+static int paged_blocks(const PagedParams& p) { return (p.group * p.q_len + 15) / 16; }
+static int paged_short_chunks(int batch, int n_kv_heads, int n_blocks, int head_dim, int64_t places)
 {
+    if ((int64_t)batch * n_kv_heads * n_blocks * (head_dim / 16) > kNumCu) return 0;
+    if (places > (head_dim == 64 ? 1536 : batch == 1 && n_blocks == 1 ? 704 : 1024)) return 0;
+    return (int)(places + 511) / 512;
+}
+
+template <int D, int CH>
+static int launch_short_paged(PagedParams p, hipStream_t stream)
+{
+    p.n_rgroups = paged_blocks(p); p.inv_rgroups = reciprocal(p.n_rgroups);
+    p.n_units = p.batch * p.n_rgroups * p.n_kv_heads;
+    p.last_units = (p.n_units - 1) % kNumXcd + 1; p.inv_last = reciprocal(p.last_units);
+    constexpr size_t lds = (size_t)16 * (kChunkKeys * (D + 16) * 2 + 2 * 16 * sizeof(float));
+    if (lds > 64 * 1024)
+        if (const int rc = allow_lds<&paged_short_kernel<D, CH>>((int)lds)) return rc;
+    hipLaunchKernelGGL((paged_short_kernel<D, CH>), dim3(p.n_units * (D / 16)), dim3(16 * kWave), lds, stream, p);
+    return launch_status();
+}
+
+template <int D>
+static int launch_paged_d(const PagedParams& p, int mb, bool whole, int short_chunks, hipStream_t stream)
+{
+    if (short_chunks) {
+        if constexpr (D == 64) switch (short_chunks) {
+            case 1: return launch_short_paged<D, 1>(p, stream);
+            case 2: return launch_short_paged<D, 2>(p, stream);
+            case 3: return launch_short_paged<D, 3>(p, stream);
+        }
+        else switch (short_chunks) {
+            case 1: return launch_short_paged<D, 1>(p, stream);
+            case 2: return launch_short_paged<D, 2>(p, stream);
+        }
+        return SPECVLM_EUNSUPPORTED;
+    }
     if (whole) {
         if constexpr (D == 64) switch (mb) {
             case 1: return launch_paged<D, 1, 4, 3, 4, true>(p, stream);
@@ -717,6 +962,8 @@ extern "C" int specvlm_paged_attn(
     const size_t slots = ((size_t)s.max_groups + batch) * n_kv_heads * s.rows_pad;
     p.part_o = (float*)workspace;
     p.part_ml = (float*)((char*)workspace + align256(slots * head_dim * sizeof(float)));
-    const bool whole = paged_takes_whole(batch, n_kv_heads, s.n_rgroups, head_dim, paged_most_places(q_len, kv_len, window, n_sinks));
-    return head_dim == 128 ? launch_paged_d<128>(p, s.mb, whole, (hipStream_t)stream) : launch_paged_d<64>(p, s.mb, whole, (hipStream_t)stream);
+    const int64_t places = paged_most_places(q_len, kv_len, window, n_sinks);
+    const bool whole = paged_takes_whole(batch, n_kv_heads, s.n_rgroups, head_dim, places);
+    const int short_chunks = paged_short_chunks(batch, n_kv_heads, paged_blocks(p), head_dim, places);
+    return head_dim == 128 ? launch_paged_d<128>(p, s.mb, whole, short_chunks, (hipStream_t)stream) : launch_paged_d<64>(p, s.mb, whole, short_chunks, (hipStream_t)stream);
 }

@@ -8,6 +8,7 @@ from gpu_util import dev_bf16, host_f64, rnd_bits
 
 pytestmark = pytest.mark.gpu
 POISON = 0x7fc1                                     # a bf16 NaN: what rows that nobody wrote may hold
+CROWD = 257                                         # more requests than CUs
 
 
 @pytest.fixture(scope="module")
@@ -51,22 +52,26 @@ def i32(x):
 
 
 def check(B, q, k, v, table, kv_lens, q_lens, scale, *, head_major=False, window=0, n_sinks=0, masks=None, ragged=None, max_kv_len=None, **kw):
-    """The call against the plain implementation: as it is, and unless the caller has a bound, with room for long caches, which
-    takes launches that share a request's keys among workgroups."""
+    """The call against the plain implementation: as it is; among many requests with nothing to do, which leaves a workgroup to each; and unless
+    the caller has a bound, with room for long caches, which takes launches that share a request's keys among workgroups."""
     ragged = len(set(q_lens)) > 1 if ragged is None else ragged
-    more = dict(kw)
+    more, crowd = dict(kw), dict(kw)
+    cu_q = np.concatenate([[0], np.cumsum(q_lens)])
+    crowd.update(cu_q=i32(np.concatenate([cu_q, [cu_q[-1]] * CROWD])), max_q_len=kw.get("max_q_len", max(q_lens)))
     if ragged:
-        more.update(cu_q=i32(np.concatenate([[0], np.cumsum(q_lens)])), max_q_len=more.get("max_q_len", max(q_lens)))
+        more.update(cu_q=i32(cu_q), max_q_len=crowd["max_q_len"])
     if masks is not None:
-        more["ancestor_mask"] = torch.from_numpy(np.asarray(masks, dtype=np.uint64).view(np.int64)).cuda()
+        more["ancestor_mask"] = crowd["ancestor_mask"] = torch.from_numpy(np.asarray(masks, dtype=np.uint64).view(np.int64)).cuda()
     qd = dev_bf16(q)
     want, want_lse, tol, tol_lse, written = R.paged_attention(R.values(q), R.values(k), R.values(v), table, kv_lens, q_lens, scale, window, n_sinks,
                                                               masks, max_kv_len)
     wide = np.concatenate([table, np.full((len(table), -(-8192 // k.shape[1])), -1, dtype=np.int32)], axis=1)
-    for entries in ([table] if max_kv_len else [wide, table]):
+    many = np.concatenate([table, np.full((CROWD, table.shape[1]), -1, dtype=np.int32)])
+    runs = [(many, list(kv_lens) + [0] * CROWD, crowd), (wide, kv_lens, more), (table, kv_lens, more)]
+    for entries, lens, how in runs[:1] + runs[2:] if max_kv_len else runs:
         out = torch.full_like(qd, 7.0)
-        got, lse = B.paged_attn(qd, on_gpu(k, head_major), on_gpu(v, head_major), i32(entries), i32(kv_lens), scale, window=window, n_sinks=n_sinks,
-                                out=out, want_lse=True, max_kv_len=max_kv_len, **more)
+        got, lse = B.paged_attn(qd, on_gpu(k, head_major), on_gpu(v, head_major), i32(entries), i32(lens), scale, window=window, n_sinks=n_sinks,
+                                out=out, want_lse=True, max_kv_len=max_kv_len, **how)
         torch.cuda.synchronize()
         assert got is out
         got, lse = host_f64(got), host_f64(lse)
@@ -96,6 +101,24 @@ def test_one_request(B, heads, kv_len, q_len, ps):
 def test_split_and_joined(B, heads, kv_len, q_len):
     q, k, v, table = build(kv_len, [kv_len], [q_len], heads, 16)
     check(B, q, k, v, table, [kv_len], [q_len], heads[2] ** -0.5)
+
+
+@pytest.mark.parametrize("heads,batch,kv_len", [((14, 2, 64), 1, n) for n in (512, 513, 1024, 1025, 1536, 1537)] + [((28, 4, 128), 1, n) for n in (512, 513, 704, 705)]
+                         + [((16, 2, 128), 2, n) for n in (1024, 1025)] + [((8, 8, 64), 8, 40), ((8, 8, 64), 9, 40), ((3, 3, 64), 7, 200)])
+def test_lengths_and_batches_between_the_kernels(B, heads, batch, kv_len):
+    """The last size of one variant and the first of the next."""
+    q, k, v, table = build(kv_len, [kv_len] * batch, [2] * batch, heads, 16)
+    check(B, q, k, v, table, [kv_len] * batch, [2] * batch, heads[2] ** -0.5)
+
+
+@pytest.mark.parametrize("window,n_sinks,q_len", [(1536 - 14 - 3 - 16, 16, 3), (1536 - 14 - 1, 0, 1), (1536 - 14 - 3, 1, 3), (512 - 14 - 2 - 32, 17, 2)])
+def test_windows_that_fill_the_waves(B, window, n_sinks, q_len):
+    """As many places as a window can have, at every offset of its first key in a group of 16."""
+    kv_lens = [2600 + i for i in range(17)]
+    for at in range(0, 17, 4):
+        part = kv_lens[at:at + 4]
+        q, k, v, table = build(window + at, part, [q_len] * len(part), (4, 1, 64), 16)
+        check(B, q, k, v, table, part, [q_len] * len(part), 0.125, window=window, n_sinks=n_sinks)
 
 
 @pytest.mark.parametrize("head_major", [False, True])
@@ -205,8 +228,10 @@ def test_values_that_a_row_does_not_see_do_not_reach_it(B):
     masks = np.array([1, 3, 5, 9, 17, 33] * 2, dtype=np.uint64)         # node i sees the root and itself
     wide = np.concatenate([table, np.full((2, 600), -1, dtype=np.int32)], axis=1)
     mask = torch.from_numpy(masks.view(np.int64)).cuda()
-    for entries in (table, wide):
-        run = lambda kk, vv, **more: host_f64(B.paged_attn(dev_bf16(q), dev_bf16(kk), dev_bf16(vv), i32(entries), i32(kv_lens), 0.088, **more))
+    many = np.concatenate([table, np.full((CROWD, table.shape[1]), -1, dtype=np.int32)])
+    crowd = dict(cu_q=i32([0, 6] + [12] * (CROWD + 1)), max_q_len=6)
+    for entries, lens, how in ((table, kv_lens, {}), (wide, kv_lens, {}), (many, kv_lens + [0] * CROWD, crowd)):
+        run = lambda kk, vv, **more: host_f64(B.paged_attn(dev_bf16(q), dev_bf16(kk), dev_bf16(vv), i32(entries), i32(lens), 0.088, **how, **more))
         clean = run(k, v, ancestor_mask=mask)
         dirty = [x.copy() for x in (k, v)]
         for b, n in enumerate(kv_lens):
@@ -307,16 +332,18 @@ def test_same_as_over_a_contiguous_cache(B):
         assert (np.abs(a - b) <= 2 * tol + 2 * 2.0 ** -8 * np.nanmax(np.abs(R.values(v)))).all()
 
 
-def test_runs_are_alike_and_replays_follow_the_lengths(B):
+@pytest.mark.parametrize("room", [1500, 8000])
+def test_runs_are_alike_and_replays_follow_the_lengths(B, room):
     """A captured call over caches that grow, with eager calls between the replays; the workspace is poisoned."""
     heads, ps, q_len = (14, 2, 64), 16, 3
     kv_lens = [400, 35, 1500]
     q, k, v, table = build(23, kv_lens, [q_len] * 3, heads, ps)
-    qd, kd, vd, td = dev_bf16(q), dev_bf16(k), dev_bf16(v), i32(table)
+    wide = np.concatenate([table, np.full((3, 8000 // ps - table.shape[1]), -1, dtype=np.int32)], axis=1)
+    qd, kd, vd, td = dev_bf16(q), dev_bf16(k), dev_bf16(v), i32(wide)
     lens = i32([3, 3, 3])
     ws = B.new_workspace(B.paged_attn_workspace_bytes(3, q_len, *heads))
     out = torch.empty_like(qd)
-    call = lambda o, w: B.paged_attn(qd, kd, vd, td, lens, 0.125, max_kv_len=1500, out=o, workspace=w)
+    call = lambda o, w: B.paged_attn(qd, kd, vd, td, lens, 0.125, max_kv_len=room, out=o, workspace=w)
     call(out, ws)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
