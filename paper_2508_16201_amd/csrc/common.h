@@ -40,6 +40,20 @@ template <int CTRL> __device__ __forceinline__ float row_move(float x)
     return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
 }
 
+// Sum over the lanes of a wave up to and with this one, all lanes active:  1, 2, 4, 8 lanes back inside each row of 16, then the last
+// lane of a row to the next one, then of the lower half to the upper (by shuffles a step is a round trip through LDS).
+template <int CTRL, int ROWS> __device__ __forceinline__ int add_moved(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int wave_prefix(int x)
+{
+    x = add_moved<0x111, 0xf>(x);
+    x = add_moved<0x112, 0xf>(x);
+    x = add_moved<0x114, 0xf>(x);
+    x = add_moved<0x118, 0xf>(x);
+    x = add_moved<0x142, 0xa>(x);
+    return add_moved<0x143, 0xc>(x);
+}
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_prefix(x), kWave - 1); }
+
 // Workgroups are dealt to the XCDs round-robin by linear id.  Map the hardware
 // id to a logical id so that consecutive logical ids share an XCD (and its L2).
 // `padded` is the launch size, a multiple of kNumXcd; ids >= the real count exit.

@@ -97,28 +97,6 @@ __device__ __forceinline__ PagedRequest paged_request(const PagedParams& p, int 
     return r;
 }
 
-__device__ __forceinline__ int wave_prefix(int x, int lane)            // sum over the lanes up to this one
-{
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-        const int y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
-    return x;
-}
-__device__ __forceinline__ int wave_total(int x)
-{
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) x += __shfl_xor(x, d);
-    return __builtin_amdgcn_readfirstlane(x);
-}
-// Tiles of the whole batch (all lanes of a wave together).
-__device__ __forceinline__ int paged_total(const PagedParams& p, int lane)
-{
-    int n = 0;
-    for (int c = 0; c < p.batch; c += kWave) n += c + lane < p.batch ? paged_tiles(p, c + lane) : 0;
-    return wave_total(n);
-}
 // Tiles that a group takes.
 __device__ __forceinline__ int paged_run(const PagedParams& p, int total) { return max(kMinRun, divide(total + p.max_groups - 1, p.max_groups, p.inv_groups).q); }
 
@@ -139,16 +117,23 @@ template <class F>
 __device__ __forceinline__ void paged_walk(const PagedParams& p, int lane, int j, F&& f)
 {
     // one request: its tiles are the numbering;  more: a prefix sum over the requests, 64 at a time
-    int total, tiles = 0, upto = 0, base = 0;                     // (upto: tiles up to and with the lane's request; base: with all 64)
+    int total, tiles = 0, upto = 0, base;                         // (upto: tiles up to and with the lane's request; base: with all 64)
     PagedRequest rq = {};
     if (p.batch == 1) {
         rq = paged_request(p, 0);
         total = base = (paged_view(p, rq.ql, rq.kvl).n + kTileKeys - 1) / kTileKeys;
     } else {
-        total = paged_total(p, lane);
+        tiles = lane < p.batch ? paged_tiles(p, lane) : 0;
+        upto = wave_prefix(tiles);
+        total = base = __builtin_amdgcn_readlane(upto, kWave - 1);
+        if (p.batch > kWave) {
+            int more = 0;
+            for (int c = kWave; c < p.batch; c += kWave) more += c + lane < p.batch ? paged_tiles(p, c + lane) : 0;
+            total += wave_total(more);
+        }
     }
     const int run = paged_run(p, total);
-    int x = j * run, c64 = -kWave;
+    int x = j * run, c64 = 0;
     const int x_end = min(total, x + run);
     while (x < x_end) {
         int b = 0, first = 0, last = total;
@@ -156,7 +141,7 @@ __device__ __forceinline__ void paged_walk(const PagedParams& p, int lane, int j
             while (x >= base) {
                 c64 += kWave;
                 tiles = c64 + lane < p.batch ? paged_tiles(p, c64 + lane) : 0;
-                upto = base + wave_prefix(tiles, lane);
+                upto = base + wave_prefix(tiles);
                 base = __builtin_amdgcn_readlane(upto, kWave - 1);
             }
             const int at = __builtin_ctzll(__ballot(upto > x));              // the request that holds tile x

@@ -93,12 +93,7 @@ template <int THREADS>
 __device__ __forceinline__ int block_before(int x, int* total, int* s_wave)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int upto = x;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-        const int y = __shfl_up(upto, d);
-        if (lane >= d) upto += y;
-    }
+    const int upto = wave_prefix(x);
     __syncthreads();
     if (lane == kWave - 1) s_wave[wave] = upto;
     __syncthreads();
@@ -176,8 +171,7 @@ void assign_write_kernel(const AssignParams p)
         free += f;
         before += i < (int)blockIdx.x ? f : 0;
     }
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) { free += __shfl_xor(free, d); before += __shfl_xor(before, d); }
+    free = wave_total(free); before = wave_total(before);
     if (hands_out) {
         constexpr int EACH = kPageBlock / kAssignThreads;
         const int needed = p.start[p.batch];
