@@ -80,14 +80,21 @@ __device__ __forceinline__ PagedView paged_view(const PagedParams& p, int ql, in
     if (lo <= sinks) return {0, 0, kvl};
     return {sinks, lo - sinks, kvl - (lo - sinks)};
 }
-__device__ __forceinline__ int paged_tiles(const PagedParams& p, int b)
-{
-    const int ql = p.cu_q ? p.cu_q[b + 1] - p.cu_q[b] : p.q_len;
-    return (paged_view(p, ql, p.kv_lens[b]).n + kTileKeys - 1) / kTileKeys;
-}
-
-// The same for a request that all lanes have in common, and its first query.
+// A request's new tokens and length, and the tiles of its sweep: each lane's own request (one behind the last has no tiles).
 struct PagedRequest { int q0, ql, kvl; };
+__device__ __forceinline__ PagedRequest paged_lane_request(const PagedParams& p, int b)
+{
+    PagedRequest r = {0, 0, 0};
+    if (b < p.batch) {
+        r.kvl = p.kv_lens[b];
+        r.q0 = p.cu_q ? p.cu_q[b] : b * p.q_len;
+        r.ql = p.cu_q ? p.cu_q[b + 1] - r.q0 : p.q_len;
+    }
+    return r;
+}
+__device__ __forceinline__ int paged_tiles(const PagedParams& p, const PagedRequest& r) { return (paged_view(p, r.ql, r.kvl).n + kTileKeys - 1) / kTileKeys; }
+
+// A request that all lanes have in common.
 __device__ __forceinline__ PagedRequest paged_request(const PagedParams& p, int b)
 {
     PagedRequest r;
@@ -118,17 +125,18 @@ __device__ __forceinline__ void paged_walk(const PagedParams& p, int lane, int j
 {
     // one request: its tiles are the numbering;  more: a prefix sum over the requests, 64 at a time
     int total, tiles = 0, upto = 0, base;                         // (upto: tiles up to and with the lane's request; base: with all 64)
-    PagedRequest rq = {};
+    PagedRequest rq = {}, mine = {};                              // (the piece's request; the lane's)
     if (p.batch == 1) {
         rq = paged_request(p, 0);
-        total = base = (paged_view(p, rq.ql, rq.kvl).n + kTileKeys - 1) / kTileKeys;
+        total = base = paged_tiles(p, rq);
     } else {
-        tiles = lane < p.batch ? paged_tiles(p, lane) : 0;
+        mine = paged_lane_request(p, lane);
+        tiles = paged_tiles(p, mine);
         upto = wave_prefix(tiles);
         total = base = __builtin_amdgcn_readlane(upto, kWave - 1);
         if (p.batch > kWave) {
             int more = 0;
-            for (int c = kWave; c < p.batch; c += kWave) more += c + lane < p.batch ? paged_tiles(p, c + lane) : 0;
+            for (int c = kWave; c < p.batch; c += kWave) more += paged_tiles(p, paged_lane_request(p, c + lane));
             total += wave_total(more);
         }
     }
@@ -140,7 +148,8 @@ __device__ __forceinline__ void paged_walk(const PagedParams& p, int lane, int j
         if (p.batch > 1) {
             while (x >= base) {
                 c64 += kWave;
-                tiles = c64 + lane < p.batch ? paged_tiles(p, c64 + lane) : 0;
+                mine = paged_lane_request(p, c64 + lane);
+                tiles = paged_tiles(p, mine);
                 upto = base + wave_prefix(tiles);
                 base = __builtin_amdgcn_readlane(upto, kWave - 1);
             }
@@ -148,7 +157,9 @@ __device__ __forceinline__ void paged_walk(const PagedParams& p, int lane, int j
             last = __builtin_amdgcn_readlane(upto, at);
             first = last - __builtin_amdgcn_readlane(tiles, at);
             b = c64 + at;
-            rq = paged_request(p, b);
+            rq.q0 = __builtin_amdgcn_readlane(mine.q0, at);
+            rq.ql = __builtin_amdgcn_readlane(mine.ql, at);
+            rq.kvl = __builtin_amdgcn_readlane(mine.kvl, at);
         }
         const int to = min(last, x_end);
         f(b, rq, x - first, to - first, x == first && to == last);
@@ -696,13 +707,13 @@ void paged_join_kernel(const PagedParams p)
     const QuotRem at = divide(blockIdx.x, nbh, p.inv_all_heads), head = divide(at.r, p.n_kv_heads, p.inv_heads);
     const int b = head.q, g = head.r, lane = threadIdx.x & 63;
     const PagedRequest rq = paged_request(p, b);
-    const int n_rows = p.group * rq.ql, row0 = at.q * ROWS, tiles = (paged_view(p, rq.ql, rq.kvl).n + kTileKeys - 1) / kTileKeys;
+    const int n_rows = p.group * rq.ql, row0 = at.q * ROWS, tiles = paged_tiles(p, rq);
     if (row0 >= n_rows || tiles == 0) return;
     int first = 0, total = tiles;
     if (p.batch > 1) {
         int before = 0, all = 0;
         for (int c = 0; c < p.batch; c += kWave) {
-            const int t = c + lane < p.batch ? paged_tiles(p, c + lane) : 0;
+            const int t = paged_tiles(p, paged_lane_request(p, c + lane));
             all += t;
             before += c + lane < b ? t : 0;
         }

@@ -88,20 +88,22 @@ void assign_mark_kernel(const AssignParams p)
     atomicMin(p.first + page, i < r.whole ? -1 : b);
 }
 
-// Prefix sum over the workgroup's threads: what is before the thread's x, and the total.
+// Prefix sums over the workgroup's threads: what is before the thread's x and y, and the totals.
+struct Pair { int x, y; };
 template <int THREADS>
-__device__ __forceinline__ int block_before(int x, int* total, int* s_wave)
+__device__ __forceinline__ Pair block_before(Pair v, Pair* total, Pair* s_wave)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int upto = wave_prefix(x);
+    const Pair upto = {wave_prefix(v.x), wave_prefix(v.y)};
     __syncthreads();
     if (lane == kWave - 1) s_wave[wave] = upto;
     __syncthreads();
-    int before = upto - x, all = 0;
+    Pair before = {upto.x - v.x, upto.y - v.y}, all = {0, 0};
 #pragma unroll
     for (int i = 0; i < THREADS / kWave; ++i) {
-        if (i < wave) before += s_wave[i];
-        all += s_wave[i];
+        const Pair w = s_wave[i];
+        if (i < wave) { before.x += w.x; before.y += w.y; }
+        all.x += w.x; all.y += w.y;
     }
     *total = all;
     return before;
@@ -111,29 +113,31 @@ __device__ __forceinline__ int block_before(int x, int* total, int* s_wave)
 __global__ __launch_bounds__(kAssignThreads)
 void assign_plan_kernel(const AssignParams p)
 {
-    __shared__ int s_wave[kAssignThreads / kWave];
+    __shared__ Pair s_wave[kAssignThreads / kWave];
     if ((int)blockIdx.x < p.n_blocks) {
-        int n = 0, all;
+        int n = 0;
+        Pair all;
 #pragma unroll
         for (int i = 0; i < kPageBlock / kAssignThreads; ++i) {
             const int page = blockIdx.x * kPageBlock + i * kAssignThreads + threadIdx.x;
             n += page < p.n_pages && p.ref_counts[page] == 0;
         }
-        block_before<kAssignThreads>(n, &all, s_wave);
-        if (threadIdx.x == 0) p.block_free[blockIdx.x] = all;
+        block_before<kAssignThreads>({n, 0}, &all, s_wave);
+        if (threadIdx.x == 0) p.block_free[blockIdx.x] = all.x;
         return;
     }
     int needed = 0;
     for (int base = 0; base < p.batch; base += kAssignThreads) {
         const int b = base + threadIdx.x;
-        int need = 0, all;
+        int need = 0;
+        Pair all;
         if (b < p.batch) {
             const AssignRow r = assign_row(p, b);
             const int page = r.kept > r.whole ? assign_page(p, r, r.whole) : -1;
             need = r.wanted - (page >= 0 && !assign_leaves(p, page, b) ? r.kept : r.whole);
         }
-        const int before = needed + block_before<kAssignThreads>(need, &all, s_wave);
-        needed += all;
+        const int before = needed + block_before<kAssignThreads>({need, 0}, &all, s_wave).x;
+        needed += all.x;
         if (b < p.batch) p.start[b] = before;
     }
     if (threadIdx.x == 0) p.start[p.batch] = needed;
@@ -162,7 +166,7 @@ __device__ __forceinline__ int assign_owner(const int32_t* start, int batch, int
 __global__ __launch_bounds__(kAssignThreads)
 void assign_write_kernel(const AssignParams p)
 {
-    __shared__ int s_wave[kAssignThreads / kWave];
+    __shared__ Pair s_wave[kAssignThreads / kWave];
     const bool hands_out = (int)blockIdx.x < p.n_blocks;
     // free pages: all of them, and those of the blocks before (each wave for itself: no barrier)
     int before = 0, free = 0;
@@ -178,13 +182,14 @@ void assign_write_kernel(const AssignParams p)
         if (before >= needed) return;
         const int page0 = blockIdx.x * kPageBlock + threadIdx.x * EACH;
         bool is_free[EACH];
-        int n = 0, all;
+        int n = 0;
+        Pair all;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             is_free[i] = page0 + i < p.n_pages && p.ref_counts[page0 + i] == 0;
             n += is_free[i];
         }
-        int rank = before + block_before<kAssignThreads>(n, &all, s_wave);
+        int rank = before + block_before<kAssignThreads>({n, 0}, &all, s_wave).x;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             if (!is_free[i] || rank >= needed) continue;
@@ -221,7 +226,7 @@ void assign_small_kernel(const AssignParams p)
     int* const refs = s_all;                          // [n_pages]
     int* const first = refs + p.n_pages;              // [n_pages]
     int* const start = first + p.n_pages;             // [batch + 1]
-    __shared__ int s_wave[kPlanThreads / kWave];
+    __shared__ Pair s_wave[kPlanThreads / kWave];
     __shared__ AssignRow s_row[kSmallRows];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     constexpr int WAVES = kPlanThreads / kWave;
@@ -241,13 +246,15 @@ void assign_small_kernel(const AssignParams p)
     __syncthreads();
     // the rows' needs; the free pages of this thread's share of the pool
     const int each = (p.n_pages + kPlanThreads - 1) / kPlanThreads, page0 = min(tid * each, p.n_pages), page1 = min(page0 + each, p.n_pages);
-    int n = 0, free, needed, need = 0, page = -1;
+    int n = 0, need = 0, page = -1;
     for (int i = page0; i < page1; ++i) n += refs[i] == 0;
     if (mine.kept > mine.whole) page = assign_page(p, mine, mine.whole);
     const bool leaves = page >= 0 && first[page] != tid;
     need = mine.wanted - (page >= 0 && !leaves ? mine.kept : mine.whole);
-    int rank = block_before<kPlanThreads>(n, &free, s_wave);
-    const int before = block_before<kPlanThreads>(need, &needed, s_wave);
+    Pair all;
+    const Pair sums = block_before<kPlanThreads>({n, need}, &all, s_wave);
+    const int before = sums.y, free = all.x, needed = all.y;
+    int rank = sums.x;
     if (tid < p.batch) start[tid] = before;
     if (tid == 0) start[p.batch] = needed;
     __syncthreads();
