@@ -35,8 +35,9 @@ constexpr int kAssignThreads = 256;
 constexpr int kPlanThreads = 1024;
 constexpr int kPageBlock = 1024;                 // pages of a block, whose free ones are counted together
 // What one workgroup takes: a wave goes over a row, 64 entries at a time, and over every sixteenth row.  Us a call, four launches / one, by
-// rows, pages a row, pages of the pool:  1 x 100 of 1000 9.75 / 5.0;  8 x 129 of 4096 12.5 / 6.4;  16 x 500 of 6100 13.4 / 9.4;  32 x 240 of 6100 13.5 /
-// 10.0;  128 x 40 of 6100 14.4 / 13.4;  but 64 x 250 of 12200 14.1 / 16.9, 120 x 16 of 12200 14.1 / 17.8, 2 x 3900 of 6100 11.5 / 17.6, 250 x 48 15.2 / 23.6.
+// rows, pages a row, pages of the pool:  1 x 100 of 1000 8.1 / 4.0;  8 x 129 of 4096 11.0 / 6.1;  16 x 500 of 6100 11.9 / 8.5;  32 x 240 of 6100 12.0 /
+// 9.1;  128 x 40 of 6100 12.8 / 12.5;  8 x 800 of 8100 11.6 / 11.6;  but 64 x 250 of 12200 12.9 / 16.3, 120 x 16 of 12200 13.1 / 17.1, 64 x 100 of 8100 12.3 /
+// 13.0, 250 x 48 of 15200 13.9 / 25.3.
 constexpr int kSmallPages = 8192, kSmallTrips = 8, kSmallRows = kSmallTrips * kPlanThreads / kWave;
 
 // A row of the new table: pages [0, whole) whole, one more if `part`; pages [0, wanted) in the end.
