@@ -558,3 +558,75 @@ def test_copy_of_empty_lists(B):
 def test_turns_of_an_unknown_scaling(B):
     with pytest.raises(ValueError):
         B.rope_turns(64, 1e4, scaling="cubic")
+
+
+@pytest.mark.parametrize("room", [8, 140])
+def test_a_captured_step(B, room):
+    """A whole step of two layers in one graph: room for the block, a fork's last page, positions and append, attention, rows to the front.  It is
+    replayed over lengths and parents that change, each time beside the same calls made eagerly on a copy.  (room: pages a row, which
+    decide the attention's variant)"""
+    batch, layers, block, ps, n_pages = 3, 2, 4, 16, 64
+    hq, hkv, d = 8, 2, 64
+    torch.manual_seed(3)
+    rnd = lambda *shape: torch.randn(shape, device="cuda").to(torch.bfloat16)
+    q, k, v = rnd(layers, batch * block, hq, d), rnd(layers, batch * block, hkv, d), rnd(layers, batch * block, hkv, d)
+    turns, idx = B.rope_turns(d, 1e4), i32([[0, 1, 3, 0], [0, 2, 0, 0], [0, 1, 2, 3]])
+    counts, parent, keep, new = i32([3, 2, 4]), i32([0, 1, 2]), i32([0, 0, 0]), i32([block] * 3)
+    pools = [rnd(layers, n_pages, ps, hkv, d) for _ in range(2)]
+    table = torch.full((batch, room), -1, dtype=torch.int32, device="cuda")
+
+    def step(pools, old, out):
+        now, start, rows, refs, status = B.pages_assign(old, parent, keep, new, n_pages, ps, out=torch.empty_like(old))
+        B.pages_copy(*pools, old, *pools, now, rows, ps - 1, src_row=parent, src_start=start, dst_start=start)
+        for i in range(layers):
+            turned = B.rope_append(k[i], v[i], pools[0][i], pools[1][i], now, new, q=q[i], turns=turns)
+            B.paged_attn(turned, pools[0][i], pools[1][i], now, new, 0.125, out=out[i])
+        first = new - block
+        B.pages_copy(*pools, now, *pools, now, counts, block, src_start=first, dst_start=first, row_idx=idx)
+        old.copy_(now)
+        return refs, status
+
+    out = torch.zeros_like(q)
+    state = [x.clone() for x in pools], table.clone()
+    step(*state, torch.zeros_like(out))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        refs, status = step(pools, table, out)
+    state = [x.clone() for x in pools], table.clone()
+    lens = [0, 0, 0]
+    for parents, grow in (([-1, -1, -1], 40), ([0, 1, 2], 0), ([0, 0, 1], 7), ([2, 1, 1], 0), ([0, 1, 2], 23), ([1, 1, 1], 1)):
+        kept = [lens[p] if p >= 0 else 0 for p in parents]
+        lens = [n + block + grow for n in kept]
+        for t, x in ((parent, parents), (keep, kept), (new, lens)):
+            t.copy_(i32(x))
+        graph.replay()
+        want = torch.zeros_like(out)
+        want_refs, want_status = step(*state, want)
+        torch.cuda.synchronize()
+        assert status.tolist() == [0, 0, 0] and torch.equal(refs, want_refs) and torch.equal(status, want_status)
+        assert torch.equal(table, state[1])
+        for a, b in zip([out] + pools, [want] + state[0]):
+            assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+def test_two_calls_at_once(B):
+    """Calls on two streams, each with what the binding allocates for it, over one cache that neither writes."""
+    batch, n, ps, (hq, hkv, d) = 4, 3000, 16, (28, 4, 128)
+    table, total = tables(1, [n] * batch, ps)
+    torch.manual_seed(4)
+    k, v = (torch.randn((total, ps, hkv, d), device="cuda").to(torch.bfloat16) for _ in range(2))
+    q = [torch.randn((batch * 3, hq, d), device="cuda").to(torch.bfloat16) for _ in range(2)]
+    t, lens = i32(table), [i32([n, n - 7, 100, 3]), i32([2000, 5, n, n])]
+    want = [B.paged_attn(a, k, v, t, b, 0.088) for a, b in zip(q, lens)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(B.paged_attn(q[i], k, v, t, lens[i], 0.088))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for x in got[i]:
+            assert torch.equal(x.view(torch.int16), want[i].view(torch.int16))
