@@ -50,9 +50,10 @@ struct PagedParams {
     int n_pages, page_size;
     int batch, q_len, kv_len, n_q_heads, n_kv_heads, group;
     int window, n_sinks;
-    uint32_t inv_page, inv_heads, inv_all_heads, inv_group, inv_rgroups, inv_groups;
+    uint32_t inv_page, inv_heads, inv_all_heads, inv_group, inv_rgroups, inv_groups, inv_fold;
     float scale_log2;
     int n_rgroups, rows_pad, max_groups;
+    int fold;                // kFold * batch
     int n_units;             // (paged_short_kernel) requests' kv heads' blocks of 16 rows
     int last_units;          // of them, what is left of the last eight (1 to 8)
     uint32_t inv_last;
@@ -62,7 +63,10 @@ struct PagedParams {
 
 constexpr int kTileKeys = 64;
 constexpr int kRing = 3;                 // tiles of a ring (four: 0.4 us more a call, no faster for long caches)
-constexpr int kMinRun = 2;               // tiles a group takes at least
+// A group takes a tile or more: as many as the launch's workgroups need, and up to four where a request (of the mean length) would else have more than
+// the 32 pieces that eight groups of threads of the join fetch in one round.  Us a call, two tiles at least / this:  14/2 heads of size 64, 2000 keys 7.3 / 6.7, 5000
+// 7.9 / 7.8;  28/4 of 128, 2000 8.0 / 7.6, 6 queries 6000 12.3 / 11.5, 8000 13.5 / 12.1;  three ragged requests of 2000 13.2 / 11.9;  4/1 of 64, 16000 9.9 / 9.0.
+constexpr int kFold = 32, kFoldRun = 4;
 constexpr int kTargetGroups = 256;       // workgroups of a launch
 constexpr int kMostBlocks = 4;           // row blocks of a workgroup: two compute waves on each SIMD
 
@@ -105,7 +109,11 @@ __device__ __forceinline__ PagedRequest paged_request(const PagedParams& p, int 
 }
 
 // Tiles that a group takes.
-__device__ __forceinline__ int paged_run(const PagedParams& p, int total) { return max(kMinRun, divide(total + p.max_groups - 1, p.max_groups, p.inv_groups).q); }
+__device__ __forceinline__ int paged_run(const PagedParams& p, int total)
+{
+    const int fewest = min(kFoldRun, divide(total + p.fold - 1, p.fold, p.inv_fold).q);       // (total: 1 and more, or nobody asks)
+    return max(fewest, divide(total + p.max_groups - 1, p.max_groups, p.inv_groups).q);
+}
 
 // Places [x0, x0 + 16) of the sweep that hold keys k0.. : bit i is set if a query row sees key k0 + i.  before: keys before the block; seen: the
 // row's mask of the block; hidden_to: the last key that the window hides (-1: none).
@@ -936,7 +944,7 @@ extern "C" int specvlm_paged_attn(
     if (((uintptr_t)q | (uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)out) & 15) return SPECVLM_EUNSUPPORTED;
     // (a lane's offset inside 16 keys has 32 bits; tiles and places of the sweep are ints)
     if (tok_stride < 0 || tok_stride >= ((int64_t)1 << 26) || kv_len > (1 << 30)) return SPECVLM_EUNSUPPORTED;
-    if ((int64_t)batch * ((kv_len + kTileKeys - 1) / kTileKeys) >= ((int64_t)1 << 30)) return SPECVLM_EUNSUPPORTED;
+    if ((int64_t)batch * ((kv_len + kTileKeys - 1) / kTileKeys) >= ((int64_t)1 << 30) || batch > (1 << 30) / kFold) return SPECVLM_EUNSUPPORTED;
     if ((int64_t)batch * q_len >= ((int64_t)1 << 31) / n_q_heads) return SPECVLM_EUNSUPPORTED;        // (a launch's workgroups)
     const PagedPlan s = paged_plan(q_len, n_q_heads, n_kv_heads);
     const size_t need = specvlm_paged_attn_workspace_bytes(batch, q_len, n_q_heads, n_kv_heads, head_dim);
@@ -953,6 +961,7 @@ extern "C" int specvlm_paged_attn(
     p.window = window; p.n_sinks = n_sinks;
     p.inv_page = reciprocal(page_size); p.inv_heads = reciprocal(n_kv_heads); p.inv_all_heads = reciprocal(batch * n_kv_heads);
     p.inv_group = reciprocal(p.group); p.inv_rgroups = reciprocal(s.n_rgroups); p.inv_groups = reciprocal(s.max_groups);
+    p.fold = kFold * batch; p.inv_fold = reciprocal(p.fold);
     p.scale_log2 = softmax_scale * kLog2e;
     p.n_rgroups = s.n_rgroups; p.rows_pad = s.rows_pad; p.max_groups = s.max_groups;
     const size_t slots = ((size_t)s.max_groups + batch) * n_kv_heads * s.rows_pad;

@@ -43,6 +43,7 @@ REFUSED = [
     ("specvlm_paged_attn", {"softmax_scale": -1.0}, -1), ("specvlm_paged_attn", {"softmax_scale": float("nan")}, -1),
     ("specvlm_paged_attn", {"kv_len": 801}, -1), ("specvlm_paged_attn", {"kv_len": 1}, -1), ("specvlm_paged_attn", {"n_pages": 0}, -1),
     ("specvlm_paged_attn", {"head_dim": 96}, -2), ("specvlm_paged_attn", {"page_size": 24}, -2), ("specvlm_paged_attn", {"q_len": 65}, -2),
+    ("specvlm_paged_attn", {"batch": (1 << 25) + 1, "q_len": 1, "kv_len": 16, "n_q_heads": 4}, -2),
     ("specvlm_paged_attn", {"page_size": 1 << 24, "kv_len": (1 << 24) * 50}, 0), ("specvlm_paged_attn", {"page_size": 1 << 26, "kv_len": (1 << 30) + 1}, -2),
     *[("specvlm_paged_attn", {k: 12}, -2) for k in ("q_tok_stride", "q_head_stride", "page_stride", "tok_stride", "head_stride")],
     *[("specvlm_paged_attn", {k: AT + 8}, -2) for k in ("q", "k_pages", "v_pages", "out")],
