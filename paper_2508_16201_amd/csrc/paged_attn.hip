@@ -813,15 +813,17 @@ static int launch_paged(const PagedParams& p, hipStream_t stream)
 }
 
 // Whether a workgroup takes a request whole: one launch and no plan, but no more than a CU's share of the memory and two or four waves at
-// work.  `places` is the most that a request's sweep can have.  Us a call, equal runs and join / whole, ragged batches:
-//   size 64, 14/2 heads:   one request, 512 keys 7.2 / 5.6, 1024 7.0 / 7.8 (42 rows, 512 8.3 / 7.5, 1024 8.4 / 10.5);  2 of 1024 8.4 / 7.8;  8 of 1024 9.7 / 8.0,
-//     2048 10.5 / 13.2;  32 of 1024 11.0 / 8.6, 2048 12.3 / 13.9;  64 of 2048 15.3 / 14.4
-//   size 128, 28/4 heads:  one request, 256 keys 7.4 / 5.5, 512 7.5 / 7.6, 1024 7.5 / 12.8;  8 of 512 11.3 / 8.6, 1024 11.6 / 13.8;  32 of 1024 16.7 / 15.1
-//   size 128, 64/8 heads:  8 of 512 11.4 / 8.8, 1024 12.4 / 14.5, 6 queries 16.4 / 16.2;  32 of 1024 20.6 / 17.5, 2048 29.8 / 31.2, 6 queries 40.3 / 33.0
+// work.  `places` is the most that a request's sweep can have.  Us a call, equal runs and join / whole, requests of equal lengths (where slices of the value
+// columns take the call, see below, neither does; equal runs are 2 us less where they end with the requests, as with 512 and 1024 keys):
+//   size 64, 14/2 heads:   one request, 256 keys 6.2 / 4.6, 512 6.5 / 5.6, 1024 6.8 / 7.8 (42 rows, 512 7.4 / 7.5, 1024 7.7 / 10.5);  8 of 1024 7.9 / 8.5;  16 of 42 rows, 700
+//     keys 11.8 / 9.2, 1200 12.7 / 12.2;  32 of 1200 11.6 / 10.3, 1500 10.7 / 11.9;  64 of 2048 16.8 / 16.2
+//   size 128, 28/4 heads:  one request, 256 keys 6.5 / 5.5, 512 6.4 / 7.5;  6 queries, 4 of 450 10.2 / 10.3, 700 11.2 / 12.2, 8 of 700 14.4 / 12.3, 900 14.7 / 15.5, 16 of
+//     700 17.0 / 12.7, 24 of 1200 22.1 / 19.6;  16 of 700 12.3 / 11.5, 900 13.2 / 14.3;  32 of 1024 17.8 / 16.9
+//   size 128, 64/8 heads:  8 of 700 11.9 / 11.6, 900 12.8 / 14.3;  32 of 1024 25.8 / 23.2, 2048 47.4 / 44.7, 6 queries 52.5 / 47.1 (ragged 29.8 / 31.2)
 static bool paged_takes_whole(int batch, int n_kv_heads, int n_rgroups, int head_dim, int64_t places)
 {
     const int64_t wgs = (int64_t)batch * n_kv_heads * n_rgroups;
-    const int eighths = batch == 1 ? 8 : wgs < 64 ? 11 : wgs < 128 ? 14 : wgs < 256 ? 20 : 32;
+    const int eighths = batch == 1 ? 8 : wgs < 32 ? 9 : wgs < 96 ? 14 : wgs < 256 ? 20 : 32;
     return places * 8 <= (head_dim == 64 ? 768 : 448) * eighths;
 }
 static int64_t paged_most_places(int q_len, int kv_len, int window, int n_sinks)
@@ -832,17 +834,16 @@ static int64_t paged_most_places(int q_len, int kv_len, int window, int n_sinks)
 
 // Chunks of a wave of paged_short_kernel, or 0: not this one.  It takes one round of workgroups (slices of a unit wait for nobody, but two rounds of them read
 // everything twice), and as many keys as its waves hold.  Us a call, the best of the others / this:
-//   size 64, 14/2 heads:   one request, 256 keys 4.5 / 3.7, 512 5.6 / 4.3, 1024 6.9 / 5.6, 1511 7.2 / 6.8 (42 rows 8.7 / 7.2);  8 of 1024 8.3 / 6.6, 1511 9.2 / 9.0;
-//     32 of 500 6.4 / 5.7, 1024 9.1 / 7.8;  but 64 of 100 4.4 / 6.9, 16 of 512 of 42 rows 7.8 / 10.2
-//   size 128, 28/4 heads:  one request, 512 keys 7.4 / 5.4, 700 7.2 / 7.1, 1024 7.5 / 8.8, 42 rows 600 9.1 / 6.8, 1000 9.3 / 9.0;  8 of 500 8.8 / 6.9, 800 11.8 /
-//     9.0;  but 16 of 500 9.4 / 12.4, 250 6.5 / 9.5
-//   size 128, 64/8 heads:  2 of 512 8.6 / 6.5, 800 11.1 / 8.5, 4 of 512 8.8 / 7.0
-// (A single block of query rows of a request alone has the cheapest plan: there the line is lower.)
+//   size 64, 14/2 heads:   one request, 256 keys 4.6 / 3.8, 512 5.6 / 4.4, 1024 6.8 / 5.7, 1511 6.8 / 6.8 in one launch for two (42 rows 7.7 / 7.2);  8 of 1024 7.9 / 6.6, 1511
+//     8.6 / 8.7;  32 of 500 6.4 / 5.7, 1024 9.1 / 7.8;  but 64 of 100 4.4 / 6.9, 16 of 512 of 42 rows 7.8 / 10.2
+//   size 128, 28/4 heads:  one request, 512 keys 6.5 / 5.4, 700 6.9 / 7.1, 42 rows 600 8.3 / 6.8, 800 8.4 / 8.2, 1000 8.6 / 8.9;  8 of 500 8.4 / 6.9, 1000 9.6 / 9.6;  but
+//     16 of 500 9.4 / 12.4, 250 6.5 / 9.5
+//   size 128, 64/8 heads:  one request, 700 keys 6.9 / 6.5, 8 queries 9.4 / 7.6;  2 of 512 8.6 / 6.5, 1000 8.0 / 9.0, 4 of 800 10.3 / 9.0
 static int paged_blocks(const PagedParams& p) { return (p.group * p.q_len + 15) / 16; }
 static int paged_short_chunks(int batch, int n_kv_heads, int n_blocks, int head_dim, int64_t places)
 {
     if ((int64_t)batch * n_kv_heads * n_blocks * (head_dim / 16) > kNumCu) return 0;
-    if (places > (head_dim == 64 ? 1536 : batch == 1 && n_blocks == 1 ? 704 : 1024)) return 0;
+    if (places > (head_dim == 64 ? 1536 : 832)) return 0;
     return (int)(places + 511) / 512;
 }
 

@@ -103,8 +103,8 @@ def test_split_and_joined(B, heads, kv_len, q_len):
     check(B, q, k, v, table, [kv_len], [q_len], heads[2] ** -0.5)
 
 
-@pytest.mark.parametrize("heads,batch,kv_len", [((14, 2, 64), 1, n) for n in (512, 513, 1024, 1025, 1536, 1537)] + [((28, 4, 128), 1, n) for n in (512, 513, 704, 705)]
-                         + [((16, 2, 128), 2, n) for n in (1024, 1025)] + [((8, 8, 64), 8, 40), ((8, 8, 64), 9, 40), ((3, 3, 64), 7, 200)])
+@pytest.mark.parametrize("heads,batch,kv_len", [((14, 2, 64), 1, n) for n in (512, 513, 1024, 1025, 1536, 1537)] + [((28, 4, 128), 1, n) for n in (512, 513, 832, 833)]
+                         + [((16, 2, 128), 2, n) for n in (832, 833)] + [((8, 8, 64), 8, 40), ((8, 8, 64), 9, 40), ((3, 3, 64), 7, 200)])
 def test_lengths_and_batches_between_the_kernels(B, heads, batch, kv_len):
     """The last size of one variant and the first of the next."""
     q, k, v, table = build(kv_len, [kv_len] * batch, [2] * batch, heads, 16)
