@@ -18,8 +18,8 @@
 //
 // Work decomposition.  The lengths are on the device.  Tiles of 64 keys of all requests are numbered request after
 // request; group j (a workgroup for each kv head and row group) takes a run of equal length, which every workgroup
-// finds by a prefix sum over the lengths, 64 requests at a time in the lanes of a wave.  A captured launch so stays
-// balanced as the caches grow.  A request that one group covers is written out directly; the others leave partial
+// finds by a prefix sum over the lengths, 64 requests at a time in the lanes of a wave (paged_cut: where the runs begin).  A captured
+// launch so stays balanced as the caches grow.  A request that one group covers is written out directly; the others leave partial
 // results that the second launch joins.  Short caches take one launch: a workgroup has a request's keys of a head whole (paged_takes_whole has the
 // line), and where those would be few workgroups a slice of its value columns (paged_short_kernel, paged_short_chunks).
 //
@@ -59,6 +59,7 @@ struct PagedParams {
     uint32_t inv_last;
     float* part_o;           // [(groups + batch) * H_kv][rows_pad][D] unnormalised partial outputs
     float* part_ml;          // [(groups + batch) * H_kv][rows_pad][2] running maximum in log2 units, sum
+    int32_t* part_of;        // [batch][2] (of a batch) the first group that has a piece of the request, and how many have
 };
 
 constexpr int kTileKeys = 64;
@@ -115,6 +116,28 @@ __device__ __forceinline__ int paged_run(const PagedParams& p, int total)
     return max(fewest, divide(total + p.max_groups - 1, p.max_groups, p.inv_groups).q);
 }
 
+// How a batch is cut: runs of `run` tiles over all requests one behind the other, or (from_first: up to 64 requests, one to a lane) from each request's first tile on,
+// where there are so many groups, with one tile more if need be.  A group with the end of one request and the start of another drains its ring and exchanges
+// twice, 2 us;  a tile more is 0.5 to 1.3.  Us a call, one behind the other / this:  28/4 heads, 16 requests of 900 keys 13.1 / 11.7, 6 queries 18.5 / 15.5;  64/8 heads, 6
+// queries, 8 ragged requests of 3000 20.0 / 17.8;  14/2 heads, 24 of 2000 10.6 / 9.2;  the worst 16 of 1500, 6 queries 10.8 / 11.0.  (Runs beyond 16 tiles: not worth the look.)
+constexpr int kCutRun = 16;
+struct PagedCut { int run; bool from_first; int pieces; };       // (pieces: the lane's request's)
+__device__ __forceinline__ PagedCut paged_cut(const PagedParams& p, int tiles, int total)
+{
+    const int run = paged_run(p, total);
+    if (run > 1 && run <= kCutRun) {
+#pragma unroll
+        for (int more = 0; more < 2; ++more) {
+            const int r = run + more, x = tiles + r - 1;          // (x < 2^24 + 16: the product is off by less than one)
+            int pieces = (int)((float)x * __builtin_amdgcn_rcpf((float)r));
+            pieces += x >= (pieces + 1) * r;
+            pieces -= x < pieces * r;
+            if (wave_total(pieces) <= p.max_groups) return {r, true, pieces};
+        }
+    }
+    return {run, false, 0};
+}
+
 // Places [x0, x0 + 16) of the sweep that hold keys k0.. : bit i is set if a query row sees key k0 + i.  before: keys before the block; seen: the
 // row's mask of the block; hidden_to: the last key that the window hides (-1: none).
 __device__ __forceinline__ uint32_t low_bits(int n) { return (1u << min(max(n, 0), 16)) - 1u; }
@@ -127,9 +150,9 @@ __device__ __forceinline__ uint32_t paged_sees(int k0, int before, int kvl, uint
 }
 
 // The runs of group j, request by request: f(request's number, request, first tile, end, whether that is all of it).  All waves of the
-// workgroup pass here, and a barrier between two of them.
+// workgroup pass here, and a barrier between two of them.  tells: this wave leaves the join where a request's pieces are.
 template <class F>
-__device__ __forceinline__ void paged_walk(const PagedParams& p, int lane, int j, F&& f)
+__device__ __forceinline__ void paged_walk(const PagedParams& p, int lane, int j, bool tells, F&& f)
 {
     // one request: its tiles are the numbering;  more: a prefix sum over the requests, 64 at a time
     int total, tiles = 0, upto = 0, base;                         // (upto: tiles up to and with the lane's request; base: with all 64)
@@ -148,9 +171,23 @@ __device__ __forceinline__ void paged_walk(const PagedParams& p, int lane, int j
             total += wave_total(more);
         }
     }
-    const int run = paged_run(p, total);
-    int x = j * run, c64 = 0;
-    const int x_end = min(total, x + run);
+    int x, x_end, c64 = 0, run = 0;
+    PagedCut cut = {0, false, 0};
+    if (p.batch > 1 && p.batch <= kWave) cut = paged_cut(p, tiles, total);
+    if (cut.from_first) {                                        // group j has piece j of all
+        const int ends = wave_prefix(cut.pieces);
+        x = x_end = 0;
+        if (j < __builtin_amdgcn_readlane(ends, kWave - 1)) {
+            const int at = __builtin_ctzll(__ballot(ends > j));
+            const int last_of = __builtin_amdgcn_readlane(upto, at);
+            x = last_of - __builtin_amdgcn_readlane(tiles, at) + (j - __builtin_amdgcn_readlane(ends, at) + __builtin_amdgcn_readlane(cut.pieces, at)) * cut.run;
+            x_end = min(last_of, x + cut.run);
+        }
+    } else {
+        run = paged_run(p, total);
+        x = j * run;
+        x_end = min(total, x + run);
+    }
     while (x < x_end) {
         int b = 0, first = 0, last = total;
         if (p.batch > 1) {
@@ -168,6 +205,10 @@ __device__ __forceinline__ void paged_walk(const PagedParams& p, int lane, int j
             rq.q0 = __builtin_amdgcn_readlane(mine.q0, at);
             rq.ql = __builtin_amdgcn_readlane(mine.ql, at);
             rq.kvl = __builtin_amdgcn_readlane(mine.kvl, at);
+            if (tells && x == first) {
+                const int live = cut.from_first ? __builtin_amdgcn_readlane(cut.pieces, at) : (last - 1) / run - j + 1;
+                if (lane < 2) p.part_of[2 * b + lane] = lane ? live : j;
+            }
         }
         const int to = min(last, x_end);
         f(b, rq, x - first, to - first, x == first && to == last);
@@ -266,7 +307,7 @@ void paged_split_kernel(const PagedParams p)
             const int n = paged_view(p, rq.ql, rq.kvl).n;
             if (n > 0) f(j, rq, 0, (n + TK - 1) / TK, true);
         } else {
-            paged_walk(p, lane, j, f);
+            paged_walk(p, lane, j, g == 0 && row0 == 0 && wave == NW - 1, f);
         }
     };
 
@@ -713,22 +754,16 @@ void paged_join_kernel(const PagedParams p)
     __shared__ __align__(16) float s_o[ROWS][GP][D + 4];
     const int nbh = p.batch * p.n_kv_heads;
     const QuotRem at = divide(blockIdx.x, nbh, p.inv_all_heads), head = divide(at.r, p.n_kv_heads, p.inv_heads);
-    const int b = head.q, g = head.r, lane = threadIdx.x & 63;
+    const int b = head.q, g = head.r;
     const PagedRequest rq = paged_request(p, b);
     const int n_rows = p.group * rq.ql, row0 = at.q * ROWS, tiles = paged_tiles(p, rq);
     if (row0 >= n_rows || tiles == 0) return;
-    int first = 0, total = tiles;
+    int j0, live;                                    // the first group that has a piece, and how many have
     if (p.batch > 1) {
-        int before = 0, all = 0;
-        for (int c = 0; c < p.batch; c += kWave) {
-            const int t = paged_tiles(p, paged_lane_request(p, c + lane));
-            all += t;
-            before += c + lane < b ? t : 0;
-        }
-        total = wave_total(all); first = wave_total(before);
+        j0 = uniform_load(p.part_of, 2 * b); live = uniform_load(p.part_of, 2 * b + 1);
+    } else {
+        j0 = 0; live = (tiles - 1) / paged_run(p, tiles) + 1;
     }
-    const int run = paged_run(p, total);
-    const int j0 = first / run, live = (first + tiles - 1) / run - j0 + 1;
     if (live == 1) return;
     const int sub = threadIdx.x / TPR, grp = sub % GP, lr = sub / GP, col = (threadIdx.x % TPR) * 4, row = row0 + lr;
     const int64_t slot0 = (int64_t)((j0 + b) * p.n_kv_heads + g) * p.rows_pad + min(row, n_rows - 1);
@@ -813,17 +848,17 @@ static int launch_paged(const PagedParams& p, hipStream_t stream)
 }
 
 // Whether a workgroup takes a request whole: one launch and no plan, but no more than a CU's share of the memory and two or four waves at
-// work.  `places` is the most that a request's sweep can have.  Us a call, equal runs and join / whole, requests of equal lengths (where slices of the value
-// columns take the call, see below, neither does; equal runs are 2 us less where they end with the requests, as with 512 and 1024 keys):
-//   size 64, 14/2 heads:   one request, 256 keys 6.2 / 4.6, 512 6.5 / 5.6, 1024 6.8 / 7.8 (42 rows, 512 7.4 / 7.5, 1024 7.7 / 10.5);  8 of 1024 7.9 / 8.5;  16 of 42 rows, 700
-//     keys 11.8 / 9.2, 1200 12.7 / 12.2;  32 of 1200 11.6 / 10.3, 1500 10.7 / 11.9;  64 of 2048 16.8 / 16.2
-//   size 128, 28/4 heads:  one request, 256 keys 6.5 / 5.5, 512 6.4 / 7.5;  6 queries, 4 of 450 10.2 / 10.3, 700 11.2 / 12.2, 8 of 700 14.4 / 12.3, 900 14.7 / 15.5, 16 of
-//     700 17.0 / 12.7, 24 of 1200 22.1 / 19.6;  16 of 700 12.3 / 11.5, 900 13.2 / 14.3;  32 of 1024 17.8 / 16.9
-//   size 128, 64/8 heads:  8 of 700 11.9 / 11.6, 900 12.8 / 14.3;  32 of 1024 25.8 / 23.2, 2048 47.4 / 44.7, 6 queries 52.5 / 47.1 (ragged 29.8 / 31.2)
-static bool paged_takes_whole(int batch, int n_kv_heads, int n_rgroups, int head_dim, int64_t places)
+// work.  `places` is the most that a request's sweep can have.  Us a call, shared keys and join / whole, requests of equal lengths (where slices of the value
+// columns take the call, see below, neither does):
+//   size 64, 14/2 heads:   one request, 256 keys 6.2 / 4.6, 512 6.5 / 5.6, 1024 6.8 / 7.8 (42 rows, 512 7.4 / 7.5, 1024 7.7 / 10.5);  8 of 1024 8.0 / 8.2;  16 of 42 rows, 700
+//     keys 9.9 / 9.2, 900 10.4 / 10.9;  32 of 1000 9.6 / 9.1, 1200 9.9 / 10.3;  64 of 1500 14.3 / 12.9, 2048 16.7 / 16.2
+//   size 128, 28/4 heads:  one request, 256 keys 6.5 / 5.5, 512 6.4 / 7.5;  6 queries, 4 of 450 10.2 / 10.3, 580 10.7 / 11.7, 8 of 450 12.3 / 10.5, 700 12.2 / 12.4, 16 of 700 14.6 /
+//     12.7, 900 15.7 / 16.0, 24 of 1200 21.9 / 19.6;  16 of 580 10.3 / 10.6;  32 of 1024 17.3 / 17.0
+//   size 128, 64/8 heads:  8 of 450 9.5 / 9.4, 580 9.6 / 10.6, 6 queries 700 14.0 / 13.0;  32 of 1800 42.0 / 40.0, 6 queries 46.0 / 42.7 (2048 ragged 29.6 / 31.2)
+static bool paged_takes_whole(int batch, int n_kv_heads, int n_rgroups, int mb, int head_dim, int64_t places)
 {
     const int64_t wgs = (int64_t)batch * n_kv_heads * n_rgroups;
-    const int eighths = batch == 1 ? 8 : wgs < 32 ? 9 : wgs < 96 ? 14 : wgs < 256 ? 20 : 32;
+    const int eighths = batch == 1 ? 8 : wgs < 64 || (wgs < 96 && mb == 1) ? 9 : wgs < 96 ? 14 : wgs < 256 ? 20 : 32;
     return places * 8 <= (head_dim == 64 ? 768 : 448) * eighths;
 }
 static int64_t paged_most_places(int q_len, int kv_len, int window, int n_sinks)
@@ -834,9 +869,9 @@ static int64_t paged_most_places(int q_len, int kv_len, int window, int n_sinks)
 
 // Chunks of a wave of paged_short_kernel, or 0: not this one.  It takes one round of workgroups (slices of a unit wait for nobody, but two rounds of them read
 // everything twice), and as many keys as its waves hold.  Us a call, the best of the others / this:
-//   size 64, 14/2 heads:   one request, 256 keys 4.6 / 3.8, 512 5.6 / 4.4, 1024 6.8 / 5.7, 1511 6.8 / 6.8 in one launch for two (42 rows 7.7 / 7.2);  8 of 1024 7.9 / 6.6, 1511
-//     8.6 / 8.7;  32 of 500 6.4 / 5.7, 1024 9.1 / 7.8;  but 64 of 100 4.4 / 6.9, 16 of 512 of 42 rows 7.8 / 10.2
-//   size 128, 28/4 heads:  one request, 512 keys 6.5 / 5.4, 700 6.9 / 7.1, 42 rows 600 8.3 / 6.8, 800 8.4 / 8.2, 1000 8.6 / 8.9;  8 of 500 8.4 / 6.9, 1000 9.6 / 9.6;  but
+//   size 64, 14/2 heads:   one request, 256 keys 4.6 / 3.8, 512 5.6 / 4.4, 1024 6.8 / 5.7, 1511 6.8 / 6.8 in one launch for two (42 rows 7.7 / 7.2);  8 of 1024 7.9 / 6.6, 1300
+//     8.3 / 8.6;  32 of 500 6.4 / 5.7, 1000 9.1 / 7.5, 1500 10.8 / 9.7;  but 64 of 100 4.4 / 6.9, 16 of 512 of 42 rows 7.8 / 10.2
+//   size 128, 28/4 heads:  one request, 512 keys 6.5 / 5.4, 700 6.9 / 7.1, 42 rows 600 8.3 / 6.8, 800 8.4 / 8.2, 1000 8.6 / 8.9;  8 of 500 8.4 / 6.9, 700 9.0 / 8.1;  but
 //     16 of 500 9.4 / 12.4, 250 6.5 / 9.5
 //   size 128, 64/8 heads:  one request, 700 keys 6.9 / 6.5, 8 queries 9.4 / 7.6;  2 of 512 8.6 / 6.5, 1000 8.0 / 9.0, 4 of 800 10.3 / 9.0
 static int paged_blocks(const PagedParams& p) { return (p.group * p.q_len + 15) / 16; }
@@ -922,7 +957,7 @@ extern "C" size_t specvlm_paged_attn_workspace_bytes(int batch, int q_len, int n
         return 0;
     const PagedPlan s = paged_plan(q_len, n_q_heads, n_kv_heads);
     const size_t slots = ((size_t)s.max_groups + batch) * n_kv_heads * s.rows_pad;
-    return align256(slots * head_dim * sizeof(float)) + align256(slots * 2 * sizeof(float));
+    return align256(slots * head_dim * sizeof(float)) + align256(slots * 2 * sizeof(float)) + align256((size_t)batch * 2 * sizeof(int32_t));
 }
 
 extern "C" int specvlm_paged_attn(
@@ -968,8 +1003,9 @@ extern "C" int specvlm_paged_attn(
     const size_t slots = ((size_t)s.max_groups + batch) * n_kv_heads * s.rows_pad;
     p.part_o = (float*)workspace;
     p.part_ml = (float*)((char*)workspace + align256(slots * head_dim * sizeof(float)));
+    p.part_of = (int32_t*)((char*)p.part_ml + align256(slots * 2 * sizeof(float)));
     const int64_t places = paged_most_places(q_len, kv_len, window, n_sinks);
-    const bool whole = paged_takes_whole(batch, n_kv_heads, s.n_rgroups, head_dim, places);
+    const bool whole = paged_takes_whole(batch, n_kv_heads, s.n_rgroups, s.mb, head_dim, places);
     const int short_chunks = paged_short_chunks(batch, n_kv_heads, paged_blocks(p), head_dim, places);
     return head_dim == 128 ? launch_paged_d<128>(p, s.mb, whole, short_chunks, (hipStream_t)stream) : launch_paged_d<64>(p, s.mb, whole, short_chunks, (hipStream_t)stream);
 }

@@ -143,6 +143,15 @@ def test_many_heads_and_requests_share_few_groups(B):
     check(B, q, k, v, table, kv_lens, [1] * 5, 0.125)
 
 
+@pytest.mark.parametrize("tiles", [[4, 4, 4], [7, 5], [5, 5], [9, 9, 1], [6, 6, 6, 6, 6, 6], [1, 30, 1], [12, 0, 12], [2, 2, 2, 2, 2, 2, 2], [40, 41], [100, 96]])
+@pytest.mark.parametrize("heads", [(40, 40, 64), (32, 32, 128)])
+def test_requests_in_few_groups(B, heads, tiles):
+    """Six or eight groups: runs from each request's first tile on, with a tile more, one request behind the other, several requests to a group."""
+    kv_lens = [max(64 * n - 3 - i, 0) for i, n in enumerate(tiles)]
+    q, k, v, table = build(sum(tiles), [max(n, 1) for n in kv_lens], [2] * len(tiles), heads, 16)
+    check(B, q, k, v, table, kv_lens, [2] * len(tiles), heads[2] ** -0.5)
+
+
 @pytest.mark.parametrize("q_len,heads", [(64, (4, 1, 64)), (33, (16, 2, 128)), (17, (4, 4, 128)), (12, (28, 4, 128)), (40, (3, 1, 128))])
 def test_row_blocks_and_groups(B, q_len, heads):
     kv_lens = [300, 64 + q_len, q_len]
