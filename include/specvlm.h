@@ -394,7 +394,7 @@ int specvlm_tree_attn(
  * query's window are never looked at and may be freed.
  * Results do not depend on the run; they may differ by roundings when the other
  * requests of the batch change, since the lengths of all decide how each is cut.
- * Limits: q_len <= 64, kv_len <= 2^30.
+ * Limits: q_len <= 64, kv_len <= 2^30, batch <= 2^25.
  * -------------------------------------------------------------------------- */
 size_t specvlm_paged_attn_workspace_bytes(int batch, int q_len, int n_q_heads, int n_kv_heads, int head_dim);
 
