@@ -384,7 +384,10 @@ int specvlm_tree_attn(
  *   q    bf16 [sum q_len_b, H_q, d]      out  bf16, same shape and strides as q
  *   lse  optional fp32 [sum q_len_b, H_q]: natural log of each row's softmax sum
  * A row that sees no key gets 0, and -infinity in lse.  What a hidden key or value
- * holds (a page's rows behind the last token, NaN, infinities) changes nothing.
+ * holds (a page's rows behind the last token, NaN, infinities) changes nothing; an
+ * infinite value that a row sees makes that column of it infinite, however small its
+ * weight, a NaN or infinities of both signs make it NaN (a sweep with such values takes
+ * a few times as long).
  *   q_len   the maximum over the requests with cu_q, else every request's number
  *   kv_len  the maximum that kv_lens may hold, at most max_pages * page_size
  * A request with q_len_b or kv_lens[b] beyond these, with none of either, or with

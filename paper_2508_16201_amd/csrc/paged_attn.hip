@@ -227,9 +227,9 @@ __device__ __forceinline__ void wait_tiles(int younger)
     wait_vmcnt<MOST * LPW>();
 }
 
-// A value that is no number (an infinity, rows never written) belongs only to the rows that see its key, and 0 times it is no zero (by which the
-// products with 0 find it): it is left out of the product, and the rows get it by how many such values they see.  sees: bits 0..3 and 16..19,
-// the lane's keys that its row sees.
+// A value that is no finite number (an infinity, rows never written) belongs only to the rows that see its key, and a product with 0 (by which it is
+// found) or with both parts of a probability, of which the second may be negative, is no number: it is left out of the products, and the rows get it by
+// how many such values they see.  sees: bits 0..3 and 16..19, the lane's keys that its row sees.
 template <int DJ>
 __device__ __forceinline__ void take_odd_values(bf16x8 (&vf)[DJ], uint32_t sees, floatx4 (&o_acc)[DJ])
 {
@@ -267,6 +267,31 @@ __device__ __forceinline__ void take_odd_values(bf16x8 (&vf)[DJ], uint32_t sees,
             __builtin_amdgcn_sched_barrier(0);        // (one after the other: the registers of all at once would be the kernel's most)
         }
     }
+}
+
+// What is done twice where a sum comes out as no finite number: as fast as it goes, and then with an eye on such values.
+typedef std::integral_constant<bool, false> Plain;
+typedef std::integral_constant<bool, true> Careful;
+// Whether one of these is no finite number (0 times it is no zero).
+__device__ __forceinline__ bool any_odd(floatx4 x)
+{
+    x *= 0.f;
+    return __any(!(x[0] + x[1] + x[2] + x[3] == 0.f));
+}
+template <int N> __device__ __forceinline__ bool any_odd(const floatx4 (&x)[N])
+{
+    floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum += 0.f * x[i];
+    return any_odd(sum);
+}
+// x by the weight w of a maximum that another has passed.  Careful: an infinity stays one however small its weight is, also where 32 bits take that for 0.
+template <class HOW> __device__ __forceinline__ floatx4 weighted(float w, floatx4 x, HOW)
+{
+    if constexpr (!HOW::value) return w * x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = fabsf(x[e]) == INFINITY ? x[e] : w * x[e];
+    return x;
 }
 
 // MB: row blocks of 16, one to a compute wave.  KS: chunks of 32 keys of a tile, a wave for each.  NS: tiles of the ring.  NLD: loader waves.
@@ -407,36 +432,13 @@ void paged_split_kernel(const PagedParams p)
         const uint32_t k_base = lds0 + (ks * kChunkKeys + r) * ROW_BYTES + (c ^ ((D == 128) ? (r & 15) : ((r >> 1) & 7))) * 16;
         const uint32_t v_base = lds0 + TILE_BYTES + v_row * ROW_BYTES + (r & 3) * 8 + (v_swizzle<D>(v_row) >> 1) * 32;
         bool fresh = true;                                        // some row has seen nothing yet
-        uint32_t at_stage = 0;
-        int base = t_begin * TK + ks * kChunkKeys;
-        for (int i = 0; i < n_tiles; ++i, base += TK, at_stage = at_stage == (NS - 1) * 2 * TILE_BYTES ? 0 : at_stage + 2 * TILE_BYTES) {
-            stage_barrier();
-            if (base >= n) continue;
-            const uint32_t ok = (uint32_t)__builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint16_t*>(s_ok + at_stage / (TILE_BYTES / 4) + 2 * ks));
-            // ---- S^T = K Q^T for 32 keys ----
-            floatx4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int kk = 0; kk < KK; ++kk) {
-                const SPECVLM_AS3 u32x4* const at = (const SPECVLM_AS3 u32x4*)(k_base + at_stage ^ kk * 64);
-                const u32x4 k0 = at[0], k1 = at[16 * ROW_BYTES / 16];
-                s0 = mfma16(__builtin_bit_cast(bf16x8, k0), qf[kk], s0);
-                s1 = mfma16(__builtin_bit_cast(bf16x8, k1), qf[kk], s1);
-            }
-            // ---- V^T fragments of the lane's keys (4c+e and 16+4c+e) by the transposing LDS read ----
-            bf16x8 vf[DJ];
-#pragma unroll
-            for (int jj = 0; jj < DJ; ++jj) {
-                typedef short s16x4 __attribute__((ext_vector_type(4)));
-                SPECVLM_AS3 s16x4* const at = (SPECVLM_AS3 s16x4*)(v_base + at_stage ^ jj * 32);
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at);
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at + 16 * ROW_BYTES / 8);
-                vf[jj] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-            }
+        // 32 places from `base` on:  their logits, values and pages (careful: with the same roundings, and every value looked at)
+        const auto take = [&](const int base, const uint32_t ok, floatx4 s0, floatx4 s1, bf16x8 (&vf)[DJ], auto careful) {
             const bool need_mask = ok != 0x0101u || base + kChunkKeys > n - rq.ql || (base < edge && base + kChunkKeys > p.n_sinks);
             float s[8];
 #pragma unroll
             for (int e = 0; e < 4; ++e) { s[e] = s0[e]; s[4 + e] = s1[e]; }
-            uint32_t sees = 0;                                    // (with need_mask) bits 0..3 and 16..19: the lane's keys that its row sees
+            uint32_t sees = 0x000f000fu;                          // bits 0..3 and 16..19: the lane's keys that its row sees
             if (need_mask) {
                 // block key b is visible where bit b is set: 0..t in a chain, the caller's ancestors in a tree
                 const uint64_t seen = p.block_mask ? p.block_mask[rq.q0 + t_blk] : ((2ull << t_blk) - 1ull);
@@ -475,13 +477,11 @@ void paged_split_kernel(const PagedParams p)
                 l_run = l_run * alpha + psum;
                 if (__any(rescale)) {
 #pragma unroll
-                    for (int jj = 0; jj < DJ; ++jj) o_acc[jj] *= alpha;
+                    for (int jj = 0; jj < DJ; ++jj) o_acc[jj] = weighted(alpha, o_acc[jj], careful);
                 }
             }
             if (need_mask || fresh) fresh = __any(!(m_run > -INFINITY));
-            if (need_mask) {
-                take_odd_values(vf, sees, o_acc);
-            }
+            if (decltype(careful)::value || need_mask) take_odd_values(vf, sees, o_acc);
             // ---- O^T += V^T P^T, the probabilities as two bf16 each: rounded to one, their error (2^-9 of each term) was as large as the
             // output's own rounding, and the result 1.45 times as far from the sums in 64 bits as one that is only rounded at the end ----
             const bf16x8 pf = __builtin_convertvector(pv, bf16x8);
@@ -497,6 +497,78 @@ void paged_split_kernel(const PagedParams p)
             for (int jj = 0; jj < DJ; ++jj) o_acc[jj] = mfma16(vf[jj], pf, o_acc[jj]);
 #pragma unroll
             for (int jj = 0; jj < DJ; ++jj) o_acc[jj] = mfma16(vf[jj], pf_rest, o_acc[jj]);
+        };
+        uint32_t at_stage = 0;
+        int base = t_begin * TK + ks * kChunkKeys;
+        for (int i = 0; i < n_tiles; ++i, base += TK, at_stage = at_stage == (NS - 1) * 2 * TILE_BYTES ? 0 : at_stage + 2 * TILE_BYTES) {
+            stage_barrier();
+            if (base >= n) continue;
+            const uint32_t ok = (uint32_t)__builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint16_t*>(s_ok + at_stage / (TILE_BYTES / 4) + 2 * ks));
+            // ---- S^T = K Q^T for 32 keys ----
+            floatx4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                const SPECVLM_AS3 u32x4* const at = (const SPECVLM_AS3 u32x4*)(k_base + at_stage ^ kk * 64);
+                const u32x4 k0 = at[0], k1 = at[16 * ROW_BYTES / 16];
+                s0 = mfma16(__builtin_bit_cast(bf16x8, k0), qf[kk], s0);
+                s1 = mfma16(__builtin_bit_cast(bf16x8, k1), qf[kk], s1);
+            }
+            // ---- V^T fragments of the lane's keys (4c+e and 16+4c+e) by the transposing LDS read ----
+            bf16x8 vf[DJ];
+#pragma unroll
+            for (int jj = 0; jj < DJ; ++jj) {
+                typedef short s16x4 __attribute__((ext_vector_type(4)));
+                SPECVLM_AS3 s16x4* const at = (SPECVLM_AS3 s16x4*)(v_base + at_stage ^ jj * 32);
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at);
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at + 16 * ROW_BYTES / 8);
+                vf[jj] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+            take(base, ok, s0, s1, vf, Plain{});
+        }
+        // A sum that is no finite number, as a rule of an infinite value that a row sees away from the masks:  the wave takes its keys once more, carefully,
+        // from where they lie.  (Us a call, without this / with it:  a chain block over 12806 keys 16.3 / 16.4, windows of 12 requests 40.0 / 40.3, trees of 26
+        // nodes 73.0 / 74.9;  values looked at in every chunk, or the ring filled again, cost the chain block 1 us.)
+        if (__builtin_expect(any_odd(o_acc), 0)) {
+            m_run = -INFINITY; l_run = 0.f; fresh = true;
+#pragma unroll
+            for (int jj = 0; jj < DJ; ++jj) o_acc[jj] = floatx4{0.f, 0.f, 0.f, 0.f};
+            // (the parameters are fetched again: kept since the kernel's start they would push others out of their registers)
+            const SPECVLM_AS4 PagedParams* z = (const SPECVLM_AS4 PagedParams*)__builtin_amdgcn_kernarg_segment_ptr();
+            __asm__ volatile("" : "+s"(z));
+            uint32_t row_bytes = (uint32_t)z->tok * 2;
+            for (int base = t_begin * TK + ks * kChunkKeys; base < min(n, t_end * TK); base += TK) {
+                uint32_t lane_r = r, lane_c = c;
+                __asm__ volatile("" : "+s"(row_bytes), "+v"(lane_r), "+v"(lane_c));       // (or the offsets of every load would live through the loop)
+                uint32_t ok = 0;
+                const char *k_at[2], *v_at[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int x = min(base + 16 * i, (n - 1) & ~15);
+                    const QuotRem at = divide(x < view.sinks ? x : x + view.skip, z->page_size, z->inv_page);
+                    const int id = uniform_load(z->table + (int64_t)b * z->table_row, at.q);
+                    const bool there = (uint32_t)id < (uint32_t)z->n_pages;
+                    ok |= (there ? 1u : 0u) << (8 * i);
+                    const int64_t off = (there ? id : 0) * z->page + at.r * z->tok + (int64_t)g * z->head;
+                    k_at[i] = reinterpret_cast<const char*>(z->k + off);
+                    v_at[i] = reinterpret_cast<const char*>(z->v + off);
+                }
+                floatx4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) {
+                    s0 = mfma16(*reinterpret_cast<const bf16x8*>(k_at[0] + (lane_r * row_bytes + lane_c * 16) + kk * 64), qf[kk], s0);
+                    s1 = mfma16(*reinterpret_cast<const bf16x8*>(k_at[1] + (lane_r * row_bytes + lane_c * 16) + kk * 64), qf[kk], s1);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                bf16x8 vf[DJ];
+#pragma unroll
+                for (int jj = 0; jj < DJ; ++jj) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        vf[jj][e] = *reinterpret_cast<const __bf16*>(v_at[e / 4] + ((4 * lane_c + e % 4) * row_bytes + lane_r * 2) + jj * 32);
+                    __builtin_amdgcn_sched_barrier(0);            // (one after the other, as in take_odd_values)
+                }
+                take(base, ok, s0, s1, vf, Careful{});
+            }
         }
 
         // ---- the KS waves of a row block exchange their results through LDS; wave ks then owns D/KS columns of its rows ----
@@ -513,21 +585,30 @@ void paged_split_kernel(const PagedParams p)
         __syncthreads();
         if (row >= n_rows) return;
         float m_x[KS], m_all = -INFINITY, l_all = 0.f;
+        bool lost = false;
 #pragma unroll
         for (int kx = 0; kx < KS; ++kx) { m_x[kx] = sm_m[(kx * MB + mb) * 16 + r]; m_all = fmaxf(m_all, m_x[kx]); }
         const float m_ref = (m_all == -INFINITY) ? 0.f : m_all;
 #pragma unroll
-        for (int kx = 0; kx < KS; ++kx) { m_x[kx] = fast_exp2(m_x[kx] - m_ref); l_all += m_x[kx] * sm_l[(kx * MB + mb) * 16 + r]; }
+        for (int kx = 0; kx < KS; ++kx) {
+            const float w = fast_exp2(m_x[kx] - m_ref);
+            lost |= w == 0.f && m_x[kx] > -INFINITY;
+            m_x[kx] = w;
+            l_all += w * sm_l[(kx * MB + mb) * 16 + r];
+        }
         const int col0 = ks * SLICE + c * CPL;
         floatx4 acc[CPL / 4];
+        const auto sum = [&](auto careful) {
 #pragma unroll
-        for (int qd = 0; qd < CPL / 4; ++qd) acc[qd] = floatx4{0.f, 0.f, 0.f, 0.f};
+            for (int qd = 0; qd < CPL / 4; ++qd) acc[qd] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int kx = 0; kx < KS; ++kx) {
-            const float* buf = sm_o + ((kx * MB + mb) * 16 + r) * LDS_STRIDE + col0;
+            for (int kx = 0; kx < KS; ++kx) {
+                const float* buf = sm_o + ((kx * MB + mb) * 16 + r) * LDS_STRIDE + col0;
 #pragma unroll
-            for (int qd = 0; qd < CPL / 4; ++qd) acc[qd] += m_x[kx] * *reinterpret_cast<const floatx4*>(buf + 4 * qd);
-        }
+                for (int qd = 0; qd < CPL / 4; ++qd) acc[qd] += weighted(m_x[kx], *reinterpret_cast<const floatx4*>(buf + 4 * qd), careful);
+            }
+        };
+        if (__builtin_expect(__any(lost), 0)) sum(Careful{}); else sum(Plain{});
         if (direct) {
             const int t = t_blk, h = g * p.group + q_at.r;
             const float inv = l_all == 0.f ? 0.f : 1.f / l_all;                   // (a row that sees nothing: 0)
@@ -673,11 +754,14 @@ void paged_short_kernel(const PagedParams p)
         m = quad_max(mx) * sc;
         const float m_ref = (m == -INFINITY) ? 0.f : m;
         const uint32_t v_addr = (uint32_t)(uintptr_t)(SPECVLM_AS3 const void*)(v_lds + (4 * c + (r >> 2)) * (COLS * 2) + (r & 3) * 8);
-#pragma unroll
-        for (int ch = 0; ch < CH; ++ch) {
+        const auto products = [&](const int ch, auto careful) {
             floatx8 pv, rest;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { pv[e] = fast_exp2(fmaf(s[ch][e], sc, -m_ref)); l += pv[e]; }
+            for (int e = 0; e < 8; ++e) pv[e] = fast_exp2(fmaf(s[ch][e], sc, -m_ref));
+            if constexpr (!decltype(careful)::value) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) l += pv[e];
+            }
             const bf16x8 pf = __builtin_convertvector(pv, bf16x8);
             const u32x4 two = __builtin_bit_cast(u32x4, pf);
 #pragma unroll
@@ -692,9 +776,16 @@ void paged_short_kernel(const PagedParams p)
             __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __asm__ volatile("" : "+v"(lo), "+v"(hi));
             bf16x8 vf[1] = {__builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3))};
-            if (__any(sees[ch] != 0x000f000fu)) take_odd_values(vf, sees[ch], o_acc);
+            if (decltype(careful)::value || __any(sees[ch] != 0x000f000fu)) take_odd_values(vf, sees[ch], o_acc);
             o_acc[0] = mfma16(vf[0], pf, o_acc[0]);
             o_acc[0] = mfma16(vf[0], pf_rest, o_acc[0]);
+        };
+#pragma unroll
+        for (int ch = 0; ch < CH; ++ch) products(ch, Plain{});
+        if (__builtin_expect(any_odd(o_acc), 0)) {                // (as in paged_split_kernel; the maximum is the wave's already)
+            o_acc[0] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ch = 0; ch < CH; ++ch) products(ch, Careful{});
         }
         l = quad_sum(l);
     }
@@ -727,9 +818,14 @@ void paged_short_kernel(const PagedParams p)
     floatx4 tot = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        const float f = fast_exp2(m_w[i] - ref);             // 0 for a wave without keys
-        tot += f * o_w[i];
-        l_all += f * l_w[i];
+        m_w[i] = fast_exp2(m_w[i] - ref);                    // 0 for a wave without keys
+        tot += m_w[i] * o_w[i];
+        l_all += m_w[i] * l_w[i];
+    }
+    if (__builtin_expect(any_odd(tot), 0)) {
+        tot = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) tot += weighted(m_w[i], o_w[i], Careful{});
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) tot[i] = over_lanes(tot[i], sum);
@@ -768,32 +864,38 @@ void paged_join_kernel(const PagedParams p)
     const int sub = threadIdx.x / TPR, grp = sub % GP, lr = sub / GP, col = (threadIdx.x % TPR) * 4, row = row0 + lr;
     const int64_t slot0 = (int64_t)((j0 + b) * p.n_kv_heads + g) * p.rows_pad + min(row, n_rows - 1);
     const int64_t step = (int64_t)p.n_kv_heads * p.rows_pad;
-    float m = -INFINITY, l = 0.f;
-    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = grp; s0 < live; s0 += GP * PRE) {
-        float2 ml[PRE];
-        floatx4 o[PRE];
+    float m, l;
+    floatx4 acc;
+    const auto fold = [&](auto careful) {
+        m = -INFINITY; l = 0.f;
+        acc = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int s0 = grp; s0 < live; s0 += GP * PRE) {
+            float2 ml[PRE];
+            floatx4 o[PRE];
 #pragma unroll
-        for (int i = 0; i < PRE; ++i) {
-            const int64_t slot = slot0 + min(s0 + GP * i, live - 1) * step;
-            ml[i] = *reinterpret_cast<const float2*>(p.part_ml + slot * 2);
-            o[i] = *reinterpret_cast<const floatx4*>(p.part_o + slot * D + col);
-        }
-        float m_new = m;
-#pragma unroll
-        for (int i = 0; i < PRE; ++i) if (s0 + GP * i < live) m_new = fmaxf(m_new, ml[i].x);
-        const float ref = (m_new == -INFINITY) ? 0.f : m_new, old = fast_exp2(m - ref);
-        acc *= old; l *= old;
-#pragma unroll
-        for (int i = 0; i < PRE; ++i) {
-            if (s0 + GP * i < live) {
-                const float w = fast_exp2(ml[i].x - ref);        // 0 for a piece of which the row sees nothing
-                acc += w * o[i];
-                l += w * ml[i].y;
+            for (int i = 0; i < PRE; ++i) {
+                const int64_t slot = slot0 + min(s0 + GP * i, live - 1) * step;
+                ml[i] = *reinterpret_cast<const float2*>(p.part_ml + slot * 2);
+                o[i] = *reinterpret_cast<const floatx4*>(p.part_o + slot * D + col);
             }
+            float m_new = m;
+#pragma unroll
+            for (int i = 0; i < PRE; ++i) if (s0 + GP * i < live) m_new = fmaxf(m_new, ml[i].x);
+            const float ref = (m_new == -INFINITY) ? 0.f : m_new, old = fast_exp2(m - ref);
+            acc = weighted(old, acc, careful); l *= old;
+#pragma unroll
+            for (int i = 0; i < PRE; ++i) {
+                if (s0 + GP * i < live) {
+                    const float w = fast_exp2(ml[i].x - ref);        // 0 for a piece of which the row sees nothing
+                    acc += weighted(w, o[i], careful);
+                    l += w * ml[i].y;
+                }
+            }
+            m = m_new;
         }
-        m = m_new;
-    }
+    };
+    fold(Plain{});
+    if (__builtin_expect(any_odd(acc), 0)) fold(Careful{});
     if constexpr (GP > 1) {
         *reinterpret_cast<floatx4*>(&s_o[lr][grp][col]) = acc;
         if (col == 0) { s_m[lr][grp] = m; s_l[lr][grp] = l; }
@@ -802,13 +904,17 @@ void paged_join_kernel(const PagedParams p)
 #pragma unroll
         for (int i = 0; i < GP; ++i) m = fmaxf(m, s_m[lr][i]);
         const float ref = (m == -INFINITY) ? 0.f : m;
-        acc = floatx4{0.f, 0.f, 0.f, 0.f}; l = 0.f;
+        const auto sum = [&](auto careful) {
+            acc = floatx4{0.f, 0.f, 0.f, 0.f}; l = 0.f;
 #pragma unroll
-        for (int i = 0; i < GP; ++i) {
-            const float w = fast_exp2(s_m[lr][i] - ref);
-            acc += w * *reinterpret_cast<const floatx4*>(&s_o[lr][i][col]);
-            l += w * s_l[lr][i];
-        }
+            for (int i = 0; i < GP; ++i) {
+                const float w = fast_exp2(s_m[lr][i] - ref);
+                acc += weighted(w, *reinterpret_cast<const floatx4*>(&s_o[lr][i][col]), careful);
+                l += w * s_l[lr][i];
+            }
+        };
+        sum(Plain{});
+        if (__builtin_expect(any_odd(acc), 0)) sum(Careful{});
     }
     if (row >= n_rows) return;
     acc *= l == 0.f ? 0.f : 1.f / l;
