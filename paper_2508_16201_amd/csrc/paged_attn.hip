@@ -62,6 +62,10 @@ struct PagedParams {
     int32_t* part_of;        // [batch][2] (of a batch) the first group that has a piece of the request, and how many have
 };
 
+// A lane's sum of one chunk at or above this (or NaN), against the maximum of earlier chunks, is done once more with the maximum tracked.  It bounds what a probability
+// can grow to before its product with a value:  with 2^100 values of 2^28 went beyond 32 bits (a logit 62 above those before it is a probability of 2^89), though
+// the sum does not.
+constexpr float kPagedRedo = 0x1p20f;
 constexpr int kTileKeys = 64;
 constexpr int kRing = 3;                 // tiles of a ring (four: 0.4 us more a call, no faster for long caches)
 // A group takes a tile or more: as many as the launch's workgroups need, and up to four where a request (of the mean length) would else have more than
@@ -458,7 +462,7 @@ void paged_split_kernel(const PagedParams p)
                 float psum = 0.f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) { pv[e] = fast_exp2(fmaf(s[e], sc, -m_run)); psum += pv[e]; }
-                if (!__any(!(psum < kSumRedo))) {
+                if (!__any(!(psum < kPagedRedo))) {
                     l_run += psum;
                     settled = true;
                 }

@@ -1,5 +1,5 @@
-"""specvlm_paged_attn over values that are no finite numbers: what a row sees of them comes out, wherever their keys lie, and what it does
-not see changes no bit of it."""
+"""specvlm_paged_attn over values that are no finite numbers (what a row sees of them comes out, wherever their keys lie, and what it does
+not see changes no bit of it), and over values too large for a product with an early maximum's probability."""
 import numpy as np
 import pytest
 import torch
@@ -37,7 +37,7 @@ def variants(table, kv_lens, q_lens, ps):
     return {"short": (table, kv_lens, {}), "shared": (wide, kv_lens, {}), "whole": (many, list(kv_lens) + [0] * CROWD, crowd)}
 
 
-def check(B, q, k, v, table, kv_lens, q_lens, scale, odd, **more):
+def check(B, q, k, v, table, kv_lens, q_lens, scale, odd, *, what=None, **more):
     """odd: what columns hold (inf, -inf or nan), in every head; the others are held to 64 bits over values that are 0 in the odd places."""
     ps = k.shape[1]
     flat = v.copy()
@@ -45,6 +45,8 @@ def check(B, q, k, v, table, kv_lens, q_lens, scale, odd, **more):
     want, want_lse, tol, tol_lse, _ = R.paged_attention(R.values(q), R.values(k), R.values(flat), table, kv_lens, q_lens, scale, **more)
     plain = [c for c in range(q.shape[2]) if c not in odd]
     for name, (entries, lens, how) in variants(table, kv_lens, q_lens, ps).items():
+        if what and name not in what:
+            continue
         got, lse = B.paged_attn(dev_bf16(q), dev_bf16(k), dev_bf16(v), i32(entries), i32(lens), scale, want_lse=True, **how, **more)
         got, lse = host_f64(got), host_f64(lse)
         assert (np.abs(got - want)[:, :, plain] <= tol[:, :, plain]).all(), name
@@ -108,3 +110,19 @@ def test_values_that_one_row_sees_do_not_touch_the_others(B, heads):
         got[[1, 5], :, 0], clean[[1, 5], :, 0] = 0, 0
         got[:, :, 5], clean[:, :, 5] = 0, 0
         assert np.array_equal(got, clean), name
+
+
+@pytest.mark.parametrize("heads,n,what", [((3, 3, 64), 700, ("short", "whole")), ((5, 5, 128), 440, ("short", "whole")), ((5, 5, 128), 9000, ("short",)),
+                                          ((4, 4, 64), 20000, ("short",))])
+def test_large_values_behind_a_small_maximum(B, heads, n, what):
+    """A key whose logit is 62 over those before it, with values of 2^60: its probability against the early maximum, 2^89, times that is too
+    large for 32 bits, the sum divided by its normaliser is not."""
+    hq, hkv, d = heads
+    scale = d ** -0.5
+    q, k, v, table = build(34, [n], [1], heads, 16)
+    qf = R.values(q)[0]
+    high = bits(62 * qf / (qf ** 2).sum(1, keepdims=True) / scale)
+    for j in range(150, n - 20, 800):
+        k[at(table, 0, 16, j)] = high
+        v[at(table, 0, 16, j)][:, :3] = bits([2.0 ** 60, -2.0 ** 61, 1.5 * 2.0 ** 60])
+    check(B, q, k, v, table, [n], [1], scale, {}, what=what)
