@@ -381,7 +381,8 @@ int specvlm_tree_attn(
  *     is its place in the block)
  *   and the key's page is one of the pool's.
  *
- *   q    bf16 [sum q_len_b, H_q, d]      out  bf16, same shape and strides as q
+ *   q    bf16 [sum q_len_b, H_q, d]      out  bf16, same shape and strides as q (q itself
+ *        is allowed, else it must not overlap q)
  *   lse  optional fp32 [sum q_len_b, H_q]: natural log of each row's softmax sum
  * A row that sees no key gets 0, and -infinity in lse.  What a hidden key or value
  * holds (a page's rows behind the last token, NaN, infinities) changes nothing; an

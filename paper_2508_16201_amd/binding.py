@@ -562,7 +562,7 @@ def paged_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, pa
     page_table int32 [batch, max_pages], kv_lens int32 [batch] (the block included); without cu_q every request has
     q.shape[0] / batch queries, with it max_q_len says the most.  max_kv_len: the most that kv_lens may hold (the whole
     table's worth by default).  window > 0: a query sees that many tokens up to its own, and the first n_sinks.
-    ancestor_mask int64/uint64 [sum q_len]: a draft tree's, as in tree_attn."""
+    ancestor_mask int64/uint64 [sum q_len]: a draft tree's, as in tree_attn.  out may be q."""
     got = (_calls or _load_calls()).paged_attn(q, k_pages, v_pages, page_table, kv_lens, softmax_scale, cu_q, max_q_len, max_kv_len, window, n_sinks,
                                                ancestor_mask, out, want_lse, workspace)
     if got is not None:

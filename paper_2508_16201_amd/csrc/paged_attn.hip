@@ -422,7 +422,7 @@ void paged_split_kernel(const PagedParams p)
         for (int jj = 0; jj < DJ; ++jj) o_acc[jj] = floatx4{0.f, 0.f, 0.f, 0.f};
         bf16x8 qf[KK];
         const int row = row0 + mb * 16 + r;
-        const QuotRem q_at = divide(row < n_rows ? row : 0, p.group, p.inv_group);   // (padding rows take row 0: never stored)
+        const QuotRem q_at = divide(row < n_rows ? row : row0, p.group, p.inv_group);   // (padding rows take the first: never stored)
         const int t_blk = q_at.q;
         const __bf16* qp = p.q + (int64_t)(rq.q0 + t_blk) * p.q_tok + (int64_t)(g * p.group + q_at.r) * p.q_head + c * 8;
 #pragma unroll
@@ -1116,6 +1116,7 @@ extern "C" int specvlm_paged_attn(
     p.part_of = (int32_t*)((char*)p.part_ml + align256(slots * 2 * sizeof(float)));
     const int64_t places = paged_most_places(q_len, kv_len, window, n_sinks);
     const bool whole = paged_takes_whole(batch, n_kv_heads, s.n_rgroups, s.mb, head_dim, places);
-    const int short_chunks = paged_short_chunks(batch, n_kv_heads, paged_blocks(p), head_dim, places);
+    // (over the queries themselves the slices of a row would write what the others still read; in the other kernels a row is read by who writes it)
+    const int short_chunks = out == q ? 0 : paged_short_chunks(batch, n_kv_heads, paged_blocks(p), head_dim, places);
     return head_dim == 128 ? launch_paged_d<128>(p, s.mb, whole, short_chunks, (hipStream_t)stream) : launch_paged_d<64>(p, s.mb, whole, short_chunks, (hipStream_t)stream);
 }
