@@ -398,7 +398,9 @@ int specvlm_tree_attn(
  * query's window are never looked at and may be freed.
  * Results do not depend on the run; they may differ by roundings when the other
  * requests of the batch change, since the lengths of all decide how each is cut.
- * Limits: q_len <= 64, kv_len <= 2^30, batch <= 2^25.
+ * Limits: q_len <= 64, kv_len <= 2^30, batch * ceil(kv_len / 64) < 2^30.  A launch has fewer
+ * than 2^32 threads: batch * H_kv up to 2^22 with batch * q_len * H_q up to 2^24 is always
+ * served, more is refused (SPECVLM_EUNSUPPORTED) where a launch would be larger.
  * -------------------------------------------------------------------------- */
 size_t specvlm_paged_attn_workspace_bytes(int batch, int q_len, int n_q_heads, int n_kv_heads, int head_dim);
 
@@ -454,6 +456,7 @@ int specvlm_rope_turns(int rot_dim, const specvlm_rope_spec* spec, uint64_t* tur
  * Without cu_q n_tokens is a multiple of batch.  kv_lens may be NULL with k NULL and
  * positions given.  Tokens behind the last request, and those of a request with fewer
  * cached tokens than new ones, are left alone.  k, v must not overlap the pool.
+ * Limits: n_tokens <= 2^26 - 4, heads <= 2^20 (a launch's threads).
  * -------------------------------------------------------------------------- */
 int specvlm_rope_append(
     const void* q, int64_t q_tok_stride, int64_t q_head_stride, void* q_out, int64_t out_tok_stride, int64_t out_head_stride,
@@ -493,6 +496,8 @@ int specvlm_rope_append(
  * A row that needs pages gets them if the needs of all rows up to it fit the free ones.
  * The table has to hold all rows that own pages of the pool: what is in no row is free.
  * Integer arithmetic throughout: the result depends on the arguments alone.
+ * Limits: batch * max_pages < 2^30; batch * ceil(max(old_max_pages, max_pages) / 256) +
+ * ceil(n_pages / 1024) < 2^24.
  * -------------------------------------------------------------------------- */
 size_t specvlm_pages_assign_workspace_bytes(int batch, int n_pages);
 
@@ -526,7 +531,8 @@ int specvlm_pages_assign(
  * request may then overlap if its indices ascend and no row moves to a later token of the
  * same table row.  No request's destination may be another's source or destination.  Pools that are not
  * the same must not overlap.
- * Limits: batch <= 65535, max_rows <= 2^30.
+ * Limits: batch <= 65535, max_rows <= 2^30, and between different pools max_rows * H_kv * d
+ * up to 2^35 is always served (a launch's threads).
  * -------------------------------------------------------------------------- */
 int specvlm_pages_copy(
     const void* k_src, const void* v_src, int64_t src_layer_stride, int64_t src_page_stride, int64_t src_tok_stride, int64_t src_head_stride,

@@ -88,6 +88,10 @@ inline uint32_t reciprocal(int d) { return d > 1 ? (uint32_t)((1ull << 32) / (ui
 inline int round_up(int x, int m) { return (x + m - 1) / m * m; }
 inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
+// Whether there can be a launch of so many workgroups: it has fewer than 2^32 threads.  (Asked before the first launch of a call: one that is refused
+// behind others would leave half a result.)
+inline bool launchable(int64_t workgroups, int threads) { return workgroups <= (int64_t)(UINT32_MAX / (uint32_t)threads); }
+
 inline int launch_status()
 {
     return hipGetLastError() == hipSuccess ? SPECVLM_OK : SPECVLM_ELAUNCH;

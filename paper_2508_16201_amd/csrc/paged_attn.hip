@@ -950,6 +950,7 @@ static int launch_paged(const PagedParams& p, hipStream_t stream)
     constexpr size_t ring = (size_t)NS * (2 * KS * kChunkKeys * D * 2 + 8);
     constexpr size_t exchange = sizeof(float) * (size_t)(NW * 16 * (D + 4 + 2));
     constexpr size_t lds = ring > exchange ? ring : exchange;
+    if (!launchable((int64_t)(WHOLE ? p.batch : p.max_groups) * p.n_rgroups * p.n_kv_heads, (NW + NLD) * kWave)) return SPECVLM_EUNSUPPORTED;
     if (lds > 64 * 1024)
         if (const int rc = allow_lds<&paged_split_kernel<D, MB, KS, NS, NLD, WHOLE>>((int)lds)) return rc;
     hipLaunchKernelGGL((paged_split_kernel<D, MB, KS, NS, NLD, WHOLE>), dim3((WHOLE ? p.batch : p.max_groups) * p.n_rgroups * p.n_kv_heads),
@@ -1035,6 +1036,14 @@ static int launch_paged_d(const PagedParams& p, int mb, bool whole, int short_ch
         }
         return SPECVLM_EUNSUPPORTED;
     }
+    // few rows: eight groups of threads share a row's pieces;  where the rows fill the chip two do, in a quarter of the workgroups.  Us a call, eight /
+    // two:  64/8 heads, 12806 keys, 8 queries 18.1 / 19.4;  14/2 heads, one, 1511 keys 7.3 / 8.0;  but 64 requests of up to 1000 keys, 28/4 heads 22.2 / 21.1,
+    // windows of 12 requests, 4 queries, 40/8 heads 43.1 / 41.5, trees of 208 rows, four requests, the join alone 11 / 5.2.
+    const int rows = p.group * p.q_len;
+    const bool few = (int64_t)rows * p.batch * p.n_kv_heads < 1024;
+    const int join_rows = 256 / (D / 4 * (few ? 8 : 2));
+    const int64_t joins = (int64_t)((rows + join_rows - 1) / join_rows) * p.batch * p.n_kv_heads;
+    if (!launchable(joins, 256)) return SPECVLM_EUNSUPPORTED;
     int rc = SPECVLM_EUNSUPPORTED;
     switch (mb) {
         case 1: rc = launch_paged<D, 1, 2, kRing, 4, false>(p, stream); break;
@@ -1043,16 +1052,8 @@ static int launch_paged_d(const PagedParams& p, int mb, bool whole, int short_ch
         case 4: rc = launch_paged<D, 4, 2, kRing, 4, false>(p, stream); break;
     }
     if (rc != SPECVLM_OK) return rc;
-    const int rows = p.group * p.q_len;
-    const auto join = [&](auto gp) {
-        constexpr int GP = decltype(gp)::value, ROWS = 256 / (D / 4 * GP);
-        hipLaunchKernelGGL((paged_join_kernel<D, GP>), dim3((rows + ROWS - 1) / ROWS * p.batch * p.n_kv_heads), dim3(256), 0, stream, p);
-    };
-    // few rows: eight groups of threads share a row's pieces;  where the rows fill the chip two do, in a quarter of the workgroups.  Us a call, eight /
-    // two:  64/8 heads, 12806 keys, 8 queries 18.1 / 19.4;  14/2 heads, one, 1511 keys 7.3 / 8.0;  but 64 requests of up to 1000 keys, 28/4 heads 22.2 / 21.1,
-    // windows of 12 requests, 4 queries, 40/8 heads 43.1 / 41.5, trees of 208 rows, four requests, the join alone 11 / 5.2.
-    if ((int64_t)rows * p.batch * p.n_kv_heads < 1024) join(std::integral_constant<int, 8>{});
-    else                                               join(std::integral_constant<int, 2>{});
+    if (few) hipLaunchKernelGGL((paged_join_kernel<D, 8>), dim3((unsigned)joins), dim3(256), 0, stream, p);
+    else     hipLaunchKernelGGL((paged_join_kernel<D, 2>), dim3((unsigned)joins), dim3(256), 0, stream, p);
     return launch_status();
 }
 
@@ -1091,7 +1092,7 @@ extern "C" int specvlm_paged_attn(
     // (a lane's offset inside 16 keys has 32 bits; tiles and places of the sweep are ints)
     if (tok_stride < 0 || tok_stride >= ((int64_t)1 << 26) || kv_len > (1 << 30)) return SPECVLM_EUNSUPPORTED;
     if ((int64_t)batch * ((kv_len + kTileKeys - 1) / kTileKeys) >= ((int64_t)1 << 30) || batch > (1 << 30) / kFold) return SPECVLM_EUNSUPPORTED;
-    if ((int64_t)batch * q_len >= ((int64_t)1 << 31) / n_q_heads) return SPECVLM_EUNSUPPORTED;        // (a launch's workgroups)
+    if ((int64_t)batch * q_len >= ((int64_t)1 << 31) / n_q_heads) return SPECVLM_EUNSUPPORTED;        // (rows are ints; a launch's threads: launchable)
     const PagedPlan s = paged_plan(q_len, n_q_heads, n_kv_heads);
     const size_t need = specvlm_paged_attn_workspace_bytes(batch, q_len, n_q_heads, n_kv_heads, head_dim);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return SPECVLM_EWORKSPACE;

@@ -407,7 +407,7 @@ static int launch_copy(CopyParams& p, hipStream_t stream)
     p.slices = (p.pieces + p.slice - 1) / p.slice;
     const int step = kCopyThreads / p.slice * kCopyEach;
     p.row_blocks = IN_PLACE ? 1 : (p.max_rows + step - 1) / step;
-    if ((int64_t)p.row_blocks * p.slices > (int64_t)UINT32_MAX / kCopyThreads) return SPECVLM_EUNSUPPORTED;      // (a launch's threads)
+    if (!launchable((int64_t)p.row_blocks * p.slices, kCopyThreads)) return SPECVLM_EUNSUPPORTED;
     // layers of K and V that share a workgroup, and its lookups: as many as leave workgroups enough
     const int64_t each = (int64_t)p.row_blocks * p.slices * p.batch;
     int64_t z = (kCopyTarget + each - 1) / each;
@@ -465,7 +465,7 @@ extern "C" int specvlm_pages_assign(
     if (tables_overlap(old_table, old_stride, old_rows, old_max_pages, page_table, table_stride, batch, max_pages)) return SPECVLM_EINVAL;
     const int most = old_max_pages > max_pages ? old_max_pages : max_pages;
     const int chunks = most ? (most + kAssignThreads - 1) / kAssignThreads : 1;
-    if ((int64_t)batch * max_pages > INT_MAX / 2 || (int64_t)batch * chunks + assign_blocks(n_pages) > INT_MAX / 2) return SPECVLM_EUNSUPPORTED;
+    if ((int64_t)batch * max_pages > INT_MAX / 2 || !launchable((int64_t)batch * chunks + assign_blocks(n_pages), kAssignThreads)) return SPECVLM_EUNSUPPORTED;
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < specvlm_pages_assign_workspace_bytes(batch, n_pages)) return SPECVLM_EWORKSPACE;
 
     AssignParams p;

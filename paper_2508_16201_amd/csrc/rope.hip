@@ -155,6 +155,7 @@ static int launch_rope(RopeParams& p, int n_tokens, hipStream_t stream)
     if ((int64_t)n_tokens * p.parts > 0x7fffffff - kRopeWaves) return SPECVLM_EUNSUPPORTED;
     p.n_waves = n_tokens * p.parts;
     const dim3 grid((p.n_waves + kRopeWaves - 1) / kRopeWaves), block(kRopeWaves * kWave);
+    if (!launchable(grid.x, kRopeWaves * kWave)) return SPECVLM_EUNSUPPORTED;
     if ((int64_t)n_tokens * p.rows * D * 4 >= kRopeStreamBytes) hipLaunchKernelGGL((rope_append_kernel<D, true>), grid, block, 0, stream, p);
     else                                                        hipLaunchKernelGGL((rope_append_kernel<D, false>), grid, block, 0, stream, p);
     return launch_status();
