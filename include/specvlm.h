@@ -365,7 +365,7 @@ int specvlm_tree_attn(
  *
  * An entry of a table outside [0, n_pages) is no page.  Nothing is read or written
  * through it: its keys are hidden, its rows are dropped.  Entries that no token of a
- * request lies in are not looked at.
+ * request lies in may hold anything: no page is read or written through them.
  * All of these live on the device, so a captured call serves caches as they grow.
  * -------------------------------------------------------------------------- */
 

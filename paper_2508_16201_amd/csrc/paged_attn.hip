@@ -702,9 +702,10 @@ void paged_short_kernel(const PagedParams p)
         int64_t page_at[2 * CH];
 #pragma unroll
         for (int i = 0; i < 2 * CH; ++i) {
-            const bool there = (uint32_t)id[i] < (uint32_t)p.n_pages;
+            // (looked up before the request's length was there: behind it an entry may hold anything, and the wave's first group is loaded again)
+            const bool inside = i == 0 || x0 + 16 * i < n, there = inside && (uint32_t)id[i] < (uint32_t)p.n_pages;
             ok |= (there ? 1u : 0u) << i;
-            page_at[i] = 2 * ((there ? id[i] : 0) * p.page + at_row[i] * p.tok);
+            page_at[i] = inside ? 2 * ((there ? id[i] : 0) * p.page + at_row[i] * p.tok) : page_at[0];
         }
 #pragma unroll
         for (int ch = 0; ch < CH; ++ch)
