@@ -1094,6 +1094,7 @@ extern "C" int specvlm_paged_attn(
     if (tok_stride < 0 || tok_stride >= ((int64_t)1 << 26) || kv_len > (1 << 30)) return SPECVLM_EUNSUPPORTED;
     if ((int64_t)batch * ((kv_len + kTileKeys - 1) / kTileKeys) >= ((int64_t)1 << 30) || batch > (1 << 30) / kFold) return SPECVLM_EUNSUPPORTED;
     if ((int64_t)batch * q_len >= ((int64_t)1 << 31) / n_q_heads) return SPECVLM_EUNSUPPORTED;        // (rows are ints; a launch's threads: launchable)
+    if (window >= kv_len) window = 0;                 // (no position is that far on; sums with the others stay in 32 bits)
     const PagedPlan s = paged_plan(q_len, n_q_heads, n_kv_heads);
     const size_t need = specvlm_paged_attn_workspace_bytes(batch, q_len, n_q_heads, n_kv_heads, head_dim);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return SPECVLM_EWORKSPACE;
