@@ -484,15 +484,22 @@ int specvlm_rope_append(
  *   - With window > 0, kept pages that no later token will see (wholly behind the first
  *     n_sinks tokens and wholly before the window of the next one) are given up: -1.
  *
- *   old_table   int32 [old_rows, old_max_pages], rows old_stride apart; an entry that is no
- *               page of the pool stays -1
+ *   old_table   int32 [old_rows, old_max_pages], rows old_stride apart.  An entry that is no
+ *               page of the pool stays -1 where its tokens are kept as a whole page.  Where the
+ *               kept tokens end in such an entry, the row gets a free page there as for new
+ *               tokens, with nothing to copy: what the page's rows held before would be seen as
+ *               the row's last keep_len % page_size kept tokens.  Who has lost that page (see
+ *               SPECVLM_ENOPAGES) keeps whole pages only, or writes those rows before they are read
  *   page_table  int32 [batch, max_pages], rows table_stride apart (>= max_pages); every entry is
  *               written, -1 behind the last page.  Must not overlap old_table (SPECVLM_EINVAL).
  *   ref_counts  int32 [n_pages]: rows of the new table that hold each page (with batch 0, none)
  *   status      int32 [batch]: SPECVLM_OK; SPECVLM_EINVAL for a row that does not fit together
  *               (parent outside [-1, old_rows), keep_len > new_len, negative, kept tokens of
  *               nothing, more pages than a table has), which gets none; SPECVLM_ENOPAGES for a
- *               row for which too few pages were left: it has what it shares and -1 for the rest
+ *               row for which too few pages were left: it has what it shares and -1 for the rest,
+ *               also in the place of a page that it ends in and shares with a row that goes on in
+ *               it.  The old table is as it was: until something is written to the pages, the
+ *               assignment can be made again from it, for fewer rows
  * A row that needs pages gets them if the needs of all rows up to it fit the free ones.
  * The table has to hold all rows that own pages of the pool: what is in no row is free.
  * Integer arithmetic throughout: the result depends on the arguments alone.

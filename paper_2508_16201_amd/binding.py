@@ -684,7 +684,8 @@ def pages_assign(page_table: torch.Tensor, parent: torch.Tensor, keep_len: torch
     -> (table [batch, max_pages], copy_start [batch], copy_rows [batch], ref_counts [n_pages], status [batch]), all int32:
     copy_rows[b] tokens from copy_start[b] on are to be copied from row parent[b] of the old table to row b of the new one
     (pages_copy), ref_counts says how many rows hold each page, status is 0, -1 (the row does not fit together) or -5 (too
-    few pages are free)."""
+    few pages are free: the row is without those, and without the page that its kept tokens end in where another row goes on in
+    that; assign again from page_table for fewer rows, or go on later from the row's whole pages)."""
     got = (_calls or _load_calls()).pages_assign(page_table, parent, keep_len, new_len, n_pages, page_size, max_pages, window, n_sinks, out, workspace)
     if got is not None:
         if type(got) is int:

@@ -4,6 +4,7 @@
 // are shared.  The page that it ends in is written next: it stays with one row, the lowest that goes on in it, if no row
 // holds it as a whole page; the others get a page of their own, with rows to copy into it.  With  whole/first(page) =
 // minimum over the rows that keep it of (-1 if it is a whole page there, else the row),  row b keeps its page iff first == b.
+// (A row whose prefix ends in an entry that is no page needs one there too, with nothing to copy.)
 // Free pages (kept by no row) go out lowest first to the lowest rows first: page of rank r to the row whose prefix sum of needs
 // holds r.  Everything is a sum, a minimum or a prefix sum of integers: the order of the atomics does not matter.
 // Bound: launches and round trips (one launch where a workgroup can do it, else four: clear, mark, plan, write).
