@@ -6,7 +6,7 @@ import torch
 
 import paged_reference as R
 from gpu_util import dev_bf16, host_f64
-from test_gpu_paged_attn import CROWD, build, i32
+from test_gpu_paged_attn import CROWD, build, i32, on_gpu
 
 pytestmark = pytest.mark.gpu
 INF, DOWN, NAN = 0x7f80, 0xff80, 0x7fc0
@@ -74,6 +74,24 @@ def test_values_inside_a_window(B):
         for j, c, x in ((n - 100, 0, INF), (n - 131, 1, DOWN), (2, 2, INF), (n - 201, 3, INF), (6, 5, DOWN)):
             v[at(table, b, 16, j)][:, c] = x                                 # (the last two: between the first keys and every window)
     check(B, q, k, v, table, kv_lens, q_lens, 0.088, {0: np.inf, 1: -np.inf, 2: np.inf}, window=180, n_sinks=4)
+
+
+@pytest.mark.parametrize("heads,ps", [((16, 2, 64), 48), ((16, 2, 128), 32)])
+def test_values_in_pools_by_heads_with_pages_that_are_none(B, heads, ps):
+    """Keys of a missing page are hidden in the second look too, whatever lies in the pool's first page."""
+    kv_lens, q_lens = [600, 300], [3, 3]
+    q, k, v, table = build(36, kv_lens, q_lens, heads, ps, drop={(0, 1), (0, 5), (1, 2)})
+    for b in range(2):
+        for j, c, x in ((7, 0, INF), (7, 1, DOWN), (ps * 4 + 3, 2, NAN)):
+            v[at(table, b, ps, j)][:, c] = x
+    flat = v.copy()
+    flat[~np.isfinite(R.values(v))] = 0
+    want, _, tol, _, _ = R.paged_attention(R.values(q), R.values(k), R.values(flat), table, kv_lens, q_lens, 0.1)
+    kd, vd = on_gpu(k, True), on_gpu(v, True)
+    for name, (entries, lens, how) in variants(table, kv_lens, q_lens, ps).items():
+        got = host_f64(B.paged_attn(dev_bf16(q), kd, vd, i32(entries), i32(lens), 0.1, **how))
+        assert (got[:, :, 0] == np.inf).all() and (got[:, :, 1] == -np.inf).all() and np.isnan(got[:, :, 2]).all(), name
+        assert (np.abs(got - want)[:, :, 3:] <= tol[:, :, 3:]).all(), name
 
 
 @pytest.mark.parametrize("heads", [(3, 3, 64), (5, 5, 128)])
