@@ -7,8 +7,8 @@
 // each (16 bits), the output is rounded once.
 //
 // Bound.  Every visible K and V row is read once for up to 64 query rows of a kv head: HBM for long caches, launches and
-// round trips for short ones.  More rows than 64 are groups that read the keys again, from the L2, which is their bound: 208 rows (trees of 26 nodes of
-// 64/8 heads) load 520 MB of it, which alone takes 52 of the 68 us.
+// round trips for short ones.  More rows than 64 are groups that read the keys again: 208 rows (trees of 26 nodes of 64/8 heads), cut into four, load
+// 520 MB through the L2, which alone takes 52 of the 72 us (the fourth group has one of the 13 row blocks).
 //
 // Pages.  A page holds a multiple of 16 keys, so 16 consecutive keys starting at a multiple of 16 lie in one page and
 // one scalar table lookup serves them: the address of a wave-wide load is a scalar base plus a lane offset that never
