@@ -22,6 +22,12 @@
  *   specvlm_pages_assign which pages every request holds next: grown, cut short, forked, freed
  *   specvlm_pages_copy   rows between pages: accepted tree nodes, a pruned cache, a fork's last page
  *
+ * and, for many texts over one video:
+ *
+ *   specvlm_pages_shared which neighbouring requests share how many tokens of their pages
+ *   specvlm_shared_attn  attention over paged caches, what a group of requests shares taken once for all
+ *   specvlm_cross_attn   attention of texts of any length over encoders' states
+ *
  * Conventions shared by every call
  * --------------------------------
  *  - Return value: SPECVLM_OK (0) or a negative SPECVLM_E* code.  Arguments are
@@ -70,7 +76,7 @@ extern "C" {
 const char* specvlm_status_string(int status);
 
 /* Library version as major*10000 + minor*100 + patch: that of the header it was built with. */
-#define SPECVLM_VERSION 200
+#define SPECVLM_VERSION 300
 int specvlm_version(void);
 
 /* --------------------------------------------------------------------------
@@ -549,6 +555,99 @@ int specvlm_pages_copy(
     int n_layers, int batch, const int32_t* n_rows, int max_rows, const int32_t* src_row, const int32_t* src_start,
     const int32_t* dst_start, const int32_t* row_idx, int64_t idx_stride, const int32_t* cu_idx,
     int n_kv_heads, int head_dim, void* stream);
+
+/* --------------------------------------------------------------------------
+ * specvlm_pages_shared -- which neighbouring requests of a batch share how many tokens,
+ * found from the page table:  several questions about one video, samples and beams of one
+ * prompt, whose rows specvlm_pages_assign made begin with the same pages.
+ *
+ *   c_b   the number of first entries in which row b agrees with row b - 1, that are pages
+ *         of the pool and lie wholly before both requests' blocks of new tokens
+ *   b goes with b - 1 if  c_b > 0,  c_b * page_size >= min_tokens  and
+ *   2 c_b >= max(c_(b-1), c_(b+1))  (of the first row, and behind the last, 0: two videos
+ *   behind one common instruction stay two groups)
+ *   A group is a run of requests that go with each other; what it shares is the least of
+ *   their c_b, in tokens.  Requests that share pages have to be neighbours to be found.
+ *
+ *   kv_lens   int32 [batch], the block included; cu_q int32 [batch + 1] or NULL: every block
+ *             has q_len tokens.  A request with no block, or a longer one than its cache,
+ *             has no pages before it
+ *   groups    int32 [3][batch], for specvlm_shared_attn: the first request of each one's group;
+ *             for the first request the number of them, 0 for the others; the tokens that
+ *             the group shares (a multiple of page_size; 0 for a request alone)
+ * Integer arithmetic: the result depends on the arguments alone.
+ * Limits: batch <= 8192, max_pages * page_size < 2^31.
+ * -------------------------------------------------------------------------- */
+size_t specvlm_pages_shared_workspace_bytes(int batch);
+
+int specvlm_pages_shared(
+    const int32_t* page_table, int64_t table_stride, int max_pages, int n_pages, int page_size,
+    const int32_t* kv_lens, const int32_t* cu_q, int batch, int q_len, int min_tokens,
+    int32_t* groups, void* workspace, size_t workspace_bytes, void* stream);
+
+/* --------------------------------------------------------------------------
+ * specvlm_shared_attn -- specvlm_paged_attn, without a window, where neighbouring requests
+ * share their first pages:  what a group of them shares is read once and computed once for
+ * the queries of all, and each request's own keys for its own.  Blocks may be of any length
+ * (a verified chain, one token, a whole question) without ancestor_mask, of 64 with it.
+ *
+ *   groups     int32 [3][batch] as specvlm_pages_shared writes it, or made by the caller: the
+ *              first groups[2][f] tokens (a multiple of 16) of request f lie, for the
+ *              groups[1][f] >= 2 requests from f on that have f in groups[0], in the
+ *              same pages, and before their blocks.  The other requests' tables are trusted to
+ *              name the pages of the first one's row there; they are not looked at.
+ *              What does not fit together (a group beyond the batch, more tokens than lie
+ *              before a block, no multiple of 16) is left out, and the requests are
+ *              taken alone: groups say how the work is cut, not what the result is
+ *   n_queries  rows of q: batch * q_len without cu_q.  q_len, kv_len: the maxima, as there
+ * Everything else, hidden and infinite values, skipped requests and rows behind the last one
+ * too, is as for specvlm_paged_attn.  Results do not depend on the run; they may differ by
+ * roundings with the other requests of the batch and the groups.
+ * Limits: n_queries * H_q < 2^29, batch * H_kv < 2^23, (n_queries * H_q / 128 + (2 * batch + 1) * H_kv)
+ * * (kv_len / 128 + 1) < 2^31 - 2^16, kv_len <= 2^30.
+ * -------------------------------------------------------------------------- */
+size_t specvlm_shared_attn_workspace_bytes(int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim);
+
+int specvlm_shared_attn(
+    const void* q, int64_t q_tok_stride, int64_t q_head_stride,
+    const void* k_pages, const void* v_pages, int64_t page_stride, int64_t tok_stride, int64_t head_stride,
+    int n_pages, int page_size, const int32_t* page_table, int64_t table_stride, int max_pages,
+    const int32_t* kv_lens, const int32_t* groups, const int32_t* cu_q, int batch, int n_queries, int q_len, int kv_len,
+    int n_q_heads, int n_kv_heads, int head_dim, float softmax_scale,
+    const uint64_t* ancestor_mask, void* out, float* lse,
+    void* workspace, size_t workspace_bytes, void* stream);
+
+/* --------------------------------------------------------------------------
+ * specvlm_cross_attn -- attention of texts over the states of encoders (the video's tower),
+ * whose keys and values a model keeps beside its own cache, of another length than the text
+ * and not hidden by a causal mask.
+ *
+ *   q    bf16 [n_queries, H_q, d]        out  bf16, same shape and strides as q (q itself is
+ *        allowed, else it must not overlap q)
+ *   k,v  bf16 [n_states, H_kv, d]        lse  optional fp32 [n_queries, H_q]
+ *   cu_q, cu_kv   int32 [batch + 1]: the queries [cu_q[e], cu_q[e + 1]) look at the states
+ *        [cu_kv[e], cu_kv[e + 1]).  Either may be empty, and of any length up to the tensors':
+ *        texts about one video are one entry, one text behind the other.  Both NULL: batch 1,
+ *        all queries and all states
+ *   key_ranges    int32 [n_queries, 2] or NULL: a query sees the states [from, to) of its
+ *        entry, counted from the entry's first (text between the frames of a stream); what lies
+ *        outside of the entry is not there
+ * A query that sees no state gets 0, and -infinity in lse.  Hidden and infinite values are as
+ * for specvlm_paged_attn.  An entry whose offsets leave the tensors or descend is skipped, its
+ * rows of out and lse left as they are, as are rows of no entry.  Results do not depend on
+ * the run.
+ * Limits: n_queries * H_q < 2^29, batch * H_kv < 2^24, (n_queries * H_q / 128 + (batch + 1) * H_kv)
+ * * (n_states / 128 + 1) < 2^31 - 2^16, n_states <= 2^30.
+ * -------------------------------------------------------------------------- */
+size_t specvlm_cross_attn_workspace_bytes(int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim);
+
+int specvlm_cross_attn(
+    const void* q, int64_t q_tok_stride, int64_t q_head_stride,
+    const void* k, const void* v, int64_t kv_tok_stride, int64_t kv_head_stride,
+    const int32_t* cu_q, const int32_t* cu_kv, int batch, int n_queries, int n_states,
+    int n_q_heads, int n_kv_heads, int head_dim, float softmax_scale,
+    const int32_t* key_ranges, void* out, float* lse,
+    void* workspace, size_t workspace_bytes, void* stream);
 
 /* --------------------------------------------------------------------------
  * specvlm_accept -- which drafted tokens survive verification  (Sec. 2.1).

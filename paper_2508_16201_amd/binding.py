@@ -41,6 +41,8 @@ EXPORTS = (
     "specvlm_paged_attn_workspace_bytes", "specvlm_paged_attn",
     "specvlm_rope_turns", "specvlm_rope_append",
     "specvlm_pages_assign_workspace_bytes", "specvlm_pages_assign", "specvlm_pages_copy",
+    "specvlm_pages_shared_workspace_bytes", "specvlm_pages_shared", "specvlm_shared_attn_workspace_bytes", "specvlm_shared_attn",
+    "specvlm_cross_attn_workspace_bytes", "specvlm_cross_attn",
 )
 
 
@@ -107,7 +109,7 @@ def lib() -> C.CDLL:
         for name in ("specvlm_score", "specvlm_select", "specvlm_top_p_count", "specvlm_gather_kv",
                      "specvlm_decode_attn", "specvlm_decode_attn_static", "specvlm_accept", "specvlm_tree_attn",
                      "specvlm_accept_tree", "specvlm_paged_attn", "specvlm_rope_turns", "specvlm_rope_append", "specvlm_pages_assign",
-                     "specvlm_pages_copy"):
+                     "specvlm_pages_copy", "specvlm_pages_shared", "specvlm_shared_attn", "specvlm_cross_attn"):
             getattr(l, name).restype = C.c_int
         l.specvlm_paged_attn_workspace_bytes.argtypes = [i32] * 5
         l.specvlm_paged_attn.argtypes = [vp, i64, i64, vp, vp, i64, i64, i64, i32, i32, vp, i64, i32, vp, vp, i32, i32, i32,
@@ -119,6 +121,13 @@ def lib() -> C.CDLL:
         l.specvlm_pages_assign.argtypes = [vp, i64, i32, i32, vp, vp, vp, i32, vp, i64, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
         l.specvlm_pages_copy.argtypes = [vp, vp, i64, i64, i64, i64, i32, i32, vp, i64, i32, i32, vp, vp, i64, i64, i64, i64, i32, i32,
                                          vp, i64, i32, i32, i32, vp, i32, vp, vp, vp, vp, i64, vp, i32, i32, vp]
+        l.specvlm_pages_shared_workspace_bytes.argtypes = [i32]
+        l.specvlm_pages_shared.argtypes = [vp, i64, i32, i32, i32, vp, vp, i32, i32, i32, vp, vp, sz, vp]
+        l.specvlm_shared_attn_workspace_bytes.argtypes = [i32] * 5
+        l.specvlm_shared_attn.argtypes = [vp, i64, i64, vp, vp, i64, i64, i64, i32, i32, vp, i64, i32, vp, vp, vp, i32, i32, i32, i32,
+                                          i32, i32, i32, f32, vp, vp, vp, vp, sz, vp]
+        l.specvlm_cross_attn_workspace_bytes.argtypes = [i32] * 5
+        l.specvlm_cross_attn.argtypes = [vp, i64, i64, vp, vp, i64, i64, vp, vp, i32, i32, i32, i32, i32, i32, f32, vp, vp, vp, vp, sz, vp]
         _lib = l
     return _lib
 
@@ -603,6 +612,148 @@ def paged_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, pa
                                   float(softmax_scale), window, n_sinks, _ptr(ancestor_mask), _ptr(out), _ptr(lse),
                                   _ptr(workspace), workspace.numel(), _stream())
     _check("specvlm_paged_attn", rc)
+    return (out, lse) if want_lse else out
+
+
+def pages_shared_workspace_bytes(batch) -> int:
+    return lib().specvlm_pages_shared_workspace_bytes(batch)
+
+
+def pages_shared(page_table: torch.Tensor, kv_lens: torch.Tensor, n_pages: int, page_size: int, q_len: int, *, cu_q: Optional[torch.Tensor] = None,
+                 min_tokens: int = 256, groups: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Which neighbouring requests share how many tokens of their first pages -> groups int32 [3, batch] for shared_attn: each
+    one's first neighbour of its group, for that one the number of them (0 for the others), the tokens that they share.
+
+    page_table int32 [batch, max_pages], kv_lens int32 [batch], the block of q_len tokens (cu_q: of their own numbers) included.
+    min_tokens: fewer common tokens are not worth a group."""
+    got = (_calls or _load_calls()).pages_shared(page_table, kv_lens, n_pages, page_size, q_len, cu_q, min_tokens, groups, workspace)
+    if got is not None:
+        if type(got) is int:
+            _check("specvlm_pages_shared", got)
+        return got
+    _on_device(page_table=page_table, kv_lens=kv_lens, cu_q=cu_q, groups=groups, workspace=workspace)
+    row, max_pages = _table("page_table", page_table)
+    batch = page_table.shape[0]
+    _int32s(batch, kv_lens=kv_lens)
+    _int32s(batch + 1, cu_q=cu_q)
+    if groups is None:
+        groups = torch.empty((3, batch), dtype=torch.int32, device=page_table.device)
+    _groups(batch, groups)
+    if workspace is None:
+        workspace = new_workspace(pages_shared_workspace_bytes(batch), page_table.device)
+    rc = lib().specvlm_pages_shared(_ptr(page_table), row, max_pages, n_pages, page_size, _ptr(kv_lens), _ptr(cu_q), batch, q_len, min_tokens,
+                                    _ptr(groups), _ptr(workspace), workspace.numel(), _stream())
+    _check("specvlm_pages_shared", rc)
+    return groups
+
+
+def _groups(batch: int, groups: torch.Tensor):
+    _typed(torch.int32, groups=groups)
+    if groups.shape != (3, batch) or not groups.is_contiguous():
+        raise ValueError("groups must be contiguous [3, requests]")
+
+
+def shared_attn_workspace_bytes(batch, n_queries, n_q_heads, n_kv_heads, head_dim) -> int:
+    return lib().specvlm_shared_attn_workspace_bytes(batch, n_queries, n_q_heads, n_kv_heads, head_dim)
+
+
+def shared_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, kv_lens: torch.Tensor,
+                softmax_scale: float, groups: torch.Tensor, *, cu_q: Optional[torch.Tensor] = None, max_q_len: Optional[int] = None,
+                max_kv_len: Optional[int] = None, ancestor_mask: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                want_lse: bool = False, workspace: Optional[torch.Tensor] = None):
+    """paged_attn for a batch whose neighbouring requests share their first pages, which are read and computed once for all of a
+    group; groups int32 [3, batch] from pages_shared.  Blocks may be of any length (with ancestor_mask up to 64).
+
+    The other arguments are paged_attn's; without cu_q every request has q.shape[0] / batch queries."""
+    got = (_calls or _load_calls()).shared_attn(q, k_pages, v_pages, page_table, kv_lens, softmax_scale, groups, cu_q, max_q_len, max_kv_len,
+                                                ancestor_mask, out, want_lse, workspace)
+    if got is not None:
+        if type(got) is int:
+            _check("specvlm_shared_attn", got)
+        return got
+    _on_device(q=q, k_pages=k_pages, v_pages=v_pages, page_table=page_table, kv_lens=kv_lens, groups=groups, cu_q=cu_q,
+               ancestor_mask=ancestor_mask, out=out, workspace=workspace)
+    _typed(torch.bfloat16, q=q, out=out)
+    (page, tok, head, _), (row, max_pages) = _pool(k_pages, v_pages, 4), _table("page_table", page_table)
+    batch, (tq, hq, d), (n_pages, page_size, hkv, kd) = page_table.shape[0], q.shape, k_pages.shape
+    if kd != d:
+        raise ValueError("q and the pages must have one head dimension")
+    _int32s(batch, kv_lens=kv_lens)
+    _groups(batch, groups)
+    if cu_q is None:
+        if batch and tq % batch:
+            raise ValueError("without cu_q every request has as many queries")
+        q_len = tq // batch if batch else 0
+    else:
+        _int32s(batch + 1, cu_q=cu_q)
+        if max_q_len is None:
+            raise ValueError("max_q_len is required with cu_q")
+        q_len = max_q_len
+    kv_len = max_pages * page_size if max_kv_len is None else max_kv_len
+    if ancestor_mask is not None and (ancestor_mask.dtype not in (torch.int64, torch.uint64) or not ancestor_mask.is_contiguous()
+                                      or ancestor_mask.numel() < tq):
+        raise ValueError("ancestor_mask must be a contiguous int64 or uint64 value for every query")
+    if out is None:
+        out = torch.empty_like(q)
+    if out.shape != q.shape or out.stride() != q.stride():
+        raise ValueError("out must share q's shape and strides")
+    lse = torch.empty((tq, hq), dtype=torch.float32, device=q.device) if want_lse else None
+    if workspace is None:
+        workspace = new_workspace(shared_attn_workspace_bytes(batch, tq, hq, hkv, d), q.device)
+    q_tok, q_head = _thd(q)
+    rc = lib().specvlm_shared_attn(_ptr(q), q_tok, q_head, _ptr(k_pages), _ptr(v_pages), page, tok, head, n_pages, page_size,
+                                   _ptr(page_table), row, max_pages, _ptr(kv_lens), _ptr(groups), _ptr(cu_q), batch, tq, q_len, kv_len, hq, hkv, d,
+                                   float(softmax_scale), _ptr(ancestor_mask), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(), _stream())
+    _check("specvlm_shared_attn", rc)
+    return (out, lse) if want_lse else out
+
+
+def cross_attn_workspace_bytes(batch, n_queries, n_q_heads, n_kv_heads, head_dim) -> int:
+    return lib().specvlm_cross_attn_workspace_bytes(batch, n_queries, n_q_heads, n_kv_heads, head_dim)
+
+
+def cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, softmax_scale: float, *, cu_q: Optional[torch.Tensor] = None,
+               cu_kv: Optional[torch.Tensor] = None, key_ranges: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+               want_lse: bool = False, workspace: Optional[torch.Tensor] = None):
+    """Attention of texts, q [queries, H_q, d] bf16, over encoders' states, k and v [states, H_kv, d] bf16 -> out like q (and lse fp32).
+
+    cu_q and cu_kv int32 [batch + 1], prefix offsets of each entry's queries and states, of any lengths; None: all look at all.
+    key_ranges int32 [queries, 2]: the states [from, to) of its entry that a query sees.  out may be q."""
+    got = (_calls or _load_calls()).cross_attn(q, k, v, softmax_scale, cu_q, cu_kv, key_ranges, out, want_lse, workspace)
+    if got is not None:
+        if type(got) is int:
+            _check("specvlm_cross_attn", got)
+        return got
+    _on_device(q=q, k=k, v=v, cu_q=cu_q, cu_kv=cu_kv, key_ranges=key_ranges, out=out, workspace=workspace)
+    _typed(torch.bfloat16, q=q, k=k, v=v, out=out)
+    (tq, hq, d), (tk, hkv, kd) = q.shape, k.shape
+    if kd != d:
+        raise ValueError("q and the states must have one head dimension")
+    if v.shape != k.shape or v.stride() != k.stride():
+        raise ValueError("K and V must share shape and strides")
+    if (cu_q is None) != (cu_kv is None):
+        raise ValueError("cu_q and cu_kv go together")
+    batch = 1
+    if cu_q is not None:
+        batch = cu_q.numel() - 1
+        if batch < 0:
+            raise ValueError("cu_q has an entry more than there are entries")
+        _int32s(batch + 1, cu_q=cu_q, cu_kv=cu_kv)
+    if key_ranges is not None:
+        _typed(torch.int32, key_ranges=key_ranges)
+        if key_ranges.shape != (tq, 2) or not key_ranges.is_contiguous():
+            raise ValueError("key_ranges must be contiguous [queries, 2]")
+    if out is None:
+        out = torch.empty_like(q)
+    if out.shape != q.shape or out.stride() != q.stride():
+        raise ValueError("out must share q's shape and strides")
+    lse = torch.empty((tq, hq), dtype=torch.float32, device=q.device) if want_lse else None
+    if workspace is None:
+        workspace = new_workspace(cross_attn_workspace_bytes(batch, tq, hq, hkv, d), q.device)
+    (q_tok, q_head), (k_tok, k_head) = _thd(q), _thd(k)
+    rc = lib().specvlm_cross_attn(_ptr(q), q_tok, q_head, _ptr(k), _ptr(v), k_tok, k_head, _ptr(cu_q), _ptr(cu_kv), batch, tq, tk, hq, hkv, d,
+                                  float(softmax_scale), _ptr(key_ranges), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(), _stream())
+    _check("specvlm_cross_attn", rc)
     return (out, lse) if want_lse else out
 
 

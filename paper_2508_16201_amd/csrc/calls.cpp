@@ -39,6 +39,12 @@ decltype(&specvlm_rope_append) c_rope_append;
 decltype(&specvlm_pages_assign) c_pages_assign;
 decltype(&specvlm_pages_assign_workspace_bytes) c_assign_bytes;
 decltype(&specvlm_pages_copy) c_pages_copy;
+decltype(&specvlm_pages_shared) c_pages_shared;
+decltype(&specvlm_pages_shared_workspace_bytes) c_pages_shared_bytes;
+decltype(&specvlm_shared_attn) c_shared_attn;
+decltype(&specvlm_shared_attn_workspace_bytes) c_shared_attn_bytes;
+decltype(&specvlm_cross_attn) c_cross_attn;
+decltype(&specvlm_cross_attn_workspace_bytes) c_cross_attn_bytes;
 
 // A call's arguments.  What reads one that is not plain clears `plain` and gets nothing; a function looks at it before it uses what it read.
 struct Args {
@@ -470,6 +476,81 @@ PyObject* pages_copy(Args& a)
     return status ? PyLong_FromLong(status) : Py_NewRef(Py_True);
 }
 
+// page_table, kv_lens, n_pages, page_size, q_len, cu_q, min_tokens, groups, workspace
+PyObject* pages_shared(Args& a)
+{
+    const at::Tensor* const table = a.table(0);
+    if (!a.plain || a.none(1)) return nullptr;
+    const int64_t batch = table->size(0);
+    const int b = a.as_int(batch), width = a.as_int(table->size(1)), pages = a.number(2), ps = a.number(3), q_len = a.number(4), least = a.number(6);
+    const int32_t *const lens = a.vector(1, batch), *const cu = a.vector(5, batch + 1);
+    if (!a.none(7)) a.tensor(7, 2, at::kInt);
+    const Out groups(a, 7, [&] { return make({3, batch}, at::kInt, *table); });
+    if (!a.plain || groups.tensor().size(0) != 3 || groups.tensor().size(1) != batch || !groups.tensor().is_contiguous()) return nullptr;
+    const Workspace ws(a, 8, *table, [&] { return c_pages_shared_bytes(b); });
+    if (!a.plain || (!a.none(8) && THPVariable_Unpack(a.o[8]).get_device() != a.device())) return nullptr;
+    const int status = call(c_pages_shared, (const int32_t*)table->data_ptr(), table->stride(0), width, pages, ps, lens, cu, b, q_len, least,
+                            (int32_t*)groups.at, ws.at, ws.bytes);
+    return status ? PyLong_FromLong(status) : groups.result();
+}
+
+// q, k_pages, v_pages, page_table, kv_lens, softmax_scale, groups, cu_q, max_q_len, max_kv_len, ancestor_mask, out, want_lse, workspace
+PyObject* shared_attn(Args& a)
+{
+    const at::Tensor *const q = a.tensor(0, 3, at::kBFloat16), *const k = a.pool(1, 2, 4), *const table = a.table(3), *const groups = a.tensor(6, 2, at::kInt);
+    if (!a.plain || a.none(2) || a.none(4) || q->stride(2) != 1 || k->size(3) != q->size(2)) return nullptr;
+    const int64_t batch = table->size(0), tq = q->size(0), hq = q->size(1);
+    const int b = a.as_int(batch), n = a.as_int(tq), h = a.as_int(hq), d = a.as_int(q->size(2)), pages = a.as_int(k->size(0)), ps = a.as_int(k->size(1)),
+              hkv = a.as_int(k->size(2)), width = a.as_int(table->size(1));
+    const int32_t *const lens = a.vector(4, batch), *const cu = a.vector(7, batch + 1);
+    if (!a.plain || (cu ? a.none(8) : batch == 0 || tq % batch) || groups->size(0) != 3 || groups->size(1) != batch || !groups->is_contiguous()) return nullptr;
+    const int q_len = cu ? a.number(8) : a.as_int(tq / batch), kv_len = a.none(9) ? a.as_int((int64_t)width * ps) : a.number(9);
+    const float scale = (float)a.real(5);
+    const uint64_t* const mask = (const uint64_t*)a.words(10, tq);
+    const bool want_lse = a.truth(12);
+    if (!a.none(11)) a.tensor(11, 3, at::kBFloat16);
+    const Out out(a, 11, [&] { return at::empty_like(*q); });
+    if (!a.plain || out.tensor().sizes() != q->sizes() || out.tensor().strides() != q->strides()) return nullptr;
+    std::optional<at::Tensor> lse;
+    if (want_lse) lse = make({tq, hq}, at::kFloat, *q);
+    const Workspace ws(a, 13, *q, [&] { return c_shared_attn_bytes(b, n, h, hkv, d); });
+    if (!a.plain || (!a.none(13) && THPVariable_Unpack(a.o[13]).get_device() != a.device())) return nullptr;
+    const int status = call(c_shared_attn, q->data_ptr(), q->stride(0), q->stride(1), k->data_ptr(), THPVariable_Unpack(a.o[2]).data_ptr(), k->stride(0),
+                            k->stride(1), k->stride(2), pages, ps, (const int32_t*)table->data_ptr(), table->stride(0), width, lens,
+                            (const int32_t*)groups->data_ptr(), cu, b, n, q_len, kv_len, h, hkv, d, scale, mask, out.at,
+                            (float*)(lse ? lse->data_ptr() : nullptr), ws.at, ws.bytes);
+    if (status) return PyLong_FromLong(status);
+    return want_lse ? pair(out.result(), THPVariable_Wrap(*lse)) : out.result();
+}
+
+// q, k, v, softmax_scale, cu_q, cu_kv, key_ranges, out, want_lse, workspace
+PyObject* cross_attn(Args& a)
+{
+    const at::Tensor *const q = a.tensor(0, 3, at::kBFloat16), *const k = a.pool(1, 2, 3);
+    if (!a.plain || a.none(2) || a.none(4) != a.none(5) || q->stride(2) != 1 || k->size(2) != q->size(2)) return nullptr;
+    const int64_t tq = q->size(0), hq = q->size(1);
+    const at::Tensor *const cu = a.none(4) ? nullptr : a.tensor(4, 1, at::kInt), *const ranges = a.none(6) ? nullptr : a.tensor(6, 2, at::kInt);
+    if (!a.plain || (cu && cu->numel() == 0)) return nullptr;
+    if (ranges && (ranges->size(0) != tq || ranges->size(1) != 2 || !ranges->is_contiguous())) return nullptr;
+    const int64_t batch = cu ? cu->numel() - 1 : 1;
+    const int b = a.as_int(batch), n = a.as_int(tq), h = a.as_int(hq), d = a.as_int(q->size(2)), states = a.as_int(k->size(0)), hkv = a.as_int(k->size(1));
+    const int32_t *const cu_q = a.vector(4, batch + 1), *const cu_kv = a.vector(5, batch + 1);
+    const float scale = (float)a.real(3);
+    const bool want_lse = a.truth(8);
+    if (!a.none(7)) a.tensor(7, 3, at::kBFloat16);
+    const Out out(a, 7, [&] { return at::empty_like(*q); });
+    if (!a.plain || out.tensor().sizes() != q->sizes() || out.tensor().strides() != q->strides()) return nullptr;
+    std::optional<at::Tensor> lse;
+    if (want_lse) lse = make({tq, hq}, at::kFloat, *q);
+    const Workspace ws(a, 9, *q, [&] { return c_cross_attn_bytes(b, n, h, hkv, d); });
+    if (!a.plain || (!a.none(9) && THPVariable_Unpack(a.o[9]).get_device() != a.device())) return nullptr;
+    const int status = call(c_cross_attn, q->data_ptr(), q->stride(0), q->stride(1), k->data_ptr(), THPVariable_Unpack(a.o[2]).data_ptr(), k->stride(0),
+                            k->stride(1), cu_q, cu_kv, b, n, states, h, hkv, d, scale, (const int32_t*)(ranges ? ranges->data_ptr() : nullptr), out.at,
+                            (float*)(lse ? lse->data_ptr() : nullptr), ws.at, ws.bytes);
+    if (status) return PyLong_FromLong(status);
+    return want_lse ? pair(out.result(), THPVariable_Wrap(*lse)) : out.result();
+}
+
 template <PyObject* (*F)(Args&), Py_ssize_t N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
@@ -496,7 +577,10 @@ struct { const char* name; void** at; } const functions[] = {
     {"specvlm_decode_attn_workspace_bytes", (void**)&c_attn_bytes}, {"specvlm_paged_attn", (void**)&c_paged_attn},
     {"specvlm_paged_attn_workspace_bytes", (void**)&c_paged_bytes}, {"specvlm_rope_append", (void**)&c_rope_append},
     {"specvlm_pages_assign", (void**)&c_pages_assign}, {"specvlm_pages_assign_workspace_bytes", (void**)&c_assign_bytes},
-    {"specvlm_pages_copy", (void**)&c_pages_copy}};
+    {"specvlm_pages_copy", (void**)&c_pages_copy}, {"specvlm_pages_shared", (void**)&c_pages_shared},
+    {"specvlm_pages_shared_workspace_bytes", (void**)&c_pages_shared_bytes}, {"specvlm_shared_attn", (void**)&c_shared_attn},
+    {"specvlm_shared_attn_workspace_bytes", (void**)&c_shared_attn_bytes}, {"specvlm_cross_attn", (void**)&c_cross_attn},
+    {"specvlm_cross_attn_workspace_bytes", (void**)&c_cross_attn_bytes}};
 
 // connect(version, address of every function by its name), once, before any call: the version is the library's, which has to be the one whose
 // header this was compiled with.
@@ -523,6 +607,7 @@ PyMethodDef methods[] = {
     {"connect", (PyCFunction)(void (*)())connect, METH_FASTCALL, nullptr},
     SPECVLM_CALL(accept, 8), SPECVLM_CALL(score, 11), SPECVLM_CALL(select, 9), SPECVLM_CALL(top_p_count, 6), SPECVLM_CALL(gather_kv, 10),
     SPECVLM_CALL(decode_attn, 13), SPECVLM_CALL(paged_attn, 15), SPECVLM_CALL(rope_append, 13), SPECVLM_CALL(pages_assign, 11), SPECVLM_CALL(pages_copy, 13),
+    SPECVLM_CALL(pages_shared, 9), SPECVLM_CALL(shared_attn, 14), SPECVLM_CALL(cross_attn, 10),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,841 @@
+// specvlm_shared_attn and specvlm_cross_attn: softmax attention in which many query rows meet the same keys.
+//
+// specvlm_shared_attn is attention of every request's block of new tokens over its paged cache, where neighbouring requests
+// have the same first pages (several questions about one video): those keys are read once and meet the rows of all of the
+// group's requests, then each request's rows meet its own keys.  specvlm_cross_attn is attention of texts of any length over an
+// encoder's states, which no causal mask hides.
+//
+// Mathematics.  One pass over the keys with the running maximum m and sum l of each query row (online softmax); a row's keys are
+// cut into pieces (of the shared keys, of its own), and pieces are joined by  o = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
+// Statistics, sums and partial outputs are fp32, the output is rounded once.
+//
+// Work decomposition.  Rows of a kv head (query, head of the group) are taken 256 at a time ("a set"), keys in tiles of 128.  The
+// tiles of all sets, heads and requests are numbered one after the other, and each workgroup takes a run of equal length, which it
+// finds by a prefix sum over the requests: lengths and groups are on the device, and a captured launch serves them as they change.
+// A piece that is all a row has is written out directly; the others leave partial results that the second launch joins.
+//
+// A workgroup has eight waves of 32 rows (v_mfma_f32_32x32x16_bf16 with the keys as rows of the product and the queries as its
+// columns: a lane then holds 16 logits of one row, which are, packed, the second product's operand).  Where a set has fewer rows,
+// two or four waves share them and take every other 32 keys.  Tiles go to LDS by direct loads, two in turn.
+#include <climits>
+
+#include "attn_tile.h"
+
+namespace specvlm {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+
+constexpr int kRowsTile = 128;           // keys of a tile
+constexpr int kRowsWaves = 8;
+constexpr int kRowsThreads = kRowsWaves * kWave;
+constexpr int kSetRows = kRowsWaves * 32;
+constexpr int kChunks = kRowsTile / 32;
+constexpr float kRowsRedo = 0x1p20f;     // a lane's sum of 32 keys at or above this (or NaN) is done again with the maximum tracked
+
+// D = A(32x16 bf16) * B(16x32 bf16) + C.  Per lane (r = lane % 32, h = lane / 32):
+//   A holds row r, contraction indices 8h..8h+7;  B holds column r, the same;  C/D hold column r, element i row 8(i/4) + 4h + i%4
+__device__ __forceinline__ floatx16 mfma32(bf16x8 a, bf16x8 b, floatx16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+struct RowsParams {
+    const __bf16* q;
+    const __bf16* k;
+    const __bf16* v;
+    __bf16* out;
+    float* lse;
+    int64_t q_tok, q_head, page, tok, head;      // strides in elements
+    const int32_t* table;                        // (paged)
+    int64_t table_row;
+    const int32_t* kv_lens;
+    const int32_t* groups;
+    const uint64_t* block_mask;
+    const int32_t* cu_q;
+    const int32_t* cu_kv;                        // (flat)
+    const int32_t* ranges;
+    int n_pages, page_size, most_shared;         // most_shared: tokens of a whole table row
+    int batch, q_len, kv_len, n_queries;
+    int n_q_heads, n_kv_heads, group;
+    uint32_t inv_page, inv_heads, inv_group;
+    float scale_log2;
+    int workgroups, padded;                      // that take runs; the launch
+    float* part_o;                               // [rows_parts][D] unnormalised partial outputs (part_row)
+    float* part_ml;                              // [rows_parts][2] running maximum in log2 units, sum
+    int32_t* starts;                             // [2 * entries] first tile and first row of every entry;  behind them the run, and whether the groups count
+    int most_rows;                               // that the entries may have, for partial results
+};
+
+// What is numbered.  Entry b is the keys that request b's group shares, if it is the group's first request; entry batch + b request b's own keys.
+// (Flat: entry b alone.)  An item is an entry's set of rows of a kv head.
+struct Entry { int q0, n_q, key0, key1; };
+
+template <bool PAGED> __device__ __forceinline__ Entry query_range(const RowsParams& p, int b)
+{
+    if (!p.cu_q) return {b * p.q_len, p.q_len, 0, 0};
+    const int q0 = p.cu_q[b];
+    return {q0, p.cu_q[b + 1] - q0, 0, 0};
+}
+
+// The keys that the group of first request b shares, with the queries of all of its requests; none where what is said of it does not fit together (its
+// requests are then taken alone).
+__device__ __forceinline__ Entry shared_entry(const RowsParams& p, int b)
+{
+    const int n = p.groups[2 * p.batch + b], members = p.groups[p.batch + b], kvl = p.kv_lens[b];
+    Entry e = query_range<true>(p, b);
+    if (p.groups[b] != b || members < 2 || members > p.batch - b) return {0, 0, 0, 0};
+    if (n <= 0 || n % 16 || n > p.most_shared || e.n_q <= 0 || kvl > p.kv_len || n > kvl - e.n_q) return {0, 0, 0, 0};
+    e.n_q = (p.cu_q ? p.cu_q[b + members] : (b + members) * p.q_len) - e.q0;
+    if (e.n_q <= 0 || e.q0 < 0 || e.q0 > p.n_queries - e.n_q) return {0, 0, 0, 0};
+    e.key1 = n;
+    return e;
+}
+
+template <bool PAGED> __device__ __forceinline__ Entry entry_of(const RowsParams& p, int e, bool grouped)
+{
+    if constexpr (!PAGED) {
+        if (e >= p.batch) return {0, 0, 0, 0};
+        Entry r = query_range<false>(p, e);
+        const int k0 = p.cu_kv ? p.cu_kv[e] : 0;
+        const int n = p.cu_kv ? p.cu_kv[e + 1] - k0 : p.kv_len;
+        // (offsets that leave the tensors: nothing is read or written by them)
+        if (r.n_q <= 0 || r.q0 < 0 || r.q0 > p.n_queries - r.n_q || n < 0 || k0 < 0 || k0 > p.kv_len - n) return {0, 0, 0, 0};
+        r.key1 = n;
+        return r;
+    } else {
+        if (e >= 2 * p.batch) return {0, 0, 0, 0};
+        const int b = e < p.batch ? e : e - p.batch;
+        if (e < p.batch) return grouped ? shared_entry(p, b) : Entry{0, 0, 0, 0};
+        Entry r = query_range<true>(p, b);
+        const int kvl = p.kv_lens[b];
+        if (r.n_q <= 0 || r.n_q > p.q_len || r.q0 < 0 || r.q0 > p.n_queries - r.n_q || kvl < r.n_q || kvl > p.kv_len) return {0, 0, 0, 0};
+        r.key1 = kvl;
+        const int first = grouped ? p.groups[b] : -1;
+        if (first >= 0 && first <= b && b - first < p.groups[p.batch + first]) {
+            const Entry all = shared_entry(p, first);
+            if (all.key1 <= kvl - r.n_q) r.key0 = all.key1;
+        }
+        return r;
+    }
+}
+
+// Sets of rows: blocks of 32, at most eight to a set, as many to each.
+struct Sets { int n, blocks; };              // blocks: of a set
+__device__ __forceinline__ Sets sets_of(int rows)
+{
+    const int blocks = (rows + 31) >> 5, n = (blocks + kRowsWaves - 1) / kRowsWaves;
+    return {n, n > 1 ? (blocks + n - 1) / n : blocks};
+}
+__device__ __forceinline__ int tiles_of(const Entry& e) { return max(1, (e.key1 - e.key0 + kRowsTile - 1) / kRowsTile); }
+
+__device__ __forceinline__ int padded_rows(const RowsParams& p, const Entry& e) { return (e.n_q * p.group + 31) & ~31; }      // of a kv head
+
+struct Numbers { int tiles, rows; };         // of an entry, or in front of one
+__device__ __forceinline__ Numbers numbers_of(const RowsParams& p, const Entry& e)
+{
+    if (e.n_q <= 0) return {0, 0};
+    return {sets_of(e.n_q * p.group).n * p.n_kv_heads * tiles_of(e), padded_rows(p, e) * p.n_kv_heads};
+}
+
+// The row of the partial results that workgroup j's piece of an item has: the rows of all items one after the other, and 256 on for every workgroup, so
+// that two pieces of an item do not meet, nor two items of a workgroup.
+__device__ __forceinline__ int64_t part_row(int j, int row_of_items) { return (int64_t)j * kSetRows + row_of_items; }
+
+// Tiles of a run.
+__device__ __forceinline__ int rows_run(const RowsParams& p, int total) { return max(1, (total + p.workgroups - 1) / p.workgroups); }
+
+// LDS behind the tiles:  what a workgroup knows of 512 entries.
+struct RowsPlan {
+    Numbers front[kRowsThreads];
+    Numbers wave[kRowsWaves];
+    int found;
+    unsigned char ok[2][8];
+};
+
+// Inclusive prefix sums over the workgroup's threads, and the total; `s` is free again behind the next barrier.
+__device__ __forceinline__ Numbers block_prefix(RowsPlan& s, Numbers x, int wave, int lane, Numbers* total)
+{
+    Numbers up = {wave_prefix(x.tiles), wave_prefix(x.rows)};
+    if (lane == kWave - 1) s.wave[wave] = up;
+    __syncthreads();
+    Numbers all = {0, 0};
+#pragma unroll
+    for (int w = 0; w < kRowsWaves; ++w) {
+        const Numbers t = s.wave[w];
+        if (w < wave) { up.tiles += t.tiles; up.rows += t.rows; }
+        all.tiles += t.tiles;
+        all.rows += t.rows;
+    }
+    *total = {__builtin_amdgcn_readfirstlane(all.tiles), __builtin_amdgcn_readfirstlane(all.rows)};
+    __syncthreads();
+    return up;
+}
+
+// A direct load of 16 bytes a lane to LDS, lane after lane from `lds` on (wave-uniform).  Issued as assembly: of the builtin the compiler knows that it writes
+// LDS, and waits for all of them before every read of LDS that might be of the other stage.  (M0 takes one state to be seen by the load.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load_to_lds(const char* base, uint32_t lane_offset, uint32_t lds)
+{
+    __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane_offset), "s"(base) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// XOR on the number of a value row's 16-byte piece.  The transposing read of 16 keys and 32 columns touches, per 32 lanes, 4 keys x 64 bytes (pieces 4j..4j+3):
+// with this they fall on 64 distinct banks.
+template <int D> __device__ __forceinline__ constexpr int rows_v_swizzle(int key) { return D == 128 ? (key & 3) << 2 : (key >> 1 & 1) << 2; }
+
+template <class T> __device__ __forceinline__ SPECVLM_AS3 T* in_lds(uint32_t at) { return (SPECVLM_AS3 T*)(uintptr_t)at; }
+
+__device__ __forceinline__ uint32_t first_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+
+// See take_odd_values of the paged attention:  a value that is no finite number is left out of the products, and the rows that see its key get it by how many such values they see.
+// sees8: bit e is set if the lane's row sees the key of contraction index 8h + e.
+__device__ __forceinline__ void take_odd_rows(bf16x8& vf, uint32_t sees8, floatx16& o)
+{
+    floatx16 none;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) none[i] = 0.f;
+    const floatx16 odd = mfma32(vf, __builtin_bit_cast(bf16x8, u32x4{}), none);
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += odd[i];
+    if (__builtin_expect(__any(!(sum == 0.f)), 0)) {
+        u32x4 seen, w = __builtin_bit_cast(u32x4, vf), up, down, nan;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t two = sees8 >> (2 * e);
+            seen[e] = (two & 1u) * 0x3f80u | (two & 2u) * (0x3f800000u / 2);
+            const uint32_t size = w[e] & 0x7fff7fffu, odd2 = (size + 0x00800080u) >> 15 & 0x00010001u;
+            nan[e] = (size + 0x007f007fu) >> 15 & 0x00010001u;
+            down[e] = (odd2 ^ nan[e]) & w[e] >> 15;
+            up[e] = odd2 ^ nan[e] ^ down[e];
+            w[e] &= ~(odd2 * 0xffffu);
+        }
+        vf = __builtin_bit_cast(bf16x8, w);
+        const auto count = [&](u32x4 x) { return mfma32(__builtin_bit_cast(bf16x8, x * 0x3f80u), __builtin_bit_cast(bf16x8, seen), none); };
+        const floatx16 n_up = count(up), n_down = count(down), n_nan = count(nan);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if (n_up[i] > 0.f) o[i] += INFINITY;
+            if (n_down[i] > 0.f) o[i] += -INFINITY;
+            if (n_nan[i] > 0.f) o[i] = NAN;
+        }
+    }
+}
+
+__device__ __forceinline__ float half_max(float x)
+{
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float half_sum(float x)
+{
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+template <int D, bool PAGED>
+__global__ __launch_bounds__(kRowsThreads, 2)
+void rows_kernel(const RowsParams p)
+{
+    constexpr int KK = D / 16, JB = D / 32, CH = D / 8, ROW_BYTES = D * 2;
+    constexpr int TILE_BYTES = kRowsTile * ROW_BYTES;        // of K or V
+    constexpr int KEYS_PER_LOAD = kWave / CH, LOADS = 16 / KEYS_PER_LOAD;
+    constexpr int O_STRIDE = D + 4;
+    static_assert((kRowsWaves - 2) * 32 * O_STRIDE * 4 <= 4 * TILE_BYTES, "the exchange of waves that share rows");
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 31, h = lane >> 5;
+    extern __shared__ __align__(1024) unsigned char smem[];  // stage s: K tile at s * 2 * TILE_BYTES, V tile behind it
+    RowsPlan& plan = *reinterpret_cast<RowsPlan*>(smem + 4 * TILE_BYTES);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(SPECVLM_AS3 unsigned char*)smem;
+
+    const int j = xcd_logical_id(blockIdx.x, p.padded);
+    if (j >= p.workgroups) return;
+
+    // ---- the numbering ----
+    const int entries = PAGED ? 2 * p.batch : p.batch;
+    Numbers total, here;
+    bool grouped = PAGED;
+    Numbers mine, upto;
+    for (;;) {
+        mine = numbers_of(p, entry_of<PAGED>(p, threadIdx.x, grouped));
+        upto = block_prefix(plan, mine, wave, lane, &here);
+        total = here;
+        for (int c = kRowsThreads; c < entries; c += kRowsThreads) {
+            Numbers more;
+            block_prefix(plan, numbers_of(p, entry_of<PAGED>(p, c + threadIdx.x, grouped)), wave, lane, &more);
+            total.tiles += more.tiles;
+            total.rows += more.rows;
+        }
+        // (groups that overlap would have rows more than once: there is no room for them)
+        if (total.rows <= p.most_rows || !grouped) break;
+        grouped = false;
+    }
+    if (total.rows > p.most_rows) total.tiles = 0;           // (offsets that overlap)
+    const int run = rows_run(p, total.tiles);
+    int x = j * run;
+    const int x_end = min(total.tiles, x + run);
+    Numbers base = {0, 0};                                   // in front of the 512 entries at hand
+    int c0 = 0;
+    const auto publish = [&] {
+        const Numbers front = {base.tiles + upto.tiles - mine.tiles, base.rows + upto.rows - mine.rows};
+        plan.front[threadIdx.x] = front;
+        if (j == 0) {                                        // (the join reads where every entry begins)
+            const int e = c0 + threadIdx.x;
+            if (e < entries) { p.starts[2 * e] = front.tiles; p.starts[2 * e + 1] = front.rows; }
+            if (e == 0) { p.starts[2 * entries] = total.tiles ? run : 0; p.starts[2 * entries + 1] = grouped; }
+        }
+    };
+    const auto next_entries = [&] {
+        base.tiles += here.tiles;
+        base.rows += here.rows;
+        c0 += kRowsThreads;
+        mine = numbers_of(p, entry_of<PAGED>(p, c0 + threadIdx.x, grouped));
+        upto = block_prefix(plan, mine, wave, lane, &here);
+        publish();
+    };
+    publish();
+    if (j == 0) {
+        // (workgroup 0 tells of all, then begins again)
+        if (entries > kRowsThreads) {
+            while (c0 + kRowsThreads < entries) next_entries();
+            base = {0, 0};
+            c0 = 0;
+            __syncthreads();
+            mine = numbers_of(p, entry_of<PAGED>(p, threadIdx.x, grouped));
+            upto = block_prefix(plan, mine, wave, lane, &here);
+            publish();
+        }
+    }
+
+    const float sc = fmaxf(p.scale_log2, 1e-30f);            // (a zero scale as a vanishing one: -inf stays -inf)
+
+    while (x < x_end) {
+        while (x >= base.tiles + here.tiles) next_entries();
+        if (base.tiles + upto.tiles > x && base.tiles + upto.tiles - mine.tiles <= x) plan.found = threadIdx.x;
+        __syncthreads();
+        const int at = __builtin_amdgcn_readfirstlane(plan.found), e = c0 + at;
+        const Numbers front = {__builtin_amdgcn_readfirstlane(plan.front[at].tiles), __builtin_amdgcn_readfirstlane(plan.front[at].rows)};
+        const bool own = !PAGED || e >= p.batch;
+        const int b = PAGED && own ? e - p.batch : e;
+        Entry en = entry_of<PAGED>(p, e, grouped);
+        en.q0 = __builtin_amdgcn_readfirstlane(en.q0); en.n_q = __builtin_amdgcn_readfirstlane(en.n_q);
+        en.key0 = __builtin_amdgcn_readfirstlane(en.key0); en.key1 = __builtin_amdgcn_readfirstlane(en.key1);
+        const int tiles = tiles_of(en), rows = en.n_q * p.group;
+        const Sets sets = sets_of(rows);
+        const int item = (x - front.tiles) / tiles, t_begin = x - front.tiles - item * tiles;
+        const int t_end = min(tiles, t_begin + x_end - x);
+        const int g = item / sets.n, set = item - g * sets.n;
+        const int row0 = set * sets.blocks * 32, n_rows = min(rows - row0, sets.blocks * 32), n_blocks = (n_rows + 31) >> 5;
+        const int log_blocks = n_blocks > 4 ? 3 : n_blocks > 2 ? 2 : n_blocks - 1;       // waves of a kind
+        const int blk = wave & ((1 << log_blocks) - 1), ks = wave >> log_blocks, n_ks = min(kChunks, kRowsWaves >> log_blocks);
+        const bool works = blk < n_blocks && ks < n_ks;
+        const bool direct = own && en.key0 == 0 && t_begin == 0 && t_end == tiles;
+        const bool two_parts = n_blocks <= 4;
+        x += t_end - t_begin;
+
+        // this wave's rows
+        const int my_row = blk * 32 + r;
+        const QuotRem q_at = divide(row0 + (my_row < n_rows ? my_row : 0), p.group, p.inv_group);  // (padding rows take the first: never stored)
+        const int64_t q_tok = en.q0 + q_at.q;
+        const int q_hd = g * p.group + q_at.r;
+        bf16x8 qf[KK];
+        const __bf16* const qp = p.q + q_tok * p.q_tok + (int64_t)q_hd * p.q_head + h * 8;
+#pragma unroll
+        for (int s = 0; s < KK; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qp + s * 16);
+        // the keys that it sees: [lo, hi), of the block those of a tree node's mask
+        int lo = en.key0, hi = en.key1;
+        const int before = en.key1 - en.n_q;                 // (own keys of a block)
+        uint64_t tree = 0;
+        bool is_tree = false;
+        if constexpr (PAGED) {
+            if (own) {
+                is_tree = p.block_mask != nullptr;
+                if (is_tree) tree = p.block_mask[q_tok];
+                else hi = before + q_at.q + 1;
+            }
+        } else if (p.ranges) {
+            lo = max(p.ranges[2 * q_tok], 0);
+            hi = min(p.ranges[2 * q_tok + 1], en.key1);
+        }
+        // of all of the wave's rows: keys that all see, and that some see
+        int all_lo = lo, all_hi = is_tree ? before : hi, any_lo = lo < hi ? lo : INT_MAX, any_hi = lo < hi ? hi : 0;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            all_lo = max(all_lo, __shfl_xor(all_lo, d)); all_hi = min(all_hi, __shfl_xor(all_hi, d));
+            any_lo = min(any_lo, __shfl_xor(any_lo, d)); any_hi = max(any_hi, __shfl_xor(any_hi, d));
+        }
+        all_lo = __builtin_amdgcn_readfirstlane(all_lo); all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+        any_lo = __builtin_amdgcn_readfirstlane(any_lo); any_hi = __builtin_amdgcn_readfirstlane(any_hi);
+
+        // ---- loads: wave w brings keys 16w..16w+15 of a tile ----
+        const int64_t kv0 = (int64_t)g * p.head + (PAGED ? 0 : (int64_t)(p.cu_kv ? __builtin_amdgcn_readfirstlane(p.cu_kv[e]) : 0) * p.tok);
+        const char* const k_at = reinterpret_cast<const char*>(p.k + kv0);
+        const char* const v_at = reinterpret_cast<const char*>(p.v + kv0);
+        const int table_b = PAGED ? b : 0;
+        int ids = 0, places = 0;                             // of the next 64 tiles, one to a lane
+        const auto look_up = [&](int tile) {
+            const int key = min(en.key0 + (tile + lane) * kRowsTile + wave * 16, (en.key1 - 1) & ~15);
+            const QuotRem pg = divide(key, p.page_size, p.inv_page);
+            ids = p.table[(int64_t)table_b * p.table_row + pg.q];
+            places = pg.r;
+        };
+        const auto issue = [&](int tile, int stage) {
+            const uint32_t to = lds0 + stage * 2 * TILE_BYTES + wave * 16 * ROW_BYTES;
+            int64_t first;
+            int last = 15;                                   // the last of the 16 rows that may be read
+            if constexpr (PAGED) {
+                const int l = (tile - t_begin) & 63;
+                if (l == 0 && tile != t_begin) look_up(tile);
+                const int id = __builtin_amdgcn_readlane(ids, l), row = __builtin_amdgcn_readlane(places, l);
+                // (a page that is not one of the pool's is not read: the pool's first is, and its keys are masked)
+                const bool there = (uint32_t)id < (uint32_t)p.n_pages;
+                if (lane == 0) plan.ok[stage][wave] = there;
+                first = (there ? id : 0) * p.page + row * p.tok;
+            } else {
+                const int key = min(tile * kRowsTile + wave * 16, en.key1 - 1);
+                first = (int64_t)key * p.tok;
+                last = en.key1 - 1 - key;
+            }
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int kl = i * KEYS_PER_LOAD + lane / CH, piece = lane % CH;
+                const uint32_t row = (uint32_t)(PAGED ? kl : min(kl, last)) * (uint32_t)(p.tok * 2);
+                load_to_lds(k_at + 2 * first, row + (piece ^ (D == 128 ? kl & 15 : kl >> 1 & 7)) * 16, to + i * 1024);
+                load_to_lds(v_at + 2 * first, row + (piece ^ rows_v_swizzle<D>(kl)) * 16, to + TILE_BYTES + i * 1024);
+            }
+        };
+
+        float m_run, l_run;
+        floatx16 o[JB];
+        // where this lane reads in a stage
+        const uint32_t k_base = lds0 + r * ROW_BYTES + (h ^ (D == 128 ? r & 15 : r >> 1 & 7)) * 16;
+        const int v_row = 4 * h + ((lane & 15) >> 2);
+        const uint32_t v_base = lds0 + TILE_BYTES + v_row * ROW_BYTES + ((((lane >> 4 & 1) * 2 + ((lane & 3) >> 1)) ^ rows_v_swizzle<D>(v_row)) * 16) + (lane & 1) * 8;
+
+        for (bool careful = false;;) {
+            m_run = -INFINITY;
+            l_run = 0.f;
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[jb][i] = 0.f;
+            bool fresh = true;                               // some row has seen nothing yet
+            if (en.key1 > en.key0) {
+                if constexpr (PAGED) look_up(t_begin);
+                issue(t_begin, 0);
+                for (int t = t_begin; t < t_end; ++t) {
+                    const int stage = (t - t_begin) & 1;
+                    wait_vmcnt<0>();
+                    __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    stage_barrier();                         // the tile is there for everyone, and everyone has left the other stage
+                    if (t + 1 < t_end) issue(t + 1, stage ^ 1);
+                    if (!works) continue;
+                    for (int ch = ks; ch < kChunks; ch += n_ks) {
+                        const int k0 = en.key0 + t * kRowsTile + ch * 32;
+                        if (k0 >= any_hi || k0 + 31 < any_lo) continue;
+                        uint32_t pages = ~0u;                // keys whose page is there
+                        if constexpr (PAGED) {
+                            const int two = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint16_t*>(&plan.ok[stage][2 * ch]));
+                            pages = (two & 1 ? 0xffffu : 0u) | (two & 0x100 ? 0xffff0000u : 0u);
+                        }
+                        const uint32_t at_chunk = stage * 2 * TILE_BYTES + ch * 32 * ROW_BYTES;
+                        // ---- S^T = K Q^T for 32 keys ----
+                        floatx16 s;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+                        for (int kk = 0; kk < KK; ++kk) {
+                            const u32x4 kf = *in_lds<const u32x4>(k_base + at_chunk ^ kk * 32);
+                            s = mfma32(__builtin_bit_cast(bf16x8, kf), qf[kk], s);
+                        }
+                        const bool need_mask = pages != ~0u || k0 < all_lo || k0 + 32 > all_hi;
+                        uint32_t sees = ~0u;
+                        if (need_mask) {
+                            sees = first_bits(hi - k0) & ~first_bits(lo - k0) & pages;
+                            if (is_tree) {
+                                const int in = k0 - before;
+                                const uint64_t block = in >= 0 ? (in < 64 ? tree >> in : 0) : (in > -32 ? tree << -in : 0);
+                                sees &= (uint32_t)block | first_bits(-in);
+                            }
+                            sees >>= 4 * h;                  // bit 8(i/4) + i%4: the lane's i-th key
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) s[i] = sees >> (8 * (i / 4) + i % 4) & 1u ? s[i] : -INFINITY;
+                        }
+                        // Away from the masks the exponentials are taken against the reference that the earlier keys left, and the maximum is
+                        // tracked only where a lane's sum does not stay moderate.
+                        bool settled = false;
+                        float pv[16];
+                        if (!need_mask && !fresh) {
+                            float psum = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) { pv[i] = fast_exp2(fmaf(s[i], sc, -m_run)); psum += pv[i]; }
+                            if (!__any(!(psum < kRowsRedo))) {
+                                l_run += psum;
+                                settled = true;
+                            }
+                        }
+                        if (!settled) {
+                            float mx = s[0];
+#pragma unroll
+                            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+                            const float m_new = fmaxf(m_run, half_max(mx) * sc);
+                            const float m_ref = m_new == -INFINITY ? 0.f : m_new;
+                            const float alpha = fast_exp2(m_run - m_ref);
+                            const bool rescale = m_new != m_run;
+                            m_run = m_new;
+                            float psum = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) { pv[i] = fast_exp2(fmaf(s[i], sc, -m_ref)); psum += pv[i]; }
+                            l_run = l_run * alpha + psum;
+                            if (__any(rescale)) {
+#pragma unroll
+                                for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i)         // (an infinity stays one, also where 32 bits take its weight for 0)
+                                        o[jb][i] = careful && fabsf(o[jb][i]) == INFINITY ? o[jb][i] : alpha * o[jb][i];
+                            }
+                        }
+                        if (need_mask || fresh) fresh = __any(!(m_run > -INFINITY));
+                        // ---- O^T += V^T P^T ----
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            floatx8 pu;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) pu[i] = pv[8 * u + i];
+                            const bf16x8 pf = __builtin_convertvector(pu, bf16x8);
+                            bf16x8 vf[JB];
+#pragma unroll
+                            for (int jb = 0; jb < JB; ++jb) {
+                                typedef short s16x4 __attribute__((ext_vector_type(4)));
+                                SPECVLM_AS3 s16x4* const src = in_lds<s16x4>((v_base + at_chunk ^ jb * 64) + u * 16 * ROW_BYTES);
+                                const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(src);
+                                const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16(src + 8 * ROW_BYTES / 8);
+                                vf[jb] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7));
+                            }
+                            if (need_mask || careful) {
+                                const uint32_t s16 = sees >> 16 * u;
+#pragma unroll
+                                for (int jb = 0; jb < JB; ++jb) take_odd_rows(vf[jb], (s16 & 0xfu) | (s16 >> 4 & 0xf0u), o[jb]);
+                            }
+#pragma unroll
+                            for (int jb = 0; jb < JB; ++jb) o[jb] = mfma32(vf[jb], pf, o[jb]);
+                            if (two_parts) {
+                                const u32x4 two = __builtin_bit_cast(u32x4, pf);
+                                floatx8 rest;
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    rest[2 * i] = pu[2 * i] - __uint_as_float(two[i] << 16);
+                                    rest[2 * i + 1] = pu[2 * i + 1] - __uint_as_float(two[i] & 0xffff0000u);
+                                }
+                                const bf16x8 pr = __builtin_convertvector(rest, bf16x8);
+#pragma unroll
+                                for (int jb = 0; jb < JB; ++jb) o[jb] = mfma32(vf[jb], pr, o[jb]);
+                            }
+                        }
+                    }
+                }
+            }
+            // A sum that is no finite number, as a rule of an infinite value that a row sees:  all keys once more, with an eye on such values.
+            float odd = 0.f;
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) odd += 0.f * o[jb][i];
+            if (!__syncthreads_or(works && !(odd == 0.f)) || careful) break;
+            careful = true;
+        }
+
+        // ---- waves that share rows: the sums of the others to the first ----
+        l_run = half_sum(l_run);
+        float* const s_o = reinterpret_cast<float*>(smem);
+        float* const s_ml = reinterpret_cast<float*>(plan.front);         // (the numbering is made again for the next piece)
+        if (n_ks > 1) {
+            if (works && ks > 0) {
+                const int slot = (ks - 1) * n_blocks + blk;
+                if (h == 0) { s_ml[(slot * 32 + r) * 2] = m_run; s_ml[(slot * 32 + r) * 2 + 1] = l_run; }
+#pragma unroll
+                for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                    for (int i4 = 0; i4 < 4; ++i4)
+                        *reinterpret_cast<floatx4*>(s_o + (slot * 32 + r) * O_STRIDE + jb * 32 + i4 * 8 + h * 4) =
+                            floatx4{o[jb][4 * i4], o[jb][4 * i4 + 1], o[jb][4 * i4 + 2], o[jb][4 * i4 + 3]};
+            }
+            __syncthreads();
+            if (works && ks == 0) {
+                for (int k = 1; k < n_ks; ++k) {
+                    const int slot = (k - 1) * n_blocks + blk;
+                    const float m2 = s_ml[(slot * 32 + r) * 2], l2 = s_ml[(slot * 32 + r) * 2 + 1];
+                    const float m_new = fmaxf(m_run, m2), m_ref = m_new == -INFINITY ? 0.f : m_new;
+                    const float w1 = fast_exp2(m_run - m_ref), w2 = fast_exp2(m2 - m_ref);
+                    m_run = m_new;
+                    l_run = l_run * w1 + l2 * w2;
+#pragma unroll
+                    for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                        for (int i4 = 0; i4 < 4; ++i4) {
+                            const floatx4 y = *reinterpret_cast<const floatx4*>(s_o + (slot * 32 + r) * O_STRIDE + jb * 32 + i4 * 8 + h * 4);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float a = o[jb][4 * i4 + i];
+                                o[jb][4 * i4 + i] = (fabsf(a) == INFINITY ? a : a * w1) + (fabsf(y[i]) == INFINITY ? y[i] : y[i] * w2);
+                            }
+                        }
+                }
+            }
+        }
+        if (works && ks == 0 && my_row < n_rows) {
+            if (direct) {
+                const float inv = l_run > 0.f ? 1.f / l_run : l_run == 0.f ? 0.f : NAN;
+                __bf16* const op = p.out + q_tok * p.q_tok + (int64_t)q_hd * p.q_head + h * 4;
+#pragma unroll
+                for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                    for (int i4 = 0; i4 < 4; ++i4) {
+                        const floatx4 y = floatx4{o[jb][4 * i4], o[jb][4 * i4 + 1], o[jb][4 * i4 + 2], o[jb][4 * i4 + 3]} * inv;
+                        *reinterpret_cast<bf16x4*>(op + jb * 32 + i4 * 8) = __builtin_convertvector(y, bf16x4);
+                    }
+                if (p.lse && h == 0) p.lse[q_tok * p.n_q_heads + q_hd] = l_run == 0.f ? -INFINITY : (m_run + fast_log2(l_run)) * kLn2;
+            } else {
+                const int64_t row = part_row(j, front.rows + g * padded_rows(p, en) + row0 + my_row);
+                if (h == 0) { p.part_ml[2 * row] = m_run; p.part_ml[2 * row + 1] = l_run; }
+#pragma unroll
+                for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                    for (int i4 = 0; i4 < 4; ++i4)
+                        *reinterpret_cast<floatx4*>(p.part_o + row * D + jb * 32 + i4 * 8 + h * 4) =
+                            floatx4{o[jb][4 * i4], o[jb][4 * i4 + 1], o[jb][4 * i4 + 2], o[jb][4 * i4 + 3]};
+            }
+        }
+        if (x < x_end) {
+            __syncthreads();                                 // the ring, and what the plan holds, are free again
+            publish();
+            __syncthreads();
+        }
+    }
+}
+
+// Joins the pieces of the rows that were cut (one that was not is in its place already), D / 4 threads to a row.
+template <int D, bool PAGED>
+__global__ __launch_bounds__(256)
+void rows_join_kernel(const RowsParams p)
+{
+    constexpr int TPR = D / 4, RPW = kWave / TPR;            // threads of a row, rows of a wave: heads of one query
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int units = (p.n_q_heads + RPW - 1) / RPW;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
+    const int tok = (int)(unit / units);
+    if (tok >= p.n_queries) return;
+    const int hd = (int)(unit - (int64_t)tok * units) * RPW + lane / TPR, c = lane % TPR;
+    // the request
+    int b = 0;
+    if (!p.cu_q) {
+        b = PAGED ? tok / p.q_len : 0;
+    } else {
+        uint64_t behind = 0;
+        for (; b < p.batch; b += kWave) {
+            behind = __ballot(b + lane < p.batch && p.cu_q[min(b + lane, p.batch - 1) + 1] > tok);
+            if (behind) break;
+        }
+        if (!behind) return;                                 // (a row behind the last request)
+        b += __builtin_ctzll(behind);
+    }
+    const int entries = PAGED ? 2 * p.batch : p.batch, e = PAGED ? p.batch + b : b;
+    const int run = p.starts[2 * entries];
+    const Entry own = entry_of<PAGED>(p, e, p.starts[2 * entries + 1]);
+    if (run == 0 || own.n_q <= 0 || tok < own.q0 || hd >= p.n_q_heads) return;
+    const QuotRem head = divide(hd, p.group, p.inv_group);
+    struct Pieces { int first, n, row; };                    // workgroups that have one, the row of their results
+    const auto pieces_of = [&](int e, const Entry& en) {
+        const int row = (tok - en.q0) * p.group + head.r, tiles = tiles_of(en);
+        const Sets sets = sets_of(en.n_q * p.group);
+        const int x = p.starts[2 * e] + (head.q * sets.n + row / (sets.blocks * 32)) * tiles;
+        const int first = x / run;
+        return Pieces{first, (x + tiles - 1) / run - first + 1, p.starts[2 * e + 1] + head.q * padded_rows(p, en) + row};
+    };
+    const Pieces mine = pieces_of(e, own);
+    Pieces theirs = {0, 0, 0};
+    if (PAGED && own.key0 > 0) {
+        const int first = p.groups[b];
+        theirs = pieces_of(first, shared_entry(p, first));
+    } else if (mine.n == 1) {
+        return;
+    }
+    const int n = theirs.n + mine.n;
+    const auto row_of = [&](int i) { return i < theirs.n ? part_row(theirs.first + i, theirs.row) : part_row(mine.first + i - theirs.n, mine.row); };
+    float m = -INFINITY, l = 0.f;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < n; i0 += TPR) {
+        // a piece to a thread: its maximum and sum;  then the outputs, weighted by their thread's word
+        float pm = -INFINITY, pl = 0.f;
+        if (i0 + c < n) {
+            const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * row_of(i0 + c));
+            pm = ml.x;
+            pl = ml.y;
+        }
+        float top = pm;
+#pragma unroll
+        for (int d = 1; d < TPR; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+        const float m_new = fmaxf(m, top), m_ref = m_new == -INFINITY ? 0.f : m_new;
+        const float w = fast_exp2(pm - m_ref), keep = fast_exp2(m - m_ref);
+        float sum = pl * w;
+#pragma unroll
+        for (int d = 1; d < TPR; d *= 2) sum += __shfl_xor(sum, d);
+        l = l * keep + sum;
+        m = m_new;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = fabsf(o[i]) == INFINITY ? o[i] : o[i] * keep;
+        const int most = min(TPR, n - i0);
+        for (int i1 = 0; i1 < most; i1 += 4) {               // (behind the last piece: the last again, left out)
+            floatx4 y[4];
+            float wi[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = min(i1 + u, most - 1);
+                y[u] = *reinterpret_cast<const floatx4*>(p.part_o + row_of(i0 + i) * D + c * 4);
+                wi[u] = __shfl(w, (lane & ~(TPR - 1)) + i);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (i1 + u < most)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) o[k] += fabsf(y[u][k]) == INFINITY ? y[u][k] : y[u][k] * wi[u];
+        }
+    }
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+    *reinterpret_cast<bf16x4*>(p.out + (int64_t)tok * p.q_tok + (int64_t)hd * p.q_head + c * 4) = __builtin_convertvector(o * inv, bf16x4);
+    if (p.lse && c == 0) p.lse[(int64_t)tok * p.n_q_heads + hd] = l == 0.f ? -INFINITY : (m + fast_log2(l)) * kLn2;
+}
+
+namespace {
+
+// Rows of partial results: 256 for every workgroup, and those of all entries, each a multiple of 32 (a query is in one entry of own keys and at most one of
+// shared ones, of which there are at most half as many as requests).
+int64_t rows_parts(bool paged, int workgroups, int batch, int n_queries, int n_q_heads, int n_kv_heads)
+{
+    const int64_t rows = (int64_t)n_queries * n_q_heads * (paged ? 2 : 1), entries = paged ? batch + batch / 2 : batch;
+    return (int64_t)workgroups * kSetRows + rows + entries * 32 * n_kv_heads;
+}
+size_t rows_workspace(bool paged, int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim)
+{
+    const size_t rows = (size_t)rows_parts(paged, kNumCu, batch, n_queries, n_q_heads, n_kv_heads);
+    return align256(rows * head_dim * sizeof(float)) + align256(rows * 2 * sizeof(float)) + align256(((size_t)(paged ? 4 : 2) * batch + 2) * sizeof(int32_t));
+}
+bool rows_shape(int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim)
+{
+    return batch > 0 && n_queries > 0 && n_kv_heads > 0 && n_q_heads > 0 && n_q_heads % n_kv_heads == 0 && (head_dim == 64 || head_dim == 128);
+}
+
+template <int D, bool PAGED>
+int launch_rows(RowsParams& p, hipStream_t stream)
+{
+    constexpr int lds = 4 * kRowsTile * D * 2 + (int)sizeof(RowsPlan);
+    if (const int rc = allow_lds<&rows_kernel<D, PAGED>>(lds)) return rc;
+    const int units = (p.n_q_heads + 256 / D - 1) / (256 / D);
+    const int64_t joins = ((int64_t)p.n_queries * units + 3) / 4;
+    if (!launchable(joins, 256)) return SPECVLM_EUNSUPPORTED;
+    p.workgroups = kNumCu;
+    p.padded = round_up(p.workgroups, kNumXcd);
+    rows_kernel<D, PAGED><<<p.padded, kRowsThreads, lds, stream>>>(p);
+    if (const int rc = launch_status()) return rc;
+    rows_join_kernel<D, PAGED><<<(unsigned)joins, 256, 0, stream>>>(p);
+    return launch_status();
+}
+
+// What both calls ask of the queries, and what they share of the parameters.
+int rows_start(RowsParams& p, bool paged, const void* q, int64_t q_tok, int64_t q_head, const void* k, const void* v, int64_t tok, int64_t head, int batch,
+               int n_queries, int most_keys, int n_q_heads, int n_kv_heads, int head_dim, float scale, void* out, float* lse, void* workspace,
+               size_t workspace_bytes)
+{
+    if (!q || !out || !k || !v) return SPECVLM_EINVAL;
+    if ((q_tok | q_head | tok | head) & 7) return SPECVLM_EUNSUPPORTED;
+    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 15) return SPECVLM_EUNSUPPORTED;
+    // (a lane's offset inside 16 keys has 32 bits; rows, and tiles of all sets and heads, are ints)
+    if (tok < 0 || tok >= ((int64_t)1 << 26)) return SPECVLM_EUNSUPPORTED;
+    const int64_t rows = (int64_t)n_queries * n_q_heads, entries = paged ? 2 * (int64_t)batch : batch;
+    if (rows >= ((int64_t)1 << 29) || entries * 32 * n_kv_heads >= ((int64_t)1 << 29)) return SPECVLM_EUNSUPPORTED;
+    const int64_t sets = (2 * rows / kSetRows + n_kv_heads) + entries * n_kv_heads;
+    if (sets * (most_keys / kRowsTile + 1) >= ((int64_t)1 << 31) - 65536) return SPECVLM_EUNSUPPORTED;
+    const size_t need = rows_workspace(paged, batch, n_queries, n_q_heads, n_kv_heads, head_dim);
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return SPECVLM_EWORKSPACE;
+    p = {};
+    p.q = (const __bf16*)q; p.k = (const __bf16*)k; p.v = (const __bf16*)v; p.out = (__bf16*)out; p.lse = lse;
+    p.q_tok = q_tok; p.q_head = q_head; p.tok = tok; p.head = head;
+    p.batch = batch; p.n_queries = n_queries; p.kv_len = most_keys;
+    p.n_q_heads = n_q_heads; p.n_kv_heads = n_kv_heads; p.group = n_q_heads / n_kv_heads;
+    p.inv_group = reciprocal(p.group);
+    p.scale_log2 = scale * kLog2e;
+    p.most_rows = (int)(rows_parts(paged, 0, batch, n_queries, n_q_heads, n_kv_heads));
+    const size_t parts = (size_t)rows_parts(paged, kNumCu, batch, n_queries, n_q_heads, n_kv_heads);
+    p.part_o = (float*)workspace;
+    p.part_ml = (float*)((char*)workspace + align256(parts * head_dim * sizeof(float)));
+    p.starts = (int32_t*)((char*)p.part_ml + align256(parts * 2 * sizeof(float)));
+    return SPECVLM_OK;
+}
+
+}  // namespace
+}  // namespace specvlm
+
+using namespace specvlm;
+
+extern "C" size_t specvlm_shared_attn_workspace_bytes(int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim)
+{
+    return rows_shape(batch, n_queries, n_q_heads, n_kv_heads, head_dim) ? rows_workspace(true, batch, n_queries, n_q_heads, n_kv_heads, head_dim) : 0;
+}
+
+extern "C" int specvlm_shared_attn(
+    const void* q, int64_t q_tok_stride, int64_t q_head_stride,
+    const void* k_pages, const void* v_pages, int64_t page_stride, int64_t tok_stride, int64_t head_stride,
+    int n_pages, int page_size, const int32_t* page_table, int64_t table_stride, int max_pages,
+    const int32_t* kv_lens, const int32_t* groups, const int32_t* cu_q, int batch, int n_queries, int q_len, int kv_len,
+    int n_q_heads, int n_kv_heads, int head_dim, float softmax_scale,
+    const uint64_t* ancestor_mask, void* out, float* lse,
+    void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (batch < 0 || n_queries < 0 || q_len < 0 || kv_len < 0 || n_q_heads <= 0 || n_kv_heads <= 0 || n_pages < 0 || max_pages < 0) return SPECVLM_EINVAL;
+    if (n_q_heads % n_kv_heads || page_size <= 0) return SPECVLM_EINVAL;
+    if (!(softmax_scale >= 0.f) || !(softmax_scale < INFINITY)) return SPECVLM_EINVAL;
+    if ((head_dim != 64 && head_dim != 128) || page_size % 16 || (ancestor_mask && q_len > kMaxQueryBlock)) return SPECVLM_EUNSUPPORTED;
+    if (batch == 0 || q_len == 0 || n_queries == 0) return SPECVLM_OK;
+    if (!cu_q && (int64_t)batch * q_len != n_queries) return SPECVLM_EINVAL;
+    if (q_len > kv_len || kv_len > (int64_t)max_pages * page_size || n_pages == 0 || table_stride < 0) return SPECVLM_EINVAL;
+    if (!page_table || !kv_lens || !groups) return SPECVLM_EINVAL;
+    if (page_stride & 7 || kv_len > (1 << 30)) return SPECVLM_EUNSUPPORTED;
+    RowsParams p;
+    if (const int rc = rows_start(p, true, q, q_tok_stride, q_head_stride, k_pages, v_pages, tok_stride, head_stride, batch, n_queries, kv_len, n_q_heads,
+                                  n_kv_heads, head_dim, softmax_scale, out, lse, workspace, workspace_bytes))
+        return rc;
+    p.page = page_stride; p.n_pages = n_pages; p.page_size = page_size; p.inv_page = reciprocal(page_size);
+    p.table = page_table; p.table_row = table_stride; p.most_shared = kv_len;
+    p.kv_lens = kv_lens; p.groups = groups; p.cu_q = cu_q; p.q_len = q_len; p.block_mask = ancestor_mask;
+    return head_dim == 128 ? launch_rows<128, true>(p, (hipStream_t)stream) : launch_rows<64, true>(p, (hipStream_t)stream);
+}
+
+extern "C" size_t specvlm_cross_attn_workspace_bytes(int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim)
+{
+    return rows_shape(batch, n_queries, n_q_heads, n_kv_heads, head_dim) ? rows_workspace(false, batch, n_queries, n_q_heads, n_kv_heads, head_dim) : 0;
+}
+
+extern "C" int specvlm_cross_attn(
+    const void* q, int64_t q_tok_stride, int64_t q_head_stride,
+    const void* k, const void* v, int64_t kv_tok_stride, int64_t kv_head_stride,
+    const int32_t* cu_q, const int32_t* cu_kv, int batch, int n_queries, int n_states,
+    int n_q_heads, int n_kv_heads, int head_dim, float softmax_scale,
+    const int32_t* key_ranges, void* out, float* lse,
+    void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (batch < 0 || n_queries < 0 || n_states < 0 || n_q_heads <= 0 || n_kv_heads <= 0 || n_q_heads % n_kv_heads) return SPECVLM_EINVAL;
+    if (!(softmax_scale >= 0.f) || !(softmax_scale < INFINITY)) return SPECVLM_EINVAL;
+    if ((cu_q == nullptr) != (cu_kv == nullptr) || (!cu_q && batch > 1)) return SPECVLM_EINVAL;
+    if (head_dim != 64 && head_dim != 128) return SPECVLM_EUNSUPPORTED;
+    if (batch == 0 || n_queries == 0) return SPECVLM_OK;
+    if (n_states > (1 << 30)) return SPECVLM_EUNSUPPORTED;
+    RowsParams p;
+    if (const int rc = rows_start(p, false, q, q_tok_stride, q_head_stride, k, v, kv_tok_stride, kv_head_stride, batch, n_queries, n_states, n_q_heads,
+                                  n_kv_heads, head_dim, softmax_scale, out, lse, workspace, workspace_bytes))
+        return rc;
+    p.cu_q = cu_q; p.cu_kv = cu_kv; p.q_len = n_queries; p.ranges = key_ranges;
+    return head_dim == 128 ? launch_rows<128, false>(p, (hipStream_t)stream) : launch_rows<64, false>(p, (hipStream_t)stream);
+}
