@@ -18,6 +18,7 @@
 // columns: a lane then holds 16 logits of one row, which are, packed, the second product's operand).  Where a set has fewer rows,
 // two or four waves share them and take every other 32 keys.  Tiles go to LDS by direct loads, two in turn.
 #include <climits>
+#include <type_traits>
 
 #include "attn_tile.h"
 
@@ -38,6 +39,8 @@ __device__ __forceinline__ floatx16 mfma32(bf16x8 a, bf16x8 b, floatx16 c)
 {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
+
+struct RowsStart { int work, rows, q0, n_q, key0, key1, first, total; };       // in front of the entry; the entry; of all
 
 struct RowsParams {
     const __bf16* q;
@@ -62,60 +65,73 @@ struct RowsParams {
     int workgroups, padded;                      // that take runs; the launch
     float* part_o;                               // [rows_parts][D] unnormalised partial outputs (part_row)
     float* part_ml;                              // [rows_parts][2] running maximum in log2 units, sum
-    int32_t* starts;                             // [2 * entries] first tile and first row of every entry;  behind them the run, and whether the groups count
+    RowsStart* starts;                           // [entries] what the join has to know of them
     int most_rows;                               // that the entries may have, for partial results
 };
 
 // What is numbered.  Entry b is the keys that request b's group shares, if it is the group's first request; entry batch + b request b's own keys.
-// (Flat: entry b alone.)  An item is an entry's set of rows of a kv head.
-struct Entry { int q0, n_q, key0, key1; };
+// (Flat: entry b alone.)  An item is an entry's set of rows of a kv head.  first: (own keys) of the group that the request is taken with.
+struct Entry { int q0, n_q, key0, key1, first; };
 
-template <bool PAGED> __device__ __forceinline__ Entry query_range(const RowsParams& p, int b)
+// What the call says of a request.
+struct Request { int q0, n_q, kvl, first, members, shared; };
+template <bool PAGED> __device__ __forceinline__ Request request_of(const RowsParams& p, int b)
 {
-    if (!p.cu_q) return {b * p.q_len, p.q_len, 0, 0};
-    const int q0 = p.cu_q[b];
-    return {q0, p.cu_q[b + 1] - q0, 0, 0};
+    Request r = {b * p.q_len, p.q_len, 0, -1, 0, 0};
+    if (p.cu_q) {
+        r.q0 = p.cu_q[b];
+        r.n_q = p.cu_q[b + 1] - r.q0;
+    }
+    if constexpr (PAGED) {
+        r.kvl = p.kv_lens[b];
+        r.first = p.groups[b];
+        r.members = p.groups[p.batch + b];
+        r.shared = p.groups[2 * p.batch + b];
+    }
+    return r;
 }
-
-// The keys that the group of first request b shares, with the queries of all of its requests; none where what is said of it does not fit together (its
-// requests are then taken alone).
-__device__ __forceinline__ Entry shared_entry(const RowsParams& p, int b)
+// Whether b can be the first of a group of so many members that share so many tokens.
+__device__ __forceinline__ bool leads(const RowsParams& p, int b, const Request& r)
 {
-    const int n = p.groups[2 * p.batch + b], members = p.groups[p.batch + b], kvl = p.kv_lens[b];
-    Entry e = query_range<true>(p, b);
-    if (p.groups[b] != b || members < 2 || members > p.batch - b) return {0, 0, 0, 0};
-    if (n <= 0 || n % 16 || n > p.most_shared || e.n_q <= 0 || kvl > p.kv_len || n > kvl - e.n_q) return {0, 0, 0, 0};
-    e.n_q = (p.cu_q ? p.cu_q[b + members] : (b + members) * p.q_len) - e.q0;
-    if (e.n_q <= 0 || e.q0 < 0 || e.q0 > p.n_queries - e.n_q) return {0, 0, 0, 0};
-    e.key1 = n;
-    return e;
+    return r.first == b && r.members >= 2 && r.members <= p.batch - b && r.shared > 0 && r.shared % 16 == 0 && r.n_q > 0 && r.kvl <= p.kv_len &&
+           r.shared <= r.kvl - r.n_q;
+}
+// The keys that a group shares, with the queries of all of its requests, up to q_end; none where what is said of it does not fit together (its requests
+// are then taken alone).
+__device__ __forceinline__ Entry shared_entry(const RowsParams& p, const Request& r, int q_end)
+{
+    const int n_q = q_end - r.q0;
+    if (n_q <= 0 || r.q0 < 0 || r.q0 > p.n_queries - n_q) return {0, 0, 0, 0, -1};
+    return {r.q0, n_q, 0, r.shared, -1};
+}
+// A request's own keys, behind those that it shares (with a group that begins at r.first, and has so many members).
+__device__ __forceinline__ Entry own_entry(const RowsParams& p, int b, const Request& r, int members, int shared)
+{
+    if (r.n_q <= 0 || r.n_q > p.q_len || r.q0 < 0 || r.q0 > p.n_queries - r.n_q || r.kvl < r.n_q || r.kvl > p.kv_len) return {0, 0, 0, 0, -1};
+    const bool with = shared > 0 && b - r.first < members && shared <= r.kvl - r.n_q;
+    return {r.q0, r.n_q, with ? shared : 0, r.kvl, with ? r.first : -1};
 }
 
 template <bool PAGED> __device__ __forceinline__ Entry entry_of(const RowsParams& p, int e, bool grouped)
 {
+    if (e >= (PAGED ? 2 : 1) * p.batch) return {0, 0, 0, 0, -1};
+    const int b = PAGED && e >= p.batch ? e - p.batch : e;
+    const Request r = request_of<PAGED>(p, b);
     if constexpr (!PAGED) {
-        if (e >= p.batch) return {0, 0, 0, 0};
-        Entry r = query_range<false>(p, e);
-        const int k0 = p.cu_kv ? p.cu_kv[e] : 0;
-        const int n = p.cu_kv ? p.cu_kv[e + 1] - k0 : p.kv_len;
+        const int k0 = p.cu_kv ? p.cu_kv[e] : 0, n = p.cu_kv ? p.cu_kv[e + 1] - k0 : p.kv_len;
         // (offsets that leave the tensors: nothing is read or written by them)
-        if (r.n_q <= 0 || r.q0 < 0 || r.q0 > p.n_queries - r.n_q || n < 0 || k0 < 0 || k0 > p.kv_len - n) return {0, 0, 0, 0};
-        r.key1 = n;
-        return r;
+        if (r.n_q <= 0 || r.q0 < 0 || r.q0 > p.n_queries - r.n_q || n < 0 || k0 < 0 || k0 > p.kv_len - n) return {0, 0, 0, 0, -1};
+        return {r.q0, r.n_q, 0, n, -1};
     } else {
-        if (e >= 2 * p.batch) return {0, 0, 0, 0};
-        const int b = e < p.batch ? e : e - p.batch;
-        if (e < p.batch) return grouped ? shared_entry(p, b) : Entry{0, 0, 0, 0};
-        Entry r = query_range<true>(p, b);
-        const int kvl = p.kv_lens[b];
-        if (r.n_q <= 0 || r.n_q > p.q_len || r.q0 < 0 || r.q0 > p.n_queries - r.n_q || kvl < r.n_q || kvl > p.kv_len) return {0, 0, 0, 0};
-        r.key1 = kvl;
-        const int first = grouped ? p.groups[b] : -1;
-        if (first >= 0 && first <= b && b - first < p.groups[p.batch + first]) {
-            const Entry all = shared_entry(p, first);
-            if (all.key1 <= kvl - r.n_q) r.key0 = all.key1;
+        const int f = e < p.batch ? b : r.first;
+        Entry all = {0, 0, 0, 0, -1};
+        int members = 0;
+        if (grouped && f >= 0 && f <= b) {
+            const Request first = f == b ? r : request_of<true>(p, f);
+            members = first.members;
+            if (leads(p, f, first)) all = shared_entry(p, first, p.cu_q ? p.cu_q[f + members] : (f + members) * p.q_len);
         }
-        return r;
+        return e < p.batch ? all : own_entry(p, b, r, members, all.key1);
     }
 }
 
@@ -126,47 +142,80 @@ __device__ __forceinline__ Sets sets_of(int rows)
     const int blocks = (rows + 31) >> 5, n = (blocks + kRowsWaves - 1) / kRowsWaves;
     return {n, n > 1 ? (blocks + n - 1) / n : blocks};
 }
-__device__ __forceinline__ int tiles_of(const Entry& e) { return max(1, (e.key1 - e.key0 + kRowsTile - 1) / kRowsTile); }
+__device__ __forceinline__ int chunks_of(const Entry& e) { return max(1, (e.key1 - e.key0 + 31) >> 5); }       // of 32 keys
 
 __device__ __forceinline__ int padded_rows(const RowsParams& p, const Entry& e) { return (e.n_q * p.group + 31) & ~31; }      // of a kv head
 
-struct Numbers { int tiles, rows; };         // of an entry, or in front of one
+// Work is counted in 32 keys of a set, and an item has kBegin more in front of its first: what a piece costs before and behind its keys.
+constexpr int kBegin = 5, kLeastRun = 9;
+
+struct Numbers { int work, rows; };          // of an entry, or in front of one
 __device__ __forceinline__ Numbers numbers_of(const RowsParams& p, const Entry& e)
 {
     if (e.n_q <= 0) return {0, 0};
-    return {sets_of(e.n_q * p.group).n * p.n_kv_heads * tiles_of(e), padded_rows(p, e) * p.n_kv_heads};
+    return {sets_of(e.n_q * p.group).n * p.n_kv_heads * (chunks_of(e) + kBegin), padded_rows(p, e) * p.n_kv_heads};
 }
 
 // The row of the partial results that workgroup j's piece of an item has: the rows of all items one after the other, and 256 on for every workgroup, so
 // that two pieces of an item do not meet, nor two items of a workgroup.
 __device__ __forceinline__ int64_t part_row(int j, int row_of_items) { return (int64_t)j * kSetRows + row_of_items; }
 
-// Tiles of a run.
-__device__ __forceinline__ int rows_run(const RowsParams& p, int total) { return max(1, (total + p.workgroups - 1) / p.workgroups); }
+// The work is dealt to `sharers` workgroups, to j from j * total / sharers on.
+__device__ __forceinline__ int sharers_of(const RowsParams& p, int total) { return min(p.workgroups, max(1, total / kLeastRun)); }
+__device__ __forceinline__ int share_begin(int j, int total, int sharers) { return (int)((int64_t)j * total / sharers); }
+__device__ __forceinline__ int sharer_of(int x, int total, int sharers) { return (int)((((int64_t)x + 1) * sharers - 1) / total); }
 
 // LDS behind the tiles:  what a workgroup knows of 512 entries.
 struct RowsPlan {
+    Entry entry[kRowsThreads];
     Numbers front[kRowsThreads];
     Numbers wave[kRowsWaves];
-    int found;
+    float ml[kSetRows * 2];                  // maxima and sums of waves that share rows
+    int word[3][kRowsThreads / 2];           // of requests
     unsigned char ok[2][8];
+    int found;
 };
+
+// entry_of of all entries, one to a thread, where there are no more than threads:  what requests say of each other goes through LDS (each look at another's
+// words in memory takes 0.7 us).
+__device__ __forceinline__ Entry entry_at_once(const RowsParams& p, RowsPlan& s, bool grouped)
+{
+    const int t = threadIdx.x, b = t < p.batch ? t : t - p.batch;
+    Request r = {0, 0, 0, -1, 0, 0};
+    if (b < p.batch) r = request_of<true>(p, b);
+    if (t < p.batch) {
+        s.word[0][b] = r.q0 + r.n_q;
+        s.word[1][b] = r.members;
+    }
+    __syncthreads();
+    Entry e = {0, 0, 0, 0, -1};
+    if (t < p.batch) {
+        if (grouped && leads(p, b, r)) e = shared_entry(p, r, s.word[0][b + r.members - 1]);
+        s.word[2][b] = e.key1;
+    }
+    __syncthreads();
+    if (t >= p.batch && b < p.batch) {
+        const bool in = grouped && r.first >= 0 && r.first <= b;
+        e = own_entry(p, b, r, in ? s.word[1][r.first] : 0, in ? s.word[2][r.first] : 0);
+    }
+    return e;
+}
 
 // Inclusive prefix sums over the workgroup's threads, and the total; `s` is free again behind the next barrier.
 __device__ __forceinline__ Numbers block_prefix(RowsPlan& s, Numbers x, int wave, int lane, Numbers* total)
 {
-    Numbers up = {wave_prefix(x.tiles), wave_prefix(x.rows)};
+    Numbers up = {wave_prefix(x.work), wave_prefix(x.rows)};
     if (lane == kWave - 1) s.wave[wave] = up;
     __syncthreads();
     Numbers all = {0, 0};
 #pragma unroll
     for (int w = 0; w < kRowsWaves; ++w) {
         const Numbers t = s.wave[w];
-        if (w < wave) { up.tiles += t.tiles; up.rows += t.rows; }
-        all.tiles += t.tiles;
+        if (w < wave) { up.work += t.work; up.rows += t.rows; }
+        all.work += t.work;
         all.rows += t.rows;
     }
-    *total = {__builtin_amdgcn_readfirstlane(all.tiles), __builtin_amdgcn_readfirstlane(all.rows)};
+    *total = {__builtin_amdgcn_readfirstlane(all.work), __builtin_amdgcn_readfirstlane(all.rows)};
     __syncthreads();
     return up;
 }
@@ -235,6 +284,8 @@ __device__ __forceinline__ float half_sum(float x)
     return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
+__device__ __forceinline__ int first_of_last(int entries) { return (entries - 1) / kRowsThreads * kRowsThreads; }
+
 template <int D, bool PAGED>
 __global__ __launch_bounds__(kRowsThreads, 2)
 void rows_kernel(const RowsParams p)
@@ -242,8 +293,7 @@ void rows_kernel(const RowsParams p)
     constexpr int KK = D / 16, JB = D / 32, CH = D / 8, ROW_BYTES = D * 2;
     constexpr int TILE_BYTES = kRowsTile * ROW_BYTES;        // of K or V
     constexpr int KEYS_PER_LOAD = kWave / CH, LOADS = 16 / KEYS_PER_LOAD;
-    constexpr int O_STRIDE = D + 4;
-    static_assert((kRowsWaves - 2) * 32 * O_STRIDE * 4 <= 4 * TILE_BYTES, "the exchange of waves that share rows");
+    static_assert(kSetRows * D * 4 <= 4 * TILE_BYTES, "the exchange of waves that share rows");
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 31, h = lane >> 5;
@@ -251,6 +301,7 @@ void rows_kernel(const RowsParams p)
     RowsPlan& plan = *reinterpret_cast<RowsPlan*>(smem + 4 * TILE_BYTES);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(SPECVLM_AS3 unsigned char*)smem;
 
+    const float sc = fmaxf(p.scale_log2, 1e-30f);            // (a zero scale as a vanishing one: -inf stays -inf)
     const int j = xcd_logical_id(blockIdx.x, p.padded);
     if (j >= p.workgroups) return;
 
@@ -258,83 +309,130 @@ void rows_kernel(const RowsParams p)
     const int entries = PAGED ? 2 * p.batch : p.batch;
     Numbers total, here;
     bool grouped = PAGED;
+    Entry entry;
     Numbers mine, upto;
-    for (;;) {
-        mine = numbers_of(p, entry_of<PAGED>(p, threadIdx.x, grouped));
+    const auto look_at = [&](int e) {
+        if (PAGED && entries <= kRowsThreads) entry = entry_at_once(p, plan, grouped);
+        else entry = entry_of<PAGED>(p, e, grouped);
+        mine = numbers_of(p, entry);
         upto = block_prefix(plan, mine, wave, lane, &here);
-        total = here;
-        for (int c = kRowsThreads; c < entries; c += kRowsThreads) {
-            Numbers more;
-            block_prefix(plan, numbers_of(p, entry_of<PAGED>(p, c + threadIdx.x, grouped)), wave, lane, &more);
-            total.tiles += more.tiles;
-            total.rows += more.rows;
+    };
+    for (;;) {
+        total = {0, 0};
+        for (int c = first_of_last(entries); c >= 0; c -= kRowsThreads) {     // (the first 512 last: they are looked up next)
+            look_at(c + threadIdx.x);
+            total.work += here.work;
+            total.rows += here.rows;
         }
         // (groups that overlap would have rows more than once: there is no room for them)
         if (total.rows <= p.most_rows || !grouped) break;
         grouped = false;
     }
-    if (total.rows > p.most_rows) total.tiles = 0;           // (offsets that overlap)
-    const int run = rows_run(p, total.tiles);
-    int x = j * run;
-    const int x_end = min(total.tiles, x + run);
+    if (total.rows > p.most_rows) total.work = 0;            // (offsets that overlap)
+    const int sharers = sharers_of(p, total.work);
+    if (j >= sharers) return;
+    int x = share_begin(j, total.work, sharers);
+    const int x_end = share_begin(j + 1, total.work, sharers);
     Numbers base = {0, 0};                                   // in front of the 512 entries at hand
     int c0 = 0;
     const auto publish = [&] {
-        const Numbers front = {base.tiles + upto.tiles - mine.tiles, base.rows + upto.rows - mine.rows};
+        const Numbers front = {base.work + upto.work - mine.work, base.rows + upto.rows - mine.rows};
+        plan.entry[threadIdx.x] = entry;
         plan.front[threadIdx.x] = front;
         if (j == 0) {                                        // (the join reads where every entry begins)
             const int e = c0 + threadIdx.x;
-            if (e < entries) { p.starts[2 * e] = front.tiles; p.starts[2 * e + 1] = front.rows; }
-            if (e == 0) { p.starts[2 * entries] = total.tiles ? run : 0; p.starts[2 * entries + 1] = grouped; }
+            if (e < entries) p.starts[e] = {front.work, front.rows, entry.q0, entry.n_q, entry.key0, entry.key1, entry.first, total.work};
         }
-    };
-    const auto next_entries = [&] {
-        base.tiles += here.tiles;
-        base.rows += here.rows;
-        c0 += kRowsThreads;
-        mine = numbers_of(p, entry_of<PAGED>(p, c0 + threadIdx.x, grouped));
-        upto = block_prefix(plan, mine, wave, lane, &here);
-        publish();
     };
     publish();
-    if (j == 0) {
-        // (workgroup 0 tells of all, then begins again)
-        if (entries > kRowsThreads) {
-            while (c0 + kRowsThreads < entries) next_entries();
-            base = {0, 0};
-            c0 = 0;
+    bool told = entries <= kRowsThreads || j > 0;            // (workgroup 0 tells of all entries, then begins again)
+    while (x < x_end || !told) {
+        while (!told || x >= base.work + here.work) {
+            base.work += here.work;
+            base.rows += here.rows;
+            c0 += kRowsThreads;
+            if (c0 >= entries) {
+                told = true;
+                base = {0, 0};
+                c0 = 0;
+            }
             __syncthreads();
-            mine = numbers_of(p, entry_of<PAGED>(p, threadIdx.x, grouped));
-            upto = block_prefix(plan, mine, wave, lane, &here);
+            look_at(c0 + threadIdx.x);
             publish();
         }
-    }
-
-    const float sc = fmaxf(p.scale_log2, 1e-30f);            // (a zero scale as a vanishing one: -inf stays -inf)
-
-    while (x < x_end) {
-        while (x >= base.tiles + here.tiles) next_entries();
-        if (base.tiles + upto.tiles > x && base.tiles + upto.tiles - mine.tiles <= x) plan.found = threadIdx.x;
+        if (x >= x_end) break;
+        if (base.work + upto.work > x && base.work + upto.work - mine.work <= x) plan.found = threadIdx.x;
         __syncthreads();
         const int at = __builtin_amdgcn_readfirstlane(plan.found), e = c0 + at;
-        const Numbers front = {__builtin_amdgcn_readfirstlane(plan.front[at].tiles), __builtin_amdgcn_readfirstlane(plan.front[at].rows)};
+        const Numbers front = {__builtin_amdgcn_readfirstlane(plan.front[at].work), __builtin_amdgcn_readfirstlane(plan.front[at].rows)};
         const bool own = !PAGED || e >= p.batch;
         const int b = PAGED && own ? e - p.batch : e;
-        Entry en = entry_of<PAGED>(p, e, grouped);
+        Entry en = plan.entry[at];
         en.q0 = __builtin_amdgcn_readfirstlane(en.q0); en.n_q = __builtin_amdgcn_readfirstlane(en.n_q);
         en.key0 = __builtin_amdgcn_readfirstlane(en.key0); en.key1 = __builtin_amdgcn_readfirstlane(en.key1);
-        const int tiles = tiles_of(en), rows = en.n_q * p.group;
+        const int chunks = chunks_of(en), rows = en.n_q * p.group;
         const Sets sets = sets_of(rows);
-        const int item = (x - front.tiles) / tiles, t_begin = x - front.tiles - item * tiles;
-        const int t_end = min(tiles, t_begin + x_end - x);
+        const int item = (x - front.work) / (chunks + kBegin), begin = x - front.work - item * (chunks + kBegin);
+        const int c_begin = max(0, begin - kBegin), c_end = min(chunks, begin + x_end - x - kBegin);
+        x = min(x_end, x + chunks + kBegin - begin);
+        if (c_end <= c_begin) {                              // (the front of an item alone)
+            __syncthreads();
+            continue;
+        }
         const int g = item / sets.n, set = item - g * sets.n;
         const int row0 = set * sets.blocks * 32, n_rows = min(rows - row0, sets.blocks * 32), n_blocks = (n_rows + 31) >> 5;
         const int log_blocks = n_blocks > 4 ? 3 : n_blocks > 2 ? 2 : n_blocks - 1;       // waves of a kind
         const int blk = wave & ((1 << log_blocks) - 1), ks = wave >> log_blocks, n_ks = min(kChunks, kRowsWaves >> log_blocks);
         const bool works = blk < n_blocks && ks < n_ks;
-        const bool direct = own && en.key0 == 0 && t_begin == 0 && t_end == tiles;
+        const bool direct = own && en.key0 == 0 && c_begin == 0 && c_end == chunks;
+        const int key0 = en.key0 + c_begin * 32, key1 = min(en.key1, en.key0 + c_end * 32), tiles = (key1 - key0 + kRowsTile - 1) / kRowsTile;       // of the piece
         const bool two_parts = n_blocks <= 4;
-        x += t_end - t_begin;
+
+        // ---- loads: wave w brings keys 16w..16w+15 of a tile ----
+        const int64_t kv0 = (int64_t)g * p.head + (PAGED ? 0 : (int64_t)(p.cu_kv ? __builtin_amdgcn_readfirstlane(p.cu_kv[e]) : 0) * p.tok);
+        const char* const k_at = reinterpret_cast<const char*>(p.k + kv0);
+        const char* const v_at = reinterpret_cast<const char*>(p.v + kv0);
+        const int table_b = PAGED ? b : 0;
+        int ids = 0, places = 0;                             // of the next 64 tiles, one to a lane
+        const auto look_up = [&](int tile) {
+            const int key = min(key0 + (tile + lane) * kRowsTile + wave * 16, (key1 - 1) & ~15);
+            const QuotRem pg = divide(key, p.page_size, p.inv_page);
+            ids = p.table[(int64_t)table_b * p.table_row + pg.q];
+            places = pg.r;
+        };
+        const auto issue = [&](int tile, int stage) {
+            const uint32_t to = lds0 + stage * 2 * TILE_BYTES + wave * 16 * ROW_BYTES;
+            int64_t first;
+            int last;                                        // the last of the 16 keys that there is: it stands for those behind it, whatever lies there
+            if constexpr (PAGED) {
+                const int l = tile & 63;
+                if (l == 0 && tile > 0) look_up(tile);
+                const int id = __builtin_amdgcn_readlane(ids, l), row = __builtin_amdgcn_readlane(places, l);
+                // (a page that is not one of the pool's is not read: the pool's first is, and its keys are masked)
+                const bool there = (uint32_t)id < (uint32_t)p.n_pages;
+                if (lane == 0) plan.ok[stage][wave] = there;
+                first = (there ? id : 0) * p.page + row * p.tok;
+                last = key1 - 1 - (key0 + tile * kRowsTile + wave * 16);
+                if (last < 0) last = (key1 - 1) & 15;        // (a group behind the last: that one again)
+            } else {
+                const int key = min(key0 + tile * kRowsTile + wave * 16, key1 - 1);
+                first = (int64_t)key * p.tok;
+                last = key1 - 1 - key;
+            }
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int kl = i * KEYS_PER_LOAD + lane / CH, piece = lane % CH;
+                const uint32_t row = (uint32_t)min(kl, last) * (uint32_t)(p.tok * 2);
+                load_to_lds(k_at + 2 * first, row + (piece ^ (D == 128 ? kl & 15 : kl >> 1 & 7)) * 16, to + i * 1024);
+                load_to_lds(v_at + 2 * first, row + (piece ^ rows_v_swizzle<D>(kl)) * 16, to + TILE_BYTES + i * 1024);
+            }
+        };
+
+        const auto begin_loads = [&] {
+            if constexpr (PAGED) look_up(0);
+            issue(0, 0);
+        };
+        if (tiles > 0) begin_loads();                        // (on their way while the rows are looked at)
 
         // this wave's rows
         const int my_row = blk * 32 + r;
@@ -346,7 +444,7 @@ void rows_kernel(const RowsParams p)
 #pragma unroll
         for (int s = 0; s < KK; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qp + s * 16);
         // the keys that it sees: [lo, hi), of the block those of a tree node's mask
-        int lo = en.key0, hi = en.key1;
+        int lo = en.key0, hi = key1;
         const int before = en.key1 - en.n_q;                 // (own keys of a block)
         uint64_t tree = 0;
         bool is_tree = false;
@@ -354,14 +452,14 @@ void rows_kernel(const RowsParams p)
             if (own) {
                 is_tree = p.block_mask != nullptr;
                 if (is_tree) tree = p.block_mask[q_tok];
-                else hi = before + q_at.q + 1;
+                else hi = min(hi, before + q_at.q + 1);
             }
         } else if (p.ranges) {
             lo = max(p.ranges[2 * q_tok], 0);
-            hi = min(p.ranges[2 * q_tok + 1], en.key1);
+            hi = min(p.ranges[2 * q_tok + 1], key1);
         }
         // of all of the wave's rows: keys that all see, and that some see
-        int all_lo = lo, all_hi = is_tree ? before : hi, any_lo = lo < hi ? lo : INT_MAX, any_hi = lo < hi ? hi : 0;
+        int all_lo = lo, all_hi = is_tree ? min(before, hi) : hi, any_lo = lo < hi ? lo : INT_MAX, any_hi = lo < hi ? hi : 0;
 #pragma unroll
         for (int d = 1; d < 32; d *= 2) {
             all_lo = max(all_lo, __shfl_xor(all_lo, d)); all_hi = min(all_hi, __shfl_xor(all_hi, d));
@@ -370,44 +468,6 @@ void rows_kernel(const RowsParams p)
         all_lo = __builtin_amdgcn_readfirstlane(all_lo); all_hi = __builtin_amdgcn_readfirstlane(all_hi);
         any_lo = __builtin_amdgcn_readfirstlane(any_lo); any_hi = __builtin_amdgcn_readfirstlane(any_hi);
 
-        // ---- loads: wave w brings keys 16w..16w+15 of a tile ----
-        const int64_t kv0 = (int64_t)g * p.head + (PAGED ? 0 : (int64_t)(p.cu_kv ? __builtin_amdgcn_readfirstlane(p.cu_kv[e]) : 0) * p.tok);
-        const char* const k_at = reinterpret_cast<const char*>(p.k + kv0);
-        const char* const v_at = reinterpret_cast<const char*>(p.v + kv0);
-        const int table_b = PAGED ? b : 0;
-        int ids = 0, places = 0;                             // of the next 64 tiles, one to a lane
-        const auto look_up = [&](int tile) {
-            const int key = min(en.key0 + (tile + lane) * kRowsTile + wave * 16, (en.key1 - 1) & ~15);
-            const QuotRem pg = divide(key, p.page_size, p.inv_page);
-            ids = p.table[(int64_t)table_b * p.table_row + pg.q];
-            places = pg.r;
-        };
-        const auto issue = [&](int tile, int stage) {
-            const uint32_t to = lds0 + stage * 2 * TILE_BYTES + wave * 16 * ROW_BYTES;
-            int64_t first;
-            int last = 15;                                   // the last of the 16 rows that may be read
-            if constexpr (PAGED) {
-                const int l = (tile - t_begin) & 63;
-                if (l == 0 && tile != t_begin) look_up(tile);
-                const int id = __builtin_amdgcn_readlane(ids, l), row = __builtin_amdgcn_readlane(places, l);
-                // (a page that is not one of the pool's is not read: the pool's first is, and its keys are masked)
-                const bool there = (uint32_t)id < (uint32_t)p.n_pages;
-                if (lane == 0) plan.ok[stage][wave] = there;
-                first = (there ? id : 0) * p.page + row * p.tok;
-            } else {
-                const int key = min(tile * kRowsTile + wave * 16, en.key1 - 1);
-                first = (int64_t)key * p.tok;
-                last = en.key1 - 1 - key;
-            }
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int kl = i * KEYS_PER_LOAD + lane / CH, piece = lane % CH;
-                const uint32_t row = (uint32_t)(PAGED ? kl : min(kl, last)) * (uint32_t)(p.tok * 2);
-                load_to_lds(k_at + 2 * first, row + (piece ^ (D == 128 ? kl & 15 : kl >> 1 & 7)) * 16, to + i * 1024);
-                load_to_lds(v_at + 2 * first, row + (piece ^ rows_v_swizzle<D>(kl)) * 16, to + TILE_BYTES + i * 1024);
-            }
-        };
-
         float m_run, l_run;
         floatx16 o[JB];
         // where this lane reads in a stage
@@ -415,7 +475,20 @@ void rows_kernel(const RowsParams p)
         const int v_row = 4 * h + ((lane & 15) >> 2);
         const uint32_t v_base = lds0 + TILE_BYTES + v_row * ROW_BYTES + ((((lane >> 4 & 1) * 2 + ((lane & 3) >> 1)) ^ rows_v_swizzle<D>(v_row)) * 16) + (lane & 1) * 8;
 
-        for (bool careful = false;;) {
+        // V^T fragments of 16 keys, by the transposing read
+        const auto read_values = [&](bf16x8 (&vf)[JB], uint32_t at) {
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb) {
+                typedef short s16x4 __attribute__((ext_vector_type(4)));
+                SPECVLM_AS3 s16x4* const src = in_lds<s16x4>(v_base + at ^ jb * 64);
+                const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(src);
+                const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16(src + 8 * ROW_BYTES / 8);
+                vf[jb] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+        };
+
+        // The sweep.  careful: with an eye on values that are no finite numbers.
+        const auto sweep = [&](auto careful) {
             m_run = -INFINITY;
             l_run = 0.f;
 #pragma unroll
@@ -423,172 +496,182 @@ void rows_kernel(const RowsParams p)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[jb][i] = 0.f;
             bool fresh = true;                               // some row has seen nothing yet
-            if (en.key1 > en.key0) {
-                if constexpr (PAGED) look_up(t_begin);
-                issue(t_begin, 0);
-                for (int t = t_begin; t < t_end; ++t) {
-                    const int stage = (t - t_begin) & 1;
-                    wait_vmcnt<0>();
-                    __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                    stage_barrier();                         // the tile is there for everyone, and everyone has left the other stage
-                    if (t + 1 < t_end) issue(t + 1, stage ^ 1);
-                    if (!works) continue;
-                    for (int ch = ks; ch < kChunks; ch += n_ks) {
-                        const int k0 = en.key0 + t * kRowsTile + ch * 32;
-                        if (k0 >= any_hi || k0 + 31 < any_lo) continue;
-                        uint32_t pages = ~0u;                // keys whose page is there
-                        if constexpr (PAGED) {
-                            const int two = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint16_t*>(&plan.ok[stage][2 * ch]));
-                            pages = (two & 1 ? 0xffffu : 0u) | (two & 0x100 ? 0xffff0000u : 0u);
+            if (tiles <= 0) return;
+            if constexpr (decltype(careful)::value) begin_loads();
+            for (int t = 0; t < tiles; ++t) {
+                const int stage = t & 1;
+                wait_vmcnt<0>();
+                __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                stage_barrier();                             // the tile is there for everyone, and everyone has left the other stage
+                if (t + 1 < tiles) issue(t + 1, stage ^ 1);
+                if (!works) continue;
+                uint64_t there = ~0ull;                      // a byte for 16 keys: their page is there
+                if constexpr (PAGED) {
+                    const u32x2 ok = *reinterpret_cast<const u32x2*>(plan.ok[stage]);
+                    there = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(ok[1]) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane(ok[0]);
+                }
+                for (int ch = ks; ch < kChunks; ch += n_ks) {
+                    const int k0 = key0 + t * kRowsTile + ch * 32;
+                    if (k0 >= any_hi || k0 + 31 < any_lo) continue;
+                    const uint32_t at_chunk = stage * 2 * TILE_BYTES + ch * 32 * ROW_BYTES;
+                    // ---- S^T = K Q^T for 32 keys ----
+                    bf16x8 kf[KK];
+#pragma unroll
+                    for (int kk = 0; kk < KK; ++kk) kf[kk] = __builtin_bit_cast(bf16x8, *in_lds<const u32x4>(k_base + at_chunk ^ kk * 32));
+                    floatx16 s;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+                    for (int kk = 0; kk < KK; ++kk) s = mfma32(kf[kk], qf[kk], s);
+                    // (the reads of all of them first: one by one, each waits for its own)
+                    __builtin_amdgcn_sched_group_barrier(0x100, KK, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x008, KK, 0);
+                    bf16x8 vf[2][JB];
+                    read_values(vf[0], at_chunk);
+                    const uint32_t two = PAGED ? (uint32_t)(there >> (16 * ch)) & 0xffffu : 0x101u;
+                    const bool need_mask = two != 0x101u || k0 < all_lo || k0 + 32 > all_hi;
+                    uint32_t sees = ~0u;
+                    if (need_mask) {
+                        sees = first_bits(hi - k0) & ~first_bits(lo - k0) & ((two & 1 ? 0xffffu : 0u) | (two & 0x100 ? 0xffff0000u : 0u));
+                        if (is_tree) {
+                            const int in = k0 - before;
+                            const uint64_t block = in >= 0 ? (in < 64 ? tree >> in : 0) : (in > -32 ? tree << -in : 0);
+                            sees &= (uint32_t)block | first_bits(-in);
                         }
-                        const uint32_t at_chunk = stage * 2 * TILE_BYTES + ch * 32 * ROW_BYTES;
-                        // ---- S^T = K Q^T for 32 keys ----
-                        floatx16 s;
+                        sees >>= 4 * h;                      // bit 8(i/4) + i%4: the lane's i-th key
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+                        for (int i = 0; i < 16; ++i) s[i] = sees >> (8 * (i / 4) + i % 4) & 1u ? s[i] : -INFINITY;
+                    }
+                    // Away from the masks the exponentials are taken against the reference that the earlier keys left, and the maximum is
+                    // tracked only where a lane's sum does not stay moderate.
+                    bool settled = false;
+                    float pv[16];
+                    if (!need_mask && !fresh) {
+                        float psum = 0.f;
 #pragma unroll
-                        for (int kk = 0; kk < KK; ++kk) {
-                            const u32x4 kf = *in_lds<const u32x4>(k_base + at_chunk ^ kk * 32);
-                            s = mfma32(__builtin_bit_cast(bf16x8, kf), qf[kk], s);
+                        for (int i = 0; i < 16; ++i) { pv[i] = fast_exp2(fmaf(s[i], sc, -m_run)); psum += pv[i]; }
+                        if (!__any(!(psum < kRowsRedo))) {
+                            l_run += psum;
+                            settled = true;
                         }
-                        const bool need_mask = pages != ~0u || k0 < all_lo || k0 + 32 > all_hi;
-                        uint32_t sees = ~0u;
-                        if (need_mask) {
-                            sees = first_bits(hi - k0) & ~first_bits(lo - k0) & pages;
-                            if (is_tree) {
-                                const int in = k0 - before;
-                                const uint64_t block = in >= 0 ? (in < 64 ? tree >> in : 0) : (in > -32 ? tree << -in : 0);
-                                sees &= (uint32_t)block | first_bits(-in);
-                            }
-                            sees >>= 4 * h;                  // bit 8(i/4) + i%4: the lane's i-th key
+                    }
+                    if (!settled) {
+                        float mx = s[0];
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) s[i] = sees >> (8 * (i / 4) + i % 4) & 1u ? s[i] : -INFINITY;
+                        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+                        const float m_new = fmaxf(m_run, half_max(mx) * sc);
+                        const float m_ref = m_new == -INFINITY ? 0.f : m_new;
+                        const float alpha = fast_exp2(m_run - m_ref);
+                        const bool rescale = m_new != m_run;
+                        m_run = m_new;
+                        float psum = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) { pv[i] = fast_exp2(fmaf(s[i], sc, -m_ref)); psum += pv[i]; }
+                        l_run = l_run * alpha + psum;
+                        if (__any(rescale)) {
+#pragma unroll
+                            for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                                for (int i = 0; i < 16; ++i)             // (an infinity stays one, also where 32 bits take its weight for 0)
+                                    o[jb][i] = decltype(careful)::value && fabsf(o[jb][i]) == INFINITY ? o[jb][i] : alpha * o[jb][i];
                         }
-                        // Away from the masks the exponentials are taken against the reference that the earlier keys left, and the maximum is
-                        // tracked only where a lane's sum does not stay moderate.
-                        bool settled = false;
-                        float pv[16];
-                        if (!need_mask && !fresh) {
-                            float psum = 0.f;
+                    }
+                    if (need_mask || fresh) fresh = __any(!(m_run > -INFINITY));
+                    // ---- O^T += V^T P^T ----
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) { pv[i] = fast_exp2(fmaf(s[i], sc, -m_run)); psum += pv[i]; }
-                            if (!__any(!(psum < kRowsRedo))) {
-                                l_run += psum;
-                                settled = true;
-                            }
+                    for (int u = 0; u < 2; ++u) {
+                        floatx8 pu;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) pu[i] = pv[8 * u + i];
+                        const bf16x8 pf = __builtin_convertvector(pu, bf16x8);
+                        if (u == 0) read_values(vf[1], at_chunk + 16 * ROW_BYTES);
+                        if constexpr (decltype(careful)::value) {
+                            const uint32_t s16 = sees >> 16 * u;
+#pragma unroll
+                            for (int jb = 0; jb < JB; ++jb) take_odd_rows(vf[u][jb], (s16 & 0xfu) | (s16 >> 4 & 0xf0u), o[jb]);
                         }
-                        if (!settled) {
-                            float mx = s[0];
 #pragma unroll
-                            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
-                            const float m_new = fmaxf(m_run, half_max(mx) * sc);
-                            const float m_ref = m_new == -INFINITY ? 0.f : m_new;
-                            const float alpha = fast_exp2(m_run - m_ref);
-                            const bool rescale = m_new != m_run;
-                            m_run = m_new;
-                            float psum = 0.f;
+                        for (int jb = 0; jb < JB; ++jb) o[jb] = mfma32(vf[u][jb], pf, o[jb]);
+                        if (two_parts) {
+                            const u32x4 w = __builtin_bit_cast(u32x4, pf);
+                            floatx8 rest;
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) { pv[i] = fast_exp2(fmaf(s[i], sc, -m_ref)); psum += pv[i]; }
-                            l_run = l_run * alpha + psum;
-                            if (__any(rescale)) {
-#pragma unroll
-                                for (int jb = 0; jb < JB; ++jb)
-#pragma unroll
-                                    for (int i = 0; i < 16; ++i)         // (an infinity stays one, also where 32 bits take its weight for 0)
-                                        o[jb][i] = careful && fabsf(o[jb][i]) == INFINITY ? o[jb][i] : alpha * o[jb][i];
+                            for (int i = 0; i < 4; ++i) {
+                                rest[2 * i] = pu[2 * i] - __uint_as_float(w[i] << 16);
+                                rest[2 * i + 1] = pu[2 * i + 1] - __uint_as_float(w[i] & 0xffff0000u);
                             }
-                        }
-                        if (need_mask || fresh) fresh = __any(!(m_run > -INFINITY));
-                        // ---- O^T += V^T P^T ----
+                            const bf16x8 pr = __builtin_convertvector(rest, bf16x8);
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            floatx8 pu;
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) pu[i] = pv[8 * u + i];
-                            const bf16x8 pf = __builtin_convertvector(pu, bf16x8);
-                            bf16x8 vf[JB];
-#pragma unroll
-                            for (int jb = 0; jb < JB; ++jb) {
-                                typedef short s16x4 __attribute__((ext_vector_type(4)));
-                                SPECVLM_AS3 s16x4* const src = in_lds<s16x4>((v_base + at_chunk ^ jb * 64) + u * 16 * ROW_BYTES);
-                                const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(src);
-                                const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16(src + 8 * ROW_BYTES / 8);
-                                vf[jb] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7));
-                            }
-                            if (need_mask || careful) {
-                                const uint32_t s16 = sees >> 16 * u;
-#pragma unroll
-                                for (int jb = 0; jb < JB; ++jb) take_odd_rows(vf[jb], (s16 & 0xfu) | (s16 >> 4 & 0xf0u), o[jb]);
-                            }
-#pragma unroll
-                            for (int jb = 0; jb < JB; ++jb) o[jb] = mfma32(vf[jb], pf, o[jb]);
-                            if (two_parts) {
-                                const u32x4 two = __builtin_bit_cast(u32x4, pf);
-                                floatx8 rest;
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    rest[2 * i] = pu[2 * i] - __uint_as_float(two[i] << 16);
-                                    rest[2 * i + 1] = pu[2 * i + 1] - __uint_as_float(two[i] & 0xffff0000u);
-                                }
-                                const bf16x8 pr = __builtin_convertvector(rest, bf16x8);
-#pragma unroll
-                                for (int jb = 0; jb < JB; ++jb) o[jb] = mfma32(vf[jb], pr, o[jb]);
-                            }
+                            for (int jb = 0; jb < JB; ++jb) o[jb] = mfma32(vf[u][jb], pr, o[jb]);
                         }
                     }
                 }
             }
-            // A sum that is no finite number, as a rule of an infinite value that a row sees:  all keys once more, with an eye on such values.
-            float odd = 0.f;
+        };
+        sweep(std::false_type());
+        // A sum that is no finite number, as a rule of an infinite value that a row sees, or of a hidden one that is none:  all keys once more, with an eye on
+        // such values.
+        float odd = 0.f;
 #pragma unroll
-            for (int jb = 0; jb < JB; ++jb)
+        for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) odd += 0.f * o[jb][i];
-            if (!__syncthreads_or(works && !(odd == 0.f)) || careful) break;
-            careful = true;
+            for (int i = 0; i < 16; ++i) odd += 0.f * o[jb][i];
+        if (__builtin_expect(__syncthreads_or(works && !(odd == 0.f)), 0)) {
+            sweep(std::true_type());
+            __syncthreads();
         }
 
-        // ---- waves that share rows: the sums of the others to the first ----
         l_run = half_sum(l_run);
-        float* const s_o = reinterpret_cast<float*>(smem);
-        float* const s_ml = reinterpret_cast<float*>(plan.front);         // (the numbering is made again for the next piece)
+        const int64_t part = part_row(j, front.rows + g * padded_rows(p, en) + row0);
+        const auto inverse = [](float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN; };
         if (n_ks > 1) {
-            if (works && ks > 0) {
-                const int slot = (ks - 1) * n_blocks + blk;
-                if (h == 0) { s_ml[(slot * 32 + r) * 2] = m_run; s_ml[(slot * 32 + r) * 2 + 1] = l_run; }
+            // ---- waves that share rows: all sums to LDS (16-byte pieces of a row XORed by its number: its banks), then a row's four columns to a thread ----
+            float* const s_o = reinterpret_cast<float*>(smem);
+            if (works) {
+                const int row = (ks * n_blocks + blk) * 32 + r;
+                if (h == 0) *reinterpret_cast<float2*>(plan.ml + 2 * row) = float2{m_run, l_run};
 #pragma unroll
                 for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
                     for (int i4 = 0; i4 < 4; ++i4)
-                        *reinterpret_cast<floatx4*>(s_o + (slot * 32 + r) * O_STRIDE + jb * 32 + i4 * 8 + h * 4) =
+                        *reinterpret_cast<floatx4*>(s_o + row * D + ((jb * 8 + i4 * 2 + h) ^ (r & (D / 4 - 1))) * 4) =
                             floatx4{o[jb][4 * i4], o[jb][4 * i4 + 1], o[jb][4 * i4 + 2], o[jb][4 * i4 + 3]};
             }
             __syncthreads();
-            if (works && ks == 0) {
-                for (int k = 1; k < n_ks; ++k) {
-                    const int slot = (k - 1) * n_blocks + blk;
-                    const float m2 = s_ml[(slot * 32 + r) * 2], l2 = s_ml[(slot * 32 + r) * 2 + 1];
-                    const float m_new = fmaxf(m_run, m2), m_ref = m_new == -INFINITY ? 0.f : m_new;
-                    const float w1 = fast_exp2(m_run - m_ref), w2 = fast_exp2(m2 - m_ref);
-                    m_run = m_new;
-                    l_run = l_run * w1 + l2 * w2;
+            for (int at = threadIdx.x; at < n_rows * (D / 4); at += kRowsThreads) {
+                const int row = at / (D / 4), c = at % (D / 4);
+                float2 ml[kChunks];
+                float m = -INFINITY, l = 0.f;
 #pragma unroll
-                    for (int jb = 0; jb < JB; ++jb)
+                for (int k = 0; k < kChunks; ++k) {
+                    ml[k] = k < n_ks ? *reinterpret_cast<const float2*>(plan.ml + 2 * (k * n_blocks * 32 + row)) : float2{-INFINITY, 0.f};
+                    m = fmaxf(m, ml[k].x);
+                }
+                const float m_ref = m == -INFINITY ? 0.f : m;
+                floatx4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int i4 = 0; i4 < 4; ++i4) {
-                            const floatx4 y = *reinterpret_cast<const floatx4*>(s_o + (slot * 32 + r) * O_STRIDE + jb * 32 + i4 * 8 + h * 4);
+                for (int k = 0; k < kChunks; ++k) {
+                    if (k >= n_ks) break;
+                    const float w = fast_exp2(ml[k].x - m_ref);
+                    l += ml[k].y * w;
+                    const floatx4 y = *reinterpret_cast<const floatx4*>(s_o + (k * n_blocks * 32 + row) * D + (c ^ (row & 31 & (D / 4 - 1))) * 4);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float a = o[jb][4 * i4 + i];
-                                o[jb][4 * i4 + i] = (fabsf(a) == INFINITY ? a : a * w1) + (fabsf(y[i]) == INFINITY ? y[i] : y[i] * w2);
-                            }
-                        }
+                    for (int i = 0; i < 4; ++i) sum[i] += fabsf(y[i]) == INFINITY ? y[i] : y[i] * w;
+                }
+                if (direct) {
+                    const QuotRem at_q = divide(row0 + row, p.group, p.inv_group);
+                    const int64_t tok = en.q0 + at_q.q;
+                    const int hd = g * p.group + at_q.r;
+                    *reinterpret_cast<bf16x4*>(p.out + tok * p.q_tok + (int64_t)hd * p.q_head + c * 4) = __builtin_convertvector(sum * inverse(l), bf16x4);
+                    if (p.lse && c == 0) p.lse[tok * p.n_q_heads + hd] = l == 0.f ? -INFINITY : (m + fast_log2(l)) * kLn2;
+                } else {
+                    *reinterpret_cast<floatx4*>(p.part_o + (part + row) * D + c * 4) = sum;
+                    if (c == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (part + row)) = float2{m, l};
                 }
             }
-        }
-        if (works && ks == 0 && my_row < n_rows) {
+        } else if (works && my_row < n_rows) {
             if (direct) {
-                const float inv = l_run > 0.f ? 1.f / l_run : l_run == 0.f ? 0.f : NAN;
+                const float inv = inverse(l_run);
                 __bf16* const op = p.out + q_tok * p.q_tok + (int64_t)q_hd * p.q_head + h * 4;
 #pragma unroll
                 for (int jb = 0; jb < JB; ++jb)
@@ -599,36 +682,42 @@ void rows_kernel(const RowsParams p)
                     }
                 if (p.lse && h == 0) p.lse[q_tok * p.n_q_heads + q_hd] = l_run == 0.f ? -INFINITY : (m_run + fast_log2(l_run)) * kLn2;
             } else {
-                const int64_t row = part_row(j, front.rows + g * padded_rows(p, en) + row0 + my_row);
-                if (h == 0) { p.part_ml[2 * row] = m_run; p.part_ml[2 * row + 1] = l_run; }
+                if (h == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (part + my_row)) = float2{m_run, l_run};
 #pragma unroll
                 for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
                     for (int i4 = 0; i4 < 4; ++i4)
-                        *reinterpret_cast<floatx4*>(p.part_o + row * D + jb * 32 + i4 * 8 + h * 4) =
+                        *reinterpret_cast<floatx4*>(p.part_o + (part + my_row) * D + jb * 32 + i4 * 8 + h * 4) =
                             floatx4{o[jb][4 * i4], o[jb][4 * i4 + 1], o[jb][4 * i4 + 2], o[jb][4 * i4 + 3]};
             }
         }
-        if (x < x_end) {
-            __syncthreads();                                 // the ring, and what the plan holds, are free again
-            publish();
-            __syncthreads();
-        }
+        __syncthreads();                                     // the ring, and what the plan holds, are free again
     }
 }
 
-// Joins the pieces of the rows that were cut (one that was not is in its place already), D / 4 threads to a row.
-template <int D, bool PAGED>
+// Joins the pieces of the rows that were cut (one that was not is in its place already): D / 4 threads to a row, and `GP` groups of them take every GP-th
+// of its pieces (GP = 1: a wave to as many rows as it holds).
+template <int D, bool PAGED, int GP>
 __global__ __launch_bounds__(256)
 void rows_join_kernel(const RowsParams p)
 {
-    constexpr int TPR = D / 4, RPW = kWave / TPR;            // threads of a row, rows of a wave: heads of one query
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int TPR = D / 4, RPW = kWave / TPR, WAVES = 4;       // threads of a row, rows of a wave
+    static_assert(GP == 1 || GP == 256 / TPR, "a wave's row, or the workgroup's");
+    __shared__ float s_ml[GP > 1 ? 2 * GP : 1];
+    __shared__ __align__(16) float s_o[GP > 1 ? GP * D : 4];
+    const int lane = threadIdx.x & 63, group = threadIdx.x / TPR, c = threadIdx.x % TPR;
     const int units = (p.n_q_heads + RPW - 1) / RPW;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
-    const int tok = (int)(unit / units);
+    int tok, hd;
+    if constexpr (GP == 1) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int64_t unit = (int64_t)blockIdx.x * WAVES + wave;
+        tok = (int)(unit / units);
+        hd = (int)(unit - (int64_t)tok * units) * RPW + lane / TPR;
+    } else {
+        tok = blockIdx.x / p.n_q_heads;
+        hd = blockIdx.x - tok * p.n_q_heads;
+    }
     if (tok >= p.n_queries) return;
-    const int hd = (int)(unit - (int64_t)tok * units) * RPW + lane / TPR, c = lane % TPR;
     // the request
     int b = 0;
     if (!p.cu_q) {
@@ -642,39 +731,43 @@ void rows_join_kernel(const RowsParams p)
         if (!behind) return;                                 // (a row behind the last request)
         b += __builtin_ctzll(behind);
     }
-    const int entries = PAGED ? 2 * p.batch : p.batch, e = PAGED ? p.batch + b : b;
-    const int run = p.starts[2 * entries];
-    const Entry own = entry_of<PAGED>(p, e, p.starts[2 * entries + 1]);
-    if (run == 0 || own.n_q <= 0 || tok < own.q0 || hd >= p.n_q_heads) return;
+    const RowsStart own = p.starts[PAGED ? p.batch + b : b];
+    const int total = own.total, sharers = sharers_of(p, total);
+    if (total == 0 || own.n_q <= 0 || tok < own.q0 || hd >= p.n_q_heads) return;
     const QuotRem head = divide(hd, p.group, p.inv_group);
     struct Pieces { int first, n, row; };                    // workgroups that have one, the row of their results
-    const auto pieces_of = [&](int e, const Entry& en) {
-        const int row = (tok - en.q0) * p.group + head.r, tiles = tiles_of(en);
+    const auto pieces_of = [&](const RowsStart& s) {
+        const Entry en = {s.q0, s.n_q, s.key0, s.key1, -1};
+        const int row = (tok - en.q0) * p.group + head.r, chunks = chunks_of(en);
         const Sets sets = sets_of(en.n_q * p.group);
-        const int x = p.starts[2 * e] + (head.q * sets.n + row / (sets.blocks * 32)) * tiles;
-        const int first = x / run;
-        return Pieces{first, (x + tiles - 1) / run - first + 1, p.starts[2 * e + 1] + head.q * padded_rows(p, en) + row};
+        const int x = s.work + (head.q * sets.n + row / (sets.blocks * 32)) * (chunks + kBegin) + kBegin;
+        const int first = sharer_of(x, total, sharers);
+        return Pieces{first, sharer_of(x + chunks - 1, total, sharers) - first + 1, s.rows + head.q * padded_rows(p, en) + row};
     };
-    const Pieces mine = pieces_of(e, own);
+    const Pieces mine = pieces_of(own);
     Pieces theirs = {0, 0, 0};
-    if (PAGED && own.key0 > 0) {
-        const int first = p.groups[b];
-        theirs = pieces_of(first, shared_entry(p, first));
-    } else if (mine.n == 1) {
-        return;
-    }
+    if (PAGED && own.key0 > 0) theirs = pieces_of(p.starts[own.first]);
+    else if (mine.n == 1) return;
     const int n = theirs.n + mine.n;
     const auto row_of = [&](int i) { return i < theirs.n ? part_row(theirs.first + i, theirs.row) : part_row(mine.first + i - theirs.n, mine.row); };
+    const int g0 = GP == 1 ? 0 : group;                      // this group's first piece
     float m = -INFINITY, l = 0.f;
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int i0 = 0; i0 < n; i0 += TPR) {
+    for (int i0 = g0; i0 < n; i0 += TPR * GP) {
         // a piece to a thread: its maximum and sum;  then the outputs, weighted by their thread's word
         float pm = -INFINITY, pl = 0.f;
-        if (i0 + c < n) {
-            const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * row_of(i0 + c));
+        if (i0 + c * GP < n) {
+            const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * row_of(i0 + c * GP));
             pm = ml.x;
             pl = ml.y;
         }
+        const int most = min(TPR, (n - i0 + GP - 1) / GP);
+        floatx4 y[4];
+        const auto fetch = [&](int i1) {                     // (behind the last piece: the last again, left out)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) y[u] = *reinterpret_cast<const floatx4*>(p.part_o + row_of(i0 + min(i1 + u, most - 1) * GP) * D + c * 4);
+        };
+        fetch(0);
         float top = pm;
 #pragma unroll
         for (int d = 1; d < TPR; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
@@ -687,21 +780,33 @@ void rows_join_kernel(const RowsParams p)
         m = m_new;
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = fabsf(o[i]) == INFINITY ? o[i] : o[i] * keep;
-        const int most = min(TPR, n - i0);
-        for (int i1 = 0; i1 < most; i1 += 4) {               // (behind the last piece: the last again, left out)
-            floatx4 y[4];
-            float wi[4];
+        for (int i1 = 0; i1 < most; i1 += 4) {
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int i = min(i1 + u, most - 1);
-                y[u] = *reinterpret_cast<const floatx4*>(p.part_o + row_of(i0 + i) * D + c * 4);
-                wi[u] = __shfl(w, (lane & ~(TPR - 1)) + i);
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
+                const float wi = __shfl(w, (lane & ~(TPR - 1)) + min(i1 + u, most - 1));
                 if (i1 + u < most)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) o[k] += fabsf(y[u][k]) == INFINITY ? y[u][k] : y[u][k] * wi[u];
+                    for (int k = 0; k < 4; ++k) o[k] += fabsf(y[u][k]) == INFINITY ? y[u][k] : y[u][k] * wi;
+            }
+            if (i1 + 4 < most) fetch(i1 + 4);
+        }
+    }
+    if constexpr (GP > 1) {
+        if (c == 0) { s_ml[2 * group] = m; s_ml[2 * group + 1] = l; }
+        *reinterpret_cast<floatx4*>(s_o + group * D + c * 4) = o;
+        __syncthreads();
+        if (group > 0) return;
+        for (int k = 1; k < GP; ++k) m = fmaxf(m, s_ml[2 * k]);
+        const float m_ref = m == -INFINITY ? 0.f : m;
+        l = 0.f;
+        o = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < GP; ++k) {
+            const float w = fast_exp2(s_ml[2 * k] - m_ref);
+            l += s_ml[2 * k + 1] * w;
+            const floatx4 y = *reinterpret_cast<const floatx4*>(s_o + k * D + c * 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] += fabsf(y[i]) == INFINITY ? y[i] : y[i] * w;
         }
     }
     const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
@@ -721,7 +826,7 @@ int64_t rows_parts(bool paged, int workgroups, int batch, int n_queries, int n_q
 size_t rows_workspace(bool paged, int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim)
 {
     const size_t rows = (size_t)rows_parts(paged, kNumCu, batch, n_queries, n_q_heads, n_kv_heads);
-    return align256(rows * head_dim * sizeof(float)) + align256(rows * 2 * sizeof(float)) + align256(((size_t)(paged ? 4 : 2) * batch + 2) * sizeof(int32_t));
+    return align256(rows * head_dim * sizeof(float)) + align256(rows * 2 * sizeof(float)) + align256((size_t)(paged ? 2 : 1) * batch * sizeof(RowsStart));
 }
 bool rows_shape(int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim)
 {
@@ -734,13 +839,17 @@ int launch_rows(RowsParams& p, hipStream_t stream)
     constexpr int lds = 4 * kRowsTile * D * 2 + (int)sizeof(RowsPlan);
     if (const int rc = allow_lds<&rows_kernel<D, PAGED>>(lds)) return rc;
     const int units = (p.n_q_heads + 256 / D - 1) / (256 / D);
-    const int64_t joins = ((int64_t)p.n_queries * units + 3) / 4;
+    const int64_t rows = (int64_t)p.n_queries * p.n_q_heads;
+    // few rows have many pieces each
+    const bool few = rows <= 2048;
+    const int64_t joins = few ? rows : ((int64_t)p.n_queries * units + 3) / 4;
     if (!launchable(joins, 256)) return SPECVLM_EUNSUPPORTED;
     p.workgroups = kNumCu;
     p.padded = round_up(p.workgroups, kNumXcd);
     rows_kernel<D, PAGED><<<p.padded, kRowsThreads, lds, stream>>>(p);
     if (const int rc = launch_status()) return rc;
-    rows_join_kernel<D, PAGED><<<(unsigned)joins, 256, 0, stream>>>(p);
+    if (few) rows_join_kernel<D, PAGED, 1024 / D><<<(unsigned)joins, 256, 0, stream>>>(p);
+    else rows_join_kernel<D, PAGED, 1><<<(unsigned)joins, 256, 0, stream>>>(p);
     return launch_status();
 }
 
@@ -757,7 +866,7 @@ int rows_start(RowsParams& p, bool paged, const void* q, int64_t q_tok, int64_t 
     const int64_t rows = (int64_t)n_queries * n_q_heads, entries = paged ? 2 * (int64_t)batch : batch;
     if (rows >= ((int64_t)1 << 29) || entries * 32 * n_kv_heads >= ((int64_t)1 << 29)) return SPECVLM_EUNSUPPORTED;
     const int64_t sets = (2 * rows / kSetRows + n_kv_heads) + entries * n_kv_heads;
-    if (sets * (most_keys / kRowsTile + 1) >= ((int64_t)1 << 31) - 65536) return SPECVLM_EUNSUPPORTED;
+    if (sets * (most_keys / 32 + 1 + kBegin) >= ((int64_t)1 << 31)) return SPECVLM_EUNSUPPORTED;
     const size_t need = rows_workspace(paged, batch, n_queries, n_q_heads, n_kv_heads, head_dim);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return SPECVLM_EWORKSPACE;
     p = {};
@@ -771,7 +880,7 @@ int rows_start(RowsParams& p, bool paged, const void* q, int64_t q_tok, int64_t 
     const size_t parts = (size_t)rows_parts(paged, kNumCu, batch, n_queries, n_q_heads, n_kv_heads);
     p.part_o = (float*)workspace;
     p.part_ml = (float*)((char*)workspace + align256(parts * head_dim * sizeof(float)));
-    p.starts = (int32_t*)((char*)p.part_ml + align256(parts * 2 * sizeof(float)));
+    p.starts = (RowsStart*)((char*)p.part_ml + align256(parts * 2 * sizeof(float)));
     return SPECVLM_OK;
 }
 
