@@ -603,8 +603,8 @@ int specvlm_pages_shared(
  * Everything else, hidden and infinite values, skipped requests and rows behind the last one
  * too, is as for specvlm_paged_attn.  Results do not depend on the run; they may differ by
  * roundings with the other requests of the batch and the groups.
- * Limits: n_queries * H_q < 2^29, batch * H_kv < 2^23, (n_queries * H_q / 128 + (2 * batch + 1) * H_kv)
- * * (kv_len / 128 + 1) < 2^31 - 2^16, kv_len <= 2^30.
+ * Limits: n_queries * H_q up to 2^26 is always served (a launch's threads); batch * H_kv < 2^23,
+ * (n_queries * H_q / 128 + (2 * batch + 1) * H_kv) * (kv_len / 32 + 6) < 2^31, kv_len <= 2^30.
  * -------------------------------------------------------------------------- */
 size_t specvlm_shared_attn_workspace_bytes(int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim);
 
@@ -636,8 +636,8 @@ int specvlm_shared_attn(
  * for specvlm_paged_attn.  An entry whose offsets leave the tensors or descend is skipped, its
  * rows of out and lse left as they are, as are rows of no entry.  Results do not depend on
  * the run.
- * Limits: n_queries * H_q < 2^29, batch * H_kv < 2^24, (n_queries * H_q / 128 + (batch + 1) * H_kv)
- * * (n_states / 128 + 1) < 2^31 - 2^16, n_states <= 2^30.
+ * Limits: n_queries * H_q up to 2^26 is always served (a launch's threads); batch * H_kv < 2^24,
+ * (n_queries * H_q / 128 + (batch + 1) * H_kv) * (n_states / 32 + 6) < 2^31, n_states <= 2^30.
  * -------------------------------------------------------------------------- */
 size_t specvlm_cross_attn_workspace_bytes(int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim);
 

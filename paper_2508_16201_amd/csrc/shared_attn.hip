@@ -455,8 +455,8 @@ void rows_kernel(const RowsParams p)
                 else hi = min(hi, before + q_at.q + 1);
             }
         } else if (p.ranges) {
-            lo = max(p.ranges[2 * q_tok], 0);
-            hi = min(p.ranges[2 * q_tok + 1], key1);
+            lo = min(max(p.ranges[2 * q_tok], 0), key1);
+            hi = min(max(p.ranges[2 * q_tok + 1], 0), key1);
         }
         // of all of the wave's rows: keys that all see, and that some see
         int all_lo = lo, all_hi = is_tree ? min(before, hi) : hi, any_lo = lo < hi ? lo : INT_MAX, any_hi = lo < hi ? hi : 0;
