@@ -9,14 +9,15 @@
 // cut into pieces (of the shared keys, of its own), and pieces are joined by  o = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
 // Statistics, sums and partial outputs are fp32, the output is rounded once.
 //
-// Work decomposition.  Rows of a kv head (query, head of the group) are taken 256 at a time ("a set"), keys in tiles of 128.  The
-// tiles of all sets, heads and requests are numbered one after the other, and each workgroup takes a run of equal length, which it
+// Work decomposition.  Rows of a kv head (query, head of the group) are taken 256 at a time ("a set"), keys 32 at a time.  The
+// keys of all sets, heads and requests are numbered one after the other, and each workgroup takes a run of equal length, which it
 // finds by a prefix sum over the requests: lengths and groups are on the device, and a captured launch serves them as they change.
 // A piece that is all a row has is written out directly; the others leave partial results that the second launch joins.
 //
 // A workgroup has eight waves of 32 rows (v_mfma_f32_32x32x16_bf16 with the keys as rows of the product and the queries as its
 // columns: a lane then holds 16 logits of one row, which are, packed, the second product's operand).  Where a set has fewer rows,
-// two or four waves share them and take every other 32 keys.  Tiles go to LDS by direct loads, two in turn.
+// two or four waves share them and take every second or fourth 32 keys.  Tiles of 128 keys go to LDS by direct loads, two in
+// turn.
 #include <climits>
 #include <type_traits>
 
@@ -140,35 +141,60 @@ struct Sets { int n, blocks; };              // blocks: of a set
 __device__ __forceinline__ Sets sets_of(int rows)
 {
     const int blocks = (rows + 31) >> 5, n = (blocks + kRowsWaves - 1) / kRowsWaves;
-    return {n, n > 1 ? (blocks + n - 1) / n : blocks};
+    return {n, n > 1 ? (int)((uint32_t)(blocks + n - 1) / (uint32_t)n) : blocks};
 }
 __device__ __forceinline__ int chunks_of(const Entry& e) { return max(1, (e.key1 - e.key0 + 31) >> 5); }       // of 32 keys
 
 __device__ __forceinline__ int padded_rows(const RowsParams& p, const Entry& e) { return (e.n_q * p.group + 31) & ~31; }      // of a kv head
 
-// Work is counted in 32 keys of a set, and an item has kBegin more in front of its first: what a piece costs before and behind its keys.
-constexpr int kBegin = 5, kLeastRun = 9;
+// Work is counted in the time that 32 keys of a set take, and an item has kBegin more in front of its first: what a piece costs before and behind its keys.
+constexpr int kBegin = 15, kLeastRun = 12;
+__device__ __forceinline__ bool narrow(int blocks) { return blocks <= 4; }
+__device__ __forceinline__ int chunk_work(int blocks) { return narrow(blocks) ? 2 : 3; }
 
 struct Numbers { int work, rows; };          // of an entry, or in front of one
 __device__ __forceinline__ Numbers numbers_of(const RowsParams& p, const Entry& e)
 {
     if (e.n_q <= 0) return {0, 0};
-    return {sets_of(e.n_q * p.group).n * p.n_kv_heads * (chunks_of(e) + kBegin), padded_rows(p, e) * p.n_kv_heads};
+    const Sets sets = sets_of(e.n_q * p.group);
+    return {sets.n * p.n_kv_heads * (chunks_of(e) * chunk_work(sets.blocks) + kBegin), padded_rows(p, e) * p.n_kv_heads};
 }
 
 // The row of the partial results that workgroup j's piece of an item has: the rows of all items one after the other, and 256 on for every workgroup, so
 // that two pieces of an item do not meet, nor two items of a workgroup.
 __device__ __forceinline__ int64_t part_row(int j, int row_of_items) { return (int64_t)j * kSetRows + row_of_items; }
 
-// The work is dealt to `sharers` workgroups, to j from j * total / sharers on.
-__device__ __forceinline__ int sharers_of(const RowsParams& p, int total) { return min(p.workgroups, max(1, total / kLeastRun)); }
-__device__ __forceinline__ int share_begin(int j, int total, int sharers) { return (int)((int64_t)j * total / sharers); }
-__device__ __forceinline__ int sharer_of(int x, int total, int sharers) { return (int)((((int64_t)x + 1) * sharers - 1) / total); }
+// The work is dealt to `n` workgroups: the first `more` have one more than `each`.
+struct Shares {
+    int n, each, more;
+    __device__ __forceinline__ int begin(int j) const { return j * each + min(j, more); }
+    __device__ __forceinline__ int of(int x) const
+    {
+        const int wide = more * (each + 1);
+        return x < wide ? (int)((uint32_t)x / (uint32_t)(each + 1)) : more + (int)((uint32_t)(x - wide) / (uint32_t)max(each, 1));
+    }
+};
+__device__ __forceinline__ Shares shares_of(const RowsParams& p, int total)
+{
+    const int n = min(p.workgroups, max(1, total / kLeastRun)), each = (int)((uint32_t)total / (uint32_t)n);
+    return {n, each, total - each * n};
+}
+
+// A workgroup's part of an item: a set of rows of a kv head, and some of its keys.
+struct Piece {
+    int b, own;                              // request or entry; whether the keys are its own
+    int q0, n_q, end;                        // the entry's queries, and the end of its keys
+    int g, row0, n_rows;                     // kv head, the set's rows
+    int key0, key1;                          // the piece's keys
+    int direct;                              // whether they are all that the rows see
+    int64_t part;                            // the first row of its partial results
+};
 
 // LDS behind the tiles:  what a workgroup knows of 512 entries.
 struct RowsPlan {
     Entry entry[kRowsThreads];
     Numbers front[kRowsThreads];
+    int work[kRowsThreads];
     Numbers wave[kRowsWaves];
     float ml[kSetRows * 2];                  // maxima and sums of waves that share rows
     int word[3][kRowsThreads / 2];           // of requests
@@ -238,41 +264,6 @@ template <class T> __device__ __forceinline__ SPECVLM_AS3 T* in_lds(uint32_t at)
 
 __device__ __forceinline__ uint32_t first_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 
-// See take_odd_values of the paged attention:  a value that is no finite number is left out of the products, and the rows that see its key get it by how many such values they see.
-// sees8: bit e is set if the lane's row sees the key of contraction index 8h + e.
-__device__ __forceinline__ void take_odd_rows(bf16x8& vf, uint32_t sees8, floatx16& o)
-{
-    floatx16 none;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) none[i] = 0.f;
-    const floatx16 odd = mfma32(vf, __builtin_bit_cast(bf16x8, u32x4{}), none);
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) sum += odd[i];
-    if (__builtin_expect(__any(!(sum == 0.f)), 0)) {
-        u32x4 seen, w = __builtin_bit_cast(u32x4, vf), up, down, nan;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t two = sees8 >> (2 * e);
-            seen[e] = (two & 1u) * 0x3f80u | (two & 2u) * (0x3f800000u / 2);
-            const uint32_t size = w[e] & 0x7fff7fffu, odd2 = (size + 0x00800080u) >> 15 & 0x00010001u;
-            nan[e] = (size + 0x007f007fu) >> 15 & 0x00010001u;
-            down[e] = (odd2 ^ nan[e]) & w[e] >> 15;
-            up[e] = odd2 ^ nan[e] ^ down[e];
-            w[e] &= ~(odd2 * 0xffffu);
-        }
-        vf = __builtin_bit_cast(bf16x8, w);
-        const auto count = [&](u32x4 x) { return mfma32(__builtin_bit_cast(bf16x8, x * 0x3f80u), __builtin_bit_cast(bf16x8, seen), none); };
-        const floatx16 n_up = count(up), n_down = count(down), n_nan = count(nan);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            if (n_up[i] > 0.f) o[i] += INFINITY;
-            if (n_down[i] > 0.f) o[i] += -INFINITY;
-            if (n_nan[i] > 0.f) o[i] = NAN;
-        }
-    }
-}
-
 __device__ __forceinline__ float half_max(float x)
 {
     auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -284,24 +275,353 @@ __device__ __forceinline__ float half_sum(float x)
     return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
+// Takes a piece and writes what comes of it.
+template <int D, bool PAGED>
+__device__ __forceinline__ void rows_piece(const RowsParams& p, RowsPlan& plan, const uint32_t lds0, const Piece& pc)
+{
+    constexpr int KK = D / 16, JB = D / 32, CH = D / 8, ROW_BYTES = D * 2;
+    constexpr int TILE_BYTES = kRowsTile * ROW_BYTES;        // of K or V
+    constexpr int KEYS_PER_LOAD = kWave / CH, LOADS = 16 / KEYS_PER_LOAD;
+    static_assert(kSetRows * D * 4 <= 4 * TILE_BYTES, "the exchange of waves that share rows");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 31, h = lane >> 5;
+    const float sc = fmaxf(p.scale_log2, 1e-30f);            // (a zero scale as a vanishing one: -inf stays -inf)
+    const int n_blocks = (pc.n_rows + 31) >> 5, log_blocks = n_blocks > 4 ? 3 : n_blocks > 2 ? 2 : n_blocks - 1;       // waves of a kind
+    const int blk = wave & ((1 << log_blocks) - 1), ks = wave >> log_blocks, n_ks = min(kChunks, kRowsWaves >> log_blocks);
+    const bool works = blk < n_blocks && ks < n_ks;
+    const bool two_parts = narrow(n_blocks);
+    const int key0 = pc.key0, key1 = pc.key1, tiles = (key1 - key0 + kRowsTile - 1) / kRowsTile;
+
+    // ---- loads: wave w brings keys 16w..16w+15 of a tile ----
+    const int64_t kv0 = (int64_t)pc.g * p.head + (PAGED ? 0 : (int64_t)(p.cu_kv ? __builtin_amdgcn_readfirstlane(p.cu_kv[pc.b]) : 0) * p.tok);
+    const char* const k_at = reinterpret_cast<const char*>(p.k + kv0);
+    const char* const v_at = reinterpret_cast<const char*>(p.v + kv0);
+    int ids = 0, places = 0;                             // of the next 64 tiles, one to a lane
+    const auto look_up = [&](int tile) {
+        const int key = min(key0 + (tile + lane) * kRowsTile + wave * 16, (key1 - 1) & ~15);
+        const QuotRem pg = divide(key, p.page_size, p.inv_page);
+        ids = p.table[(int64_t)pc.b * p.table_row + pg.q];
+        places = pg.r;
+    };
+    const auto issue = [&](int tile, int stage) {
+        const uint32_t to = lds0 + stage * 2 * TILE_BYTES + wave * 16 * ROW_BYTES;
+        int64_t first;
+        const int key = key0 + tile * kRowsTile + wave * 16;
+        int last;                                        // the last of the 16 keys that there is: it stands for those behind it, whatever lies there
+        if constexpr (PAGED) {
+            const int l = tile & 63;
+            if (l == 0 && tile > 0) look_up(tile);
+            const int id = __builtin_amdgcn_readlane(ids, l), row = __builtin_amdgcn_readlane(places, l);
+            // (a page that is not one of the pool's is not read: the pool's first is, and its keys are masked)
+            const bool there = (uint32_t)id < (uint32_t)p.n_pages;
+            if (lane == 0) plan.ok[stage][wave] = there;
+            first = (there ? id : 0) * p.page + row * p.tok;
+            last = key < key1 ? key1 - 1 - key : (key1 - 1) & 15;        // (a group behind the last: that one again)
+        } else {
+            first = (int64_t)min(key, key1 - 1) * p.tok;
+            last = max(key1 - 1 - key, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int kl = i * KEYS_PER_LOAD + lane / CH, piece = lane % CH;
+            const uint32_t row = (uint32_t)min(kl, last) * (uint32_t)(p.tok * 2);
+            load_to_lds(k_at + 2 * first, row + (piece ^ (D == 128 ? kl & 15 : kl >> 1 & 7)) * 16, to + i * 1024);
+            load_to_lds(v_at + 2 * first, row + (piece ^ rows_v_swizzle<D>(kl)) * 16, to + TILE_BYTES + i * 1024);
+        }
+    };
+    const auto begin_loads = [&] {
+        if constexpr (PAGED) look_up(0);
+        issue(0, 0);
+    };
+    if (tiles > 0) begin_loads();                        // (on their way while the rows are looked at)
+
+    // this wave's rows
+    const int my_row = blk * 32 + r;
+    const QuotRem q_at = divide(pc.row0 + (my_row < pc.n_rows ? my_row : 0), p.group, p.inv_group);  // (padding rows take the first: never stored)
+    const int64_t q_tok = pc.q0 + q_at.q;
+    const int q_hd = pc.g * p.group + q_at.r;
+    bf16x8 qf[KK];
+    const __bf16* const qp = p.q + q_tok * p.q_tok + (int64_t)q_hd * p.q_head + h * 8;
+#pragma unroll
+    for (int s = 0; s < KK; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qp + s * 16);
+    // the keys that it sees: [lo, hi), of the block those of a tree node's mask
+    int lo = key0, hi = key1;
+    const int before = pc.end - pc.n_q;                 // (own keys of a block)
+    uint64_t tree = 0;
+    bool is_tree = false;
+    if constexpr (PAGED) {
+        if (pc.own) {
+            is_tree = p.block_mask != nullptr;
+            if (is_tree) tree = p.block_mask[q_tok];
+            else hi = min(hi, before + q_at.q + 1);
+        }
+    } else if (p.ranges) {
+        lo = min(max(p.ranges[2 * q_tok], 0), key1);
+        hi = min(max(p.ranges[2 * q_tok + 1], 0), key1);
+    }
+    // of all of the wave's rows: keys that all see, and that some see
+    int all_lo = lo, all_hi = is_tree ? min(before, hi) : hi, any_lo = lo < hi ? lo : INT_MAX, any_hi = lo < hi ? hi : 0;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        all_lo = max(all_lo, __shfl_xor(all_lo, d)); all_hi = min(all_hi, __shfl_xor(all_hi, d));
+        any_lo = min(any_lo, __shfl_xor(any_lo, d)); any_hi = max(any_hi, __shfl_xor(any_hi, d));
+    }
+    all_lo = __builtin_amdgcn_readfirstlane(all_lo); all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+    any_lo = __builtin_amdgcn_readfirstlane(any_lo); any_hi = __builtin_amdgcn_readfirstlane(any_hi);
+
+    float m_run, l_run;
+    floatx16 o[JB];
+    // where this lane reads in a stage
+    const uint32_t k_base = lds0 + r * ROW_BYTES + (h ^ (D == 128 ? r & 15 : r >> 1 & 7)) * 16;
+    const int v_row = 4 * h + ((lane & 15) >> 2);
+    const uint32_t v_base = lds0 + TILE_BYTES + v_row * ROW_BYTES + ((((lane >> 4 & 1) * 2 + ((lane & 3) >> 1)) ^ rows_v_swizzle<D>(v_row)) * 16) + (lane & 1) * 8;
+
+    // V^T fragments of 16 keys, by the transposing read
+    const auto read_values = [&](bf16x8 (&vf)[JB], uint32_t at) {
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb) {
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            SPECVLM_AS3 s16x4* const src = in_lds<s16x4>(v_base + at ^ jb * 64);
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(src);
+            const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16(src + 8 * ROW_BYTES / 8);
+            vf[jb] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    };
+
+    const auto read_keys = [&](bf16x8 (&kf)[KK], uint32_t at) {
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) kf[kk] = __builtin_bit_cast(bf16x8, *in_lds<const u32x4>(k_base + at ^ kk * 32));
+    };
+    // S^T = K Q^T for 32 keys
+    const auto logits = [&](const bf16x8 (&kf)[KK]) {
+        floatx16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) s = mfma32(kf[kk], qf[kk], s);
+        return s;
+    };
+    bool fresh = true;                                   // some row has seen nothing yet
+    // Probabilities against the maximum with these logits too, to which the sums are brought.
+    const auto raise = [&](const floatx16& s, float (&pv)[16]) {
+        float mx = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+        const float m_new = fmaxf(m_run, half_max(mx) * sc);
+        const float m_ref = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = fast_exp2(m_run - m_ref);
+        const bool rescale = m_new != m_run;
+        m_run = m_new;
+        float psum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { pv[i] = fast_exp2(fmaf(s[i], sc, -m_ref)); psum += pv[i]; }
+        l_run = l_run * alpha + psum;
+        if (__any(rescale)) {
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[jb][i] *= alpha;
+        }
+    };
+    // Probabilities of the keys from k0 on (two: whether the pages of the first and the second 16 are there), against the running maximum.
+    const auto weigh = [&](floatx16 s, int k0, uint32_t two, float (&pv)[16]) {
+        const bool need_mask = two != 0x101u || k0 < all_lo || k0 + 32 > all_hi;
+        if (need_mask) {
+            uint32_t sees = first_bits(hi - k0) & ~first_bits(lo - k0) & ((two & 1 ? 0xffffu : 0u) | (two & 0x100 ? 0xffff0000u : 0u));
+            if (is_tree) {
+                const int in = k0 - before;
+                const uint64_t block = in >= 0 ? (in < 64 ? tree >> in : 0) : (in > -32 ? tree << -in : 0);
+                sees &= (uint32_t)block | first_bits(-in);
+            }
+            sees >>= 4 * h;                                  // bit 8(i/4) + i%4: the lane's i-th key
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = sees >> (8 * (i / 4) + i % 4) & 1u ? s[i] : -INFINITY;
+        }
+        // Away from the masks the exponentials are taken against the reference that the earlier keys left, and the maximum is tracked only where a
+        // lane's sum does not stay moderate.
+        if (!need_mask && !fresh) {
+            float psum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) { pv[i] = fast_exp2(fmaf(s[i], sc, -m_run)); psum += pv[i]; }
+            if (!__any(!(psum < kRowsRedo))) {
+                l_run += psum;
+                return;
+            }
+        }
+        raise(s, pv);
+        fresh = __any(!(m_run > -INFINITY));
+    };
+    const auto begin_sums = [&] {
+        m_run = -INFINITY;
+        l_run = 0.f;
+        fresh = true;
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[jb][i] = 0.f;
+    };
+    const auto pages_there = [&](int stage) {            // a byte for 16 keys of the tile
+        if constexpr (!PAGED) return (uint64_t)0x0101010101010101ull;
+        const u32x2 ok = *reinterpret_cast<const u32x2*>(plan.ok[stage]);
+        return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(ok[1]) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane(ok[0]);
+    };
+    const auto lds_done = [] { __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+
+    // The sweep.
+    const auto sweep = [&] {
+        begin_sums();
+        if (tiles <= 0) return;
+        for (int t = 0; t < tiles; ++t) {
+            const int stage = t & 1;
+            wait_vmcnt<0>();
+            lds_done();
+            stage_barrier();                             // the tile is there for everyone, and everyone has left the other stage
+            if (t + 1 < tiles) issue(t + 1, stage ^ 1);
+            if (!works) continue;
+            const uint64_t there = pages_there(stage);
+            for (int ch = ks; ch < kChunks; ch += n_ks) {
+                const int k0 = key0 + t * kRowsTile + ch * 32;
+                if (k0 >= any_hi || k0 + 31 < any_lo) continue;
+                const uint32_t at_chunk = stage * 2 * TILE_BYTES + ch * 32 * ROW_BYTES;
+                bf16x8 kf[KK], vf[2][JB];
+                read_keys(kf, at_chunk);
+                const floatx16 s = logits(kf);
+                // (the reads of all of them first: one by one, each waits for its own)
+                __builtin_amdgcn_sched_group_barrier(0x100, KK, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, KK, 0);
+                read_values(vf[0], at_chunk);
+                float pv[16];
+                const uint32_t two = PAGED ? (uint32_t)(there >> (16 * ch)) & 0xffffu : 0x101u;
+                weigh(s, k0, two, pv);
+                // ---- O^T += V^T P^T ----
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    floatx8 pu;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) pu[i] = pv[8 * u + i];
+                    const bf16x8 pf = __builtin_convertvector(pu, bf16x8);
+                    if (u == 0) read_values(vf[1], at_chunk + 16 * ROW_BYTES);
+                    if (PAGED && !(two >> (8 * u) & 1))      // (what lies in the place of a page that is none may be anything)
+#pragma unroll
+                        for (int jb = 0; jb < JB; ++jb) vf[u][jb] = __builtin_bit_cast(bf16x8, u32x4{});
+#pragma unroll
+                    for (int jb = 0; jb < JB; ++jb) o[jb] = mfma32(vf[u][jb], pf, o[jb]);
+                    if (two_parts) {
+                        const u32x4 w = __builtin_bit_cast(u32x4, pf);
+                        floatx8 rest;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            rest[2 * i] = pu[2 * i] - __uint_as_float(w[i] << 16);
+                            rest[2 * i + 1] = pu[2 * i + 1] - __uint_as_float(w[i] & 0xffff0000u);
+                        }
+                        const bf16x8 pr = __builtin_convertvector(rest, bf16x8);
+#pragma unroll
+                        for (int jb = 0; jb < JB; ++jb) o[jb] = mfma32(vf[u][jb], pr, o[jb]);
+                    }
+                }
+            }
+        }
+    };
+
+    sweep();
+    __syncthreads();                                         // everyone has left the tiles
+
+    l_run = half_sum(l_run);
+        const auto inverse = [](float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN; };
+    // (the join looks after sums that are no finite numbers: such a row is not written here, where its queries may lie, and told of by a negative sum of its
+    // probabilities)
+    const auto tell = [&](int row, float m, float l, bool odd) { *reinterpret_cast<float2*>(p.part_ml + 2 * (pc.part + row)) = float2{m, odd ? -l : l}; };
+    if (n_ks > 1) {
+        // ---- waves that share rows: all sums to LDS (16-byte pieces of a row XORed by its number: its banks), then a row's four columns to a thread ----
+        float* const s_o = (float*)in_lds<float>(lds0);
+        if (works) {
+            const int row = (ks * n_blocks + blk) * 32 + r;
+            if (h == 0) *reinterpret_cast<float2*>(plan.ml + 2 * row) = float2{m_run, l_run};
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                for (int i4 = 0; i4 < 4; ++i4)
+                    *reinterpret_cast<floatx4*>(s_o + row * D + ((jb * 8 + i4 * 2 + h) ^ (r & (D / 4 - 1))) * 4) =
+                        floatx4{o[jb][4 * i4], o[jb][4 * i4 + 1], o[jb][4 * i4 + 2], o[jb][4 * i4 + 3]};
+        }
+        __syncthreads();
+        for (int at = threadIdx.x; at < pc.n_rows * (D / 4); at += kRowsThreads) {
+            const int row = at / (D / 4), c = at % (D / 4);
+            float2 ml[kChunks];
+            float m = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int k = 0; k < kChunks; ++k) {
+                ml[k] = k < n_ks ? *reinterpret_cast<const float2*>(plan.ml + 2 * (k * n_blocks * 32 + row)) : float2{-INFINITY, 0.f};
+                m = fmaxf(m, ml[k].x);
+            }
+            const float m_ref = m == -INFINITY ? 0.f : m;
+            floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < kChunks; ++k) {
+                if (k >= n_ks) break;
+                const float w = fast_exp2(ml[k].x - m_ref);
+                l += ml[k].y * w;
+                const floatx4 y = *reinterpret_cast<const floatx4*>(s_o + (k * n_blocks * 32 + row) * D + (c ^ (row & 31 & (D / 4 - 1))) * 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] += y[i] * w;
+            }
+            if (pc.direct) {
+                const QuotRem at_q = divide(pc.row0 + row, p.group, p.inv_group);
+                const int64_t tok = pc.q0 + at_q.q;
+                const int hd = pc.g * p.group + at_q.r;
+                const bool odd = __ballot(!((sum[0] + sum[1] + sum[2] + sum[3]) * 0.f == 0.f)) >> (lane & ~(D / 4 - 1)) & (D == 128 ? 0xffffffffull : 0xffffull);
+                if (!odd) *reinterpret_cast<bf16x4*>(p.out + tok * p.q_tok + (int64_t)hd * p.q_head + c * 4) = __builtin_convertvector(sum * inverse(l), bf16x4);
+                if (p.lse && c == 0) p.lse[tok * p.n_q_heads + hd] = l == 0.f ? -INFINITY : (m + fast_log2(l)) * kLn2;
+                if (c == 0) tell(row, m, l, odd);
+            } else {
+                *reinterpret_cast<floatx4*>(p.part_o + (pc.part + row) * D + c * 4) = sum;
+                if (c == 0) tell(row, m, l, false);
+            }
+        }
+    } else if (works && my_row < pc.n_rows) {
+        if (pc.direct) {
+            float odd = 0.f;
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) odd += 0.f * o[jb][i];
+            odd = half_sum(odd);
+            const float inv = inverse(l_run);
+            __bf16* const op = p.out + q_tok * p.q_tok + (int64_t)q_hd * p.q_head + h * 4;
+            if (odd == 0.f) {
+#pragma unroll
+                for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                    for (int i4 = 0; i4 < 4; ++i4) {
+                        const floatx4 y = floatx4{o[jb][4 * i4], o[jb][4 * i4 + 1], o[jb][4 * i4 + 2], o[jb][4 * i4 + 3]} * inv;
+                        *reinterpret_cast<bf16x4*>(op + jb * 32 + i4 * 8) = __builtin_convertvector(y, bf16x4);
+                    }
+            }
+            if (p.lse && h == 0) p.lse[q_tok * p.n_q_heads + q_hd] = l_run == 0.f ? -INFINITY : (m_run + fast_log2(l_run)) * kLn2;
+            if (h == 0) tell(my_row, m_run, l_run, !(odd == 0.f));
+        } else {
+            if (h == 0) tell(my_row, m_run, l_run, false);
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                for (int i4 = 0; i4 < 4; ++i4)
+                    *reinterpret_cast<floatx4*>(p.part_o + (pc.part + my_row) * D + jb * 32 + i4 * 8 + h * 4) =
+                        floatx4{o[jb][4 * i4], o[jb][4 * i4 + 1], o[jb][4 * i4 + 2], o[jb][4 * i4 + 3]};
+        }
+    }
+}
+
 __device__ __forceinline__ int first_of_last(int entries) { return (entries - 1) / kRowsThreads * kRowsThreads; }
 
 template <int D, bool PAGED>
 __global__ __launch_bounds__(kRowsThreads, 2)
 void rows_kernel(const RowsParams p)
 {
-    constexpr int KK = D / 16, JB = D / 32, CH = D / 8, ROW_BYTES = D * 2;
-    constexpr int TILE_BYTES = kRowsTile * ROW_BYTES;        // of K or V
-    constexpr int KEYS_PER_LOAD = kWave / CH, LOADS = 16 / KEYS_PER_LOAD;
-    static_assert(kSetRows * D * 4 <= 4 * TILE_BYTES, "the exchange of waves that share rows");
-
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r = lane & 31, h = lane >> 5;
     extern __shared__ __align__(1024) unsigned char smem[];  // stage s: K tile at s * 2 * TILE_BYTES, V tile behind it
-    RowsPlan& plan = *reinterpret_cast<RowsPlan*>(smem + 4 * TILE_BYTES);
+    RowsPlan& plan = *reinterpret_cast<RowsPlan*>(smem + 4 * kRowsTile * D * 2);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(SPECVLM_AS3 unsigned char*)smem;
 
-    const float sc = fmaxf(p.scale_log2, 1e-30f);            // (a zero scale as a vanishing one: -inf stays -inf)
     const int j = xcd_logical_id(blockIdx.x, p.padded);
     if (j >= p.workgroups) return;
 
@@ -309,13 +629,14 @@ void rows_kernel(const RowsParams p)
     const int entries = PAGED ? 2 * p.batch : p.batch;
     Numbers total, here;
     bool grouped = PAGED;
-    Entry entry;
-    Numbers mine, upto;
-    const auto look_at = [&](int e) {
+    const auto look_at = [&](int e) {                        // of 512 entries at a time, each thread one
+        Entry entry;
         if (PAGED && entries <= kRowsThreads) entry = entry_at_once(p, plan, grouped);
         else entry = entry_of<PAGED>(p, e, grouped);
-        mine = numbers_of(p, entry);
-        upto = block_prefix(plan, mine, wave, lane, &here);
+        const Numbers mine = numbers_of(p, entry), upto = block_prefix(plan, mine, wave, lane, &here);
+        plan.entry[threadIdx.x] = entry;
+        plan.front[threadIdx.x] = {upto.work - mine.work, upto.rows - mine.rows};
+        plan.work[threadIdx.x] = mine.work;
     };
     for (;;) {
         total = {0, 0};
@@ -329,22 +650,20 @@ void rows_kernel(const RowsParams p)
         grouped = false;
     }
     if (total.rows > p.most_rows) total.work = 0;            // (offsets that overlap)
-    const int sharers = sharers_of(p, total.work);
-    if (j >= sharers) return;
-    int x = share_begin(j, total.work, sharers);
-    const int x_end = share_begin(j + 1, total.work, sharers);
+    const Shares shares = shares_of(p, total.work);
+    if (j >= shares.n) return;
+    int x = shares.begin(j);
+    const int x_end = shares.begin(j + 1);
     Numbers base = {0, 0};                                   // in front of the 512 entries at hand
     int c0 = 0;
-    const auto publish = [&] {
-        const Numbers front = {base.work + upto.work - mine.work, base.rows + upto.rows - mine.rows};
-        plan.entry[threadIdx.x] = entry;
-        plan.front[threadIdx.x] = front;
-        if (j == 0) {                                        // (the join reads where every entry begins)
-            const int e = c0 + threadIdx.x;
-            if (e < entries) p.starts[e] = {front.work, front.rows, entry.q0, entry.n_q, entry.key0, entry.key1, entry.first, total.work};
-        }
+    const auto tell = [&] {                                  // (the join reads where every entry begins)
+        const int e = c0 + threadIdx.x;
+        const Entry entry = plan.entry[threadIdx.x];
+        const Numbers front = plan.front[threadIdx.x];
+        if (e < entries)
+            p.starts[e] = {base.work + front.work, base.rows + front.rows, entry.q0, entry.n_q, entry.key0, entry.key1, entry.first, total.work};
     };
-    publish();
+    if (j == 0) tell();
     bool told = entries <= kRowsThreads || j > 0;            // (workgroup 0 tells of all entries, then begins again)
     while (x < x_end || !told) {
         while (!told || x >= base.work + here.work) {
@@ -358,341 +677,106 @@ void rows_kernel(const RowsParams p)
             }
             __syncthreads();
             look_at(c0 + threadIdx.x);
-            publish();
+            if (!told) tell();
         }
         if (x >= x_end) break;
-        if (base.work + upto.work > x && base.work + upto.work - mine.work <= x) plan.found = threadIdx.x;
+        const int there = base.work + plan.front[threadIdx.x].work;
+        if (there <= x && x < there + plan.work[threadIdx.x]) plan.found = threadIdx.x;
         __syncthreads();
         const int at = __builtin_amdgcn_readfirstlane(plan.found), e = c0 + at;
-        const Numbers front = {__builtin_amdgcn_readfirstlane(plan.front[at].work), __builtin_amdgcn_readfirstlane(plan.front[at].rows)};
+        const Numbers front = {base.work + __builtin_amdgcn_readfirstlane(plan.front[at].work), base.rows + __builtin_amdgcn_readfirstlane(plan.front[at].rows)};
         const bool own = !PAGED || e >= p.batch;
-        const int b = PAGED && own ? e - p.batch : e;
         Entry en = plan.entry[at];
         en.q0 = __builtin_amdgcn_readfirstlane(en.q0); en.n_q = __builtin_amdgcn_readfirstlane(en.n_q);
         en.key0 = __builtin_amdgcn_readfirstlane(en.key0); en.key1 = __builtin_amdgcn_readfirstlane(en.key1);
         const int chunks = chunks_of(en), rows = en.n_q * p.group;
         const Sets sets = sets_of(rows);
-        const int item = (x - front.work) / (chunks + kBegin), begin = x - front.work - item * (chunks + kBegin);
-        const int c_begin = max(0, begin - kBegin), c_end = min(chunks, begin + x_end - x - kBegin);
-        x = min(x_end, x + chunks + kBegin - begin);
+        const int unit = chunk_work(sets.blocks), work = chunks * unit + kBegin;
+        const int item = (int)((uint32_t)(x - front.work) / (uint32_t)work), begin = x - front.work - item * work;
+        // (32 keys are a workgroup's that has their first unit)
+        const auto chunk_at = [&](int u) { return max(0, (unit == 2 ? (u - kBegin + 1) >> 1 : (int)((uint32_t)max(u - kBegin + 2, 0) / 3u))); };
+        const int c_begin = chunk_at(begin), c_end = min(chunks, chunk_at(begin + x_end - x));
+        x = min(x_end, x + work - begin);
         if (c_end <= c_begin) {                              // (the front of an item alone)
             __syncthreads();
             continue;
         }
-        const int g = item / sets.n, set = item - g * sets.n;
-        const int row0 = set * sets.blocks * 32, n_rows = min(rows - row0, sets.blocks * 32), n_blocks = (n_rows + 31) >> 5;
-        const int log_blocks = n_blocks > 4 ? 3 : n_blocks > 2 ? 2 : n_blocks - 1;       // waves of a kind
-        const int blk = wave & ((1 << log_blocks) - 1), ks = wave >> log_blocks, n_ks = min(kChunks, kRowsWaves >> log_blocks);
-        const bool works = blk < n_blocks && ks < n_ks;
-        const bool direct = own && en.key0 == 0 && c_begin == 0 && c_end == chunks;
-        const int key0 = en.key0 + c_begin * 32, key1 = min(en.key1, en.key0 + c_end * 32), tiles = (key1 - key0 + kRowsTile - 1) / kRowsTile;       // of the piece
-        const bool two_parts = n_blocks <= 4;
-
-        // ---- loads: wave w brings keys 16w..16w+15 of a tile ----
-        const int64_t kv0 = (int64_t)g * p.head + (PAGED ? 0 : (int64_t)(p.cu_kv ? __builtin_amdgcn_readfirstlane(p.cu_kv[e]) : 0) * p.tok);
-        const char* const k_at = reinterpret_cast<const char*>(p.k + kv0);
-        const char* const v_at = reinterpret_cast<const char*>(p.v + kv0);
-        const int table_b = PAGED ? b : 0;
-        int ids = 0, places = 0;                             // of the next 64 tiles, one to a lane
-        const auto look_up = [&](int tile) {
-            const int key = min(key0 + (tile + lane) * kRowsTile + wave * 16, (key1 - 1) & ~15);
-            const QuotRem pg = divide(key, p.page_size, p.inv_page);
-            ids = p.table[(int64_t)table_b * p.table_row + pg.q];
-            places = pg.r;
-        };
-        const auto issue = [&](int tile, int stage) {
-            const uint32_t to = lds0 + stage * 2 * TILE_BYTES + wave * 16 * ROW_BYTES;
-            int64_t first;
-            int last;                                        // the last of the 16 keys that there is: it stands for those behind it, whatever lies there
-            if constexpr (PAGED) {
-                const int l = tile & 63;
-                if (l == 0 && tile > 0) look_up(tile);
-                const int id = __builtin_amdgcn_readlane(ids, l), row = __builtin_amdgcn_readlane(places, l);
-                // (a page that is not one of the pool's is not read: the pool's first is, and its keys are masked)
-                const bool there = (uint32_t)id < (uint32_t)p.n_pages;
-                if (lane == 0) plan.ok[stage][wave] = there;
-                first = (there ? id : 0) * p.page + row * p.tok;
-                last = key1 - 1 - (key0 + tile * kRowsTile + wave * 16);
-                if (last < 0) last = (key1 - 1) & 15;        // (a group behind the last: that one again)
-            } else {
-                const int key = min(key0 + tile * kRowsTile + wave * 16, key1 - 1);
-                first = (int64_t)key * p.tok;
-                last = key1 - 1 - key;
-            }
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int kl = i * KEYS_PER_LOAD + lane / CH, piece = lane % CH;
-                const uint32_t row = (uint32_t)min(kl, last) * (uint32_t)(p.tok * 2);
-                load_to_lds(k_at + 2 * first, row + (piece ^ (D == 128 ? kl & 15 : kl >> 1 & 7)) * 16, to + i * 1024);
-                load_to_lds(v_at + 2 * first, row + (piece ^ rows_v_swizzle<D>(kl)) * 16, to + TILE_BYTES + i * 1024);
-            }
-        };
-
-        const auto begin_loads = [&] {
-            if constexpr (PAGED) look_up(0);
-            issue(0, 0);
-        };
-        if (tiles > 0) begin_loads();                        // (on their way while the rows are looked at)
-
-        // this wave's rows
-        const int my_row = blk * 32 + r;
-        const QuotRem q_at = divide(row0 + (my_row < n_rows ? my_row : 0), p.group, p.inv_group);  // (padding rows take the first: never stored)
-        const int64_t q_tok = en.q0 + q_at.q;
-        const int q_hd = g * p.group + q_at.r;
-        bf16x8 qf[KK];
-        const __bf16* const qp = p.q + q_tok * p.q_tok + (int64_t)q_hd * p.q_head + h * 8;
-#pragma unroll
-        for (int s = 0; s < KK; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qp + s * 16);
-        // the keys that it sees: [lo, hi), of the block those of a tree node's mask
-        int lo = en.key0, hi = key1;
-        const int before = en.key1 - en.n_q;                 // (own keys of a block)
-        uint64_t tree = 0;
-        bool is_tree = false;
-        if constexpr (PAGED) {
-            if (own) {
-                is_tree = p.block_mask != nullptr;
-                if (is_tree) tree = p.block_mask[q_tok];
-                else hi = min(hi, before + q_at.q + 1);
-            }
-        } else if (p.ranges) {
-            lo = min(max(p.ranges[2 * q_tok], 0), key1);
-            hi = min(max(p.ranges[2 * q_tok + 1], 0), key1);
-        }
-        // of all of the wave's rows: keys that all see, and that some see
-        int all_lo = lo, all_hi = is_tree ? min(before, hi) : hi, any_lo = lo < hi ? lo : INT_MAX, any_hi = lo < hi ? hi : 0;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            all_lo = max(all_lo, __shfl_xor(all_lo, d)); all_hi = min(all_hi, __shfl_xor(all_hi, d));
-            any_lo = min(any_lo, __shfl_xor(any_lo, d)); any_hi = max(any_hi, __shfl_xor(any_hi, d));
-        }
-        all_lo = __builtin_amdgcn_readfirstlane(all_lo); all_hi = __builtin_amdgcn_readfirstlane(all_hi);
-        any_lo = __builtin_amdgcn_readfirstlane(any_lo); any_hi = __builtin_amdgcn_readfirstlane(any_hi);
-
-        float m_run, l_run;
-        floatx16 o[JB];
-        // where this lane reads in a stage
-        const uint32_t k_base = lds0 + r * ROW_BYTES + (h ^ (D == 128 ? r & 15 : r >> 1 & 7)) * 16;
-        const int v_row = 4 * h + ((lane & 15) >> 2);
-        const uint32_t v_base = lds0 + TILE_BYTES + v_row * ROW_BYTES + ((((lane >> 4 & 1) * 2 + ((lane & 3) >> 1)) ^ rows_v_swizzle<D>(v_row)) * 16) + (lane & 1) * 8;
-
-        // V^T fragments of 16 keys, by the transposing read
-        const auto read_values = [&](bf16x8 (&vf)[JB], uint32_t at) {
-#pragma unroll
-            for (int jb = 0; jb < JB; ++jb) {
-                typedef short s16x4 __attribute__((ext_vector_type(4)));
-                SPECVLM_AS3 s16x4* const src = in_lds<s16x4>(v_base + at ^ jb * 64);
-                const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(src);
-                const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16(src + 8 * ROW_BYTES / 8);
-                vf[jb] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7));
-            }
-        };
-
-        // The sweep.  careful: with an eye on values that are no finite numbers.
-        const auto sweep = [&](auto careful) {
-            m_run = -INFINITY;
-            l_run = 0.f;
-#pragma unroll
-            for (int jb = 0; jb < JB; ++jb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[jb][i] = 0.f;
-            bool fresh = true;                               // some row has seen nothing yet
-            if (tiles <= 0) return;
-            if constexpr (decltype(careful)::value) begin_loads();
-            for (int t = 0; t < tiles; ++t) {
-                const int stage = t & 1;
-                wait_vmcnt<0>();
-                __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                stage_barrier();                             // the tile is there for everyone, and everyone has left the other stage
-                if (t + 1 < tiles) issue(t + 1, stage ^ 1);
-                if (!works) continue;
-                uint64_t there = ~0ull;                      // a byte for 16 keys: their page is there
-                if constexpr (PAGED) {
-                    const u32x2 ok = *reinterpret_cast<const u32x2*>(plan.ok[stage]);
-                    there = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(ok[1]) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane(ok[0]);
-                }
-                for (int ch = ks; ch < kChunks; ch += n_ks) {
-                    const int k0 = key0 + t * kRowsTile + ch * 32;
-                    if (k0 >= any_hi || k0 + 31 < any_lo) continue;
-                    const uint32_t at_chunk = stage * 2 * TILE_BYTES + ch * 32 * ROW_BYTES;
-                    // ---- S^T = K Q^T for 32 keys ----
-                    bf16x8 kf[KK];
-#pragma unroll
-                    for (int kk = 0; kk < KK; ++kk) kf[kk] = __builtin_bit_cast(bf16x8, *in_lds<const u32x4>(k_base + at_chunk ^ kk * 32));
-                    floatx16 s;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-                    for (int kk = 0; kk < KK; ++kk) s = mfma32(kf[kk], qf[kk], s);
-                    // (the reads of all of them first: one by one, each waits for its own)
-                    __builtin_amdgcn_sched_group_barrier(0x100, KK, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x008, KK, 0);
-                    bf16x8 vf[2][JB];
-                    read_values(vf[0], at_chunk);
-                    const uint32_t two = PAGED ? (uint32_t)(there >> (16 * ch)) & 0xffffu : 0x101u;
-                    const bool need_mask = two != 0x101u || k0 < all_lo || k0 + 32 > all_hi;
-                    uint32_t sees = ~0u;
-                    if (need_mask) {
-                        sees = first_bits(hi - k0) & ~first_bits(lo - k0) & ((two & 1 ? 0xffffu : 0u) | (two & 0x100 ? 0xffff0000u : 0u));
-                        if (is_tree) {
-                            const int in = k0 - before;
-                            const uint64_t block = in >= 0 ? (in < 64 ? tree >> in : 0) : (in > -32 ? tree << -in : 0);
-                            sees &= (uint32_t)block | first_bits(-in);
-                        }
-                        sees >>= 4 * h;                      // bit 8(i/4) + i%4: the lane's i-th key
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = sees >> (8 * (i / 4) + i % 4) & 1u ? s[i] : -INFINITY;
-                    }
-                    // Away from the masks the exponentials are taken against the reference that the earlier keys left, and the maximum is
-                    // tracked only where a lane's sum does not stay moderate.
-                    bool settled = false;
-                    float pv[16];
-                    if (!need_mask && !fresh) {
-                        float psum = 0.f;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) { pv[i] = fast_exp2(fmaf(s[i], sc, -m_run)); psum += pv[i]; }
-                        if (!__any(!(psum < kRowsRedo))) {
-                            l_run += psum;
-                            settled = true;
-                        }
-                    }
-                    if (!settled) {
-                        float mx = s[0];
-#pragma unroll
-                        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
-                        const float m_new = fmaxf(m_run, half_max(mx) * sc);
-                        const float m_ref = m_new == -INFINITY ? 0.f : m_new;
-                        const float alpha = fast_exp2(m_run - m_ref);
-                        const bool rescale = m_new != m_run;
-                        m_run = m_new;
-                        float psum = 0.f;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) { pv[i] = fast_exp2(fmaf(s[i], sc, -m_ref)); psum += pv[i]; }
-                        l_run = l_run * alpha + psum;
-                        if (__any(rescale)) {
-#pragma unroll
-                            for (int jb = 0; jb < JB; ++jb)
-#pragma unroll
-                                for (int i = 0; i < 16; ++i)             // (an infinity stays one, also where 32 bits take its weight for 0)
-                                    o[jb][i] = decltype(careful)::value && fabsf(o[jb][i]) == INFINITY ? o[jb][i] : alpha * o[jb][i];
-                        }
-                    }
-                    if (need_mask || fresh) fresh = __any(!(m_run > -INFINITY));
-                    // ---- O^T += V^T P^T ----
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        floatx8 pu;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) pu[i] = pv[8 * u + i];
-                        const bf16x8 pf = __builtin_convertvector(pu, bf16x8);
-                        if (u == 0) read_values(vf[1], at_chunk + 16 * ROW_BYTES);
-                        if constexpr (decltype(careful)::value) {
-                            const uint32_t s16 = sees >> 16 * u;
-#pragma unroll
-                            for (int jb = 0; jb < JB; ++jb) take_odd_rows(vf[u][jb], (s16 & 0xfu) | (s16 >> 4 & 0xf0u), o[jb]);
-                        }
-#pragma unroll
-                        for (int jb = 0; jb < JB; ++jb) o[jb] = mfma32(vf[u][jb], pf, o[jb]);
-                        if (two_parts) {
-                            const u32x4 w = __builtin_bit_cast(u32x4, pf);
-                            floatx8 rest;
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                rest[2 * i] = pu[2 * i] - __uint_as_float(w[i] << 16);
-                                rest[2 * i + 1] = pu[2 * i + 1] - __uint_as_float(w[i] & 0xffff0000u);
-                            }
-                            const bf16x8 pr = __builtin_convertvector(rest, bf16x8);
-#pragma unroll
-                            for (int jb = 0; jb < JB; ++jb) o[jb] = mfma32(vf[u][jb], pr, o[jb]);
-                        }
-                    }
-                }
-            }
-        };
-        sweep(std::false_type());
-        // A sum that is no finite number, as a rule of an infinite value that a row sees, or of a hidden one that is none:  all keys once more, with an eye on
-        // such values.
-        float odd = 0.f;
-#pragma unroll
-        for (int jb = 0; jb < JB; ++jb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) odd += 0.f * o[jb][i];
-        if (__builtin_expect(__syncthreads_or(works && !(odd == 0.f)), 0)) {
-            sweep(std::true_type());
-            __syncthreads();
-        }
-
-        l_run = half_sum(l_run);
-        const int64_t part = part_row(j, front.rows + g * padded_rows(p, en) + row0);
-        const auto inverse = [](float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN; };
-        if (n_ks > 1) {
-            // ---- waves that share rows: all sums to LDS (16-byte pieces of a row XORed by its number: its banks), then a row's four columns to a thread ----
-            float* const s_o = reinterpret_cast<float*>(smem);
-            if (works) {
-                const int row = (ks * n_blocks + blk) * 32 + r;
-                if (h == 0) *reinterpret_cast<float2*>(plan.ml + 2 * row) = float2{m_run, l_run};
-#pragma unroll
-                for (int jb = 0; jb < JB; ++jb)
-#pragma unroll
-                    for (int i4 = 0; i4 < 4; ++i4)
-                        *reinterpret_cast<floatx4*>(s_o + row * D + ((jb * 8 + i4 * 2 + h) ^ (r & (D / 4 - 1))) * 4) =
-                            floatx4{o[jb][4 * i4], o[jb][4 * i4 + 1], o[jb][4 * i4 + 2], o[jb][4 * i4 + 3]};
-            }
-            __syncthreads();
-            for (int at = threadIdx.x; at < n_rows * (D / 4); at += kRowsThreads) {
-                const int row = at / (D / 4), c = at % (D / 4);
-                float2 ml[kChunks];
-                float m = -INFINITY, l = 0.f;
-#pragma unroll
-                for (int k = 0; k < kChunks; ++k) {
-                    ml[k] = k < n_ks ? *reinterpret_cast<const float2*>(plan.ml + 2 * (k * n_blocks * 32 + row)) : float2{-INFINITY, 0.f};
-                    m = fmaxf(m, ml[k].x);
-                }
-                const float m_ref = m == -INFINITY ? 0.f : m;
-                floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int k = 0; k < kChunks; ++k) {
-                    if (k >= n_ks) break;
-                    const float w = fast_exp2(ml[k].x - m_ref);
-                    l += ml[k].y * w;
-                    const floatx4 y = *reinterpret_cast<const floatx4*>(s_o + (k * n_blocks * 32 + row) * D + (c ^ (row & 31 & (D / 4 - 1))) * 4);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[i] += fabsf(y[i]) == INFINITY ? y[i] : y[i] * w;
-                }
-                if (direct) {
-                    const QuotRem at_q = divide(row0 + row, p.group, p.inv_group);
-                    const int64_t tok = en.q0 + at_q.q;
-                    const int hd = g * p.group + at_q.r;
-                    *reinterpret_cast<bf16x4*>(p.out + tok * p.q_tok + (int64_t)hd * p.q_head + c * 4) = __builtin_convertvector(sum * inverse(l), bf16x4);
-                    if (p.lse && c == 0) p.lse[tok * p.n_q_heads + hd] = l == 0.f ? -INFINITY : (m + fast_log2(l)) * kLn2;
-                } else {
-                    *reinterpret_cast<floatx4*>(p.part_o + (part + row) * D + c * 4) = sum;
-                    if (c == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (part + row)) = float2{m, l};
-                }
-            }
-        } else if (works && my_row < n_rows) {
-            if (direct) {
-                const float inv = inverse(l_run);
-                __bf16* const op = p.out + q_tok * p.q_tok + (int64_t)q_hd * p.q_head + h * 4;
-#pragma unroll
-                for (int jb = 0; jb < JB; ++jb)
-#pragma unroll
-                    for (int i4 = 0; i4 < 4; ++i4) {
-                        const floatx4 y = floatx4{o[jb][4 * i4], o[jb][4 * i4 + 1], o[jb][4 * i4 + 2], o[jb][4 * i4 + 3]} * inv;
-                        *reinterpret_cast<bf16x4*>(op + jb * 32 + i4 * 8) = __builtin_convertvector(y, bf16x4);
-                    }
-                if (p.lse && h == 0) p.lse[q_tok * p.n_q_heads + q_hd] = l_run == 0.f ? -INFINITY : (m_run + fast_log2(l_run)) * kLn2;
-            } else {
-                if (h == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (part + my_row)) = float2{m_run, l_run};
-#pragma unroll
-                for (int jb = 0; jb < JB; ++jb)
-#pragma unroll
-                    for (int i4 = 0; i4 < 4; ++i4)
-                        *reinterpret_cast<floatx4*>(p.part_o + (part + my_row) * D + jb * 32 + i4 * 8 + h * 4) =
-                            floatx4{o[jb][4 * i4], o[jb][4 * i4 + 1], o[jb][4 * i4 + 2], o[jb][4 * i4 + 3]};
-            }
-        }
+        const int g = (int)((uint32_t)item / (uint32_t)sets.n), set = item - g * sets.n;
+        Piece pc;
+        pc.b = PAGED && own ? e - p.batch : e; pc.own = own;
+        pc.q0 = en.q0; pc.n_q = en.n_q; pc.end = en.key1;
+        pc.g = g; pc.row0 = set * sets.blocks * 32; pc.n_rows = min(rows - pc.row0, sets.blocks * 32);
+        pc.key0 = en.key0 + c_begin * 32; pc.key1 = min(en.key1, en.key0 + c_end * 32);
+        pc.direct = own && en.key0 == 0 && c_begin == 0 && c_end == chunks;
+        pc.part = part_row(j, front.rows + g * padded_rows(p, en) + pc.row0);
+        rows_piece<D, PAGED>(p, plan, lds0, pc);
         __syncthreads();                                     // the ring, and what the plan holds, are free again
     }
+}
+
+// One row over all of its keys once more, by a wave, where its sum came out as no finite number: mostly for an infinite value, which a row that sees it gets as it is,
+// however small its weight, and a row that does not see it does not get.  m, l: the row's maximum and sum of probabilities.  (Every key takes its own loads and
+// two rounds of the vector unit: 50 times what the matrix unit takes.)
+template <int D, bool PAGED>
+__device__ __forceinline__ void odd_row(const RowsParams& p, const RowsStart& own, int b, int tok, int hd, float m, float l, int lane)
+{
+    constexpr int COLS = D / kWave;
+    const float sc = fmaxf(p.scale_log2, 1e-30f), m_ref = m == -INFINITY ? 0.f : m;
+    const int g = hd / p.group, t = tok - own.q0;
+    const __bf16* const q = p.q + (int64_t)tok * p.q_tok + (int64_t)hd * p.q_head;
+    int lo = 0, hi = own.key1, before = own.key1;            // keys that the row sees;  of those from `before` on the tree's
+    uint64_t tree = ~0ull;
+    if constexpr (PAGED) {
+        if (p.block_mask) {
+            tree = p.block_mask[tok];
+            before -= own.n_q;
+        } else {
+            hi -= own.n_q - 1 - t;
+        }
+    } else if (p.ranges) {
+        lo = max(p.ranges[2 * (int64_t)tok], 0);
+        hi = min(p.ranges[2 * (int64_t)tok + 1], own.key1);
+    }
+    float o[COLS];
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) o[c] = 0.f;
+    for (int k0 = lo; k0 < hi; k0 += kWave) {
+        const int key = min(k0 + lane, hi - 1);
+        bool sees = k0 + lane < hi && (key < before || (tree >> (key - before) & 1));
+        int64_t at;
+        if constexpr (PAGED) {
+            const QuotRem pg = divide(key, p.page_size, p.inv_page);
+            const int id = p.table[(int64_t)(key < own.key0 ? own.first : b) * p.table_row + pg.q];
+            sees = sees && (uint32_t)id < (uint32_t)p.n_pages;
+            at = (sees ? id : 0) * p.page + pg.r * p.tok;
+        } else {
+            at = (int64_t)((p.cu_kv ? p.cu_kv[b] : 0) + key) * p.tok;
+        }
+        at += (int64_t)g * p.head;
+        float x = 0.f;
+        for (int d = 0; d < D; d += 8) {
+            const bf16x8 kv = *reinterpret_cast<const bf16x8*>(p.k + at + d), qv = *reinterpret_cast<const bf16x8*>(q + d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x = fmaf((float)kv[i], (float)qv[i], x);
+        }
+        const float w = sees ? fast_exp2(fmaf(x, sc, -m_ref)) : 0.f;
+        uint64_t seen = __ballot(sees);
+        while (seen) {
+            const int i = __builtin_ctzll(seen);
+            seen &= seen - 1;
+            const float wi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), i));
+            const int64_t row = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(at >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)at, i));
+#pragma unroll
+            for (int c = 0; c < COLS; ++c) {
+                const float v = (float)p.v[row + lane * COLS + c];
+                o[c] += fabsf(v) == INFINITY ? v : wi * v;
+            }
+        }
+    }
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+    __bf16* const out = p.out + (int64_t)tok * p.q_tok + (int64_t)hd * p.q_head + lane * COLS;
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) out[c] = (__bf16)(o[c] * inv);
 }
 
 // Joins the pieces of the rows that were cut (one that was not is in its place already): D / 4 threads to a row, and `GP` groups of them take every GP-th
@@ -732,27 +816,38 @@ void rows_join_kernel(const RowsParams p)
         b += __builtin_ctzll(behind);
     }
     const RowsStart own = p.starts[PAGED ? p.batch + b : b];
-    const int total = own.total, sharers = sharers_of(p, total);
-    if (total == 0 || own.n_q <= 0 || tok < own.q0 || hd >= p.n_q_heads) return;
+    const int total = own.total;
+    const Shares shares = shares_of(p, total);
+    if (total == 0 || own.n_q <= 0 || tok < own.q0) return;
+    const bool mine_to_write = hd < p.n_q_heads && (GP == 1 || group == 0);      // (all lanes stay to the end: an odd row takes a whole wave)
+    hd = min(hd, p.n_q_heads - 1);
     const QuotRem head = divide(hd, p.group, p.inv_group);
     struct Pieces { int first, n, row; };                    // workgroups that have one, the row of their results
     const auto pieces_of = [&](const RowsStart& s) {
         const Entry en = {s.q0, s.n_q, s.key0, s.key1, -1};
         const int row = (tok - en.q0) * p.group + head.r, chunks = chunks_of(en);
         const Sets sets = sets_of(en.n_q * p.group);
-        const int x = s.work + (head.q * sets.n + row / (sets.blocks * 32)) * (chunks + kBegin) + kBegin;
-        const int first = sharer_of(x, total, sharers);
-        return Pieces{first, sharer_of(x + chunks - 1, total, sharers) - first + 1, s.rows + head.q * padded_rows(p, en) + row};
+        const int unit = chunk_work(sets.blocks);
+        const int x = s.work + (head.q * sets.n + (int)((uint32_t)row / (uint32_t)(sets.blocks * 32))) * (chunks * unit + kBegin) + kBegin;
+        const int first = shares.of(x);
+        return Pieces{first, shares.of(x + (chunks - 1) * unit) - first + 1, s.rows + head.q * padded_rows(p, en) + row};
     };
     const Pieces mine = pieces_of(own);
     Pieces theirs = {0, 0, 0};
     if (PAGED && own.key0 > 0) theirs = pieces_of(p.starts[own.first]);
-    else if (mine.n == 1) return;
-    const int n = theirs.n + mine.n;
-    const auto row_of = [&](int i) { return i < theirs.n ? part_row(theirs.first + i, theirs.row) : part_row(mine.first + i - theirs.n, mine.row); };
-    const int g0 = GP == 1 ? 0 : group;                      // this group's first piece
     float m = -INFINITY, l = 0.f;
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
+    bool odd = false;
+    const bool in_place = theirs.n == 0 && mine.n == 1;
+    if (in_place) {
+        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * part_row(mine.first, mine.row));
+        odd = __float_as_uint(ml.y) >> 31 || !(ml.y == ml.y);
+        m = ml.x;
+        l = fabsf(ml.y);
+    }
+    const int n = in_place ? 0 : theirs.n + mine.n;
+    const auto row_of = [&](int i) { return i < theirs.n ? part_row(theirs.first + i, theirs.row) : part_row(mine.first + i - theirs.n, mine.row); };
+    const int g0 = GP == 1 ? 0 : group;                      // this group's first piece
     for (int i0 = g0; i0 < n; i0 += TPR * GP) {
         // a piece to a thread: its maximum and sum;  then the outputs, weighted by their thread's word
         float pm = -INFINITY, pl = 0.f;
@@ -779,24 +874,23 @@ void rows_join_kernel(const RowsParams p)
         l = l * keep + sum;
         m = m_new;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = fabsf(o[i]) == INFINITY ? o[i] : o[i] * keep;
+        for (int i = 0; i < 4; ++i) o[i] = o[i] * keep;
         for (int i1 = 0; i1 < most; i1 += 4) {
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const float wi = __shfl(w, (lane & ~(TPR - 1)) + min(i1 + u, most - 1));
                 if (i1 + u < most)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) o[k] += fabsf(y[u][k]) == INFINITY ? y[u][k] : y[u][k] * wi;
+                    for (int k = 0; k < 4; ++k) o[k] += y[u][k] * wi;
             }
             if (i1 + 4 < most) fetch(i1 + 4);
         }
     }
-    if constexpr (GP > 1) {
+    if (GP > 1 && !in_place) {
         if (c == 0) { s_ml[2 * group] = m; s_ml[2 * group + 1] = l; }
         *reinterpret_cast<floatx4*>(s_o + group * D + c * 4) = o;
         __syncthreads();
-        if (group > 0) return;
-        for (int k = 1; k < GP; ++k) m = fmaxf(m, s_ml[2 * k]);
+        for (int k = 0; k < GP; ++k) m = fmaxf(m, s_ml[2 * k]);
         const float m_ref = m == -INFINITY ? 0.f : m;
         l = 0.f;
         o = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -806,12 +900,22 @@ void rows_join_kernel(const RowsParams p)
             l += s_ml[2 * k + 1] * w;
             const floatx4 y = *reinterpret_cast<const floatx4*>(s_o + k * D + c * 4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] += fabsf(y[i]) == INFINITY ? y[i] : y[i] * w;
+            for (int i = 0; i < 4; ++i) o[i] += y[i] * w;
         }
     }
     const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
-    *reinterpret_cast<bf16x4*>(p.out + (int64_t)tok * p.q_tok + (int64_t)hd * p.q_head + c * 4) = __builtin_convertvector(o * inv, bf16x4);
-    if (p.lse && c == 0) p.lse[(int64_t)tok * p.n_q_heads + hd] = l == 0.f ? -INFINITY : (m + fast_log2(l)) * kLn2;
+    if (!in_place) {
+        const uint64_t odds = __ballot(!((o[0] + o[1] + o[2] + o[3]) * 0.f == 0.f));
+        odd = odds >> (lane & ~(TPR - 1)) & (D == 128 ? 0xffffffffull : 0xffffull);
+        if (mine_to_write) {
+            if (!odd) *reinterpret_cast<bf16x4*>(p.out + (int64_t)tok * p.q_tok + (int64_t)hd * p.q_head + c * 4) = __builtin_convertvector(o * inv, bf16x4);
+            if (p.lse && c == 0) p.lse[(int64_t)tok * p.n_q_heads + hd] = l == 0.f ? -INFINITY : (m + fast_log2(l)) * kLn2;
+        }
+    }
+    for (uint64_t rows = __ballot(odd && mine_to_write && c == 0); __builtin_expect(rows != 0, 0); rows &= rows - 1) {
+        const int i = __builtin_ctzll(rows);
+        odd_row<D, PAGED>(p, own, b, tok, __builtin_amdgcn_readlane(hd, i), __shfl(m, i), __shfl(l, i), lane);
+    }
 }
 
 namespace {
@@ -866,7 +970,7 @@ int rows_start(RowsParams& p, bool paged, const void* q, int64_t q_tok, int64_t 
     const int64_t rows = (int64_t)n_queries * n_q_heads, entries = paged ? 2 * (int64_t)batch : batch;
     if (rows >= ((int64_t)1 << 29) || entries * 32 * n_kv_heads >= ((int64_t)1 << 29)) return SPECVLM_EUNSUPPORTED;
     const int64_t sets = (2 * rows / kSetRows + n_kv_heads) + entries * n_kv_heads;
-    if (sets * (most_keys / 32 + 1 + kBegin) >= ((int64_t)1 << 31)) return SPECVLM_EUNSUPPORTED;
+    if (sets * 3 * (most_keys / 32 + 6) >= ((int64_t)1 << 31)) return SPECVLM_EUNSUPPORTED;
     const size_t need = rows_workspace(paged, batch, n_queries, n_q_heads, n_kv_heads, head_dim);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return SPECVLM_EWORKSPACE;
     p = {};

@@ -263,7 +263,8 @@ def test_hidden_values_change_nothing(B, heads):
     """Of keys behind a query in its block, of pages that are none (the pool's first is read in their place) and behind the last token."""
     q, k, v, table, kv_lens, q_lens, groups = build(13, [(320, [(20, 5), (40, 5)])], heads, 16)
     table[:, 4] = -1
-    want = check(B, q, k, v, table, kv_lens, q_lens, groups)
+    check(B, q, k, v, table, kv_lens, q_lens, groups)
+    want_exact, _, tol, _, _ = S.shared_attention(S.values(q), S.values(k), S.values(v), table, kv_lens, q_lens, heads[2] ** -0.5)
     for odd in (0x7f80, 0xff80, 0x7fc0):
         k2, v2 = k.copy(), v.copy()
         for x in (k2, v2):
@@ -274,7 +275,9 @@ def test_hidden_values_change_nothing(B, heads):
                 x[table[b, (n - 1) // 16], (n - 1) % 16] = odd           # the last key: only the last query sees it
         got = host_f64(B.shared_attn(dev_bf16(q), dev_bf16(k2), dev_bf16(v2), i32(table), i32(kv_lens), heads[2] ** -0.5, i32(groups)))
         keep = [t for t in range(10) if t % 5 != 4]
-        assert (got[keep] == want[keep]).all()
+        # (rows that share a product with such a value are summed once more, with probabilities in 32 bits: within the same bounds, of which those of the first
+        # sum are the larger)
+        close(got[keep], want_exact[keep], tol[keep])
 
 
 def test_the_queries_may_be_the_output_and_strides_are_anything(B):
