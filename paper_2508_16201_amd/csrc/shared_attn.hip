@@ -136,28 +136,29 @@ template <bool PAGED> __device__ __forceinline__ Entry entry_of(const RowsParams
     }
 }
 
-// Sets of rows: blocks of 32, at most eight to a set, as many to each.
-struct Sets { int n, blocks; };              // blocks: of a set
-__device__ __forceinline__ Sets sets_of(int rows)
-{
-    const int blocks = (rows + 31) >> 5, n = (blocks + kRowsWaves - 1) / kRowsWaves;
-    return {n, n > 1 ? (int)((uint32_t)(blocks + n - 1) / (uint32_t)n) : blocks};
-}
 __device__ __forceinline__ int chunks_of(const Entry& e) { return max(1, (e.key1 - e.key0 + 31) >> 5); }       // of 32 keys
 
 __device__ __forceinline__ int padded_rows(const RowsParams& p, const Entry& e) { return (e.n_q * p.group + 31) & ~31; }      // of a kv head
 
 // Work is counted in the time that 32 keys of a set take, and an item has kBegin more in front of its first: what a piece costs before and behind its keys.
+// A set has 256 rows, the last one what is left: of up to four blocks of 32 the keys are half as long with the matrix unit.
 constexpr int kBegin = 15, kLeastRun = 12;
 __device__ __forceinline__ bool narrow(int blocks) { return blocks <= 4; }
-__device__ __forceinline__ int chunk_work(int blocks) { return narrow(blocks) ? 2 : 3; }
+struct Sets {
+    int full, unit, whole, head;             // whole sets; work of 32 keys in the last; of a whole set; of a kv head
+    __device__ __forceinline__ int unit_of(int set) const { return set < full ? 3 : unit; }
+};
+__device__ __forceinline__ Sets sets_of(int rows, int chunks)
+{
+    const int full = rows / kSetRows, blocks = ((rows + 31) >> 5) - full * kRowsWaves, unit = narrow(blocks) ? 2 : 3, whole = chunks * 3 + kBegin;
+    return {full, unit, whole, full * whole + (blocks ? chunks * unit + kBegin : 0)};
+}
 
 struct Numbers { int work, rows; };          // of an entry, or in front of one
 __device__ __forceinline__ Numbers numbers_of(const RowsParams& p, const Entry& e)
 {
     if (e.n_q <= 0) return {0, 0};
-    const Sets sets = sets_of(e.n_q * p.group);
-    return {sets.n * p.n_kv_heads * (chunks_of(e) * chunk_work(sets.blocks) + kBegin), padded_rows(p, e) * p.n_kv_heads};
+    return {sets_of(e.n_q * p.group, chunks_of(e)).head * p.n_kv_heads, padded_rows(p, e) * p.n_kv_heads};
 }
 
 // The row of the partial results that workgroup j's piece of an item has: the rows of all items one after the other, and 256 on for every workgroup, so
@@ -690,22 +691,21 @@ void rows_kernel(const RowsParams p)
         en.q0 = __builtin_amdgcn_readfirstlane(en.q0); en.n_q = __builtin_amdgcn_readfirstlane(en.n_q);
         en.key0 = __builtin_amdgcn_readfirstlane(en.key0); en.key1 = __builtin_amdgcn_readfirstlane(en.key1);
         const int chunks = chunks_of(en), rows = en.n_q * p.group;
-        const Sets sets = sets_of(rows);
-        const int unit = chunk_work(sets.blocks), work = chunks * unit + kBegin;
-        const int item = (int)((uint32_t)(x - front.work) / (uint32_t)work), begin = x - front.work - item * work;
+        const Sets sets = sets_of(rows, chunks);
+        const int g = (int)((uint32_t)(x - front.work) / (uint32_t)sets.head), of_head = x - front.work - g * sets.head;
+        const int set = min((int)((uint32_t)of_head / (uint32_t)sets.whole), sets.full), begin = of_head - set * sets.whole, unit = sets.unit_of(set);
         // (32 keys are a workgroup's that has their first unit)
-        const auto chunk_at = [&](int u) { return max(0, (unit == 2 ? (u - kBegin + 1) >> 1 : (int)((uint32_t)max(u - kBegin + 2, 0) / 3u))); };
+        const auto chunk_at = [&](int u) { return max(0, unit == 2 ? (u - kBegin + 1) >> 1 : (int)((uint32_t)max(u - kBegin + 2, 0) / 3u)); };
         const int c_begin = chunk_at(begin), c_end = min(chunks, chunk_at(begin + x_end - x));
-        x = min(x_end, x + work - begin);
+        x = min(x_end, x + chunks * unit + kBegin - begin);
         if (c_end <= c_begin) {                              // (the front of an item alone)
             __syncthreads();
             continue;
         }
-        const int g = (int)((uint32_t)item / (uint32_t)sets.n), set = item - g * sets.n;
         Piece pc;
         pc.b = PAGED && own ? e - p.batch : e; pc.own = own;
         pc.q0 = en.q0; pc.n_q = en.n_q; pc.end = en.key1;
-        pc.g = g; pc.row0 = set * sets.blocks * 32; pc.n_rows = min(rows - pc.row0, sets.blocks * 32);
+        pc.g = g; pc.row0 = set * kSetRows; pc.n_rows = min(rows - pc.row0, kSetRows);
         pc.key0 = en.key0 + c_begin * 32; pc.key1 = min(en.key1, en.key0 + c_end * 32);
         pc.direct = own && en.key0 == 0 && c_begin == 0 && c_end == chunks;
         pc.part = part_row(j, front.rows + g * padded_rows(p, en) + pc.row0);
@@ -826,9 +826,8 @@ void rows_join_kernel(const RowsParams p)
     const auto pieces_of = [&](const RowsStart& s) {
         const Entry en = {s.q0, s.n_q, s.key0, s.key1, -1};
         const int row = (tok - en.q0) * p.group + head.r, chunks = chunks_of(en);
-        const Sets sets = sets_of(en.n_q * p.group);
-        const int unit = chunk_work(sets.blocks);
-        const int x = s.work + (head.q * sets.n + (int)((uint32_t)row / (uint32_t)(sets.blocks * 32))) * (chunks * unit + kBegin) + kBegin;
+        const Sets sets = sets_of(en.n_q * p.group, chunks);
+        const int set = row / kSetRows, unit = sets.unit_of(set), x = s.work + head.q * sets.head + set * sets.whole + kBegin;
         const int first = shares.of(x);
         return Pieces{first, shares.of(x + (chunks - 1) * unit) - first + 1, s.rows + head.q * padded_rows(p, en) + row};
     };
