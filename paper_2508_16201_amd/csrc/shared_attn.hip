@@ -41,6 +41,11 @@ __device__ __forceinline__ floatx16 mfma32(bf16x8 a, bf16x8 b, floatx16 c)
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
+// What is numbered.  Entry b is the keys that request b's group shares, if it is the group's first request; entry batch + b request b's own keys.
+// (Flat: the call's entry b; with ranges a share of its queries, with the keys that any of them sees: RowsParams::spans.)  An item is an entry's set of rows of a
+// kv head.  first: (paged, own keys) of the group that the request is taken with;  (flat) the call's entry.
+struct Entry { int q0, n_q, key0, key1, first; };
+
 struct RowsStart { int work, rows, q0, n_q, key0, key1, first, total; };       // in front of the entry; the entry; of all
 
 struct RowsParams {
@@ -63,6 +68,8 @@ struct RowsParams {
     int n_q_heads, n_kv_heads, group;
     uint32_t inv_page, inv_heads, inv_group;
     float scale_log2;
+    int entries, span;                           // numbered; (ranges) queries of a share
+    Entry* spans;
     int workgroups, padded;                      // that take runs; the launch
     float* part_o;                               // [rows_parts][D] unnormalised partial outputs (part_row)
     float* part_ml;                              // [rows_parts][2] running maximum in log2 units, sum
@@ -70,9 +77,6 @@ struct RowsParams {
     int most_rows;                               // that the entries may have, for partial results
 };
 
-// What is numbered.  Entry b is the keys that request b's group shares, if it is the group's first request; entry batch + b request b's own keys.
-// (Flat: entry b alone.)  An item is an entry's set of rows of a kv head.  first: (own keys) of the group that the request is taken with.
-struct Entry { int q0, n_q, key0, key1, first; };
 
 // What the call says of a request.
 struct Request { int q0, n_q, kvl, first, members, shared; };
@@ -115,14 +119,15 @@ __device__ __forceinline__ Entry own_entry(const RowsParams& p, int b, const Req
 
 template <bool PAGED> __device__ __forceinline__ Entry entry_of(const RowsParams& p, int e, bool grouped)
 {
-    if (e >= (PAGED ? 2 : 1) * p.batch) return {0, 0, 0, 0, -1};
+    if (e >= p.entries) return {0, 0, 0, 0, -1};
     const int b = PAGED && e >= p.batch ? e - p.batch : e;
     const Request r = request_of<PAGED>(p, b);
     if constexpr (!PAGED) {
+        if (p.ranges) return p.spans[e];
         const int k0 = p.cu_kv ? p.cu_kv[e] : 0, n = p.cu_kv ? p.cu_kv[e + 1] - k0 : p.kv_len;
         // (offsets that leave the tensors: nothing is read or written by them)
         if (r.n_q <= 0 || r.q0 < 0 || r.q0 > p.n_queries - r.n_q || n < 0 || k0 < 0 || k0 > p.kv_len - n) return {0, 0, 0, 0, -1};
-        return {r.q0, r.n_q, 0, n, -1};
+        return {r.q0, r.n_q, 0, n, e};
     } else {
         const int f = e < p.batch ? b : r.first;
         Entry all = {0, 0, 0, 0, -1};
@@ -627,7 +632,7 @@ void rows_kernel(const RowsParams p)
     if (j >= p.workgroups) return;
 
     // ---- the numbering ----
-    const int entries = PAGED ? 2 * p.batch : p.batch;
+    const int entries = p.entries;
     Numbers total, here;
     bool grouped = PAGED;
     const auto look_at = [&](int e) {                        // of 512 entries at a time, each thread one
@@ -690,6 +695,7 @@ void rows_kernel(const RowsParams p)
         Entry en = plan.entry[at];
         en.q0 = __builtin_amdgcn_readfirstlane(en.q0); en.n_q = __builtin_amdgcn_readfirstlane(en.n_q);
         en.key0 = __builtin_amdgcn_readfirstlane(en.key0); en.key1 = __builtin_amdgcn_readfirstlane(en.key1);
+        en.first = __builtin_amdgcn_readfirstlane(en.first);
         const int chunks = chunks_of(en), rows = en.n_q * p.group;
         const Sets sets = sets_of(rows, chunks);
         const int g = (int)((uint32_t)(x - front.work) / (uint32_t)sets.head), of_head = x - front.work - g * sets.head;
@@ -703,15 +709,62 @@ void rows_kernel(const RowsParams p)
             continue;
         }
         Piece pc;
-        pc.b = PAGED && own ? e - p.batch : e; pc.own = own;
+        pc.b = !PAGED ? en.first : own ? e - p.batch : e; pc.own = own;
         pc.q0 = en.q0; pc.n_q = en.n_q; pc.end = en.key1;
         pc.g = g; pc.row0 = set * kSetRows; pc.n_rows = min(rows - pc.row0, kSetRows);
         pc.key0 = en.key0 + c_begin * 32; pc.key1 = min(en.key1, en.key0 + c_end * 32);
-        pc.direct = own && en.key0 == 0 && c_begin == 0 && c_end == chunks;
+        pc.direct = own && !(PAGED && en.key0 > 0) && c_begin == 0 && c_end == chunks;
         pc.part = part_row(j, front.rows + g * padded_rows(p, en) + pc.row0);
         rows_piece<D, PAGED>(p, plan, lds0, pc);
         __syncthreads();                                     // the ring, and what the plan holds, are free again
     }
+}
+
+// (Ranges) The queries of entry b begin at q0: the number of its first share.  There is a share's room between an entry and the next, more than half of which is
+// for a share that is not whole.
+__device__ __forceinline__ int spans_before(const RowsParams& p, int q0, int b) { return q0 / p.span + b; }
+
+// Each share of an entry's queries with the keys that any of them sees, a wave to a share: a workgroup's keys are then those that its rows see, and the work is
+// dealt by them.
+__global__ __launch_bounds__(256)
+void rows_spans_kernel(const RowsParams p)
+{
+    const int lane = threadIdx.x & 63, e = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (e >= p.entries) return;
+    // the entry: the last one whose shares begin at or before this one
+    int b = 0;
+    if (p.cu_q) {
+        b = -1;
+        for (int c = 0; c < p.batch; c += kWave) {
+            const uint64_t begun = __ballot(c + lane < p.batch && spans_before(p, p.cu_q[min(c + lane, p.batch - 1)], c + lane) <= e);
+            if (begun) b = c + 63 - __builtin_clzll(begun);
+        }
+    }
+    Entry s = {0, 0, 0, 0, b};
+    if (b >= 0) {
+        const int q0 = p.cu_q ? p.cu_q[b] : 0, n_q = p.cu_q ? p.cu_q[b + 1] - q0 : p.q_len, k0 = p.cu_kv ? p.cu_kv[b] : 0,
+                  n = p.cu_kv ? p.cu_kv[b + 1] - k0 : p.kv_len, at = (e - spans_before(p, q0, b)) * p.span;
+        if (n_q > 0 && q0 >= 0 && q0 <= p.n_queries - n_q && n >= 0 && k0 >= 0 && k0 <= p.kv_len - n && at >= 0 && at < n_q) {
+            s.q0 = q0 + at;
+            s.n_q = min(p.span, n_q - at);
+            int lo = INT_MAX, hi = 0;
+            for (int t = lane; t < s.n_q; t += kWave) {
+                const int from = max(p.ranges[2 * (int64_t)(s.q0 + t)], 0), to = min(p.ranges[2 * (int64_t)(s.q0 + t) + 1], n);
+                if (from < to) {
+                    lo = min(lo, from);
+                    hi = max(hi, to);
+                }
+            }
+#pragma unroll
+            for (int d = 1; d < kWave; d *= 2) {
+                lo = min(lo, __shfl_xor(lo, d));
+                hi = max(hi, __shfl_xor(hi, d));
+            }
+            s.key0 = min(lo, hi);
+            s.key1 = hi;
+        }
+    }
+    if (lane == 0) p.spans[e] = s;
 }
 
 // One row over all of its keys once more, by a wave, where its sum came out as no finite number: mostly for an infinite value, which a row that sees it gets as it is,
@@ -735,7 +788,7 @@ __device__ __forceinline__ void odd_row(const RowsParams& p, const RowsStart& ow
         }
     } else if (p.ranges) {
         lo = max(p.ranges[2 * (int64_t)tok], 0);
-        hi = min(p.ranges[2 * (int64_t)tok + 1], own.key1);
+        hi = min(p.ranges[2 * (int64_t)tok + 1], own.key1);         // (what lies behind the share's keys is no range of its queries)
     }
     float o[COLS];
 #pragma unroll
@@ -815,7 +868,13 @@ void rows_join_kernel(const RowsParams p)
         if (!behind) return;                                 // (a row behind the last request)
         b += __builtin_ctzll(behind);
     }
-    const RowsStart own = p.starts[PAGED ? p.batch + b : b];
+    int e = PAGED ? p.batch + b : b;
+    if (!PAGED && p.ranges) {
+        const int q0 = p.cu_q ? p.cu_q[b] : 0;
+        if (q0 < 0 || tok < q0) return;
+        e = spans_before(p, q0, b) + (tok - q0) / p.span;
+    }
+    const RowsStart own = p.starts[e];
     const int total = own.total;
     const Shares shares = shares_of(p, total);
     if (total == 0 || own.n_q <= 0 || tok < own.q0) return;
@@ -919,17 +978,26 @@ void rows_join_kernel(const RowsParams p)
 
 namespace {
 
+// What a call numbers: requests' shared and own keys;  entries;  or, with ranges, shares of the entries' queries, as many queries as fill a set of rows.
+int rows_span(int n_q_heads, int n_kv_heads) { const int group = n_q_heads / n_kv_heads; return group < kSetRows ? kSetRows / group : 1; }
+int64_t rows_entries(bool paged, bool ranges, int batch, int n_queries, int n_q_heads, int n_kv_heads)
+{
+    return paged ? 2 * (int64_t)batch : ranges ? (int64_t)batch + n_queries / rows_span(n_q_heads, n_kv_heads) + 1 : batch;
+}
 // Rows of partial results: 256 for every workgroup, and those of all entries, each a multiple of 32 (a query is in one entry of own keys and at most one of
 // shared ones, of which there are at most half as many as requests).
-int64_t rows_parts(bool paged, int workgroups, int batch, int n_queries, int n_q_heads, int n_kv_heads)
+int64_t rows_parts(bool paged, bool ranges, int workgroups, int batch, int n_queries, int n_q_heads, int n_kv_heads)
 {
-    const int64_t rows = (int64_t)n_queries * n_q_heads * (paged ? 2 : 1), entries = paged ? batch + batch / 2 : batch;
+    const int64_t rows = (int64_t)n_queries * n_q_heads * (paged ? 2 : 1),
+                  entries = paged ? batch + batch / 2 : rows_entries(paged, ranges, batch, n_queries, n_q_heads, n_kv_heads);
     return (int64_t)workgroups * kSetRows + rows + entries * 32 * n_kv_heads;
 }
+// (asked without knowing of ranges: with them there are more entries)
 size_t rows_workspace(bool paged, int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim)
 {
-    const size_t rows = (size_t)rows_parts(paged, kNumCu, batch, n_queries, n_q_heads, n_kv_heads);
-    return align256(rows * head_dim * sizeof(float)) + align256(rows * 2 * sizeof(float)) + align256((size_t)(paged ? 2 : 1) * batch * sizeof(RowsStart));
+    const size_t rows = (size_t)rows_parts(paged, true, kNumCu, batch, n_queries, n_q_heads, n_kv_heads);
+    const size_t entries = (size_t)rows_entries(paged, true, batch, n_queries, n_q_heads, n_kv_heads);
+    return align256(rows * head_dim * sizeof(float)) + align256(rows * 2 * sizeof(float)) + align256(entries * sizeof(RowsStart)) + align256(entries * sizeof(Entry));
 }
 bool rows_shape(int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim)
 {
@@ -947,6 +1015,10 @@ int launch_rows(RowsParams& p, hipStream_t stream)
     const bool few = rows <= 2048;
     const int64_t joins = few ? rows : ((int64_t)p.n_queries * units + 3) / 4;
     if (!launchable(joins, 256)) return SPECVLM_EUNSUPPORTED;
+    if (!PAGED && p.ranges) {
+        rows_spans_kernel<<<(p.entries + 3) / 4, 256, 0, stream>>>(p);
+        if (const int rc = launch_status()) return rc;
+    }
     p.workgroups = kNumCu;
     p.padded = round_up(p.workgroups, kNumXcd);
     rows_kernel<D, PAGED><<<p.padded, kRowsThreads, lds, stream>>>(p);
@@ -958,15 +1030,16 @@ int launch_rows(RowsParams& p, hipStream_t stream)
 
 // What both calls ask of the queries, and what they share of the parameters.
 int rows_start(RowsParams& p, bool paged, const void* q, int64_t q_tok, int64_t q_head, const void* k, const void* v, int64_t tok, int64_t head, int batch,
-               int n_queries, int most_keys, int n_q_heads, int n_kv_heads, int head_dim, float scale, void* out, float* lse, void* workspace,
-               size_t workspace_bytes)
+               int n_queries, int most_keys, int n_q_heads, int n_kv_heads, int head_dim, float scale, const int32_t* key_ranges, void* out, float* lse,
+               void* workspace, size_t workspace_bytes)
 {
     if (!q || !out || !k || !v) return SPECVLM_EINVAL;
     if ((q_tok | q_head | tok | head) & 7) return SPECVLM_EUNSUPPORTED;
     if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 15) return SPECVLM_EUNSUPPORTED;
     // (a lane's offset inside 16 keys has 32 bits; rows, and tiles of all sets and heads, are ints)
     if (tok < 0 || tok >= ((int64_t)1 << 26)) return SPECVLM_EUNSUPPORTED;
-    const int64_t rows = (int64_t)n_queries * n_q_heads, entries = paged ? 2 * (int64_t)batch : batch;
+    const bool ranges = key_ranges != nullptr;
+    const int64_t rows = (int64_t)n_queries * n_q_heads, entries = rows_entries(paged, ranges, batch, n_queries, n_q_heads, n_kv_heads);
     if (rows >= ((int64_t)1 << 29) || entries * 32 * n_kv_heads >= ((int64_t)1 << 29)) return SPECVLM_EUNSUPPORTED;
     const int64_t sets = (2 * rows / kSetRows + n_kv_heads) + entries * n_kv_heads;
     if (sets * 3 * (most_keys / 32 + 6) >= ((int64_t)1 << 31)) return SPECVLM_EUNSUPPORTED;
@@ -979,11 +1052,13 @@ int rows_start(RowsParams& p, bool paged, const void* q, int64_t q_tok, int64_t 
     p.n_q_heads = n_q_heads; p.n_kv_heads = n_kv_heads; p.group = n_q_heads / n_kv_heads;
     p.inv_group = reciprocal(p.group);
     p.scale_log2 = scale * kLog2e;
-    p.most_rows = (int)(rows_parts(paged, 0, batch, n_queries, n_q_heads, n_kv_heads));
-    const size_t parts = (size_t)rows_parts(paged, kNumCu, batch, n_queries, n_q_heads, n_kv_heads);
+    p.most_rows = (int)rows_parts(paged, ranges, 0, batch, n_queries, n_q_heads, n_kv_heads);
+    p.entries = (int)entries; p.ranges = key_ranges; p.span = rows_span(n_q_heads, n_kv_heads);
+    const size_t parts = (size_t)rows_parts(paged, true, kNumCu, batch, n_queries, n_q_heads, n_kv_heads);
     p.part_o = (float*)workspace;
     p.part_ml = (float*)((char*)workspace + align256(parts * head_dim * sizeof(float)));
     p.starts = (RowsStart*)((char*)p.part_ml + align256(parts * 2 * sizeof(float)));
+    p.spans = (Entry*)((char*)p.starts + align256((size_t)rows_entries(paged, true, batch, n_queries, n_q_heads, n_kv_heads) * sizeof(RowsStart)));
     return SPECVLM_OK;
 }
 
@@ -1017,7 +1092,7 @@ extern "C" int specvlm_shared_attn(
     if (page_stride & 7 || kv_len > (1 << 30)) return SPECVLM_EUNSUPPORTED;
     RowsParams p;
     if (const int rc = rows_start(p, true, q, q_tok_stride, q_head_stride, k_pages, v_pages, tok_stride, head_stride, batch, n_queries, kv_len, n_q_heads,
-                                  n_kv_heads, head_dim, softmax_scale, out, lse, workspace, workspace_bytes))
+                                  n_kv_heads, head_dim, softmax_scale, nullptr, out, lse, workspace, workspace_bytes))
         return rc;
     p.page = page_stride; p.n_pages = n_pages; p.page_size = page_size; p.inv_page = reciprocal(page_size);
     p.table = page_table; p.table_row = table_stride; p.most_shared = kv_len;
@@ -1046,8 +1121,8 @@ extern "C" int specvlm_cross_attn(
     if (n_states > (1 << 30)) return SPECVLM_EUNSUPPORTED;
     RowsParams p;
     if (const int rc = rows_start(p, false, q, q_tok_stride, q_head_stride, k, v, kv_tok_stride, kv_head_stride, batch, n_queries, n_states, n_q_heads,
-                                  n_kv_heads, head_dim, softmax_scale, out, lse, workspace, workspace_bytes))
+                                  n_kv_heads, head_dim, softmax_scale, key_ranges, out, lse, workspace, workspace_bytes))
         return rc;
-    p.cu_q = cu_q; p.cu_kv = cu_kv; p.q_len = n_queries; p.ranges = key_ranges;
+    p.cu_q = cu_q; p.cu_kv = cu_kv; p.q_len = n_queries;
     return head_dim == 128 ? launch_rows<128, false>(p, (hipStream_t)stream) : launch_rows<64, false>(p, (hipStream_t)stream);
 }
