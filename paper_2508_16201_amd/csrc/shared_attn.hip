@@ -146,9 +146,9 @@ __device__ __forceinline__ int chunks_of(const Entry& e) { return max(1, (e.key1
 __device__ __forceinline__ int padded_rows(const RowsParams& p, const Entry& e) { return (e.n_q * p.group + 31) & ~31; }      // of a kv head
 
 // Work is counted in the time that 32 keys of a set take, and an item has kBegin more in front of its first: what a piece costs before and behind its keys.
-// A set has 256 rows, the last one what is left: of up to four blocks of 32 the keys are half as long with the matrix unit.
-constexpr int kBegin = 15, kLeastRun = 12;
-__device__ __forceinline__ bool narrow(int blocks) { return blocks <= 4; }
+// A set has 256 rows, the last one what is left: of one or two blocks of 32 the keys take as long as they take to come.
+constexpr int kBegin = 18, kLeastRun = 12;
+__device__ __forceinline__ bool narrow(int blocks) { return blocks <= 2; }
 struct Sets {
     int full, unit, whole, head;             // whole sets; work of 32 keys in the last; of a whole set; of a kv head
     __device__ __forceinline__ int unit_of(int set) const { return set < full ? 3 : unit; }
@@ -262,9 +262,12 @@ __device__ __forceinline__ void load_to_lds(const char* base, uint32_t lane_offs
 }
 #pragma clang diagnostic pop
 
-// XOR on the number of a value row's 16-byte piece.  The transposing read of 16 keys and 32 columns touches, per 32 lanes, 4 keys x 64 bytes (pieces 4j..4j+3):
-// with this they fall on 64 distinct banks.
-template <int D> __device__ __forceinline__ constexpr int rows_v_swizzle(int key) { return D == 128 ? (key & 3) << 2 : (key >> 1 & 1) << 2; }
+// How a tile lies in LDS.  A direct load brings 1 KB, of ROWS rows, and its lanes may take their 16 bytes from any of them: so the bytes lie as they are read, and
+// every address is one of the lane and a constant.  Keys: piece (16 bytes) after piece, of each the rows;  32 lanes read the same piece of 32 rows, and with
+// the loads PAD apart 16 of them touch all banks once.  Values: 32 columns after 32 columns, of each the rows;  32 lanes of a transposing read touch 4 rows.
+template <int D> struct Layout {
+    static constexpr int ROWS = 512 / D, PAD = ROWS * 16, LOAD = 1024 + PAD, TILE = kRowsTile / ROWS * LOAD;
+};
 
 template <class T> __device__ __forceinline__ SPECVLM_AS3 T* in_lds(uint32_t at) { return (SPECVLM_AS3 T*)(uintptr_t)at; }
 
@@ -281,15 +284,28 @@ __device__ __forceinline__ float half_sum(float x)
     return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
+// What is computed from x stays where it is written: taken out of the loops, it would be in registers that the products need.
+__device__ __forceinline__ void held(int& x) { __asm__ volatile("" : "+v"(x)); }
+// (and the parameters are fetched where they are used: a kernel's, all held from its start, were more than there are scalar registers)
+#define SPECVLM_AS4 __attribute__((address_space(4)))
+__device__ __forceinline__ const SPECVLM_AS4 RowsParams& rows_params()
+{
+    const SPECVLM_AS4 RowsParams* z = (const SPECVLM_AS4 RowsParams*)__builtin_amdgcn_kernarg_segment_ptr();
+    __asm__ volatile("" : "+s"(z));
+    return *z;
+}
+
 // Takes a piece and writes what comes of it.
 template <int D, bool PAGED>
-__device__ __forceinline__ void rows_piece(const RowsParams& p, RowsPlan& plan, const uint32_t lds0, const Piece& pc)
+__device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, const Piece& pc)
 {
-    constexpr int KK = D / 16, JB = D / 32, CH = D / 8, ROW_BYTES = D * 2;
-    constexpr int TILE_BYTES = kRowsTile * ROW_BYTES;        // of K or V
-    constexpr int KEYS_PER_LOAD = kWave / CH, LOADS = 16 / KEYS_PER_LOAD;
+    constexpr int KK = D / 16, JB = D / 32, ROWS = Layout<D>::ROWS, LOAD_BYTES = Layout<D>::LOAD, TILE_BYTES = Layout<D>::TILE;
+    constexpr int LOADS = 16 / ROWS, CHUNK_BYTES = 32 / ROWS * LOAD_BYTES;
     static_assert(kSetRows * D * 4 <= 4 * TILE_BYTES, "the exchange of waves that share rows");
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const SPECVLM_AS4 RowsParams& p = rows_params();
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int lane = threadIdx.x & 63;
+    held(lane);
     const int r = lane & 31, h = lane >> 5;
     const float sc = fmaxf(p.scale_log2, 1e-30f);            // (a zero scale as a vanishing one: -inf stays -inf)
     const int n_blocks = (pc.n_rows + 31) >> 5, log_blocks = n_blocks > 4 ? 3 : n_blocks > 2 ? 2 : n_blocks - 1;       // waves of a kind
@@ -310,7 +326,7 @@ __device__ __forceinline__ void rows_piece(const RowsParams& p, RowsPlan& plan, 
         places = pg.r;
     };
     const auto issue = [&](int tile, int stage) {
-        const uint32_t to = lds0 + stage * 2 * TILE_BYTES + wave * 16 * ROW_BYTES;
+        const uint32_t to = lds0 + stage * 2 * TILE_BYTES + wave * LOADS * LOAD_BYTES;
         int64_t first;
         const int key = key0 + tile * kRowsTile + wave * 16;
         int last;                                        // the last of the 16 keys that there is: it stands for those behind it, whatever lies there
@@ -329,74 +345,73 @@ __device__ __forceinline__ void rows_piece(const RowsParams& p, RowsPlan& plan, 
         }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int kl = i * KEYS_PER_LOAD + lane / CH, piece = lane % CH;
-            const uint32_t row = (uint32_t)min(kl, last) * (uint32_t)(p.tok * 2);
-            load_to_lds(k_at + 2 * first, row + (piece ^ (D == 128 ? kl & 15 : kl >> 1 & 7)) * 16, to + i * 1024);
-            load_to_lds(v_at + 2 * first, row + (piece ^ rows_v_swizzle<D>(kl)) * 16, to + TILE_BYTES + i * 1024);
+            const auto from = [&](int row, int piece) { return (uint32_t)min(i * ROWS + row, last) * (uint32_t)(p.tok * 2) + piece * 16; };
+            load_to_lds(k_at + 2 * first, from(lane % ROWS, lane / ROWS), to + i * LOAD_BYTES);
+            load_to_lds(v_at + 2 * first, from((lane >> 2) % ROWS, lane / (4 * ROWS) * 4 + (lane & 3)), to + TILE_BYTES + i * LOAD_BYTES);
         }
     };
-    const auto begin_loads = [&] {
-        if constexpr (PAGED) look_up(0);
-        issue(0, 0);
-    };
-    if (tiles > 0) begin_loads();                        // (on their way while the rows are looked at)
 
-    // this wave's rows
+    // this wave's rows; their queries are fetched while the first tile's pages are looked up
+    if (PAGED && tiles > 0) look_up(0);
     const int my_row = blk * 32 + r;
     const QuotRem q_at = divide(pc.row0 + (my_row < pc.n_rows ? my_row : 0), p.group, p.inv_group);  // (padding rows take the first: never stored)
     const int64_t q_tok = pc.q0 + q_at.q;
-    const int q_hd = pc.g * p.group + q_at.r;
     bf16x8 qf[KK];
-    const __bf16* const qp = p.q + q_tok * p.q_tok + (int64_t)q_hd * p.q_head + h * 8;
+    const __bf16* const qp = p.q + q_tok * p.q_tok + (int64_t)(pc.g * p.group + q_at.r) * p.q_head + h * 8;
 #pragma unroll
     for (int s = 0; s < KK; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qp + s * 16);
-    // the keys that it sees: [lo, hi), of the block those of a tree node's mask
-    int lo = key0, hi = key1;
-    const int before = pc.end - pc.n_q;                 // (own keys of a block)
+    if (tiles > 0) issue(0, 0);
+    // the keys that it sees: [lo, hi), of the block those of a tree node's mask;  of all of the wave's rows: keys that all see, and that some see
+    int lo = key0, hi = key1, all_lo = key0, all_hi = key1, any_lo = key0, any_hi = key1;
+    const int before = pc.end - pc.n_q;                      // (own keys of a block)
     uint64_t tree = 0;
     bool is_tree = false;
     if constexpr (PAGED) {
         if (pc.own) {
             is_tree = p.block_mask != nullptr;
-            if (is_tree) tree = p.block_mask[q_tok];
-            else hi = min(hi, before + q_at.q + 1);
+            if (is_tree) {
+                tree = p.block_mask[q_tok];
+                all_hi = min(before, key1);
+            } else {
+                hi = min(hi, before + q_at.q + 1);
+                all_hi = min(key1, before + divide(pc.row0 + blk * 32, p.group, p.inv_group).q + 1);
+                any_hi = min(key1, before + divide(pc.row0 + min(blk * 32 + 31, pc.n_rows - 1), p.group, p.inv_group).q + 1);
+            }
         }
     } else if (p.ranges) {
         lo = min(max(p.ranges[2 * q_tok], 0), key1);
         hi = min(max(p.ranges[2 * q_tok + 1], 0), key1);
-    }
-    // of all of the wave's rows: keys that all see, and that some see
-    int all_lo = lo, all_hi = is_tree ? min(before, hi) : hi, any_lo = lo < hi ? lo : INT_MAX, any_hi = lo < hi ? hi : 0;
+        all_lo = lo, all_hi = hi, any_lo = lo < hi ? lo : INT_MAX, any_hi = lo < hi ? hi : 0;
 #pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-        all_lo = max(all_lo, __shfl_xor(all_lo, d)); all_hi = min(all_hi, __shfl_xor(all_hi, d));
-        any_lo = min(any_lo, __shfl_xor(any_lo, d)); any_hi = max(any_hi, __shfl_xor(any_hi, d));
+        for (int d = 1; d < 32; d *= 2) {
+            all_lo = max(all_lo, __shfl_xor(all_lo, d)); all_hi = min(all_hi, __shfl_xor(all_hi, d));
+            any_lo = min(any_lo, __shfl_xor(any_lo, d)); any_hi = max(any_hi, __shfl_xor(any_hi, d));
+        }
+        all_lo = __builtin_amdgcn_readfirstlane(all_lo); all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+        any_lo = __builtin_amdgcn_readfirstlane(any_lo); any_hi = __builtin_amdgcn_readfirstlane(any_hi);
     }
-    all_lo = __builtin_amdgcn_readfirstlane(all_lo); all_hi = __builtin_amdgcn_readfirstlane(all_hi);
-    any_lo = __builtin_amdgcn_readfirstlane(any_lo); any_hi = __builtin_amdgcn_readfirstlane(any_hi);
 
     float m_run, l_run;
     floatx16 o[JB];
     // where this lane reads in a stage
-    const uint32_t k_base = lds0 + r * ROW_BYTES + (h ^ (D == 128 ? r & 15 : r >> 1 & 7)) * 16;
+    const uint32_t k_base = lds0 + r / ROWS * LOAD_BYTES + r % ROWS * 16 + h * ROWS * 16;
     const int v_row = 4 * h + ((lane & 15) >> 2);
-    const uint32_t v_base = lds0 + TILE_BYTES + v_row * ROW_BYTES + ((((lane >> 4 & 1) * 2 + ((lane & 3) >> 1)) ^ rows_v_swizzle<D>(v_row)) * 16) + (lane & 1) * 8;
-
+    const uint32_t v_base = lds0 + TILE_BYTES + v_row / ROWS * LOAD_BYTES + v_row % ROWS * 64 + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
     // V^T fragments of 16 keys, by the transposing read
     const auto read_values = [&](bf16x8 (&vf)[JB], uint32_t at) {
 #pragma unroll
         for (int jb = 0; jb < JB; ++jb) {
             typedef short s16x4 __attribute__((ext_vector_type(4)));
-            SPECVLM_AS3 s16x4* const src = in_lds<s16x4>(v_base + at ^ jb * 64);
+            SPECVLM_AS3 s16x4* const src = in_lds<s16x4>(v_base + at) + jb * ROWS * 64 / 8;
             const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(src);
-            const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16(src + 8 * ROW_BYTES / 8);
+            const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16(src + 8 / ROWS * LOAD_BYTES / 8);
             vf[jb] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, c, 0, 1, 2, 3, 4, 5, 6, 7));
         }
     };
 
     const auto read_keys = [&](bf16x8 (&kf)[KK], uint32_t at) {
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) kf[kk] = __builtin_bit_cast(bf16x8, *in_lds<const u32x4>(k_base + at ^ kk * 32));
+        for (int kk = 0; kk < KK; ++kk) kf[kk] = __builtin_bit_cast(bf16x8, in_lds<const u32x4>(k_base + at)[kk * 2 * ROWS]);
     };
     // S^T = K Q^T for 32 keys
     const auto logits = [&](const bf16x8 (&kf)[KK]) {
@@ -473,6 +488,84 @@ __device__ __forceinline__ void rows_piece(const RowsParams& p, RowsPlan& plan, 
     };
     const auto lds_done = [] { __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
 
+    // A tile that all rows of the wave see whole, after others: while the vector unit weighs 32 keys, the matrix unit takes the products with the values of the last
+    // 32 and then the logits of the next.  (The wave's keys of a tile: all, or every second 32.)  Returns how many it has taken: those that go beyond the maximum are left.
+    const auto whole_tile = [&](auto pieces, const uint32_t at) {
+        constexpr int N = decltype(pieces)::value, STEP = kChunks / N * CHUNK_BYTES;
+        floatx16 s;
+        bf16x8 pf[2];
+        {
+            bf16x8 kf[KK];
+            read_keys(kf, at);
+            s = logits(kf);
+        }
+#pragma unroll
+        for (int ch = 0; ch <= N; ++ch) {
+            float pv[16], psum = 0.f;
+            __builtin_amdgcn_sched_barrier(0);
+            if (ch > 0) {
+                bf16x8 vf[2][JB];
+                read_values(vf[0], at + (ch - 1) * STEP);
+                read_values(vf[1], at + (ch - 1) * STEP + CHUNK_BYTES / 2);
+                __builtin_amdgcn_sched_barrier(0);
+                if (ch < N) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) pv[i] = fast_exp2(fmaf(s[i], sc, -m_run));
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int jb = 0; jb < JB; ++jb) o[jb] = mfma32(vf[u][jb], pf[u], o[jb]);
+                if (ch < N) {
+#pragma unroll
+                    for (int i = 0; i < 2 * JB; ++i) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x002, 16 / JB, 0);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) pv[i] = fast_exp2(fmaf(s[i], sc, -m_run));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (ch == N) break;
+            if (ch + 1 < N) {
+                bf16x8 kf[KK];
+                read_keys(kf, at + (ch + 1) * STEP);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) psum += pv[i];
+                s = logits(kf);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    floatx8 pu;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) pu[i] = pv[8 * u + i];
+                    pf[u] = __builtin_convertvector(pu, bf16x8);
+                }
+#pragma unroll
+                for (int i = 0; i < KK; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 24 / KK, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) psum += pv[i];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    floatx8 pu;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) pu[i] = pv[8 * u + i];
+                    pf[u] = __builtin_convertvector(pu, bf16x8);
+                }
+            }
+            if (__builtin_expect(__any(!(psum < kRowsRedo)), 0)) return ch;      // (these keys and the tile's others against another maximum)
+            l_run += psum;
+        }
+        return N;
+    };
+
     // The sweep.
     const auto sweep = [&] {
         begin_sums();
@@ -485,10 +578,15 @@ __device__ __forceinline__ void rows_piece(const RowsParams& p, RowsPlan& plan, 
             if (t + 1 < tiles) issue(t + 1, stage ^ 1);
             if (!works) continue;
             const uint64_t there = pages_there(stage);
-            for (int ch = ks; ch < kChunks; ch += n_ks) {
+            int ch0 = ks;
+            if (n_ks <= 2 && !fresh && there == 0x0101010101010101ull && key0 + t * kRowsTile >= all_lo && key0 + (t + 1) * kRowsTile <= all_hi) {
+                if (n_ks == 1) ch0 = whole_tile(std::integral_constant<int, kChunks>(), stage * 2 * TILE_BYTES);
+                else ch0 = ks + 2 * whole_tile(std::integral_constant<int, kChunks / 2>(), stage * 2 * TILE_BYTES + ks * CHUNK_BYTES);
+            }
+            for (int ch = ch0; ch < kChunks; ch += n_ks) {
                 const int k0 = key0 + t * kRowsTile + ch * 32;
                 if (k0 >= any_hi || k0 + 31 < any_lo) continue;
-                const uint32_t at_chunk = stage * 2 * TILE_BYTES + ch * 32 * ROW_BYTES;
+                const uint32_t at_chunk = stage * 2 * TILE_BYTES + ch * CHUNK_BYTES;
                 bf16x8 kf[KK], vf[2][JB];
                 read_keys(kf, at_chunk);
                 const floatx16 s = logits(kf);
@@ -506,7 +604,7 @@ __device__ __forceinline__ void rows_piece(const RowsParams& p, RowsPlan& plan, 
 #pragma unroll
                     for (int i = 0; i < 8; ++i) pu[i] = pv[8 * u + i];
                     const bf16x8 pf = __builtin_convertvector(pu, bf16x8);
-                    if (u == 0) read_values(vf[1], at_chunk + 16 * ROW_BYTES);
+                    if (u == 0) read_values(vf[1], at_chunk + CHUNK_BYTES / 2);
                     if (PAGED && !(two >> (8 * u) & 1))      // (what lies in the place of a page that is none may be anything)
 #pragma unroll
                         for (int jb = 0; jb < JB; ++jb) vf[u][jb] = __builtin_bit_cast(bf16x8, u32x4{});
@@ -533,25 +631,29 @@ __device__ __forceinline__ void rows_piece(const RowsParams& p, RowsPlan& plan, 
     __syncthreads();                                         // everyone has left the tiles
 
     l_run = half_sum(l_run);
-        const auto inverse = [](float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN; };
+    int thread = threadIdx.x;
+    held(thread);
+    const SPECVLM_AS4 RowsParams& z = rows_params();
+    const int row_in_block = thread & 31, half = thread >> 5 & 1;
+    const auto inverse = [](float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN; };
     // (the join looks after sums that are no finite numbers: such a row is not written here, where its queries may lie, and told of by a negative sum of its
     // probabilities)
-    const auto tell = [&](int row, float m, float l, bool odd) { *reinterpret_cast<float2*>(p.part_ml + 2 * (pc.part + row)) = float2{m, odd ? -l : l}; };
+    const auto tell = [&](int row, float m, float l, bool odd) { *reinterpret_cast<float2*>(z.part_ml + 2 * (pc.part + row)) = float2{m, odd ? -l : l}; };
     if (n_ks > 1) {
         // ---- waves that share rows: all sums to LDS (16-byte pieces of a row XORed by its number: its banks), then a row's four columns to a thread ----
         float* const s_o = (float*)in_lds<float>(lds0);
         if (works) {
-            const int row = (ks * n_blocks + blk) * 32 + r;
-            if (h == 0) *reinterpret_cast<float2*>(plan.ml + 2 * row) = float2{m_run, l_run};
+            const int row = (ks * n_blocks + blk) * 32 + row_in_block;
+            if (half == 0) *reinterpret_cast<float2*>(plan.ml + 2 * row) = float2{m_run, l_run};
 #pragma unroll
             for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
                 for (int i4 = 0; i4 < 4; ++i4)
-                    *reinterpret_cast<floatx4*>(s_o + row * D + ((jb * 8 + i4 * 2 + h) ^ (r & (D / 4 - 1))) * 4) =
+                    *reinterpret_cast<floatx4*>(s_o + row * D + ((jb * 8 + i4 * 2 + half) ^ (row_in_block & (D / 4 - 1))) * 4) =
                         floatx4{o[jb][4 * i4], o[jb][4 * i4 + 1], o[jb][4 * i4 + 2], o[jb][4 * i4 + 3]};
         }
         __syncthreads();
-        for (int at = threadIdx.x; at < pc.n_rows * (D / 4); at += kRowsThreads) {
+        for (int at = thread; at < pc.n_rows * (D / 4); at += kRowsThreads) {
             const int row = at / (D / 4), c = at % (D / 4);
             float2 ml[kChunks];
             float m = -INFINITY, l = 0.f;
@@ -572,20 +674,24 @@ __device__ __forceinline__ void rows_piece(const RowsParams& p, RowsPlan& plan, 
                 for (int i = 0; i < 4; ++i) sum[i] += y[i] * w;
             }
             if (pc.direct) {
-                const QuotRem at_q = divide(pc.row0 + row, p.group, p.inv_group);
+                const QuotRem at_q = divide(pc.row0 + row, z.group, z.inv_group);
                 const int64_t tok = pc.q0 + at_q.q;
-                const int hd = pc.g * p.group + at_q.r;
-                const bool odd = __ballot(!((sum[0] + sum[1] + sum[2] + sum[3]) * 0.f == 0.f)) >> (lane & ~(D / 4 - 1)) & (D == 128 ? 0xffffffffull : 0xffffull);
-                if (!odd) *reinterpret_cast<bf16x4*>(p.out + tok * p.q_tok + (int64_t)hd * p.q_head + c * 4) = __builtin_convertvector(sum * inverse(l), bf16x4);
-                if (p.lse && c == 0) p.lse[tok * p.n_q_heads + hd] = l == 0.f ? -INFINITY : (m + fast_log2(l)) * kLn2;
+                const int hd = pc.g * z.group + at_q.r;
+                const bool odd = __ballot(!((sum[0] + sum[1] + sum[2] + sum[3]) * 0.f == 0.f)) >> (thread & 63 & ~(D / 4 - 1)) & (D == 128 ? 0xffffffffull : 0xffffull);
+                if (!odd) *reinterpret_cast<bf16x4*>(z.out + tok * z.q_tok + (int64_t)hd * z.q_head + c * 4) = __builtin_convertvector(sum * inverse(l), bf16x4);
+                if (z.lse && c == 0) z.lse[tok * z.n_q_heads + hd] = l == 0.f ? -INFINITY : (m + fast_log2(l)) * kLn2;
                 if (c == 0) tell(row, m, l, odd);
             } else {
-                *reinterpret_cast<floatx4*>(p.part_o + (pc.part + row) * D + c * 4) = sum;
+                *reinterpret_cast<floatx4*>(z.part_o + (pc.part + row) * D + c * 4) = sum;
                 if (c == 0) tell(row, m, l, false);
             }
         }
-    } else if (works && my_row < pc.n_rows) {
+    } else if (works && blk * 32 + row_in_block < pc.n_rows) {
+        const int row = blk * 32 + row_in_block;
         if (pc.direct) {
+            const QuotRem at_q = divide(pc.row0 + row, z.group, z.inv_group);
+            const int64_t tok = pc.q0 + at_q.q;
+            const int hd = pc.g * z.group + at_q.r;
             float odd = 0.f;
 #pragma unroll
             for (int jb = 0; jb < JB; ++jb)
@@ -593,7 +699,7 @@ __device__ __forceinline__ void rows_piece(const RowsParams& p, RowsPlan& plan, 
                 for (int i = 0; i < 16; ++i) odd += 0.f * o[jb][i];
             odd = half_sum(odd);
             const float inv = inverse(l_run);
-            __bf16* const op = p.out + q_tok * p.q_tok + (int64_t)q_hd * p.q_head + h * 4;
+            __bf16* const op = z.out + tok * z.q_tok + (int64_t)hd * z.q_head + half * 4;
             if (odd == 0.f) {
 #pragma unroll
                 for (int jb = 0; jb < JB; ++jb)
@@ -603,15 +709,15 @@ __device__ __forceinline__ void rows_piece(const RowsParams& p, RowsPlan& plan, 
                         *reinterpret_cast<bf16x4*>(op + jb * 32 + i4 * 8) = __builtin_convertvector(y, bf16x4);
                     }
             }
-            if (p.lse && h == 0) p.lse[q_tok * p.n_q_heads + q_hd] = l_run == 0.f ? -INFINITY : (m_run + fast_log2(l_run)) * kLn2;
-            if (h == 0) tell(my_row, m_run, l_run, !(odd == 0.f));
+            if (z.lse && half == 0) z.lse[tok * z.n_q_heads + hd] = l_run == 0.f ? -INFINITY : (m_run + fast_log2(l_run)) * kLn2;
+            if (half == 0) tell(row, m_run, l_run, !(odd == 0.f));
         } else {
-            if (h == 0) tell(my_row, m_run, l_run, false);
+            if (half == 0) tell(row, m_run, l_run, false);
 #pragma unroll
             for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
                 for (int i4 = 0; i4 < 4; ++i4)
-                    *reinterpret_cast<floatx4*>(p.part_o + (pc.part + my_row) * D + jb * 32 + i4 * 8 + h * 4) =
+                    *reinterpret_cast<floatx4*>(z.part_o + (pc.part + row) * D + jb * 32 + i4 * 8 + half * 4) =
                         floatx4{o[jb][4 * i4], o[jb][4 * i4 + 1], o[jb][4 * i4 + 2], o[jb][4 * i4 + 3]};
         }
     }
@@ -625,7 +731,7 @@ void rows_kernel(const RowsParams p)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     extern __shared__ __align__(1024) unsigned char smem[];  // stage s: K tile at s * 2 * TILE_BYTES, V tile behind it
-    RowsPlan& plan = *reinterpret_cast<RowsPlan*>(smem + 4 * kRowsTile * D * 2);
+    RowsPlan& plan = *reinterpret_cast<RowsPlan*>(smem + 4 * Layout<D>::TILE);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(SPECVLM_AS3 unsigned char*)smem;
 
     const int j = xcd_logical_id(blockIdx.x, p.padded);
@@ -715,7 +821,7 @@ void rows_kernel(const RowsParams p)
         pc.key0 = en.key0 + c_begin * 32; pc.key1 = min(en.key1, en.key0 + c_end * 32);
         pc.direct = own && !(PAGED && en.key0 > 0) && c_begin == 0 && c_end == chunks;
         pc.part = part_row(j, front.rows + g * padded_rows(p, en) + pc.row0);
-        rows_piece<D, PAGED>(p, plan, lds0, pc);
+        rows_piece<D, PAGED>(plan, lds0, pc);
         __syncthreads();                                     // the ring, and what the plan holds, are free again
     }
 }
@@ -1007,7 +1113,8 @@ bool rows_shape(int batch, int n_queries, int n_q_heads, int n_kv_heads, int hea
 template <int D, bool PAGED>
 int launch_rows(RowsParams& p, hipStream_t stream)
 {
-    constexpr int lds = 4 * kRowsTile * D * 2 + (int)sizeof(RowsPlan);
+    constexpr int lds = 4 * Layout<D>::TILE + (int)sizeof(RowsPlan);
+    static_assert(lds <= 160 * 1024, "a CU's");
     if (const int rc = allow_lds<&rows_kernel<D, PAGED>>(lds)) return rc;
     const int units = (p.n_q_heads + 256 / D - 1) / (256 / D);
     const int64_t rows = (int64_t)p.n_queries * p.n_q_heads;
@@ -1042,7 +1149,7 @@ int rows_start(RowsParams& p, bool paged, const void* q, int64_t q_tok, int64_t 
     const int64_t rows = (int64_t)n_queries * n_q_heads, entries = rows_entries(paged, ranges, batch, n_queries, n_q_heads, n_kv_heads);
     if (rows >= ((int64_t)1 << 29) || entries * 32 * n_kv_heads >= ((int64_t)1 << 29)) return SPECVLM_EUNSUPPORTED;
     const int64_t sets = (2 * rows / kSetRows + n_kv_heads) + entries * n_kv_heads;
-    if (sets * 3 * (most_keys / 32 + 6) >= ((int64_t)1 << 31)) return SPECVLM_EUNSUPPORTED;
+    if (sets * 3 * (most_keys / 32 + 7) >= ((int64_t)1 << 31)) return SPECVLM_EUNSUPPORTED;
     const size_t need = rows_workspace(paged, batch, n_queries, n_q_heads, n_kv_heads, head_dim);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return SPECVLM_EWORKSPACE;
     p = {};
