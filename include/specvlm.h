@@ -604,7 +604,7 @@ int specvlm_pages_shared(
  * too, is as for specvlm_paged_attn.  Results do not depend on the run; they may differ by
  * roundings with the other requests of the batch and the groups.
  * Limits: n_queries * H_q up to 2^26 is always served (a launch's threads); batch * H_kv < 2^23,
- * 3 * (n_queries * H_q / 128 + (2 * batch + 1) * H_kv) * (kv_len / 32 + 7) < 2^31, kv_len <= 2^30.
+ * 3 * (n_queries * H_q / 128 + (2 * batch + 1) * H_kv) * (kv_len / 32 + 10) < 2^31, kv_len <= 2^30.
  * -------------------------------------------------------------------------- */
 size_t specvlm_shared_attn_workspace_bytes(int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim);
 
@@ -637,7 +637,7 @@ int specvlm_shared_attn(
  * rows of out and lse left as they are, as are rows of no entry.  Results do not depend on
  * the run.
  * Limits: n_queries * H_q up to 2^26 is always served (a launch's threads); batch * H_kv < 2^24,
- * 3 * (n_queries * H_q / 128 + (batch + 2) * H_kv) * (n_states / 32 + 7) < 2^31 (with key_ranges
+ * 3 * (n_queries * H_q / 128 + (batch + 2) * H_kv) * (n_states / 32 + 10) < 2^31 (with key_ranges
  * n_queries * H_q / 64 there), n_states <= 2^30.
  * -------------------------------------------------------------------------- */
 size_t specvlm_cross_attn_workspace_bytes(int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim);

@@ -63,10 +63,10 @@ struct RowsParams {
     const int32_t* cu_q;
     const int32_t* cu_kv;                        // (flat)
     const int32_t* ranges;
-    int n_pages, page_size, most_shared;         // most_shared: tokens of a whole table row
+    int n_pages, page_size;
     int batch, q_len, kv_len, n_queries;
     int n_q_heads, n_kv_heads, group;
-    uint32_t inv_page, inv_heads, inv_group;
+    uint32_t inv_page, inv_group;
     float scale_log2;
     int entries, span;                           // numbered; (ranges) queries of a share
     Entry* spans;
@@ -76,7 +76,6 @@ struct RowsParams {
     RowsStart* starts;                           // [entries] what the join has to know of them
     int most_rows;                               // that the entries may have, for partial results
 };
-
 
 // What the call says of a request.
 struct Request { int q0, n_q, kvl, first, members, shared; };
@@ -146,16 +145,18 @@ __device__ __forceinline__ int chunks_of(const Entry& e) { return max(1, (e.key1
 __device__ __forceinline__ int padded_rows(const RowsParams& p, const Entry& e) { return (e.n_q * p.group + 31) & ~31; }      // of a kv head
 
 // Work is counted in the time that 32 keys of a set take, and an item has kBegin more in front of its first: what a piece costs before and behind its keys.
-// A set has 256 rows, the last one what is left: of one or two blocks of 32 the keys take as long as they take to come.
-constexpr int kBegin = 18, kLeastRun = 12;
-__device__ __forceinline__ bool narrow(int blocks) { return blocks <= 2; }
+// A set has 256 rows, the last one what is left. The figures are from the pieces' own clocks: 32 keys of up to four blocks of 32 rows 0.78 us, of more
+// 1.15, a piece of one tile 9 to 12. (trees, 32 requests of 26 rows of 64 behind 4096 keys of theirs and of others: kBegin of 18 99 us a call, 27 89, 36 90;
+// prompts of 256 behind shared texts 345, 304, 304; the videos that want the copies' rate 125, 128, 130. With four blocks at 3: 107, 343 and 133 at 18.) No
+// workgroup is begun for less than kLeastRun: of the smallest calls 6 and 12 take the same, 20 takes 1 us more.
+constexpr int kBegin = 27, kLeastRun = 12;
 struct Sets {
     int full, unit, whole, head;             // whole sets; work of 32 keys in the last; of a whole set; of a kv head
     __device__ __forceinline__ int unit_of(int set) const { return set < full ? 3 : unit; }
 };
 __device__ __forceinline__ Sets sets_of(int rows, int chunks)
 {
-    const int full = rows / kSetRows, blocks = ((rows + 31) >> 5) - full * kRowsWaves, unit = narrow(blocks) ? 2 : 3, whole = chunks * 3 + kBegin;
+    const int full = rows / kSetRows, blocks = ((rows + 31) >> 5) - full * kRowsWaves, unit = blocks <= 4 ? 2 : 3, whole = chunks * 3 + kBegin;
     return {full, unit, whole, full * whole + (blocks ? chunks * unit + kBegin : 0)};
 }
 
@@ -311,7 +312,7 @@ __device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, 
     const int n_blocks = (pc.n_rows + 31) >> 5, log_blocks = n_blocks > 4 ? 3 : n_blocks > 2 ? 2 : n_blocks - 1;       // waves of a kind
     const int blk = wave & ((1 << log_blocks) - 1), ks = wave >> log_blocks, n_ks = min(kChunks, kRowsWaves >> log_blocks);
     const bool works = blk < n_blocks && ks < n_ks;
-    const bool two_parts = narrow(n_blocks);
+    const bool two_parts = n_blocks <= 2;
     const int key0 = pc.key0, key1 = pc.key1, tiles = (key1 - key0 + kRowsTile - 1) / kRowsTile;
 
     // ---- loads: wave w brings keys 16w..16w+15 of a tile ----
@@ -1149,7 +1150,7 @@ int rows_start(RowsParams& p, bool paged, const void* q, int64_t q_tok, int64_t 
     const int64_t rows = (int64_t)n_queries * n_q_heads, entries = rows_entries(paged, ranges, batch, n_queries, n_q_heads, n_kv_heads);
     if (rows >= ((int64_t)1 << 29) || entries * 32 * n_kv_heads >= ((int64_t)1 << 29)) return SPECVLM_EUNSUPPORTED;
     const int64_t sets = (2 * rows / kSetRows + n_kv_heads) + entries * n_kv_heads;
-    if (sets * 3 * (most_keys / 32 + 7) >= ((int64_t)1 << 31)) return SPECVLM_EUNSUPPORTED;
+    if (sets * 3 * (most_keys / 32 + 10) >= ((int64_t)1 << 31)) return SPECVLM_EUNSUPPORTED;
     const size_t need = rows_workspace(paged, batch, n_queries, n_q_heads, n_kv_heads, head_dim);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return SPECVLM_EWORKSPACE;
     p = {};
@@ -1202,7 +1203,7 @@ extern "C" int specvlm_shared_attn(
                                   n_kv_heads, head_dim, softmax_scale, nullptr, out, lse, workspace, workspace_bytes))
         return rc;
     p.page = page_stride; p.n_pages = n_pages; p.page_size = page_size; p.inv_page = reciprocal(page_size);
-    p.table = page_table; p.table_row = table_stride; p.most_shared = kv_len;
+    p.table = page_table; p.table_row = table_stride;
     p.kv_lens = kv_lens; p.groups = groups; p.cu_q = cu_q; p.q_len = q_len; p.block_mask = ancestor_mask;
     return head_dim == 128 ? launch_rows<128, true>(p, (hipStream_t)stream) : launch_rows<64, true>(p, (hipStream_t)stream);
 }
