@@ -874,8 +874,8 @@ void rows_spans_kernel(const RowsParams p)
     if (lane == 0) p.spans[e] = s;
 }
 
-// One row over all of its keys once more, by a wave, where its sum came out as no finite number: mostly for an infinite value, which a row that sees it gets as it is,
-// however small its weight, and a row that does not see it does not get.  m, l: the row's maximum and sum of probabilities.  (Every key takes its own loads and
+// One row over all of its keys once more, by a wave, where its sum came out as no finite number: for an infinite value, which a row that sees it gets as it is,
+// however small its weight, and a row that does not see it does not get, or for values whose sum is beyond 32 bits before it is divided.  m, l: the row's maximum and sum of probabilities.  (Every key takes its own loads and
 // two rounds of the vector unit: 50 times what the matrix unit takes.)
 template <int D, bool PAGED>
 __device__ __forceinline__ void odd_row(const RowsParams& p, const RowsStart& own, int b, int tok, int hd, float m, float l, int lane)
@@ -897,6 +897,7 @@ __device__ __forceinline__ void odd_row(const RowsParams& p, const RowsStart& ow
         lo = max(p.ranges[2 * (int64_t)tok], 0);
         hi = min(p.ranges[2 * (int64_t)tok + 1], own.key1);         // (what lies behind the share's keys is no range of its queries)
     }
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;      // (first of all: sums of the largest values stay within 32 bits so)
     float o[COLS];
 #pragma unroll
     for (int c = 0; c < COLS; ++c) o[c] = 0.f;
@@ -919,7 +920,7 @@ __device__ __forceinline__ void odd_row(const RowsParams& p, const RowsStart& ow
 #pragma unroll
             for (int i = 0; i < 8; ++i) x = fmaf((float)kv[i], (float)qv[i], x);
         }
-        const float w = sees ? fast_exp2(fmaf(x, sc, -m_ref)) : 0.f;
+        const float w = sees ? fast_exp2(fmaf(x, sc, -m_ref)) * inv : 0.f;
         uint64_t seen = __ballot(sees);
         while (seen) {
             const int i = __builtin_ctzll(seen);
@@ -933,10 +934,9 @@ __device__ __forceinline__ void odd_row(const RowsParams& p, const RowsStart& ow
             }
         }
     }
-    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
     __bf16* const out = p.out + (int64_t)tok * p.q_tok + (int64_t)hd * p.q_head + lane * COLS;
 #pragma unroll
-    for (int c = 0; c < COLS; ++c) out[c] = (__bf16)(o[c] * inv);
+    for (int c = 0; c < COLS; ++c) out[c] = (__bf16)o[c];
 }
 
 // Joins the pieces of the rows that were cut (one that was not is in its place already): D / 4 threads to a row, and `GP` groups of them take every GP-th

@@ -407,6 +407,96 @@ def test_odd_values_of_states(B, queries):
     assert (np.abs(got - want)[:, :, plain] <= tol[:, :, plain]).all()
 
 
+def grown(k, by):
+    """The keys from 300 on `by` times as long: their logits rise far above what the first tiles leave as the maximum."""
+    x = S.values(k)
+    x[300:] *= by
+    return bits(x)
+
+
+@pytest.mark.parametrize("heads", [(4, 1, 64), (16, 2, 128)])
+@pytest.mark.parametrize("queries", [1, 7, 15, 30, 70])
+@pytest.mark.parametrize("by", [1.0, 4.0])
+def test_steep_logits(B, heads, queries, by):
+    """Logits of up to a few hundred, of waves that have rows for themselves, share them by two and by four."""
+    hq, hkv, d = heads
+    scale = 6.0 * 8.0 / d / by
+    q, k, v = rnd_bits((queries, hq, d), (51, queries)), rnd_bits((2000, hkv, d), 52), rnd_bits((2000, hkv, d), 53)
+    k = grown(k, by)
+    want, want_lse, tol, tol_lse = S.cross_attention(S.values(q), S.values(k), S.values(v), [queries], [2000], scale)
+    got, lse = B.cross_attn(dev_bf16(q), dev_bf16(k), dev_bf16(v), scale, want_lse=True)
+    close(host_f64(got), want, tol)
+    assert (np.abs(host_f64(lse) - want_lse) <= tol_lse).all()
+
+
+@pytest.mark.parametrize("queries,states", [(2, 90), (2, 700), (60, 90), (60, 700)])
+def test_values_whose_sum_is_beyond_32_bits(B, queries, states):
+    """All values of two columns are nearly the type's largest: their mean is one of its numbers."""
+    q, k, v = rnd_bits((queries, 16, 128), 54), rnd_bits((states, 2, 128), 55), rnd_bits((states, 2, 128), 56)
+    v[:, :, 5], v[:, :, 6], v[::2, :, 7], v[1::2, :, 7] = 0x7f70, 0xff70, 0x7f70, 0xff70
+    want, _, tol, _ = S.cross_attention(S.values(q), S.values(k), S.values(v), [queries], [states], 0.1)
+    close(host_f64(B.cross_attn(dev_bf16(q), dev_bf16(k), dev_bf16(v), 0.1)), want, tol)
+
+
+@pytest.mark.parametrize("queries,states", [(2, 90), (2, 2700), (60, 90), (60, 2700)])
+def test_odd_values_where_the_queries_are_the_output(B, queries, states):
+    """A row that is summed once more reads its query once more: rows with one piece and with many."""
+    q, k, v = dev_bf16(rnd_bits((queries, 16, 128), 57)), dev_bf16(rnd_bits((states, 2, 128), 58)), dev_bf16(rnd_bits((states, 2, 128), 59))
+    v[states // 2, :, 5], v[7, 1, 6] = np.inf, np.nan
+    want = B.cross_attn(q, k, v, 0.1)
+    assert (want[:, :, 5] == np.inf).all() and want[:, 8:, 6].isnan().all()
+    B.cross_attn(q, k, v, 0.1, out=q)
+    assert (q.view(torch.int16) == want.view(torch.int16)).all()
+
+
+def test_ranges_of_many_entries(B):
+    """Entries of no query, of some and of more than a share, with states and without, and some that leave the tensors."""
+    rng = np.random.default_rng(60)
+    n = 700
+    q_lens, kv_lens = (rng.integers(0, 4, n) * rng.integers(0, 2, n)).tolist(), (rng.integers(0, 90, n) * rng.integers(0, 2, n)).tolist()
+    q_lens[350], kv_lens[350], q_lens[699], kv_lens[699] = 300, 1000, 70, 333
+    ranges = np.sort(rng.integers(-9, 120, (sum(q_lens), 2)), axis=1).astype(np.int32)
+    at = sum(q_lens[:350])
+    ranges[at:at + 300] *= 9
+    check_cross(B, 61, (4, 1, 64), q_lens, kv_lens, ranges=ranges)
+    cu_q, cu_kv = (np.concatenate([[0], np.cumsum(x)]) for x in (q_lens, kv_lens))
+    q, k = dev_bf16(rnd_bits((sum(q_lens), 4, 64), 62)), dev_bf16(rnd_bits((sum(kv_lens), 1, 64), 63))
+    want, _, tol, _ = S.cross_attention(host_f64(q), host_f64(k), host_f64(k), q_lens, kv_lens, 0.125, ranges)
+    cu_kv[1:200] = sum(kv_lens) + 1                          # (of the entries up to 199)
+    out = torch.full_like(q, 7.0)
+    B.cross_attn(q, k, k, 0.125, cu_q=i32(cu_q), cu_kv=i32(cu_kv), key_ranges=i32(ranges), out=out)
+    assert (out[:cu_q[200]] == 7.0).all()
+    # (where a row's states are cut depends on the other entries, so the bits may differ: the bounds hold for every cut)
+    close(host_f64(out)[cu_q[200]:], want[cu_q[200]:], tol[cu_q[200]:])
+
+
+def test_captured_graphs_that_share_a_workspace(B):
+    """One after the other, again and again, each with its own answers."""
+    one = build(64, [(800, [(20, 2)] * 5)], (14, 2, 64), 16)
+    qs, ks, vs = dev_bf16(one[0]), dev_bf16(one[1]), dev_bf16(one[2])
+    table, lens, groups = i32(one[3]), i32(one[4]), i32(one[6])
+    qc, kc = dev_bf16(rnd_bits((40, 14, 64), 65)), dev_bf16(rnd_bits((900, 2, 64), 66))
+    ranges = i32([[t * 5, 700 + t * 3] for t in range(40)])
+    bytes_ = max(B.shared_attn_workspace_bytes(5, 10, 14, 2, 64), B.cross_attn_workspace_bytes(1, 40, 14, 2, 64))
+    workspace = B.new_workspace(bytes_)
+    outs = torch.zeros_like(qs), torch.zeros_like(qc)
+    calls = [lambda **kw: B.shared_attn(qs, ks, vs, table, lens, 0.125, groups, **kw), lambda **kw: B.cross_attn(qc, kc, kc, 0.125, key_ranges=ranges, **kw)]
+    want = [call() for call in calls]
+    graphs = []
+    for call, out in zip(calls, outs):
+        call(out=out, workspace=workspace)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call(out=out, workspace=workspace)
+    for _ in range(5):
+        for g, out, w in zip(graphs, outs, want):
+            out.fill_(3.0)
+            g.replay()
+            assert (out == w).all()
+            calls[1](workspace=workspace)
+
+
 # ------------------------------------------------------------------------------------------------ who shares
 def check_groups(B, table, kv_lens, q_lens, n_pages, ps, min_tokens):
     want = S.groups(np.asarray(table), kv_lens, q_lens, n_pages, ps, min_tokens)
