@@ -32,7 +32,12 @@ constexpr int kRowsWaves = 8;
 constexpr int kRowsThreads = kRowsWaves * kWave;
 constexpr int kSetRows = kRowsWaves * 32;
 constexpr int kChunks = kRowsTile / 32;
-constexpr float kRowsRedo = 0x1p20f;     // a lane's sum of 32 keys at or above this (or NaN) is done again with the maximum tracked
+constexpr float kRowsRedo = 0x1p20f;     // a lane's sum of 32 keys above this (or NaN) is done again with the maximum tracked
+// 32 keys with more than this times what their row had before have their probabilities in two bf16, where one costs up to 2^-9 of a probability: evened out
+// over many keys of like weight, but not in a row that one key makes up. (One viewer's token over 65536 states, errors against 64 bits in parts of those of
+// outputs rounded once, over seeds: without 1.15 to 1.56, at 4 1.04 to 1.23, 2 1.03 to 1.22, 1 1.03 to 1.20, 0.25 1.03 to 1.17;  91.1 us a call, and 90.8, 91.2,
+// 92.4 and 100.)
+constexpr float kRowsPeak = 2.f;
 
 // D = A(32x16 bf16) * B(16x32 bf16) + C.  Per lane (r = lane % 32, h = lane / 32):
 //   A holds row r, contraction indices 8h..8h+7;  B holds column r, the same;  C/D hold column r, element i row 8(i/4) + 4h + i%4
@@ -425,6 +430,7 @@ __device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, 
     };
     bool fresh = true;                                   // some row has seen nothing yet
     // Probabilities against the maximum with these logits too, to which the sums are brought.
+    bool peak = false;                                   // the last 32 keys count for much of what some row has seen
     const auto raise = [&](const floatx16& s, float (&pv)[16]) {
         float mx = s[0];
 #pragma unroll
@@ -437,7 +443,9 @@ __device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, 
         float psum = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) { pv[i] = fast_exp2(fmaf(s[i], sc, -m_ref)); psum += pv[i]; }
-        l_run = l_run * alpha + psum;
+        l_run *= alpha;
+        peak = __any(psum > kRowsPeak * l_run);
+        l_run += psum;
         if (__any(rescale)) {
 #pragma unroll
             for (int jb = 0; jb < JB; ++jb)
@@ -465,7 +473,8 @@ __device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, 
             float psum = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) { pv[i] = fast_exp2(fmaf(s[i], sc, -m_run)); psum += pv[i]; }
-            if (!__any(!(psum < kRowsRedo))) {
+            if (!__any(!(psum <= kRowsRedo))) {
+                peak = __any(psum > kRowsPeak * l_run);
                 l_run += psum;
                 return;
             }
@@ -561,7 +570,7 @@ __device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, 
                     pf[u] = __builtin_convertvector(pu, bf16x8);
                 }
             }
-            if (__builtin_expect(__any(!(psum < kRowsRedo)), 0)) return ch;      // (these keys and the tile's others against another maximum)
+            if (__builtin_expect(__any(!(psum <= fminf(kRowsRedo, kRowsPeak * l_run))), 0)) return ch;      // (these keys and the tile's others against another maximum)
             l_run += psum;
         }
         return N;
@@ -611,7 +620,7 @@ __device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, 
                         for (int jb = 0; jb < JB; ++jb) vf[u][jb] = __builtin_bit_cast(bf16x8, u32x4{});
 #pragma unroll
                     for (int jb = 0; jb < JB; ++jb) o[jb] = mfma32(vf[u][jb], pf, o[jb]);
-                    if (two_parts) {
+                    if (two_parts || peak) {
                         const u32x4 w = __builtin_bit_cast(u32x4, pf);
                         floatx8 rest;
 #pragma unroll

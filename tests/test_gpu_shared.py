@@ -429,6 +429,26 @@ def test_steep_logits(B, heads, queries, by):
     assert (np.abs(host_f64(lse) - want_lse) <= tol_lse).all()
 
 
+@pytest.mark.parametrize("heads", [(2, 2, 64), (2, 2, 128)])
+def test_a_key_that_makes_up_a_row(B, heads):
+    """Where a key has nine tenths of its row's weight and more, the probabilities of its 32 are carried in two bf16: only the other keys' terms are off by one's."""
+    hq, hkv, d = heads
+    queries, states = 200, 1500
+    q, k, v = rnd_bits((queries, hq, d), 67), rnd_bits((states, hkv, d), 68), rnd_bits((states, hkv, d), 69)
+    at = 700 + 3 * np.arange(queries)
+    scale = d ** -0.5
+    k[at] = bits(S.values(q) * 12 / scale / (S.values(q) ** 2).sum(2, keepdims=True))    # a logit of 12, among others of up to 4
+    x = np.einsum("qhd,khd->hqk", S.values(q), S.values(k)) * scale
+    w = np.exp(x - x.max(2, keepdims=True))
+    w /= w.sum(2, keepdims=True)
+    own = w[:, np.arange(queries), at]
+    assert own.min() > 0.9
+    want, _, tol, _ = S.cross_attention(S.values(q), S.values(k), S.values(v), [queries], [states], scale, parts=2)
+    w[:, np.arange(queries), at] = 0
+    tol += 1.01 * 2.0 ** -8 * np.einsum("hqk,khd->qhd", w, np.abs(S.values(v)))
+    close(host_f64(B.cross_attn(dev_bf16(q), dev_bf16(k), dev_bf16(v), scale)), want, tol)
+
+
 @pytest.mark.parametrize("queries,states", [(2, 90), (2, 700), (60, 90), (60, 700)])
 def test_values_whose_sum_is_beyond_32_bits(B, queries, states):
     """All values of two columns are nearly the type's largest: their mean is one of its numbers."""
