@@ -208,9 +208,12 @@ struct RowsPlan {
     Numbers front[kRowsThreads];
     int work[kRowsThreads];
     Numbers wave[kRowsWaves];
-    float ml[kSetRows * 2];                  // maxima and sums of waves that share rows
+    union {
+        uint64_t tree[kSetRows];             // the rows' masks of the block, then
+        float ml[kSetRows * 2];              // maxima and sums of waves that share rows
+    };
     int word[3][kRowsThreads / 2];           // of requests
-    unsigned char ok[2][8];
+    uint64_t missing[2][kRowsWaves];         // of 64 tiles, by their 16 keys:  those whose page is none of the pool's
     int found;
 };
 
@@ -237,6 +240,12 @@ __device__ __forceinline__ Entry entry_at_once(const RowsParams& p, RowsPlan& s,
         e = own_entry(p, b, r, in ? s.word[1][r.first] : 0, in ? s.word[2][r.first] : 0);
     }
     return e;
+}
+
+// Lane i's word, to all.
+__device__ __forceinline__ uint64_t lane_word(uint64_t x, int i)
+{
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, i);
 }
 
 // Inclusive prefix sums over the workgroup's threads, and the total; `s` is free again behind the next barrier.
@@ -324,13 +333,24 @@ __device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, 
     const int64_t kv0 = (int64_t)pc.g * p.head + (PAGED ? 0 : (int64_t)(p.cu_kv ? __builtin_amdgcn_readfirstlane(p.cu_kv[pc.b]) : 0) * p.tok);
     const char* const k_at = reinterpret_cast<const char*>(p.k + kv0);
     const char* const v_at = reinterpret_cast<const char*>(p.v + kv0);
-    int ids = 0, places = 0;                             // of the next 64 tiles, one to a lane
+    uint64_t at = 0;                                     // of the next 64 tiles, one to a lane: the bytes from the pool's first row to this wave's 16 keys
+    int id = 0, place = 0;
     const auto look_up = [&](int tile) {
-        const int key = min(key0 + (tile + lane) * kRowsTile + wave * 16, (key1 - 1) & ~15);
+        const int key = min(key0 + (tile + lane) * kRowsTile + wave * 16, (key1 - 1) & ~15);             // (a group behind the last: that one again)
         const QuotRem pg = divide(key, p.page_size, p.inv_page);
-        ids = p.table[(int64_t)pc.b * p.table_row + pg.q];
-        places = pg.r;
+        id = p.table[(int64_t)pc.b * p.table_row + pg.q];
+        place = pg.r;
     };
+    const auto looked_up = [&](int tile) {
+        // (a page that is not one of the pool's is not read: the pool's first is, and its keys are masked)
+        const bool there = (uint32_t)id < (uint32_t)p.n_pages;
+        at = (uint64_t)((there ? id : 0) * p.page + place * p.tok) * 2;
+        const uint64_t missing = __ballot(!there && tile + lane < tiles);
+        if (lane == 0) plan.missing[tile >> 6 & 1][wave] = missing;
+    };
+    const uint32_t k_from = (uint32_t)(lane % ROWS) * (uint32_t)(p.tok * 2) + lane / ROWS * 16;
+    const uint32_t v_from = (uint32_t)((lane >> 2) % ROWS) * (uint32_t)(p.tok * 2) + (lane / (4 * ROWS) * 4 + (lane & 3)) * 16;
+    const int64_t rows_bytes = p.tok * (ROWS * 2);
     const auto issue = [&](int tile, int stage) {
         const uint32_t to = lds0 + stage * 2 * TILE_BYTES + wave * LOADS * LOAD_BYTES;
         int64_t first;
@@ -338,22 +358,29 @@ __device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, 
         int last;                                        // the last of the 16 keys that there is: it stands for those behind it, whatever lies there
         if constexpr (PAGED) {
             const int l = tile & 63;
-            if (l == 0 && tile > 0) look_up(tile);
-            const int id = __builtin_amdgcn_readlane(ids, l), row = __builtin_amdgcn_readlane(places, l);
-            // (a page that is not one of the pool's is not read: the pool's first is, and its keys are masked)
-            const bool there = (uint32_t)id < (uint32_t)p.n_pages;
-            if (lane == 0) plan.ok[stage][wave] = there;
-            first = (there ? id : 0) * p.page + row * p.tok;
-            last = key < key1 ? key1 - 1 - key : (key1 - 1) & 15;        // (a group behind the last: that one again)
+            if (l == 0 && tile > 0) {
+                look_up(tile);
+                looked_up(tile);
+            }
+            first = (int64_t)lane_word(at, l);
+            last = key < key1 ? key1 - 1 - key : (key1 - 1) & 15;
         } else {
-            first = (int64_t)min(key, key1 - 1) * p.tok;
+            first = (int64_t)min(key, key1 - 1) * (p.tok * 2);
             last = max(key1 - 1 - key, 0);
         }
+        if (last >= 15) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                load_to_lds(k_at + first + i * rows_bytes, k_from, to + i * LOAD_BYTES);
+                load_to_lds(v_at + first + i * rows_bytes, v_from, to + TILE_BYTES + i * LOAD_BYTES);
+            }
+            return;
+        }
+        const int k_row = lane % ROWS, v_of = (lane >> 2) % ROWS;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const auto from = [&](int row, int piece) { return (uint32_t)min(i * ROWS + row, last) * (uint32_t)(p.tok * 2) + piece * 16; };
-            load_to_lds(k_at + 2 * first, from(lane % ROWS, lane / ROWS), to + i * LOAD_BYTES);
-            load_to_lds(v_at + 2 * first, from((lane >> 2) % ROWS, lane / (4 * ROWS) * 4 + (lane & 3)), to + TILE_BYTES + i * LOAD_BYTES);
+            load_to_lds(k_at + first, k_from + (uint32_t)(min(i * ROWS + k_row, last) - k_row) * (uint32_t)(p.tok * 2), to + i * LOAD_BYTES);
+            load_to_lds(v_at + first, v_from + (uint32_t)(min(i * ROWS + v_of, last) - v_of) * (uint32_t)(p.tok * 2), to + TILE_BYTES + i * LOAD_BYTES);
         }
     };
 
@@ -366,17 +393,17 @@ __device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, 
     const __bf16* const qp = p.q + q_tok * p.q_tok + (int64_t)(pc.g * p.group + q_at.r) * p.q_head + h * 8;
 #pragma unroll
     for (int s = 0; s < KK; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qp + s * 16);
+    if (PAGED && tiles > 0) looked_up(0);
     if (tiles > 0) issue(0, 0);
     // the keys that it sees: [lo, hi), of the block those of a tree node's mask;  of all of the wave's rows: keys that all see, and that some see
     int lo = key0, hi = key1, all_lo = key0, all_hi = key1, any_lo = key0, any_hi = key1;
     const int before = pc.end - pc.n_q;                      // (own keys of a block)
-    uint64_t tree = 0;
     bool is_tree = false;
     if constexpr (PAGED) {
         if (pc.own) {
             is_tree = p.block_mask != nullptr;
             if (is_tree) {
-                tree = p.block_mask[q_tok];
+                if (h == 0) plan.tree[my_row] = p.block_mask[q_tok];
                 all_hi = min(before, key1);
             } else {
                 hi = min(hi, before + q_at.q + 1);
@@ -460,6 +487,7 @@ __device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, 
             uint32_t sees = first_bits(hi - k0) & ~first_bits(lo - k0) & ((two & 1 ? 0xffffu : 0u) | (two & 0x100 ? 0xffff0000u : 0u));
             if (is_tree) {
                 const int in = k0 - before;
+                const uint64_t tree = plan.tree[my_row];
                 const uint64_t block = in >= 0 ? (in < 64 ? tree >> in : 0) : (in > -32 ? tree << -in : 0);
                 sees &= (uint32_t)block | first_bits(-in);
             }
@@ -491,11 +519,6 @@ __device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, 
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[jb][i] = 0.f;
     };
-    const auto pages_there = [&](int stage) {            // a byte for 16 keys of the tile
-        if constexpr (!PAGED) return (uint64_t)0x0101010101010101ull;
-        const u32x2 ok = *reinterpret_cast<const u32x2*>(plan.ok[stage]);
-        return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(ok[1]) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane(ok[0]);
-    };
     const auto lds_done = [] { __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
 
     // A tile that all rows of the wave see whole, after others: while the vector unit weighs 32 keys, the matrix unit takes the products with the values of the last
@@ -507,6 +530,7 @@ __device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, 
         {
             bf16x8 kf[KK];
             read_keys(kf, at);
+            __builtin_amdgcn_sched_barrier(0);               // (the reads of all of them first: one by one, each waits for its own)
             s = logits(kf);
         }
 #pragma unroll
@@ -580,16 +604,26 @@ __device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, 
     const auto sweep = [&] {
         begin_sums();
         if (tiles <= 0) return;
+        uint64_t gone = 0;                                   // (pages) of 64 tiles, those with keys whose page is none
         for (int t = 0; t < tiles; ++t) {
             const int stage = t & 1;
             wait_vmcnt<0>();
             lds_done();
             stage_barrier();                             // the tile is there for everyone, and everyone has left the other stage
             if (t + 1 < tiles) issue(t + 1, stage ^ 1);
+            if constexpr (PAGED) {
+                if ((t & 63) == 0) {
+                    gone = 0;
+                    const uint64_t mine = plan.missing[t >> 6 & 1][lane % kRowsWaves];
+                    if (__any(mine != 0))
+#pragma unroll
+                        for (int w = 0; w < kRowsWaves; ++w) gone |= lane_word(mine, w);
+                }
+            }
             if (!works) continue;
-            const uint64_t there = pages_there(stage);
+            const bool all_there = !PAGED || !(gone >> (t & 63) & 1);
             int ch0 = ks;
-            if (n_ks <= 2 && !fresh && there == 0x0101010101010101ull && key0 + t * kRowsTile >= all_lo && key0 + (t + 1) * kRowsTile <= all_hi) {
+            if (n_ks <= 2 && !fresh && all_there && key0 + t * kRowsTile >= all_lo && key0 + (t + 1) * kRowsTile <= all_hi) {
                 if (n_ks == 1) ch0 = whole_tile(std::integral_constant<int, kChunks>(), stage * 2 * TILE_BYTES);
                 else ch0 = ks + 2 * whole_tile(std::integral_constant<int, kChunks / 2>(), stage * 2 * TILE_BYTES + ks * CHUNK_BYTES);
             }
@@ -605,7 +639,11 @@ __device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, 
                 __builtin_amdgcn_sched_group_barrier(0x008, KK, 0);
                 read_values(vf[0], at_chunk);
                 float pv[16];
-                const uint32_t two = PAGED ? (uint32_t)(there >> (16 * ch)) & 0xffffu : 0x101u;
+                uint32_t two = 0x101;
+                if (!all_there) {
+                    const auto there = [&](int half) { return (uint32_t)(__builtin_amdgcn_readfirstlane((int)(plan.missing[t >> 6 & 1][2 * ch + half] >> (t & 63))) & 1) ^ 1u; };
+                    two = there(0) | there(1) << 8;
+                }
                 weigh(s, k0, two, pv);
                 // ---- O^T += V^T P^T ----
 #pragma unroll
@@ -935,7 +973,7 @@ __device__ __forceinline__ void odd_row(const RowsParams& p, const RowsStart& ow
             const int i = __builtin_ctzll(seen);
             seen &= seen - 1;
             const float wi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), i));
-            const int64_t row = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(at >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)at, i));
+            const int64_t row = (int64_t)lane_word((uint64_t)at, i);
 #pragma unroll
             for (int c = 0; c < COLS; ++c) {
                 const float v = (float)p.v[row + lane * COLS + c];
