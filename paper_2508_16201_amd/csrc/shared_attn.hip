@@ -80,6 +80,7 @@ struct RowsParams {
     float* part_ml;                              // [rows_parts][2] running maximum in log2 units, sum
     RowsStart* starts;                           // [entries] what the join has to know of them
     int most_rows;                               // that the entries may have, for partial results
+    bool far;                                    // entries that overlap may have more rows than an int holds
 };
 
 // What the call says of a request.
@@ -212,7 +213,7 @@ struct RowsPlan {
         uint64_t tree[kSetRows];             // the rows' masks of the block, then
         float ml[kSetRows * 2];              // maxima and sums of waves that share rows
     };
-    int word[3][kRowsThreads / 2];           // of requests
+    alignas(8) int word[3][kRowsThreads / 2];        // of requests
     uint64_t missing[2][kRowsWaves];         // of 64 tiles, by their 16 keys:  those whose page is none of the pool's
     int found;
 };
@@ -240,6 +241,19 @@ __device__ __forceinline__ Entry entry_at_once(const RowsParams& p, RowsPlan& s,
         e = own_entry(p, b, r, in ? s.word[1][r.first] : 0, in ? s.word[2][r.first] : 0);
     }
     return e;
+}
+
+// The sum over the workgroup's threads.
+__device__ __forceinline__ int64_t block_sum(RowsPlan& s, int64_t x)
+{
+    unsigned long long* const sum = reinterpret_cast<unsigned long long*>(s.word);
+    if (threadIdx.x == 0) *sum = 0;
+    __syncthreads();
+    atomicAdd(sum, (unsigned long long)x);
+    __syncthreads();
+    x = (int64_t)*sum;
+    __syncthreads();
+    return x;
 }
 
 // Lane i's word, to all.
@@ -797,15 +811,18 @@ void rows_kernel(const RowsParams p)
         plan.entry[threadIdx.x] = entry;
         plan.front[threadIdx.x] = {upto.work - mine.work, upto.rows - mine.rows};
         plan.work[threadIdx.x] = mine.work;
+        return mine.rows;
     };
     for (;;) {
+        int64_t my_rows = 0;
         total = {0, 0};
         for (int c = first_of_last(entries); c >= 0; c -= kRowsThreads) {     // (the first 512 last: they are looked up next)
-            look_at(c + threadIdx.x);
+            my_rows += look_at(c + threadIdx.x);
             total.work += here.work;
             total.rows += here.rows;
         }
         // (groups that overlap would have rows more than once: there is no room for them)
+        if (p.far && block_sum(plan, my_rows) > p.most_rows) total.rows = INT_MAX;
         if (total.rows <= p.most_rows || !grouped) break;
         grouped = false;
     }
@@ -987,8 +1004,8 @@ __device__ __forceinline__ void odd_row(const RowsParams& p, const RowsStart& ow
 }
 
 // Joins the pieces of the rows that were cut (one that was not is in its place already): D / 4 threads to a row, and `GP` groups of them take every GP-th
-// of its pieces (GP = 1: a wave to as many rows as it holds).
-template <int D, bool PAGED, int GP>
+// of its pieces (GP = 1: a wave to as many rows as it holds, `TIMES` times: the token's request and entry, a look at memory after the other, are found once).
+template <int D, bool PAGED, int GP, int TIMES>
 __global__ __launch_bounds__(256)
 void rows_join_kernel(const RowsParams p)
 {
@@ -997,16 +1014,17 @@ void rows_join_kernel(const RowsParams p)
     __shared__ float s_ml[GP > 1 ? 2 * GP : 1];
     __shared__ __align__(16) float s_o[GP > 1 ? GP * D : 4];
     const int lane = threadIdx.x & 63, group = threadIdx.x / TPR, c = threadIdx.x % TPR;
-    const int units = (p.n_q_heads + RPW - 1) / RPW;
-    int tok, hd;
+    constexpr int HEADS = RPW * TIMES;
+    const int units = (p.n_q_heads + HEADS - 1) / HEADS;
+    int tok, hd0;
     if constexpr (GP == 1) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int64_t unit = (int64_t)blockIdx.x * WAVES + wave;
         tok = (int)(unit / units);
-        hd = (int)(unit - (int64_t)tok * units) * RPW + lane / TPR;
+        hd0 = (int)(unit - (int64_t)tok * units) * HEADS;
     } else {
         tok = blockIdx.x / p.n_q_heads;
-        hd = blockIdx.x - tok * p.n_q_heads;
+        hd0 = blockIdx.x - tok * p.n_q_heads;
     }
     if (tok >= p.n_queries) return;
     // the request
@@ -1032,11 +1050,8 @@ void rows_join_kernel(const RowsParams p)
     const int total = own.total;
     const Shares shares = shares_of(p, total);
     if (total == 0 || own.n_q <= 0 || tok < own.q0) return;
-    const bool mine_to_write = hd < p.n_q_heads && (GP == 1 || group == 0);      // (all lanes stay to the end: an odd row takes a whole wave)
-    hd = min(hd, p.n_q_heads - 1);
-    const QuotRem head = divide(hd, p.group, p.inv_group);
     struct Pieces { int first, n, row; };                    // workgroups that have one, the row of their results
-    const auto pieces_of = [&](const RowsStart& s) {
+    const auto pieces_of = [&](const RowsStart& s, const QuotRem& head) {
         const Entry en = {s.q0, s.n_q, s.key0, s.key1, -1};
         const int row = (tok - en.q0) * p.group + head.r, chunks = chunks_of(en);
         const Sets sets = sets_of(en.n_q * p.group, chunks);
@@ -1044,89 +1059,112 @@ void rows_join_kernel(const RowsParams p)
         const int first = shares.of(x);
         return Pieces{first, shares.of(x + (chunks - 1) * unit) - first + 1, s.rows + head.q * padded_rows(p, en) + row};
     };
-    const Pieces mine = pieces_of(own);
-    Pieces theirs = {0, 0, 0};
-    if (PAGED && own.key0 > 0) theirs = pieces_of(p.starts[own.first]);
-    float m = -INFINITY, l = 0.f;
-    floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    bool odd = false;
-    const bool in_place = theirs.n == 0 && mine.n == 1;
-    if (in_place) {
-        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * part_row(mine.first, mine.row));
-        odd = __float_as_uint(ml.y) >> 31 || !(ml.y == ml.y);
-        m = ml.x;
-        l = fabsf(ml.y);
-    }
-    const int n = in_place ? 0 : theirs.n + mine.n;
-    const auto row_of = [&](int i) { return i < theirs.n ? part_row(theirs.first + i, theirs.row) : part_row(mine.first + i - theirs.n, mine.row); };
-    const int g0 = GP == 1 ? 0 : group;                      // this group's first piece
-    for (int i0 = g0; i0 < n; i0 += TPR * GP) {
-        // a piece to a thread: its maximum and sum;  then the outputs, weighted by their thread's word
-        float pm = -INFINITY, pl = 0.f;
-        if (i0 + c * GP < n) {
-            const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * row_of(i0 + c * GP));
-            pm = ml.x;
-            pl = ml.y;
-        }
-        const int most = min(TPR, (n - i0 + GP - 1) / GP);
-        floatx4 y[4];
-        const auto fetch = [&](int i1) {                     // (behind the last piece: the last again, left out)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) y[u] = *reinterpret_cast<const floatx4*>(p.part_o + row_of(i0 + min(i1 + u, most - 1) * GP) * D + c * 4);
-        };
-        fetch(0);
-        float top = pm;
-#pragma unroll
-        for (int d = 1; d < TPR; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-        const float m_new = fmaxf(m, top), m_ref = m_new == -INFINITY ? 0.f : m_new;
-        const float w = fast_exp2(pm - m_ref), keep = fast_exp2(m - m_ref);
-        float sum = pl * w;
-#pragma unroll
-        for (int d = 1; d < TPR; d *= 2) sum += __shfl_xor(sum, d);
-        l = l * keep + sum;
-        m = m_new;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = o[i] * keep;
-        for (int i1 = 0; i1 < most; i1 += 4) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const float wi = __shfl(w, (lane & ~(TPR - 1)) + min(i1 + u, most - 1));
-                if (i1 + u < most)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) o[k] += y[u][k] * wi;
+    const bool shares_keys = PAGED && own.key0 > 0;
+    const RowsStart first = shares_keys ? p.starts[own.first] : own;
+    // of the wave's heads, those that something is to be done for:  a row in one piece of finite sums is in its place
+    uint64_t todo = ~0ull;
+    if (TIMES > 1 && !shares_keys) {
+        const int hd = hd0 + lane;
+        bool mine = false;
+        if (lane < HEADS && hd < p.n_q_heads) {
+            const Pieces pieces = pieces_of(own, divide(hd, p.group, p.inv_group));
+            mine = pieces.n != 1;
+            if (!mine) {
+                const float l = p.part_ml[2 * part_row(pieces.first, pieces.row) + 1];
+                mine = __float_as_uint(l) >> 31 || !(l == l);
             }
-            if (i1 + 4 < most) fetch(i1 + 4);
         }
+        todo = __ballot(mine);
     }
-    if (GP > 1 && !in_place) {
-        if (c == 0) { s_ml[2 * group] = m; s_ml[2 * group + 1] = l; }
-        *reinterpret_cast<floatx4*>(s_o + group * D + c * 4) = o;
-        __syncthreads();
-        for (int k = 0; k < GP; ++k) m = fmaxf(m, s_ml[2 * k]);
-        const float m_ref = m == -INFINITY ? 0.f : m;
-        l = 0.f;
-        o = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < TIMES; ++k) {
+        if (!(todo >> (k * RPW) & ((1u << RPW) - 1)) || hd0 + k * RPW >= p.n_q_heads) continue;
+        const int of_lane = hd0 + k * RPW + (GP == 1 ? lane / TPR : 0), hd = min(of_lane, p.n_q_heads - 1);
+        const bool mine_to_write = of_lane < p.n_q_heads && (GP == 1 || group == 0);      // (all lanes stay to the end: an odd row takes a whole wave)
+        const QuotRem head = divide(hd, p.group, p.inv_group);
+        const Pieces mine = pieces_of(own, head);
+        Pieces theirs = {0, 0, 0};
+        if (shares_keys) theirs = pieces_of(first, head);
+        float m = -INFINITY, l = 0.f;
+        floatx4 o = {0.f, 0.f, 0.f, 0.f};
+        bool odd = false;
+        const bool in_place = theirs.n == 0 && mine.n == 1;
+        if (in_place) {
+            const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * part_row(mine.first, mine.row));
+            odd = __float_as_uint(ml.y) >> 31 || !(ml.y == ml.y);
+            m = ml.x;
+            l = fabsf(ml.y);
+        }
+        const int n = in_place ? 0 : theirs.n + mine.n;
+        const auto row_of = [&](int i) { return i < theirs.n ? part_row(theirs.first + i, theirs.row) : part_row(mine.first + i - theirs.n, mine.row); };
+        const int g0 = GP == 1 ? 0 : group;                      // this group's first piece
+        for (int i0 = g0; i0 < n; i0 += TPR * GP) {
+            // a piece to a thread: its maximum and sum;  then the outputs, weighted by their thread's word
+            float pm = -INFINITY, pl = 0.f;
+            if (i0 + c * GP < n) {
+                const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * row_of(i0 + c * GP));
+                pm = ml.x;
+                pl = ml.y;
+            }
+            const int most = min(TPR, (n - i0 + GP - 1) / GP);
+            floatx4 y[4];
+            const auto fetch = [&](int i1) {                     // (behind the last piece: the last again, left out)
 #pragma unroll
-        for (int k = 0; k < GP; ++k) {
-            const float w = fast_exp2(s_ml[2 * k] - m_ref);
-            l += s_ml[2 * k + 1] * w;
-            const floatx4 y = *reinterpret_cast<const floatx4*>(s_o + k * D + c * 4);
+                for (int u = 0; u < 4; ++u) y[u] = *reinterpret_cast<const floatx4*>(p.part_o + row_of(i0 + min(i1 + u, most - 1) * GP) * D + c * 4);
+            };
+            fetch(0);
+            float top = pm;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] += y[i] * w;
+            for (int d = 1; d < TPR; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+            const float m_new = fmaxf(m, top), m_ref = m_new == -INFINITY ? 0.f : m_new;
+            const float w = fast_exp2(pm - m_ref), keep = fast_exp2(m - m_ref);
+            float sum = pl * w;
+#pragma unroll
+            for (int d = 1; d < TPR; d *= 2) sum += __shfl_xor(sum, d);
+            l = l * keep + sum;
+            m = m_new;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = o[i] * keep;
+            for (int i1 = 0; i1 < most; i1 += 4) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const float wi = __shfl(w, (lane & ~(TPR - 1)) + min(i1 + u, most - 1));
+                    if (i1 + u < most)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[i] += y[u][i] * wi;
+                }
+                if (i1 + 4 < most) fetch(i1 + 4);
+            }
         }
-    }
-    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
-    if (!in_place) {
-        const uint64_t odds = __ballot(!((o[0] + o[1] + o[2] + o[3]) * 0.f == 0.f));
-        odd = odds >> (lane & ~(TPR - 1)) & (D == 128 ? 0xffffffffull : 0xffffull);
-        if (mine_to_write) {
-            if (!odd) *reinterpret_cast<bf16x4*>(p.out + (int64_t)tok * p.q_tok + (int64_t)hd * p.q_head + c * 4) = __builtin_convertvector(o * inv, bf16x4);
-            if (p.lse && c == 0) p.lse[(int64_t)tok * p.n_q_heads + hd] = l == 0.f ? -INFINITY : (m + fast_log2(l)) * kLn2;
+        if (GP > 1 && !in_place) {
+            if (c == 0) { s_ml[2 * group] = m; s_ml[2 * group + 1] = l; }
+            *reinterpret_cast<floatx4*>(s_o + group * D + c * 4) = o;
+            __syncthreads();
+            for (int j = 0; j < GP; ++j) m = fmaxf(m, s_ml[2 * j]);
+            const float m_ref = m == -INFINITY ? 0.f : m;
+            l = 0.f;
+            o = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < GP; ++j) {
+                const float w = fast_exp2(s_ml[2 * j] - m_ref);
+                l += s_ml[2 * j + 1] * w;
+                const floatx4 y = *reinterpret_cast<const floatx4*>(s_o + j * D + c * 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] += y[i] * w;
+            }
         }
-    }
-    for (uint64_t rows = __ballot(odd && mine_to_write && c == 0); __builtin_expect(rows != 0, 0); rows &= rows - 1) {
-        const int i = __builtin_ctzll(rows);
-        odd_row<D, PAGED>(p, own, b, tok, __builtin_amdgcn_readlane(hd, i), __shfl(m, i), __shfl(l, i), lane);
+        const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+        if (!in_place) {
+            const uint64_t odds = __ballot(!((o[0] + o[1] + o[2] + o[3]) * 0.f == 0.f));
+            odd = odds >> (lane & ~(TPR - 1)) & (D == 128 ? 0xffffffffull : 0xffffull);
+            if (mine_to_write) {
+                if (!odd) *reinterpret_cast<bf16x4*>(p.out + (int64_t)tok * p.q_tok + (int64_t)hd * p.q_head + c * 4) = __builtin_convertvector(o * inv, bf16x4);
+                if (p.lse && c == 0) p.lse[(int64_t)tok * p.n_q_heads + hd] = l == 0.f ? -INFINITY : (m + fast_log2(l)) * kLn2;
+            }
+        }
+        for (uint64_t rows = __ballot(odd && mine_to_write && c == 0); __builtin_expect(rows != 0, 0); rows &= rows - 1) {
+            const int i = __builtin_ctzll(rows);
+            odd_row<D, PAGED>(p, own, b, tok, __builtin_amdgcn_readlane(hd, i), __shfl(m, i), __shfl(l, i), lane);
+        }
     }
 }
 
@@ -1164,10 +1202,12 @@ int launch_rows(RowsParams& p, hipStream_t stream)
     constexpr int lds = 4 * Layout<D>::TILE + (int)sizeof(RowsPlan);
     static_assert(lds <= 160 * 1024, "a CU's");
     if (const int rc = allow_lds<&rows_kernel<D, PAGED>>(lds)) return rc;
-    const int units = (p.n_q_heads + 256 / D - 1) / (256 / D);
     const int64_t rows = (int64_t)p.n_queries * p.n_q_heads;
-    // few rows have many pieces each
-    const bool few = rows <= 2048;
+    // Few rows of long keys have many pieces each: a workgroup to a row (8 tokens of 64 heads over 30000 states 36.7 us a call with a wave to two rows, so 33.3;
+    // but 32 tokens over 2500 46.4 and 48.6, one of 14 heads over 1254 11.2 and 12.3).  Where there are more rows than waves for long, a wave looks at 8 heads of its token at once, of
+    // which those in place cost no more than that look (2 texts of 2048 tokens and 64 heads 39 us, now 13;  but 60 thousand rows with two pieces each 18 and 24).
+    const bool few = rows <= 512 && p.kv_len >= 2048, many = rows > 131072;
+    const int heads = 256 / D * (many ? 8 : 1), units = (p.n_q_heads + heads - 1) / heads;
     const int64_t joins = few ? rows : ((int64_t)p.n_queries * units + 3) / 4;
     if (!launchable(joins, 256)) return SPECVLM_EUNSUPPORTED;
     if (!PAGED && p.ranges) {
@@ -1178,8 +1218,9 @@ int launch_rows(RowsParams& p, hipStream_t stream)
     p.padded = round_up(p.workgroups, kNumXcd);
     rows_kernel<D, PAGED><<<p.padded, kRowsThreads, lds, stream>>>(p);
     if (const int rc = launch_status()) return rc;
-    if (few) rows_join_kernel<D, PAGED, 1024 / D><<<(unsigned)joins, 256, 0, stream>>>(p);
-    else rows_join_kernel<D, PAGED, 1><<<(unsigned)joins, 256, 0, stream>>>(p);
+    if (few) rows_join_kernel<D, PAGED, 1024 / D, 1><<<(unsigned)joins, 256, 0, stream>>>(p);
+    else if (many) rows_join_kernel<D, PAGED, 1, 8><<<(unsigned)joins, 256, 0, stream>>>(p);
+    else rows_join_kernel<D, PAGED, 1, 1><<<(unsigned)joins, 256, 0, stream>>>(p);
     return launch_status();
 }
 
@@ -1208,6 +1249,7 @@ int rows_start(RowsParams& p, bool paged, const void* q, int64_t q_tok, int64_t 
     p.inv_group = reciprocal(p.group);
     p.scale_log2 = scale * kLog2e;
     p.most_rows = (int)rows_parts(paged, ranges, 0, batch, n_queries, n_q_heads, n_kv_heads);
+    p.far = entries * (rows + 32 * n_kv_heads) > INT_MAX;
     p.entries = (int)entries; p.ranges = key_ranges; p.span = rows_span(n_q_heads, n_kv_heads);
     const size_t parts = (size_t)rows_parts(paged, true, kNumCu, batch, n_queries, n_q_heads, n_kv_heads);
     p.part_o = (float*)workspace;

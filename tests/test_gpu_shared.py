@@ -390,6 +390,23 @@ def test_offsets_that_overlap_write_nothing(B):
     assert (out == 7.0).all()
 
 
+@pytest.mark.parametrize("paged", [False, True])
+def test_offsets_that_overlap_by_more_than_an_int_holds(B, paged):
+    """2^31 rows, counted with the repeated ones: as a sum of ints none."""
+    batch, queries = 16384, 4096
+    q, k = dev_bf16(rnd_bits((queries, 64, 64), 1)), dev_bf16(rnd_bits((4096, 1, 64), 2))
+    out = torch.full_like(q, 7.0)
+    cu = torch.zeros(batch + 1, dtype=torch.int32, device="cuda")
+    cu[1::2] = queries
+    if paged:
+        table = torch.arange(256, dtype=torch.int32, device="cuda").expand(batch, 256)
+        B.shared_attn(q, k.view(256, 16, 1, 64), k.view(256, 16, 1, 64), table, torch.full((batch,), 4096, dtype=torch.int32, device="cuda"), 0.125,
+                      torch.zeros((3, batch), dtype=torch.int32, device="cuda"), cu_q=cu, max_q_len=queries, max_kv_len=4096, out=out)
+    else:
+        B.cross_attn(q, k[:64], k[:64], 0.125, cu_q=cu, cu_kv=torch.clamp(cu, max=64), out=out)
+    assert (out == 7.0).all()
+
+
 @pytest.mark.parametrize("queries", [2, 60])
 def test_odd_values_of_states(B, queries):
     heads = (16, 2, 128)
