@@ -555,7 +555,7 @@ def test_who_shares(B, ps, min_tokens):
         assert (got == groups).all()
 
 
-@pytest.mark.parametrize("batch,width", [(1, 1), (2, 1), (3, 300), (40, 70), (257, 9), (1500, 5), (9, 3000)])
+@pytest.mark.parametrize("batch,width", [(1, 1), (2, 1), (3, 300), (40, 70), (257, 9), (1500, 5), (9, 3000), (16, 512), (16, 513), (17, 512), (8, 256), (5, 257)])
 @pytest.mark.parametrize("seed", [1, 2])
 def test_who_shares_in_tables_of_every_kind(B, batch, width, seed):
     """Rows that go on from the row before them at a random place; entries that are no pages; blocks longer than their caches."""

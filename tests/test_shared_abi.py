@@ -81,7 +81,7 @@ def test_refusals_launch_nothing(tmp_path):
 def test_launches(tmp_path):
     """No launch has 2^32 threads, and none asks for more LDS than a CU has."""
     big = {**ATTN, "cu_q": AT, "n_queries": (1 << 26) // 28, "batch": 2, "kv_len": 16, "q_len": 16}
-    got = L.launches([("specvlm_pages_shared", SHARED), ("specvlm_shared_attn", ATTN), ("specvlm_cross_attn", CROSS), ("specvlm_shared_attn", big),
+    got = L.launches([("specvlm_pages_shared", SHARED), ("specvlm_pages_shared", {**SHARED, "batch": 8192}), ("specvlm_shared_attn", ATTN), ("specvlm_cross_attn", CROSS), ("specvlm_shared_attn", big),
                       ("specvlm_shared_attn", {**ATTN, "head_dim": 64})], tmp_path)
     for status, launched in got:
         assert status == 0 and launched
@@ -90,7 +90,7 @@ def test_launches(tmp_path):
 
 
 def test_a_launch_that_fails_is_said(tmp_path):
-    got = L.launches([(f, args, 1) for f, args in CALLS.items()], tmp_path)
+    got = L.launches([(f, {**args, "batch": 20} if f == "specvlm_pages_shared" else args, 1) for f, args in CALLS.items()], tmp_path)
     assert [status for status, _ in got] == [-4] * 3
 
 
