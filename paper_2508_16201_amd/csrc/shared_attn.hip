@@ -18,6 +18,12 @@
 // columns: a lane then holds 16 logits of one row, which are, packed, the second product's operand).  Where a set has fewer rows,
 // two or four waves share them and take every second or fourth 32 keys.  Tiles of 128 keys go to LDS by direct loads, two in
 // turn.
+//
+// Bound.  Wide sets: 128 keys of 256 rows take 7400 to 7900 cycles of a CU, of which the matrix unit works 4096 and the reads of the tiles' fragments from LDS
+// take as many; the clock, 2.4 GHz without such work, falls to 1.9 to 1.55 under it.  2 x 2048 queries of 64 heads over 12544 states: 1.49 ms, 1.13 PFLOP/s (a
+// library's product of 8192^3 1.22).  The loop alone, without masks, lookups and pages, took 6650 cycles, and 5950 without loads.  Narrow sets: memory, 32 requests
+// about five videos of up to 32768 tokens at 3.7 TB/s.  Beside the keys a piece takes 7 to 9 us: its place 0.8, table and queries 2, the first tile's way
+// through the maxima 2 more than another's, its results 2.5; and the second launch 5 to 18 us.
 #include <climits>
 #include <type_traits>
 
@@ -34,7 +40,7 @@ constexpr int kSetRows = kRowsWaves * 32;
 constexpr int kChunks = kRowsTile / 32;
 constexpr float kRowsRedo = 0x1p20f;     // a lane's sum of 32 keys above this (or NaN) is done again with the maximum tracked
 // 32 keys with more than this times what their row had before have their probabilities in two bf16, where one costs up to 2^-9 of a probability: evened out
-// over many keys of like weight, but not in a row that one key makes up. (One viewer's token over 65536 states, errors against 64 bits in parts of those of
+// over many keys of like weight, but not in a row that one key makes up. (48 viewers' tokens over one stream of 65536, errors against 64 bits in parts of those of
 // outputs rounded once, over seeds: without 1.15 to 1.56, at 4 1.04 to 1.23, 2 1.03 to 1.22, 1 1.03 to 1.20, 0.25 1.03 to 1.17;  91.1 us a call, and 90.8, 91.2,
 // 92.4 and 100.)
 constexpr float kRowsPeak = 2.f;
@@ -152,8 +158,8 @@ __device__ __forceinline__ int padded_rows(const RowsParams& p, const Entry& e) 
 
 // Work is counted in the time that 32 keys of a set take, and an item has kBegin more in front of its first: what a piece costs before and behind its keys.
 // A set has 256 rows, the last one what is left. The figures are from the pieces' own clocks: 32 keys of up to four blocks of 32 rows 0.78 us, of more
-// 1.15, a piece of one tile 9 to 12. (trees, 32 requests of 26 rows of 64 behind 4096 keys of theirs and of others: kBegin of 18 99 us a call, 27 89, 36 90;
-// prompts of 256 behind shared texts 345, 304, 304; the videos that want the copies' rate 125, 128, 130. With four blocks at 3: 107, 343 and 133 at 18.) No
+// 1.15, a piece of one tile 9 to 12. (Trees of 26 nodes of eight requests about two videos of 12544 tokens: kBegin of 18 99 us a call, 27 89, 36 90;
+// eight prompts of up to 256 tokens about one 345, 304, 304; 32 requests about five, which memory bounds, 125, 128, 130. With four blocks at 3: 107, 343 and 133 at 18.) No
 // workgroup is begun for less than kLeastRun: of the smallest calls 6 and 12 take the same, 20 takes 1 us more.
 constexpr int kBegin = 27, kLeastRun = 12;
 struct Sets {
@@ -218,8 +224,8 @@ struct RowsPlan {
     int found;
 };
 
-// entry_of of all entries, one to a thread, where there are no more than threads:  what requests say of each other goes through LDS (each look at another's
-// words in memory takes 0.7 us).
+// entry_of of all entries, one to a thread, where there are no more than threads:  what requests say of each other goes through LDS, not by one look at memory
+// after the other (15.0 us a call of four short dialogues, 15.3 without).
 __device__ __forceinline__ Entry entry_at_once(const RowsParams& p, RowsPlan& s, bool grouped)
 {
     const int t = threadIdx.x, b = t < p.batch ? t : t - p.batch;
@@ -340,6 +346,7 @@ __device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, 
     const int n_blocks = (pc.n_rows + 31) >> 5, log_blocks = n_blocks > 4 ? 3 : n_blocks > 2 ? 2 : n_blocks - 1;       // waves of a kind
     const int blk = wave & ((1 << log_blocks) - 1), ks = wave >> log_blocks, n_ks = min(kChunks, kRowsWaves >> log_blocks);
     const bool works = blk < n_blocks && ks < n_ks;
+    // Probabilities in two bf16 for one or two blocks, whose matrix products are hidden behind the loads (errors 1.03 times as large without, 1 % less time).
     const bool two_parts = n_blocks <= 2;
     const int key0 = pc.key0, key1 = pc.key1, tiles = (key1 - key0 + kRowsTile - 1) / kRowsTile;
 
@@ -537,6 +544,8 @@ __device__ __forceinline__ void rows_piece(RowsPlan& plan, const uint32_t lds0, 
 
     // A tile that all rows of the wave see whole, after others: while the vector unit weighs 32 keys, the matrix unit takes the products with the values of the last
     // 32 and then the logits of the next.  (The wave's keys of a tile: all, or every second 32.)  Returns how many it has taken: those that go beyond the maximum are left.
+    // (Eight prompts of up to 256 tokens about one video 340 us a call without, 327 with; 48 viewers' tokens over a stream 102 and 96, 99.5 with tiles of all keys only; trees the same. Four
+    // waves that share rows have one 32 keys of a tile: nothing to work on beside.)
     const auto whole_tile = [&](auto pieces, const uint32_t at) {
         constexpr int N = decltype(pieces)::value, STEP = kChunks / N * CHUNK_BYTES;
         floatx16 s;
