@@ -634,8 +634,8 @@ int specvlm_shared_attn(
  *        outside of the entry is not there
  * A query that sees no state gets 0, and -infinity in lse.  Hidden and infinite values are as
  * for specvlm_paged_attn.  An entry whose offsets leave the tensors or descend is skipped, its
- * rows of out and lse left as they are, as are rows of no entry.  Results do not depend on
- * the run.
+ * rows of out and lse left as they are, as are rows of no entry.  No query is in two entries.
+ * Results do not depend on the run.
  * Limits: n_queries * H_q up to 2^26 is always served (a launch's threads); batch * H_kv < 2^24,
  * 3 * (n_queries * H_q / 128 + (batch + 2) * H_kv) * (n_states / 32 + 10) < 2^31 (with key_ranges
  * n_queries * H_q / 64 there), n_states <= 2^30.

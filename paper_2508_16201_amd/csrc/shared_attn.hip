@@ -900,6 +900,13 @@ void rows_kernel(const RowsParams p)
     }
 }
 
+// Whether an entry's offsets, or a request's, leave it queries: of those around it that do not, nothing else is true.
+__device__ __forceinline__ bool has_queries(const RowsParams& p, int b)
+{
+    const int from = p.cu_q[b], to = p.cu_q[b + 1];
+    return from >= 0 && from < to && to <= p.n_queries && (int64_t)to - from <= p.q_len;
+}
+
 // (Ranges) The queries of entry b begin at q0: the number of its first share.  There is a share's room between an entry and the next, more than half of which is
 // for a share that is not whole.
 __device__ __forceinline__ int spans_before(const RowsParams& p, int q0, int b) { return q0 / p.span + b; }
@@ -916,7 +923,7 @@ void rows_spans_kernel(const RowsParams p)
     if (p.cu_q) {
         b = -1;
         for (int c = 0; c < p.batch; c += kWave) {
-            const uint64_t begun = __ballot(c + lane < p.batch && spans_before(p, p.cu_q[min(c + lane, p.batch - 1)], c + lane) <= e);
+            const uint64_t begun = __ballot(c + lane < p.batch && has_queries(p, c + lane) && spans_before(p, p.cu_q[c + lane], c + lane) <= e);
             if (begun) b = c + 63 - __builtin_clzll(begun);
         }
     }
@@ -1043,10 +1050,10 @@ void rows_join_kernel(const RowsParams p)
     } else {
         uint64_t behind = 0;
         for (; b < p.batch; b += kWave) {
-            behind = __ballot(b + lane < p.batch && p.cu_q[min(b + lane, p.batch - 1) + 1] > tok);
+            behind = __ballot(b + lane < p.batch && has_queries(p, b + lane) && p.cu_q[b + lane] <= tok && p.cu_q[b + lane + 1] > tok);
             if (behind) break;
         }
-        if (!behind) return;                                 // (a row behind the last request)
+        if (!behind) return;                                 // (a row of no request)
         b += __builtin_ctzll(behind);
     }
     int e = PAGED ? p.batch + b : b;

@@ -507,6 +507,34 @@ def test_ranges_of_many_entries(B):
     close(host_f64(out)[cu_q[200]:], want[cu_q[200]:], tol[cu_q[200]:])
 
 
+@pytest.mark.parametrize("cu_q,left", [([0, 40, 999, 40, 70], [0, 3]), ([0, 40, -3, 40, 70], [0, 3]), ([5, -9, 0, 40, 70], [2, 3]), ([0, 40, 70, 2 ** 31 - 1, -(2 ** 31)], [0, 1])])
+@pytest.mark.parametrize("kind", ["cross", "ranges", "paged"])
+def test_entries_that_are_skipped_change_no_other(B, cu_q, left, kind):
+    """Offsets that make no entry, in front of and between others whose rows are cut and joined."""
+    q, k = rnd_bits((70, 14, 64), 71), rnd_bits((4 * 2000, 2, 64), 72)
+    out = torch.full((70, 14, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    ranges = np.stack([np.arange(70) * 20, 1000 + np.arange(70) * 9], 1).astype(np.int32) if kind == "ranges" else None
+    pages = k.reshape(4, 125, 16, 2, 64)
+    if kind == "paged":
+        table = np.arange(500, dtype=np.int32).reshape(4, 125)
+        B.shared_attn(dev_bf16(q), dev_bf16(pages.reshape(500, 16, 2, 64)), dev_bf16(pages.reshape(500, 16, 2, 64)), i32(table), i32([2000] * 4), 0.125,
+                      torch.zeros((3, 4), dtype=torch.int32, device="cuda"), cu_q=i32(cu_q), max_q_len=40, max_kv_len=2000, out=out)
+    else:
+        B.cross_attn(dev_bf16(q), dev_bf16(k), dev_bf16(k), 0.125, cu_q=i32(cu_q), cu_kv=i32([0, 2000, 4000, 6000, 8000]),
+                     key_ranges=None if ranges is None else i32(ranges), out=out)
+    got, written = host_f64(out), np.zeros(70, dtype=bool)
+    for e in left:
+        rows, x = slice(cu_q[e], cu_q[e + 1]), S.values(k[2000 * e:2000 * e + 2000])
+        sees = np.arange(2000)[None] <= 2000 - (cu_q[e + 1] - cu_q[e]) + np.arange(cu_q[e + 1] - cu_q[e])[:, None] if kind == "paged" else None
+        if kind == "paged":
+            want, _, tol, _ = S.all_heads(S.values(q[rows]), x, x, 0.125, sees)
+        else:
+            want, _, tol, _ = S.cross_attention(S.values(q[rows]), x, x, [cu_q[e + 1] - cu_q[e]], [2000], 0.125, None if ranges is None else ranges[rows])
+        close(got[rows], want, tol)
+        written[rows] = True
+    assert (got[~written] == 7.0).all()
+
+
 def test_captured_graphs_that_share_a_workspace(B):
     """One after the other, again and again, each with its own answers."""
     one = build(64, [(800, [(20, 2)] * 5)], (14, 2, 64), 16)
