@@ -602,7 +602,10 @@ int specvlm_pages_shared(
  *   n_queries  rows of q: batch * q_len without cu_q.  q_len, kv_len: the maxima, as there
  * Everything else, hidden and infinite values, skipped requests and rows behind the last one
  * too, is as for specvlm_paged_attn.  Results do not depend on the run; they may differ by
- * roundings with the other requests of the batch and the groups.
+ * roundings with the other requests of the batch and the groups.  Probabilities are rounded to
+ * bf16 for their products with V, to two bf16 where up to 64 rows of a kv head meet the keys or
+ * 32 keys weigh more than twice what their row had before; sums and partial results are fp32.
+ * The workspace has 4 d + 8 bytes for each row of q twice, and 65536 rows of it more.
  * Limits: n_queries * H_q up to 2^26 is always served (a launch's threads); batch * H_kv < 2^23,
  * 3 * (n_queries * H_q / 128 + (2 * batch + 1) * H_kv) * (kv_len / 32 + 10) < 2^31, kv_len <= 2^30.
  * -------------------------------------------------------------------------- */
@@ -628,14 +631,15 @@ int specvlm_shared_attn(
  *   cu_q, cu_kv   int32 [batch + 1]: the queries [cu_q[e], cu_q[e + 1]) look at the states
  *        [cu_kv[e], cu_kv[e + 1]).  Either may be empty, and of any length up to the tensors':
  *        texts about one video are one entry, one text behind the other.  Both NULL: batch 1,
- *        all queries and all states
+ *        all queries and all states (k and v may be NULL where there are none)
  *   key_ranges    int32 [n_queries, 2] or NULL: a query sees the states [from, to) of its
  *        entry, counted from the entry's first (text between the frames of a stream); what lies
  *        outside of the entry is not there
  * A query that sees no state gets 0, and -infinity in lse.  Hidden and infinite values are as
  * for specvlm_paged_attn.  An entry whose offsets leave the tensors or descend is skipped, its
  * rows of out and lse left as they are, as are rows of no entry.  No query is in two entries.
- * Results do not depend on the run.
+ * Results do not depend on the run; roundings are as in specvlm_shared_attn, and the workspace,
+ * with each row once.
  * Limits: n_queries * H_q up to 2^26 is always served (a launch's threads); batch * H_kv < 2^24,
  * 3 * (n_queries * H_q / 128 + (batch + 2) * H_kv) * (n_states / 32 + 10) < 2^31 (with key_ranges
  * n_queries * H_q / 64 there), n_states <= 2^30.

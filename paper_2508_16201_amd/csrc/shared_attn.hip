@@ -1245,7 +1245,7 @@ int rows_start(RowsParams& p, bool paged, const void* q, int64_t q_tok, int64_t 
                int n_queries, int most_keys, int n_q_heads, int n_kv_heads, int head_dim, float scale, const int32_t* key_ranges, void* out, float* lse,
                void* workspace, size_t workspace_bytes)
 {
-    if (!q || !out || !k || !v) return SPECVLM_EINVAL;
+    if (!q || !out || ((!k || !v) && most_keys > 0)) return SPECVLM_EINVAL;
     if ((q_tok | q_head | tok | head) & 7) return SPECVLM_EUNSUPPORTED;
     if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 15) return SPECVLM_EUNSUPPORTED;
     // (a lane's offset inside 16 keys has 32 bits; rows, and tiles of all sets and heads, are ints)

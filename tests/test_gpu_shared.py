@@ -365,6 +365,17 @@ def test_no_query_sees_anything(B):
     check_cross(B, 8, (4, 1, 64), [40], [500], ranges=np.zeros((40, 2), dtype=np.int32))
 
 
+@pytest.mark.parametrize("cu", [False, True])
+@pytest.mark.parametrize("ranges", [False, True])
+def test_no_states_at_all(B, cu, ranges):
+    q, none = dev_bf16(rnd_bits((43, 4, 64), 8)), torch.empty((0, 1, 64), dtype=torch.bfloat16, device="cuda")
+    more = dict(cu_q=i32([0, 3, 43]), cu_kv=i32([0, 0, 0])) if cu else {}
+    if ranges:
+        more["key_ranges"] = i32(np.full((43, 2), [0, 9]))
+    got, lse = B.cross_attn(q, none, none, 0.125, want_lse=True, **more)
+    assert (got == 0).all() and (lse == -np.inf).all()
+
+
 def test_text_between_frames(B):
     ranges = np.array([[max(0, (t // 10 - 3) * 49), t // 10 * 49] for t in range(300)], dtype=np.int32)
     check_cross(B, 9, (16, 2, 128), [300], [30 * 49], ranges=ranges)

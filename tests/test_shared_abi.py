@@ -58,7 +58,8 @@ REFUSED = [
     *[("specvlm_cross_attn", {k: -1}, -1) for k in ("batch", "n_queries", "n_states", "n_q_heads", "n_kv_heads")],
     ("specvlm_cross_attn", {"cu_q": None, "cu_kv": None}, -1), ("specvlm_cross_attn", {"cu_q": None, "cu_kv": None, "batch": 1}, 0),
     ("specvlm_cross_attn", {"n_q_heads": 27}, -1), ("specvlm_cross_attn", {"softmax_scale": -1.0}, -1), ("specvlm_cross_attn", {"softmax_scale": float("nan")}, -1),
-    ("specvlm_cross_attn", {"head_dim": 80}, -2), ("specvlm_cross_attn", {"n_states": 0}, 0), ("specvlm_cross_attn", {"n_states": (1 << 30) + 1}, -2),
+    ("specvlm_cross_attn", {"head_dim": 80}, -2), ("specvlm_cross_attn", {"n_states": 0}, 0), ("specvlm_cross_attn", {"n_states": 0, "k": None, "v": None}, 0),
+    ("specvlm_cross_attn", {"n_states": (1 << 30) + 1}, -2),
     *[("specvlm_cross_attn", {k: 12}, -2) for k in ("q_tok_stride", "q_head_stride", "kv_tok_stride", "kv_head_stride")],
     *[("specvlm_cross_attn", {k: AT + 8}, -2) for k in ("q", "k", "v", "out")],
     ("specvlm_cross_attn", {"kv_tok_stride": 1 << 26}, -2), ("specvlm_cross_attn", {"workspace": None}, -3), ("specvlm_cross_attn", {"workspace": AT + 16}, -3),
