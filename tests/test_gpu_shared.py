@@ -546,6 +546,35 @@ def test_entries_that_are_skipped_change_no_other(B, cu_q, left, kind):
     assert (got[~written] == 7.0).all()
 
 
+@pytest.mark.parametrize("ranges", [False, True])
+def test_more_heads_of_a_group_than_a_set_has_rows(B, ranges):
+    check_cross(B, 73, (300, 1, 64), [3, 2], [100, 700], ranges=np.array([[0, 90], [5, 60], [50, 100], [0, 700], [333, 650]], dtype=np.int32) if ranges else None)
+    check(B, *build(74, [(96, [(20, 2), (40, 3)])], (300, 1, 64), 16))
+
+
+@pytest.mark.parametrize("odd", [False, True])
+def test_rows_in_place_and_cut_rows_where_there_are_many(B, odd):
+    """More than 2^17 rows: a wave of the join looks at several heads of a token."""
+    heads, queries, states = (64, 8, 64), 2100, 190
+    q, k, v = rnd_bits((queries, 64, 64), 75), rnd_bits((states, 8, 64), 76), rnd_bits((states, 8, 64), 77)
+    flat = v.copy()
+    if odd:
+        v[100, 3, 7], v[40, 5, 9], flat[100, 3, 7], flat[40, 5, 9] = 0x7f80, 0x7fc0, 0, 0
+    want, want_lse, tol, tol_lse = S.cross_attention(S.values(q), S.values(k), S.values(flat), [queries], [states], 0.125)
+    got, lse = B.cross_attn(dev_bf16(q), dev_bf16(k), dev_bf16(v), 0.125, want_lse=True)
+    got = host_f64(got)
+    assert (np.abs(host_f64(lse) - want_lse) <= tol_lse).all()
+    plain = np.ones((64, 64), dtype=bool)
+    if odd:
+        assert (got[:, 24:32, 7] == np.inf).all() and np.isnan(got[:, 40:48, 9]).all()
+        plain[24:32, 7] = plain[40:48, 9] = False
+    assert (np.abs(got - want)[:, plain] <= tol[:, plain]).all()
+
+
+def test_many_rows_that_share_keys(B):
+    check(B, *build(78, [(64, [(80, 60)] * 36)], (64, 8, 64), 16))
+
+
 def test_captured_graphs_that_share_a_workspace(B):
     """One after the other, again and again, each with its own answers."""
     one = build(64, [(800, [(20, 2)] * 5)], (14, 2, 64), 16)
