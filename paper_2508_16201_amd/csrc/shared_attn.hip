@@ -20,7 +20,7 @@
 // turn.
 //
 // Bound.  Wide sets: 128 keys of 256 rows take 7400 to 7900 cycles of a CU, of which the matrix unit works 4096 and the reads of the tiles' fragments from LDS
-// take as many; the clock, 2.4 GHz without such work, falls to 1.9 to 1.55 under it.  2 x 2048 queries of 64 heads over 12544 states: 1.49 ms, 1.13 PFLOP/s (a
+// take as many; the clock, 2.4 GHz without such work, falls to 1.9 to 1.55 under it.  2 x 2048 queries of 64 heads over 12544 states: 1.50 ms, 1.12 PFLOP/s (a
 // library's product of 8192^3 1.22).  The loop alone, without masks, lookups and pages, took 6650 cycles, and 5950 without loads.  Narrow sets: memory, 32 requests
 // about five videos of up to 32768 tokens at 3.7 TB/s.  Beside the keys a piece takes 7 to 9 us: its place 0.8, table and queries 2, the first tile's way
 // through the maxima 2 more than another's, its results 2.5; and the second launch 5 to 18 us.
