@@ -86,6 +86,9 @@ struct RowsParams {
     float* part_ml;                              // [rows_parts][2] running maximum in log2 units, sum
     RowsStart* starts;                           // [entries] what the join has to know of them
     int most_rows;                               // that the entries may have, for partial results
+    // (paged) The output lies over the queries: a request that is taken alone may lie among those of a group, whose pieces read its queries too, so the join
+    // writes all.
+    bool over_q;
     bool far;                                    // entries that overlap may have more rows than an int holds
 };
 
@@ -898,7 +901,7 @@ void rows_kernel(const RowsParams p)
         pc.q0 = en.q0; pc.n_q = en.n_q; pc.end = en.key1;
         pc.g = g; pc.row0 = set * kSetRows; pc.n_rows = min(rows - pc.row0, kSetRows);
         pc.key0 = en.key0 + c_begin * 32; pc.key1 = min(en.key1, en.key0 + c_end * 32);
-        pc.direct = own && !(PAGED && en.key0 > 0) && c_begin == 0 && c_end == chunks;
+        pc.direct = own && !(PAGED && (en.key0 > 0 || p.over_q)) && c_begin == 0 && c_end == chunks;
         pc.part = part_row(j, front.rows + g * padded_rows(p, en) + pc.row0);
         rows_piece<D, PAGED>(plan, lds0, pc);
         __syncthreads();                                     // the ring, and what the plan holds, are free again
@@ -1089,7 +1092,7 @@ void rows_join_kernel(const RowsParams p)
         bool mine = false;
         if (lane < HEADS && hd < p.n_q_heads) {
             const Pieces pieces = pieces_of(own, divide(hd, p.group, p.inv_group));
-            mine = pieces.n != 1;
+            mine = pieces.n != 1 || (PAGED && p.over_q);
             if (!mine) {
                 const float l = p.part_ml[2 * part_row(pieces.first, pieces.row) + 1];
                 mine = __float_as_uint(l) >> 31 || !(l == l);
@@ -1108,7 +1111,7 @@ void rows_join_kernel(const RowsParams p)
         float m = -INFINITY, l = 0.f;
         floatx4 o = {0.f, 0.f, 0.f, 0.f};
         bool odd = false;
-        const bool in_place = theirs.n == 0 && mine.n == 1;
+        const bool in_place = theirs.n == 0 && mine.n == 1 && !(PAGED && p.over_q);
         if (in_place) {
             const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * part_row(mine.first, mine.row));
             odd = __float_as_uint(ml.y) >> 31 || !(ml.y == ml.y);
@@ -1270,6 +1273,7 @@ int rows_start(RowsParams& p, bool paged, const void* q, int64_t q_tok, int64_t 
     p.inv_group = reciprocal(p.group);
     p.scale_log2 = scale * kLog2e;
     p.most_rows = (int)rows_parts(paged, ranges, 0, batch, n_queries, n_q_heads, n_kv_heads);
+    p.over_q = q == out;
     p.far = entries * (rows + 32 * n_kv_heads) > INT_MAX;
     p.entries = (int)entries; p.ranges = key_ranges; p.span = rows_span(n_q_heads, n_kv_heads);
     const size_t parts = (size_t)rows_parts(paged, true, kNumCu, batch, n_queries, n_q_heads, n_kv_heads);

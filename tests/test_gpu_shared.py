@@ -295,6 +295,23 @@ def test_the_queries_may_be_the_output_and_strides_are_anything(B):
     assert (host_f64(wide) == want).all()
 
 
+def test_a_request_taken_alone_among_a_group_where_the_queries_are_the_output(B):
+    """The group's pieces read its queries as long as they run: nothing is written over them before."""
+    q, k, v, table, kv_lens, q_lens, groups = build(79, [(3200, [(20, 4), (17, 4), (60, 4), (33, 4)])], (28, 4, 128), 16)
+    kv_lens[1] = 50                                      # (shorter than what the group shares)
+    args = dev_bf16(k), dev_bf16(v), i32(table), i32(kv_lens), 0.1, i32(groups)
+    want = B.shared_attn(dev_bf16(q), *args)
+    exact, _, tol, _, _ = S.shared_attention(S.values(q), S.values(k), S.values(v), table, kv_lens, q_lens, 0.1)
+    close(host_f64(want), exact, tol)
+    first = None
+    for _ in range(5):
+        out = dev_bf16(q)
+        B.shared_attn(out, *args, out=out)
+        close(host_f64(out), exact, tol)
+        first = out if first is None else first
+        assert (out == first).all() and (out == want).all()
+
+
 def test_a_zero_scale_takes_the_mean(B):
     args = build(15, [(96, [(20, 2), (40, 2)])], (6, 2, 64), 16)
     check(B, *args, scale=0.0)
