@@ -696,6 +696,24 @@ def test_from_forks_to_attention(B):
         parent, keep = i32([0, 1, 2, 3]), i32(lens)
 
 
+def test_a_layer_over_caches_and_states(B):
+    """Questions about two videos: who shares, attention over their caches, then over the states of each one's encoder, in place."""
+    q, k, v, table, kv_lens, q_lens, groups = build(84, [(320, [(20, 3), (35, 1), (50, 4)]), (160, [(60, 2), (16, 5)])], (16, 2, 128), 16)
+    states = [300, 1100]
+    ks, vs = rnd_bits((sum(states), 2, 128), 85), rnd_bits((sum(states), 2, 128), 86)
+    cu_q, lens = i32(np.concatenate([[0], np.cumsum(q_lens)])), i32(kv_lens)
+    found = B.pages_shared(i32(table), lens, len(k), 16, max(q_lens), cu_q=cu_q, min_tokens=16)
+    assert found.tolist() == groups.tolist()
+    x = B.shared_attn(dev_bf16(q), dev_bf16(k), dev_bf16(v), i32(table), lens, 0.1, found, cu_q=cu_q, max_q_len=max(q_lens))
+    want, _, tol, _, _ = S.shared_attention(S.values(q), S.values(k), S.values(v), table, kv_lens, q_lens, 0.1)
+    close(host_f64(x), want, tol)
+    texts = [sum(q_lens[:3]), sum(q_lens[3:])]
+    want, _, tol, _ = S.cross_attention(host_f64(x), S.values(ks), S.values(vs), texts, states, 0.1)
+    out = B.cross_attn(x, dev_bf16(ks), dev_bf16(vs), 0.1, cu_q=i32([0, texts[0], sum(texts)]), cu_kv=i32([0, states[0], sum(states)]), out=x)
+    assert out is x
+    close(host_f64(x), want, tol)
+
+
 def test_a_captured_step_while_groups_and_lengths_change(B):
     ps, heads = 16, (4, 1, 64)
     one = build(21, [(320, [(20, 2)] * 3), (0, [(30, 2)])], heads, ps)
