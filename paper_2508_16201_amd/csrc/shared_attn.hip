@@ -813,6 +813,7 @@ void rows_kernel(const RowsParams p)
     RowsPlan& plan = *reinterpret_cast<RowsPlan*>(smem + 4 * Layout<D>::TILE);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(SPECVLM_AS3 unsigned char*)smem;
 
+    // (neighbouring runs, which meet the same keys, on one XCD: 2 x 2048 queries over 12544 states 1.51 ms a call, dealt out over all of them 1.58)
     const int j = xcd_logical_id(blockIdx.x, p.padded);
     if (j >= p.workgroups) return;
 
