@@ -7,6 +7,7 @@
 namespace specvlm {
 
 constexpr int kRowsWaves = 8;
+constexpr int kRowsThreads = kRowsWaves * kWave;
 constexpr int kSetRows = kRowsWaves * 32;
 
 // What is numbered.  Entry b is the keys that request b's group shares, if it is the group's first request; entry batch + b request b's own keys.
@@ -158,6 +159,26 @@ __host__ __device__ __forceinline__ Shares shares_of(const RowsParams& p, int to
     const int n = min(p.workgroups, max(1, total / kLeastRun)), each = (int)((uint32_t)total / (uint32_t)n);
     return {n, each, total - each * n};
 }
+
+// A workgroup's way through the entries, a thread to each, from the first ones on.  Workgroup 0 goes through all once before, to tell of them, and begins again.
+struct Walk {
+    Numbers base;                            // in front of the entries at hand
+    int c0;                                  // the first of them
+    bool told;
+    // Whether unit x is behind the entries at hand, which have so much work.  (Who has no unit to take looks for none: of skipped entries there is no work to find.)
+    __host__ __device__ __forceinline__ bool goes_on(int x, int x_end, int work) const { return !told || (x < x_end && x >= base.work + work); }
+    __host__ __device__ __forceinline__ void step(const Numbers& here, int entries)
+    {
+        base.work += here.work;
+        base.rows += here.rows;
+        c0 += kRowsThreads;
+        if (c0 >= entries) {
+            told = true;
+            base = {0, 0};
+            c0 = 0;
+        }
+    }
+};
 
 // A workgroup's part of an item: a set of rows of a kv head, and some of its keys.
 struct Piece {

@@ -35,7 +35,6 @@ namespace specvlm {
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 constexpr int kRowsTile = 128;           // keys of a tile
-constexpr int kRowsThreads = kRowsWaves * kWave;
 constexpr int kChunks = kRowsTile / 32;
 constexpr float kRowsRedo = 0x1p20f;     // a lane's sum of 32 keys above this (or NaN) is done again with the maximum tracked
 // 32 keys with more than this times what their row had before have their probabilities in two bf16, where one costs up to 2^-9 of a probability: evened out
@@ -688,8 +687,9 @@ void rows_kernel(const RowsParams p)
     if (j >= shares.n) return;
     int x = shares.begin(j);
     const int x_end = shares.begin(j + 1);
-    Numbers base = {0, 0};                                   // in front of the 512 entries at hand
-    int c0 = 0;
+    Walk at_hand = {{0, 0}, 0, entries <= kRowsThreads || j > 0};
+    const Numbers& base = at_hand.base;
+    const int& c0 = at_hand.c0;
     const auto tell = [&] {                                  // (the join reads where every entry begins)
         const int e = c0 + threadIdx.x;
         const Entry entry = plan.entry[threadIdx.x];
@@ -698,20 +698,12 @@ void rows_kernel(const RowsParams p)
             p.starts[e] = {base.work + front.work, base.rows + front.rows, entry.q0, entry.n_q, entry.key0, entry.key1, entry.first, total.work};
     };
     if (j == 0) tell();
-    bool told = entries <= kRowsThreads || j > 0;            // (workgroup 0 tells of all entries, then begins again)
-    while (x < x_end || !told) {
-        while (!told || x >= base.work + here.work) {
-            base.work += here.work;
-            base.rows += here.rows;
-            c0 += kRowsThreads;
-            if (c0 >= entries) {
-                told = true;
-                base = {0, 0};
-                c0 = 0;
-            }
+    while (x < x_end || !at_hand.told) {
+        while (at_hand.goes_on(x, x_end, here.work)) {
+            at_hand.step(here, entries);
             __syncthreads();
             look_at(c0 + threadIdx.x);
-            if (!told) tell();
+            if (!at_hand.told) tell();
         }
         if (x >= x_end) break;
         const int there = base.work + plan.front[threadIdx.x].work;

@@ -1,0 +1,78 @@
+"""specvlm_shared_attn and specvlm_cross_attn with offsets, lengths and groups of which some or all say nothing that fits together."""
+import numpy as np
+import pytest
+import torch
+
+import shared_reference as S
+from gpu_util import dev_bf16, host_f64, rnd_bits
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2508_16201_amd import binding
+    binding.lib()
+    return binding
+
+
+def i32(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32).cuda()
+
+
+def shared(B, q, pages, table, kv_lens, groups, cu_q, q_len, kv_len, scale=0.125):
+    """K and V in the same pages -> (out, lse), where nothing is written 7."""
+    out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+    batch, (tq, hq, d), (n_pages, ps, hkv, _) = len(kv_lens), q.shape, pages.shape
+    ws = B.new_workspace(B.shared_attn_workspace_bytes(batch, tq, hq, hkv, d), q.device)
+    rc = B.lib().specvlm_shared_attn(q.data_ptr(), q.stride(0), q.stride(1), pages.data_ptr(), pages.data_ptr(), pages.stride(0), pages.stride(1), pages.stride(2),
+                                     n_pages, ps, table.data_ptr(), table.stride(0), table.shape[1], kv_lens.data_ptr(), groups.data_ptr(), cu_q.data_ptr(), batch,
+                                     tq, q_len, kv_len, hq, hkv, d, scale, None, out.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(),
+                                     torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    torch.cuda.synchronize()
+    return out, lse
+
+
+def cross(B, q, k, cu_q, cu_kv, ranges=None, scale=0.125):
+    """K and V the same -> (out, lse), where nothing is written 7."""
+    out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+    batch, (tq, hq, d), (tk, hkv, _) = len(cu_q) - 1, q.shape, k.shape
+    ws = B.new_workspace(B.cross_attn_workspace_bytes(batch, tq, hq, hkv, d), q.device)
+    rc = B.lib().specvlm_cross_attn(q.data_ptr(), q.stride(0), q.stride(1), k.data_ptr(), k.data_ptr(), k.stride(0), k.stride(1), cu_q.data_ptr(), cu_kv.data_ptr(),
+                                    batch, tq, tk, hq, hkv, d, scale, None if ranges is None else ranges.data_ptr(), out.data_ptr(), lse.data_ptr(), ws.data_ptr(),
+                                    ws.numel(), torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    torch.cuda.synchronize()
+    return out, lse
+
+
+@pytest.mark.parametrize("batch", [256, 257, 600])
+@pytest.mark.parametrize("what", ["no tokens", "shorter than their blocks", "longer than the call says", "empty blocks"])
+def test_a_batch_of_skipped_requests_writes_nothing(B, batch, what):
+    """Up to 1200 entries, none of which has work (slots of a service that are all idle)."""
+    q, pages = dev_bf16(rnd_bits((2 * batch, 4, 64), 1)), dev_bf16(rnd_bits((8, 16, 1, 64), 2))
+    lens = {"no tokens": 0, "shorter than their blocks": 1, "longer than the call says": 97, "empty blocks": 60}[what]
+    cu_q = torch.zeros(batch + 1, dtype=torch.int32, device="cuda") if what == "empty blocks" else i32(2 * np.arange(batch + 1))
+    out, lse = shared(B, q, pages, torch.zeros((batch, 8), dtype=torch.int32, device="cuda"), torch.full((batch,), lens, dtype=torch.int32, device="cuda"),
+                      torch.zeros((3, batch), dtype=torch.int32, device="cuda"), cu_q, 2, 96)
+    assert (out == 7.0).all() and (lse == 7.0).all()
+
+
+@pytest.mark.parametrize("batch", [512, 513, 1500])
+@pytest.mark.parametrize("ranges", [False, True])
+def test_a_batch_of_empty_entries_writes_nothing(B, batch, ranges):
+    q, k = dev_bf16(rnd_bits((70, 4, 64), 1)), dev_bf16(rnd_bits((100, 1, 64), 2))
+    seen = i32([[0, 100]] * 70) if ranges else None
+    for first in (0, 70, 1 << 20):
+        cu_q = torch.full((batch + 1,), first, dtype=torch.int32, device="cuda")
+        out, lse = cross(B, q, k, cu_q, i32([0] * batch + [100]), seen)
+        assert (out == 7.0).all() and (lse == 7.0).all()
+
+
+def test_work_behind_many_entries_that_have_none(B):
+    """1100 empty entries, then one."""
+    q, k = rnd_bits((3, 4, 64), 5), rnd_bits((200, 1, 64), 6)
+    want, want_lse, tol, tol_lse = S.cross_attention(S.values(q), S.values(k), S.values(k), [3], [200], 0.125)
+    out, lse = cross(B, dev_bf16(q), dev_bf16(k), i32([0] * 1101 + [3]), i32([0] * 1101 + [200]))
+    assert (np.abs(host_f64(out) - want) <= tol).all() and (np.abs(lse.double().cpu().numpy() - want_lse) <= tol_lse).all()
