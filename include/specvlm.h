@@ -597,7 +597,8 @@ int specvlm_pages_shared(
  *              same pages, and before their blocks.  The other requests' tables are trusted to
  *              name the pages of the first one's row there; they are not looked at.
  *              What does not fit together (a group beyond the batch, more tokens than lie
- *              before a block, no multiple of 16) is left out, and the requests are
+ *              before a block, no multiple of 16, a request whose queries are not between
+ *              the first one's begin and the last one's end) is left out, and the requests are
  *              taken alone: groups say how the work is cut, not what the result is
  *   n_queries  rows of q: batch * q_len without cu_q.  q_len, kv_len: the maxima, as there
  * Everything else, hidden and infinite values, skipped requests and rows behind the last one

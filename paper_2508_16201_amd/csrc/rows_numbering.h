@@ -81,12 +81,13 @@ __host__ __device__ __forceinline__ Entry shared_entry(const RowsParams& p, cons
     if (n_q <= 0 || r.q0 < 0 || r.q0 > p.n_queries - n_q) return {0, 0, 0, 0, -1};
     return {r.q0, n_q, 0, r.shared, -1};
 }
-// A request's own keys, behind those that it shares (with a group that begins at r.first, and has so many members).
-__host__ __device__ __forceinline__ Entry own_entry(const RowsParams& p, int b, const Request& r, int members, int shared)
+// A request's own keys, behind those that it shares with a group that begins at r.first, has so many members and the entry `all`:  if its queries are among
+// the entry's (offsets that descend, of a request in between, leave others' outside).
+__host__ __device__ __forceinline__ Entry own_entry(const RowsParams& p, int b, const Request& r, int members, const Entry& all)
 {
     if (r.n_q <= 0 || r.n_q > p.q_len || r.q0 < 0 || r.q0 > p.n_queries - r.n_q || r.kvl < r.n_q || r.kvl > p.kv_len) return {0, 0, 0, 0, -1};
-    const bool with = shared > 0 && b - r.first < members && shared <= r.kvl - r.n_q;
-    return {r.q0, r.n_q, with ? shared : 0, r.kvl, with ? r.first : -1};
+    const bool with = all.key1 > 0 && b - r.first < members && all.key1 <= r.kvl - r.n_q && all.q0 <= r.q0 && r.q0 + r.n_q <= all.q0 + all.n_q;
+    return {r.q0, r.n_q, with ? all.key1 : 0, r.kvl, with ? r.first : -1};
 }
 
 template <bool PAGED> __host__ __device__ __forceinline__ Entry entry_of(const RowsParams& p, int e, bool grouped)
@@ -109,7 +110,7 @@ template <bool PAGED> __host__ __device__ __forceinline__ Entry entry_of(const R
             members = first.members;
             if (leads(p, f, first)) all = shared_entry(p, first, p.cu_q ? p.cu_q[f + members] : (f + members) * p.q_len);
         }
-        return e < p.batch ? all : own_entry(p, b, r, members, all.key1);
+        return e < p.batch ? all : own_entry(p, b, r, members, all);
     }
 }
 

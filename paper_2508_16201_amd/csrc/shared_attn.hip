@@ -60,7 +60,7 @@ struct RowsPlan {
         uint64_t tree[kSetRows];             // the rows' masks of the block, then
         float ml[kSetRows * 2];              // maxima and sums of waves that share rows
     };
-    alignas(8) int word[3][kRowsThreads / 2];        // of requests
+    alignas(8) int word[2][kRowsThreads / 2];        // of requests
     uint64_t missing[2][kRowsWaves];         // of 64 tiles, by their 16 keys:  those whose page is none of the pool's
     int found;
 };
@@ -80,12 +80,12 @@ __device__ __forceinline__ Entry entry_at_once(const RowsParams& p, RowsPlan& s,
     Entry e = {0, 0, 0, 0, -1};
     if (t < p.batch) {
         if (grouped && leads(p, b, r)) e = shared_entry(p, r, s.word[0][b + r.members - 1]);
-        s.word[2][b] = e.key1;
+        s.entry[b] = e;
     }
     __syncthreads();
     if (t >= p.batch && b < p.batch) {
         const bool in = grouped && r.first >= 0 && r.first <= b;
-        e = own_entry(p, b, r, in ? s.word[1][r.first] : 0, in ? s.word[2][r.first] : 0);
+        e = own_entry(p, b, r, in ? s.word[1][r.first] : 0, in ? s.entry[r.first] : e);
     }
     return e;
 }

@@ -76,3 +76,26 @@ def test_work_behind_many_entries_that_have_none(B):
     want, want_lse, tol, tol_lse = S.cross_attention(S.values(q), S.values(k), S.values(k), [3], [200], 0.125)
     out, lse = cross(B, dev_bf16(q), dev_bf16(k), i32([0] * 1101 + [3]), i32([0] * 1101 + [200]))
     assert (np.abs(host_f64(out) - want) <= tol).all() and (np.abs(lse.double().cpu().numpy() - want_lse) <= tol_lse).all()
+
+
+@pytest.mark.parametrize("cu_q,q_len,left", [([0, 5, 100, 20], 95, [0, 1]), ([50, 60, 10, 40, 45], 50, [0, 2, 3]), ([50, 60, 10, 40, 90], 30, [0, 2]),
+                                             ([10, 12, 0, 8, -5, 14], 20, [0, 2]), ([0, 5, 300, 9, 20], 20, [0, 3])])
+@pytest.mark.parametrize("shared_tokens", [0, 96])
+def test_requests_of_a_group_whose_queries_lie_elsewhere(B, cu_q, q_len, left, shared_tokens):
+    """Offsets that descend inside a group: who has no queries is skipped, whose queries are not among the group's is taken alone."""
+    batch, hq, d, n_queries, kv_len, ps = len(cu_q) - 1, 14, 64, 100, 700, 16
+    q, k = rnd_bits((n_queries, hq, d), 31), rnd_bits((batch * kv_len // ps + batch, ps, 2, d), 32)
+    width = -(-kv_len // ps)
+    table = np.arange(batch * width, dtype=np.int32).reshape(batch, width) % len(k)
+    table[:, :shared_tokens // ps] = table[0, :shared_tokens // ps]
+    groups = np.zeros((3, batch), dtype=np.int32)
+    groups[1, 0], groups[2] = batch, shared_tokens
+    out, lse = shared(B, dev_bf16(q), dev_bf16(k), i32(table), i32([kv_len] * batch), i32(groups), i32(cu_q), q_len, kv_len)
+    got, got_lse, written = host_f64(out), lse.double().cpu().numpy(), np.zeros(n_queries, dtype=bool)
+    for b in left:
+        rows = slice(cu_q[b], cu_q[b + 1])
+        x = S.values(k)[table[b]].reshape(-1, 2, d)[:kv_len]
+        want, want_lse, tol, tol_lse = S.all_heads(S.values(q[rows]), x, x, 0.125, S.block_sees(kv_len, cu_q[b + 1] - cu_q[b]))
+        assert (np.abs(got[rows] - want) <= tol).all() and (np.abs(got_lse[rows] - want_lse) <= tol_lse).all()
+        written[rows] = True
+    assert (got[~written] == 7.0).all() and (got_lse[~written] == 7.0).all()

@@ -81,7 +81,80 @@ int main()
 }
 """
 
-PROGRAMS = {"a workgroup's way through the entries": WALK}
+# Requests and groups of every kind: who is taken with a group has its queries among those of the group's entry, before its block and behind the shared
+# keys; everyone whose own words fit together is taken, once.
+GROUPS = r"""
+struct Call {
+    std::vector<int> cu_q, kv_lens, groups;
+    int n_queries, q_len, kv_len;
+};
+
+static int check(const Call& c, const std::vector<int>& with)       // with: who has to be taken with a group (empty: anyone)
+{
+    RowsParams p = {};
+    const int batch = (int)c.kv_lens.size();
+    p.cu_q = c.cu_q.data(); p.kv_lens = c.kv_lens.data(); p.groups = c.groups.data();
+    p.batch = batch; p.entries = 2 * batch; p.n_queries = c.n_queries; p.q_len = c.q_len; p.kv_len = c.kv_len;
+    for (int b = 0; b < batch; ++b) {
+        const Entry all = entry_of<true>(p, b, true), own = entry_of<true>(p, batch + b, true), alone = entry_of<true>(p, batch + b, false);
+        if (all.n_q > 0) REQUIRE(all.q0 >= 0 && all.n_q <= c.n_queries - all.q0 && all.key0 == 0 && all.key1 > 0 && all.key1 <= c.kv_len && all.key1 % 16 == 0, "%d", b);
+        const int64_t from = c.cu_q[b], to = c.cu_q[b + 1], n = to - from, kvl = c.kv_lens[b];
+        const bool fits = from >= 0 && n > 0 && n <= c.q_len && to <= c.n_queries && kvl >= n && kvl <= c.kv_len;
+        REQUIRE((own.n_q > 0) == fits && (alone.n_q > 0) == fits, "%d", b);
+        if (!fits) continue;
+        REQUIRE(own.q0 == from && own.n_q == n && own.key1 == kvl && alone.key0 == 0 && alone.key1 == kvl && alone.first == -1, "%d", b);
+        REQUIRE((own.first >= 0) == (own.key0 > 0) && own.first <= b, "%d", b);
+        if (own.key0 > 0) {
+            const Entry first = entry_of<true>(p, own.first, true);
+            REQUIRE(first.n_q > 0 && first.key1 == own.key0 && own.key0 <= kvl - n, "%d", b);
+            REQUIRE(first.q0 <= from && to <= first.q0 + first.n_q, "the queries of %d, %d to %d, are not among those of %d: %d to %d", b, (int)from, (int)to, own.first,
+                    first.q0, first.q0 + first.n_q);
+        }
+        if (!with.empty()) REQUIRE(own.first == with[b], "%d is with %d, not %d", b, own.first, with[b]);
+    }
+    return 0;
+}
+
+static int group_of(std::vector<int>& groups, int batch, int first, int members, int shared)
+{
+    for (int b = first; b < first + members; ++b) groups[b] = first, groups[batch + b] = b == first ? members : 0, groups[2 * batch + b] = shared;
+    return 0;
+}
+
+int main()
+{
+    const auto one_group = [](std::vector<int> cu_q, int n_queries, int q_len) {
+        const int batch = (int)cu_q.size() - 1;
+        Call c = {cu_q, std::vector<int>(batch, 500), std::vector<int>(3 * batch, 0), n_queries, q_len, 500};
+        group_of(c.groups, batch, 0, batch, 64);
+        return c;
+    };
+    if (check(one_group({0, 5, 9, 20}, 20, 11), {0, 0, 0})) return 1;
+    if (check(one_group({0, 5, 100, 20}, 100, 95), {0, -1, -1})) return 1;              // (the second ends behind the last one's end)
+    if (check(one_group({50, 60, 10, 40, 90}, 100, 50), {0, -1, -1, -1})) return 1;     // (the third lies in front of the first)
+    if (check(one_group({10, 12, 0, 8, -5, 14}, 20, 20), {0, -1, -1, -1, -1})) return 1;
+    if (check(one_group({0, 5, 300, 9, 20}, 20, 20), {0, -1, -1, 0})) return 1;         // (skipped ones in between change no other)
+    srand(1);
+    for (int i = 0; i < 300000; ++i) {
+        const int batch = 1 + rand() % 7, n_queries = 1 + rand() % 60;
+        Call c = {std::vector<int>(batch + 1), std::vector<int>(batch), std::vector<int>(3 * batch, 0), n_queries, 1 + rand() % 60, 40 + rand() % 100};
+        int at = rand() % 8;
+        for (int& x : c.cu_q) {
+            x = rand() % 6 ? at : rand() % (n_queries + 20) - 10;
+            at += rand() % 12;
+        }
+        for (int& x : c.kv_lens) x = rand() % 8 ? 30 + rand() % 110 : rand() % 20 - 5;
+        for (int b = 0; b < batch; ++b) {
+            if (rand() % 3 == 0) group_of(c.groups, batch, b, 1 + rand() % (batch - b), 16 * (rand() % 6));
+            if (rand() % 9 == 0) c.groups[rand() % (3 * batch)] = rand() % 40 - 5;
+        }
+        if (check(c, {})) return 1;
+    }
+    puts("ok");
+}
+"""
+
+PROGRAMS = {"a workgroup's way through the entries": WALK, "who is taken with a group": GROUPS}
 
 
 @pytest.mark.parametrize("what", PROGRAMS)
