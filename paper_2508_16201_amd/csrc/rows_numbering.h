@@ -70,8 +70,8 @@ template <bool PAGED> __host__ __device__ __forceinline__ Request request_of(con
 // Whether b can be the first of a group of so many members that share so many tokens.
 __host__ __device__ __forceinline__ bool leads(const RowsParams& p, int b, const Request& r)
 {
-    return r.first == b && r.members >= 2 && r.members <= p.batch - b && r.shared > 0 && r.shared % 16 == 0 && r.n_q > 0 && r.kvl <= p.kv_len &&
-           r.shared <= r.kvl - r.n_q;
+    return r.first == b && r.members >= 2 && r.members <= p.batch - b && r.shared > 0 && r.shared % 16 == 0 && r.n_q > 0 && r.kvl >= r.n_q &&
+           r.kvl <= p.kv_len && r.shared <= r.kvl - r.n_q;
 }
 // The keys that a group shares, with the queries of all of its requests, up to q_end; none where what is said of it does not fit together (its requests
 // are then taken alone).

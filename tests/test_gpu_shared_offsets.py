@@ -99,3 +99,18 @@ def test_requests_of_a_group_whose_queries_lie_elsewhere(B, cu_q, q_len, left, s
         assert (np.abs(got[rows] - want) <= tol).all() and (np.abs(got_lse[rows] - want_lse) <= tol_lse).all()
         written[rows] = True
     assert (got[~written] == 7.0).all() and (got_lse[~written] == 7.0).all()
+
+
+@pytest.mark.parametrize("length", [-2 ** 31, -2 ** 31 + 1, -1, 0, 2 ** 31 - 1])
+@pytest.mark.parametrize("tokens", [32, 1 << 20, 2 ** 31 - 16])
+def test_a_first_request_of_no_possible_length_has_no_group(B, length, tokens):
+    q, k = rnd_bits((6, 4, 64), 41), rnd_bits((20, 16, 1, 64), 42)
+    table = np.arange(15, dtype=np.int32).reshape(3, 5) + 2
+    groups = np.array([[0, 0, 0], [3, 0, 0], [tokens] * 3], dtype=np.int32)
+    out, lse = shared(B, dev_bf16(q), dev_bf16(k), i32(table), i32([length, 70, 33]), i32(groups), i32([0, 2, 4, 6]), 2, 80)
+    got, got_lse = host_f64(out), lse.double().cpu().numpy()
+    assert (got[:2] == 7.0).all() and (got_lse[:2] == 7.0).all()
+    for b, n in ((1, 70), (2, 33)):
+        rows, x = slice(2 * b, 2 * b + 2), S.values(k)[table[b]].reshape(-1, 1, 64)[:n]
+        want, want_lse, tol, tol_lse = S.all_heads(S.values(q[rows]), x, x, 0.125, S.block_sees(n, 2))
+        assert (np.abs(got[rows] - want) <= tol).all() and (np.abs(got_lse[rows] - want_lse) <= tol_lse).all()

@@ -154,7 +154,31 @@ int main()
 }
 """
 
-PROGRAMS = {"a workgroup's way through the entries": WALK, "who is taken with a group": GROUPS}
+# The same where lengths and offsets are any numbers at all.
+ANYTHING = GROUPS[:GROUPS.index("int main()")] + r"""
+int main()
+{
+    const int ends[] = {INT32_MIN, INT32_MIN + 1, INT32_MIN + 5, -1, 0, 1, 5, 40, INT32_MAX - 4, INT32_MAX};
+    srand(2);
+    for (int i = 0; i < 300000; ++i) {
+        const int batch = 1 + rand() % 5, n_queries = 1 + rand() % 60;
+        Call c = {std::vector<int>(batch + 1), std::vector<int>(batch), std::vector<int>(3 * batch, 0), n_queries, 1 + rand() % 60, 40 + rand() % 100};
+        int at = 0;
+        for (int& x : c.cu_q) {
+            x = rand() % 4 ? at : ends[rand() % 10];
+            at += rand() % 12;
+        }
+        for (int& x : c.kv_lens) x = rand() % 2 ? 30 + rand() % 110 : ends[rand() % 10];
+        for (int b = 0; b < batch; ++b)
+            if (rand() % 2 == 0) group_of(c.groups, batch, b, 1 + rand() % (batch - b), rand() % 2 ? 16 * (rand() % 6) : (ends[rand() % 10] & ~15));
+        if (check(c, {})) return 1;
+    }
+    puts("ok");
+}
+"""
+
+PROGRAMS = {"a workgroup's way through the entries": WALK, "who is taken with a group": GROUPS,
+            "groups of requests of which anything is said": ANYTHING}
 
 
 @pytest.mark.parametrize("what", PROGRAMS)
