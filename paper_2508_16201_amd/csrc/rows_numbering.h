@@ -198,8 +198,11 @@ __host__ __device__ __forceinline__ bool has_queries(const RowsParams& p, int b)
     return from >= 0 && from < to && to <= p.n_queries && (int64_t)to - from <= p.q_len;
 }
 
-// (Ranges) The queries of entry b begin at q0: the number of its first share.  There is a share's room between an entry and the next, more than half of which is
-// for a share that is not whole.
-__host__ __device__ __forceinline__ int spans_before(const RowsParams& p, int q0, int b) { return q0 / p.span + b; }
+// (Ranges) Shares of entry b's queries.  They are numbered behind those of the entries in front of it, wherever its queries lie; entries that have no query in
+// common have no more than `entries` in all.
+__host__ __device__ __forceinline__ int shares_of_entry(const RowsParams& p, int b)
+{
+    return b < p.batch && has_queries(p, b) ? (p.cu_q[b + 1] - p.cu_q[b] - 1) / p.span + 1 : 0;
+}
 
 }  // namespace specvlm

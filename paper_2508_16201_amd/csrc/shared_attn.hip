@@ -740,6 +740,10 @@ void rows_kernel(const RowsParams p)
     }
 }
 
+// The shares up to those of 64 entries, a lane to each that has n, of which `before` are in front of them.  (What entries with queries in common have beyond the
+// numbers that there are is not counted: an int holds it.)
+__device__ __forceinline__ int shares_upto(const RowsParams& p, int before, int n) { return min(before, p.entries) + wave_prefix(n); }
+
 // Each share of an entry's queries with the keys that any of them sees, a wave to a share: a workgroup's keys are then those that its rows see, and the work is
 // dealt by them.
 __global__ __launch_bounds__(256)
@@ -747,22 +751,28 @@ void rows_spans_kernel(const RowsParams p)
 {
     const int lane = threadIdx.x & 63, e = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (e >= p.entries) return;
-    // the entry: the last one whose shares begin at or before this one
-    int b = 0;
+    int b = 0, of_entry = e;                                 // the entry, and the number in it
     if (p.cu_q) {
         b = -1;
-        for (int c = 0; c < p.batch; c += kWave) {
-            const uint64_t begun = __ballot(c + lane < p.batch && has_queries(p, c + lane) && spans_before(p, p.cu_q[c + lane], c + lane) <= e);
-            if (begun) b = c + 63 - __builtin_clzll(begun);
+        for (int c = 0, before = 0; c < p.batch && b < 0; c += kWave) {
+            const int n = shares_of_entry(p, c + lane), upto = shares_upto(p, before, n);
+            const uint64_t here = __ballot(upto - n <= e && e < upto);
+            if (here) {
+                const int i = __builtin_ctzll(here);
+                b = c + i;
+                of_entry = e - __builtin_amdgcn_readlane(upto - n, i);
+            }
+            before = __builtin_amdgcn_readlane(upto, kWave - 1);
         }
     }
     Entry s = {0, 0, 0, 0, b};
     if (b >= 0) {
         const int q0 = p.cu_q ? p.cu_q[b] : 0, n_q = p.cu_q ? p.cu_q[b + 1] - q0 : p.q_len, k0 = p.cu_kv ? p.cu_kv[b] : 0,
-                  n = p.cu_kv ? p.cu_kv[b + 1] - k0 : p.kv_len, at = (e - spans_before(p, q0, b)) * p.span;
-        if (n_q > 0 && q0 >= 0 && q0 <= p.n_queries - n_q && n >= 0 && k0 >= 0 && k0 <= p.kv_len - n && at >= 0 && at < n_q) {
-            s.q0 = q0 + at;
-            s.n_q = min(p.span, n_q - at);
+                  n = p.cu_kv ? p.cu_kv[b + 1] - k0 : p.kv_len;
+        const int64_t at = (int64_t)of_entry * p.span;
+        if (n_q > 0 && q0 >= 0 && q0 <= p.n_queries - n_q && n >= 0 && k0 >= 0 && k0 <= p.kv_len - n && at < n_q) {
+            s.q0 = q0 + (int)at;
+            s.n_q = min(p.span, n_q - (int)at);
             int lo = INT_MAX, hi = 0;
             for (int t = lane; t < s.n_q; t += kWave) {
                 const int from = max(p.ranges[2 * (int64_t)(s.q0 + t)], 0), to = min(p.ranges[2 * (int64_t)(s.q0 + t) + 1], n);
@@ -872,14 +882,18 @@ void rows_join_kernel(const RowsParams p)
         hd0 = blockIdx.x - tok * p.n_q_heads;
     }
     if (tok >= p.n_queries) return;
-    // the request
-    int b = 0;
+    // the request;  (ranges) the shares in front of its own
+    int b = 0, shares_before = 0;
     if (!p.cu_q) {
         b = PAGED ? tok / p.q_len : 0;
     } else {
         uint64_t behind = 0;
         for (; b < p.batch; b += kWave) {
             behind = __ballot(b + lane < p.batch && has_queries(p, b + lane) && p.cu_q[b + lane] <= tok && p.cu_q[b + lane + 1] > tok);
+            if (!PAGED && p.ranges) {
+                const int n = shares_of_entry(p, b + lane), upto = shares_upto(p, shares_before, n);
+                shares_before = behind ? __builtin_amdgcn_readlane(upto - n, __builtin_ctzll(behind)) : __builtin_amdgcn_readlane(upto, kWave - 1);
+            }
             if (behind) break;
         }
         if (!behind) return;                                 // (a row of no request)
@@ -887,9 +901,8 @@ void rows_join_kernel(const RowsParams p)
     }
     int e = PAGED ? p.batch + b : b;
     if (!PAGED && p.ranges) {
-        const int q0 = p.cu_q ? p.cu_q[b] : 0;
-        if (q0 < 0 || tok < q0) return;
-        e = spans_before(p, q0, b) + (tok - q0) / p.span;
+        e = shares_before + (tok - (p.cu_q ? p.cu_q[b] : 0)) / p.span;
+        if (e >= p.entries) return;                          // (there is none for queries of so many entries)
     }
     const RowsStart own = p.starts[e];
     const int total = own.total;

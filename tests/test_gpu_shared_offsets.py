@@ -114,3 +114,61 @@ def test_a_first_request_of_no_possible_length_has_no_group(B, length, tokens):
         rows, x = slice(2 * b, 2 * b + 2), S.values(k)[table[b]].reshape(-1, 1, 64)[:n]
         want, want_lse, tol, tol_lse = S.all_heads(S.values(q[rows]), x, x, 0.125, S.block_sees(n, 2))
         assert (np.abs(got[rows] - want) <= tol).all() and (np.abs(got_lse[rows] - want_lse) <= tol_lse).all()
+
+
+def entries_in_order(order, lens, gap=0):
+    """cu_q in which the entries of these lengths lie in another order than their numbers have, with skipped ones in between -> (cu_q, numbers, begins)."""
+    begins = np.zeros(len(lens), dtype=int)
+    begins[order] = np.concatenate([[0], np.cumsum(np.asarray(lens)[order] + gap)[:-1]])
+    cu_q, numbers = [], []
+    for begin, n in zip(begins, lens):
+        if not cu_q or cu_q[-1] != begin:
+            assert not cu_q or cu_q[-1] > begin, "an entry in front of this one would have queries"
+            cu_q.append(int(begin))
+        numbers.append(len(cu_q) - 1)
+        cu_q.append(int(begin + n))
+    return cu_q, numbers, begins
+
+
+@pytest.mark.parametrize("heads", [(8, 1, 64), (28, 4, 128)])
+@pytest.mark.parametrize("lens", [[64, 32], [5, 40, 33], [70, 1, 32, 90], [3] * 90])
+@pytest.mark.parametrize("kind", ["cross", "ranges", "paged"])
+def test_entries_whose_queries_lie_in_descending_order(B, heads, lens, kind):
+    """The first entry's queries behind the second one's, and so on: a descending entry, which is skipped, between each two."""
+    hq, hkv, d = heads
+    cu_q, numbers, begins = entries_in_order(np.arange(len(lens))[::-1], lens)
+    n_queries, batch, states = sum(lens), len(cu_q) - 1, 160
+    if lens == [64, 32]:
+        assert cu_q == [32, 96, 0, 32]
+    q, k = rnd_bits((n_queries, hq, d), 51), rnd_bits((batch * states, hkv, d), 52)
+    at = np.random.default_rng(53).integers(-9, states + 20, (n_queries, 2)).astype(np.int32)
+    ranges = np.sort(at, axis=1) if kind == "ranges" else None
+    if kind == "paged":
+        out, lse = shared(B, dev_bf16(q), dev_bf16(k.reshape(-1, 16, hkv, d)), i32(np.arange(batch * 10).reshape(batch, 10)), i32([states] * batch),
+                          torch.zeros((3, batch), dtype=torch.int32, device="cuda"), i32(cu_q), max(lens), states)
+    else:
+        out, lse = cross(B, dev_bf16(q), dev_bf16(k), i32(cu_q), i32(np.arange(batch + 1) * states), None if ranges is None else i32(ranges))
+    got, got_lse = host_f64(out), lse.double().cpu().numpy()
+    for e, begin, n in zip(numbers, begins, lens):
+        rows, x = slice(begin, begin + n), S.values(k)[e * states:(e + 1) * states]
+        if kind == "paged":
+            want, want_lse, tol, tol_lse = S.all_heads(S.values(q[rows]), x, x, 0.125, S.block_sees(states, n))
+        else:
+            want, want_lse, tol, tol_lse = S.cross_attention(S.values(q[rows]), x, x, [n], [states], 0.125, None if ranges is None else ranges[rows])
+        some = np.isfinite(want_lse)
+        assert (np.abs(got[rows] - want) <= tol).all()
+        assert (got_lse[rows][~some] == -np.inf).all() and (np.abs(got_lse[rows][some] - want_lse[some]) <= tol_lse[some]).all()
+
+
+def test_ranges_of_entries_that_have_each_query_many_times(B):
+    """More shares than there are numbers for, and their sum more than an int holds: nothing is written, and the next call is as ever."""
+    n_queries = 4096
+    q, k = rnd_bits((n_queries + 9, 64, 64), 1), rnd_bits((64, 1, 64), 2)
+    seen = i32(np.tile([[0, 64]], (n_queries + 9, 1)))
+    cu = torch.zeros(8193, dtype=torch.int32, device="cuda")
+    cu[1::2] = n_queries
+    out, lse = cross(B, dev_bf16(q), dev_bf16(k), cu, torch.clamp(cu, max=64), seen)
+    assert (out == 7.0).all() and (lse == 7.0).all()
+    want, want_lse, tol, tol_lse = S.cross_attention(S.values(q), S.values(k), S.values(k), [n_queries + 9], [64], 0.125)
+    out, lse = cross(B, dev_bf16(q), dev_bf16(k), i32([0, n_queries + 9]), i32([0, 64]), seen)
+    assert (np.abs(host_f64(out) - want) <= tol).all() and (np.abs(lse.double().cpu().numpy() - want_lse) <= tol_lse).all()

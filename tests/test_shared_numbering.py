@@ -177,8 +177,49 @@ int main()
 }
 """
 
+# Shares of entries whose queries lie in any order: every one has a number of its own.
+SHARES = r"""
+static int check(const std::vector<int>& cu_q, int n_queries, int span, bool required)
+{
+    RowsParams p = {};
+    p.cu_q = cu_q.data(); p.batch = (int)cu_q.size() - 1; p.n_queries = p.q_len = n_queries; p.span = span;
+    const int entries = p.batch + n_queries / span + 1;
+    std::vector<int> in(n_queries, 0);
+    int number = 0, queries = 0;
+    for (int b = 0; b < p.batch; ++b) {
+        const int n = shares_of_entry(p, b), q0 = cu_q[b], of = has_queries(p, b) ? cu_q[b + 1] - q0 : 0;
+        REQUIRE(n * span >= of && (n - 1) * span < of, "%d", b);
+        for (int i = 0; i < of; ++i) {
+            if (in[q0 + i]++) return required;               // (a query in two entries)
+            ++queries;
+        }
+        number += n;
+    }
+    REQUIRE(number <= entries, "%d shares of %d queries, %d numbers", number, queries, entries);
+    REQUIRE(shares_of_entry(p, p.batch) == 0);
+    return 0;
+}
+
+int main()
+{
+    if (check({32, 96, 0, 32}, 96, 32, true) || check({0, 40, 999, 40, 70}, 70, 36, true) || check({64, 96, 32, 64, 0, 32}, 96, 32, true)) return 1;
+    srand(3);
+    for (int i = 0; i < 300000; ++i) {
+        const int n_queries = 1 + rand() % 200, span = 1 + rand() % 70;
+        std::vector<int> cu_q(2 + rand() % 8);
+        int at = rand() % 20;
+        for (int& x : cu_q) {
+            x = rand() % 3 ? at : rand() % (n_queries + 20) - 10;
+            at += rand() % 40;
+        }
+        if (check(cu_q, n_queries, span, false)) return 1;
+    }
+    puts("ok");
+}
+"""
+
 PROGRAMS = {"a workgroup's way through the entries": WALK, "who is taken with a group": GROUPS,
-            "groups of requests of which anything is said": ANYTHING}
+            "groups of requests of which anything is said": ANYTHING, "shares of entries in any order": SHARES}
 
 
 @pytest.mark.parametrize("what", PROGRAMS)
