@@ -1049,9 +1049,17 @@ size_t rows_workspace(bool paged, int batch, int n_queries, int n_q_heads, int n
     const size_t entries = (size_t)rows_entries(paged, true, batch, n_queries, n_q_heads, n_kv_heads);
     return align256(rows * head_dim * sizeof(float)) + align256(rows * 2 * sizeof(float)) + align256(entries * sizeof(RowsStart)) + align256(entries * sizeof(Entry));
 }
-bool rows_shape(int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim)
+// Whether rows, and rows of partial results, are ints.  (Entries by themselves first: of any two ints the product with 32 is no 64-bit number.)
+bool rows_fit(bool paged, bool ranges, int batch, int n_queries, int n_q_heads, int n_kv_heads)
 {
-    return batch > 0 && n_queries > 0 && n_kv_heads > 0 && n_q_heads > 0 && n_q_heads % n_kv_heads == 0 && (head_dim == 64 || head_dim == 128);
+    const int64_t entries = rows_entries(paged, ranges, batch, n_queries, n_q_heads, n_kv_heads), most = (int64_t)1 << 29;
+    return (int64_t)n_queries * n_q_heads < most && entries < most / 32 && entries * 32 * n_kv_heads < most;
+}
+// (no workspace for what the call refuses)
+bool rows_shape(bool paged, int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim)
+{
+    return batch > 0 && n_queries > 0 && n_kv_heads > 0 && n_q_heads > 0 && n_q_heads % n_kv_heads == 0 && (head_dim == 64 || head_dim == 128) &&
+           rows_fit(paged, false, batch, n_queries, n_q_heads, n_kv_heads);
 }
 
 template <int D, bool PAGED>
@@ -1093,8 +1101,8 @@ int rows_start(RowsParams& p, bool paged, const void* q, int64_t q_tok, int64_t 
     // (a lane's offset inside 16 keys has 32 bits; rows, and tiles of all sets and heads, are ints)
     if (tok < 0 || tok >= ((int64_t)1 << 26)) return SPECVLM_EUNSUPPORTED;
     const bool ranges = key_ranges != nullptr;
+    if (!rows_fit(paged, ranges, batch, n_queries, n_q_heads, n_kv_heads)) return SPECVLM_EUNSUPPORTED;
     const int64_t rows = (int64_t)n_queries * n_q_heads, entries = rows_entries(paged, ranges, batch, n_queries, n_q_heads, n_kv_heads);
-    if (rows >= ((int64_t)1 << 29) || entries * 32 * n_kv_heads >= ((int64_t)1 << 29)) return SPECVLM_EUNSUPPORTED;
     const int64_t sets = (2 * rows / kSetRows + n_kv_heads) + entries * n_kv_heads;
     if (sets * 3 * (most_keys / 32 + 10) >= ((int64_t)1 << 31)) return SPECVLM_EUNSUPPORTED;
     const size_t need = rows_workspace(paged, batch, n_queries, n_q_heads, n_kv_heads, head_dim);
@@ -1125,7 +1133,7 @@ using namespace specvlm;
 
 extern "C" size_t specvlm_shared_attn_workspace_bytes(int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim)
 {
-    return rows_shape(batch, n_queries, n_q_heads, n_kv_heads, head_dim) ? rows_workspace(true, batch, n_queries, n_q_heads, n_kv_heads, head_dim) : 0;
+    return rows_shape(true, batch, n_queries, n_q_heads, n_kv_heads, head_dim) ? rows_workspace(true, batch, n_queries, n_q_heads, n_kv_heads, head_dim) : 0;
 }
 
 extern "C" int specvlm_shared_attn(
@@ -1158,7 +1166,7 @@ extern "C" int specvlm_shared_attn(
 
 extern "C" size_t specvlm_cross_attn_workspace_bytes(int batch, int n_queries, int n_q_heads, int n_kv_heads, int head_dim)
 {
-    return rows_shape(batch, n_queries, n_q_heads, n_kv_heads, head_dim) ? rows_workspace(false, batch, n_queries, n_q_heads, n_kv_heads, head_dim) : 0;
+    return rows_shape(false, batch, n_queries, n_q_heads, n_kv_heads, head_dim) ? rows_workspace(false, batch, n_queries, n_q_heads, n_kv_heads, head_dim) : 0;
 }
 
 extern "C" int specvlm_cross_attn(
