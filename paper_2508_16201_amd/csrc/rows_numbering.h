@@ -35,7 +35,7 @@ struct RowsParams {
     int n_pages, page_size;
     int batch, q_len, kv_len, n_queries;
     int n_q_heads, n_kv_heads, group;
-    uint32_t inv_page, inv_group;
+    uint32_t inv_page, inv_group, inv_span;
     float scale_log2;
     int entries, span;                           // numbered; (ranges) queries of a share
     Entry* spans;
@@ -202,7 +202,7 @@ __host__ __device__ __forceinline__ bool has_queries(const RowsParams& p, int b)
 // common have no more than `entries` in all.
 __host__ __device__ __forceinline__ int shares_of_entry(const RowsParams& p, int b)
 {
-    return b < p.batch && has_queries(p, b) ? (p.cu_q[b + 1] - p.cu_q[b] - 1) / p.span + 1 : 0;
+    return b < p.batch && has_queries(p, b) ? divide(p.cu_q[b + 1] - p.cu_q[b] - 1, p.span, p.inv_span).q + 1 : 0;
 }
 
 }  // namespace specvlm

@@ -901,7 +901,7 @@ void rows_join_kernel(const RowsParams p)
     }
     int e = PAGED ? p.batch + b : b;
     if (!PAGED && p.ranges) {
-        e = shares_before + (tok - (p.cu_q ? p.cu_q[b] : 0)) / p.span;
+        e = shares_before + divide(tok - (p.cu_q ? p.cu_q[b] : 0), p.span, p.inv_span).q;
         if (e >= p.entries) return;                          // (there is none for queries of so many entries)
     }
     const RowsStart own = p.starts[e];
@@ -1118,6 +1118,7 @@ int rows_start(RowsParams& p, bool paged, const void* q, int64_t q_tok, int64_t 
     p.over_q = q == out;
     p.far = entries * (rows + 32 * n_kv_heads) > INT_MAX;
     p.entries = (int)entries; p.ranges = key_ranges; p.span = rows_span(n_q_heads, n_kv_heads);
+    p.inv_span = reciprocal(p.span);
     const size_t parts = (size_t)rows_parts(paged, true, kNumCu, batch, n_queries, n_q_heads, n_kv_heads);
     p.part_o = (float*)workspace;
     p.part_ml = (float*)((char*)workspace + align256(parts * head_dim * sizeof(float)));

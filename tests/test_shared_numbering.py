@@ -182,7 +182,7 @@ SHARES = r"""
 static int check(const std::vector<int>& cu_q, int n_queries, int span, bool required)
 {
     RowsParams p = {};
-    p.cu_q = cu_q.data(); p.batch = (int)cu_q.size() - 1; p.n_queries = p.q_len = n_queries; p.span = span;
+    p.cu_q = cu_q.data(); p.batch = (int)cu_q.size() - 1; p.n_queries = p.q_len = n_queries; p.span = span; p.inv_span = reciprocal(span);
     const int entries = p.batch + n_queries / span + 1;
     std::vector<int> in(n_queries, 0);
     int number = 0, queries = 0;
