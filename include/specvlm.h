@@ -606,7 +606,14 @@ int specvlm_pages_shared(
  * roundings with the other requests of the batch and the groups.  Probabilities are rounded to
  * bf16 for their products with V, to two bf16 where up to 64 rows of a kv head meet the keys or
  * 32 keys weigh more than twice what their row had before; sums and partial results are fp32.
- * The workspace has 4 d + 8 bytes for each row of q twice, and 65536 rows of it more.
+ * The workspace has 4 d + 8 bytes for each of 2 * n_queries * H_q + 65536 + 48 * batch * H_kv
+ * rows (65536 for the chip's workgroups, the last for pieces that begin at multiples of 32),
+ * and 104 for each request: 1.6 GB for 8192 requests of 8 kv heads of 128.
+ * Against specvlm_paged_attn: sharing costs a second launch and the pieces' begins, so it is
+ * the slower call until the other one reads much of the same again. That is so from
+ * batch * shared * H_kv * 4 d of 200 MB on for one token (100 MB at d 64), of 300 to 400 for
+ * blocks of six: at 28/4 heads of 128, 16 requests about 4096 tokens take 21 us there and 23
+ * here (six queries 27 and 33), about 12544 tokens 42 and 29 (50 and 45).
  * Limits: n_queries * H_q up to 2^26 is always served (a launch's threads); batch * H_kv < 2^23,
  * 3 * (n_queries * H_q / 128 + (2 * batch + 1) * H_kv) * (kv_len / 32 + 10) < 2^31, kv_len <= 2^30.
  * -------------------------------------------------------------------------- */
@@ -639,8 +646,13 @@ int specvlm_shared_attn(
  * A query that sees no state gets 0, and -infinity in lse.  Hidden and infinite values are as
  * for specvlm_paged_attn.  An entry whose offsets leave the tensors or descend is skipped, its
  * rows of out and lse left as they are, as are rows of no entry.  No query is in two entries.
- * Results do not depend on the run; roundings are as in specvlm_shared_attn, and the workspace,
- * with each row once.
+ * Results do not depend on the run; roundings are as in specvlm_shared_attn.
+ * The workspace has 4 d + 8 bytes for each of n_queries * H_q + 65536 + 32 * n * H_kv rows and
+ * 52 for each of n entries, n = batch + 1 + n_queries / floor(256 / (H_q / H_kv)) (the divisor at
+ * least 1), with key_ranges or without.
+ * One token over all states of its entry is what specvlm_decode_attn gives for a block of one,
+ * and faster: over 1254 states of 2 kv heads of 64 5.5 us, here 10.5; over 8000 of 8 of 128 9.6,
+ * here 15.3; eight of them over up to 6272 of 4 of 128 19.9, here 22.
  * Limits: n_queries * H_q up to 2^26 is always served (a launch's threads); batch * H_kv < 2^24,
  * 3 * (n_queries * H_q / 128 + (batch + 2) * H_kv) * (n_states / 32 + 10) < 2^31 (with key_ranges
  * n_queries * H_q / 64 there), n_states <= 2^30.

@@ -625,7 +625,8 @@ def pages_shared(page_table: torch.Tensor, kv_lens: torch.Tensor, n_pages: int, 
     one's first neighbour of its group, for that one the number of them (0 for the others), the tokens that they share.
 
     page_table int32 [batch, max_pages], kv_lens int32 [batch], the block of q_len tokens (cu_q: of their own numbers) included.
-    min_tokens: fewer common tokens are not worth a group."""
+    min_tokens: fewer common tokens are not worth a group.  (For a few requests about a video of some thousand tokens paged_attn is the faster
+    call whatever the groups: the header has the line between it and shared_attn.)"""
     got = (_calls or _load_calls()).pages_shared(page_table, kv_lens, n_pages, page_size, q_len, cu_q, min_tokens, groups, workspace)
     if got is not None:
         if type(got) is int:

@@ -23,7 +23,7 @@
 // take as many; the clock, 2.4 GHz without such work, falls to 1.9 to 1.55 under it.  2 x 2048 queries of 64 heads over 12544 states: 1.50 ms, 1.12 PFLOP/s (a
 // library's product of 8192^3 1.22).  The loop alone, without masks, lookups and pages, took 6650 cycles, and 5950 without loads.  Narrow sets: memory, 32 requests
 // about five videos of up to 32768 tokens at 3.7 TB/s.  Beside the keys a piece takes 7 to 9 us: its place 0.8, table and queries 2, the first tile's way
-// through the maxima 2 more than another's, its results 2.5; and the second launch 5 to 18 us.
+// through the maxima 2 more than another's, its results 2.5; and the second launch 3.5 to 23 us.
 #include <climits>
 #include <type_traits>
 
@@ -39,7 +39,7 @@ constexpr int kChunks = kRowsTile / 32;
 constexpr float kRowsRedo = 0x1p20f;     // a lane's sum of 32 keys above this (or NaN) is done again with the maximum tracked
 // 32 keys with more than this times what their row had before have their probabilities in two bf16, where one costs up to 2^-9 of a probability: evened out
 // over many keys of like weight, but not in a row that one key makes up. (48 viewers' tokens over one stream of 65536, errors against 64 bits in parts of those of
-// outputs rounded once, over seeds: without 1.15 to 1.56, at 4 1.04 to 1.23, 2 1.03 to 1.22, 1 1.03 to 1.20, 0.25 1.03 to 1.17;  91.1 us a call, and 90.8, 91.2,
+// outputs rounded once, over seeds: without 1.15 to 1.56, at 4 1.04 to 1.23, 2 1.03 to 1.22 (others 1.33), 1 1.03 to 1.20, 0.25 1.03 to 1.17;  91.1 us a call, and 90.8, 91.2,
 // 92.4 and 100.)
 constexpr float kRowsPeak = 2.f;
 
