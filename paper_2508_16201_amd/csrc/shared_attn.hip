@@ -1049,7 +1049,7 @@ size_t rows_workspace(bool paged, int batch, int n_queries, int n_q_heads, int n
     const size_t entries = (size_t)rows_entries(paged, true, batch, n_queries, n_q_heads, n_kv_heads);
     return align256(rows * head_dim * sizeof(float)) + align256(rows * 2 * sizeof(float)) + align256(entries * sizeof(RowsStart)) + align256(entries * sizeof(Entry));
 }
-// Whether rows, and rows of partial results, are ints.  (Entries by themselves first: of any two ints the product with 32 is no 64-bit number.)
+// Whether rows, and rows of partial results, are ints.  (Entries by themselves first: 32 times any number of them and of heads would pass 64 bits.)
 bool rows_fit(bool paged, bool ranges, int batch, int n_queries, int n_q_heads, int n_kv_heads)
 {
     const int64_t entries = rows_entries(paged, ranges, batch, n_queries, n_q_heads, n_kv_heads), most = (int64_t)1 << 29;
